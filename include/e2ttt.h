@@ -338,6 +338,145 @@ e2ttt_status e2ttt_chunk_backward_ln(const e2ttt_desc* desc, const float* ln_wei
 e2ttt_status e2ttt_apply_ln(const e2ttt_desc* desc, const float* ln_weight, const float* ln_bias,
                             const void* q, const float* w, void* out, void* stream);
 
+/*
+ * Gated delta rule: the fast weight of a linear net f(x) = W x, updated by
+ * every token at the weights the token before left (where the chunk calls take
+ * a chunk's gradients at its start).  Per unit (sequence b, value head h), with
+ * gamma_t = exp(log_gamma_t) and W [dv][dk]:
+ *   e_t = v_t - gamma_t W_{t-1} k_t
+ *   W_t = gamma_t W_{t-1} + eta_t e_t k_t^T
+ *   o_t = scale W_t q_t                        (the state after the token)
+ * H value heads share HK key heads in groups: value head h reads the queries
+ * and keys of key head h / (H / HK).  Keys are expected of about unit length
+ * with 0 <= eta <= 1 (eta |k|^2 <= 2): beyond that the rule itself diverges.
+ *
+ * Layouts: q, k [B][HK][T][dk] and v, out [B][H][T][dv] in desc.io; eta and
+ * log_gamma [B][H][T] f32 (log_gamma NULL: gamma = 1; -inf clears the state); states [B][H][dv][dk] f32,
+ * contiguous.  Token tensors and gates may have any non-negative strides
+ * (e2ttt_delta_strides, in elements; the last dimension is contiguous), for
+ * example those of a projection's [B][T][H][d]; strides NULL means C order.
+ * Rows of the io type start on 16 bytes, and elements of a written tensor do
+ * not overlap (else E2TTT_ERR_BAD_SHAPE).
+ * lengths [B] int32 (device; NULL: all T): tokens of sequence b at and after
+ * lengths[b] (clamped to 0..T) are not read and do not touch the state; their
+ * outputs and gradients are written as zero.
+ * Supported: dk <= 128 and dv <= 256, multiples of 8, either io type, T >= 1
+ * (else E2TTT_ERR_UNSUPPORTED).
+ *
+ * Precision: fp32 throughout (with bf16 tensors, fp32 values enter the matrix
+ * products as sums of three bf16 numbers, which lose nothing, or of two, to
+ * 2^-17, where only a bf16 output follows).  Within a chunk of 64 tokens
+ * (0..63, 64..127, ...) a token with a non-finite value may make the outputs
+ * of its whole chunk non-finite, as it does those after it.
+ */
+typedef struct { int64_t b, h, t; } e2ttt_strides;
+
+typedef struct {
+  int32_t B;            /* sequences                                       */
+  int32_t HK, H;        /* key heads, value heads (a multiple of HK)       */
+  int32_t T;            /* tokens                                          */
+  int32_t dk, dv;       /* head dims of keys and values                    */
+  int32_t io;           /* e2ttt_dtype                                     */
+  float scale;          /* of the outputs                                  */
+} e2ttt_delta_desc;
+
+/* The strides of each tensor of the delta calls (those of a call's other
+ * tensors are not looked at). */
+typedef struct {
+  e2ttt_strides q, k, v, out, eta, log_gamma;
+  e2ttt_strides d_out, dq, dk, dv, d_eta, d_log_gamma;
+} e2ttt_delta_strides;
+
+/* Bytes of `workspace` for e2ttt_delta_forward and of `scratch` for
+ * e2ttt_delta_backward (0 for a bad descriptor).  Without save_for_backward at
+ * most about 224 MiB and one state per unit (more only where a single chunk of
+ * every unit needs it); with it the workspace keeps, per unit and chunk, the
+ * chunk-start state and what the backward reuses, and must be passed to
+ * e2ttt_delta_backward untouched. */
+size_t e2ttt_delta_workspace_bytes(const e2ttt_delta_desc* desc, int save_for_backward);
+size_t e2ttt_delta_scratch_bytes(const e2ttt_delta_desc* desc);
+
+/* The rule over T tokens of every unit from w_in (NULL: zero) to w_out (NULL:
+ * not wanted; may be w_in itself). */
+e2ttt_status e2ttt_delta_forward(const e2ttt_delta_desc* desc, const e2ttt_delta_strides* strides,
+                                 const void* q, const void* k, const void* v, const float* eta,
+                                 const float* log_gamma, const int32_t* lengths,
+                                 const float* w_in, void* out, float* w_out, void* workspace,
+                                 size_t workspace_bytes, int save_for_backward, void* stream);
+
+/* Backward of  sum_t <d_out_t, o_t> + <d_w_out, W_T>  (d_w_out NULL: zero)
+ * with the forward's inputs and its workspace (saved, untouched).  dq, dk are
+ * summed over the value heads of a group.  d_log_gamma is NULL iff log_gamma
+ * is; d_w_in [B][H][dv][dk] NULL: not wanted. */
+e2ttt_status e2ttt_delta_backward(const e2ttt_delta_desc* desc,
+                                  const e2ttt_delta_strides* strides, const void* q,
+                                  const void* k, const void* v, const float* eta,
+                                  const float* log_gamma, const int32_t* lengths,
+                                  const void* workspace, size_t workspace_bytes,
+                                  const void* d_out, const float* d_w_out, void* dq, void* dk,
+                                  void* dv, float* d_eta, float* d_log_gamma, float* d_w_in,
+                                  void* scratch, size_t scratch_bytes, void* stream);
+
+/* The recurrent form, for decode: the T (few) arriving tokens of every
+ * sequence, in fp32 arithmetic, on states w [n_slots][H][dv][dk] that are
+ * updated in place.  Sequence b is at state slots[b] (int32, device; NULL: b,
+ * with n_slots >= B).  A slot outside 0..n_slots-1 is skipped: its outputs are
+ * zero.  Rows of the batch that name the same slot are taken in their order.
+ * The state is read and written once whatever T; no workspace. */
+e2ttt_status e2ttt_delta_step(const e2ttt_delta_desc* desc, const e2ttt_delta_strides* strides,
+                              const void* q, const void* k, const void* v, const float* eta,
+                              const float* log_gamma, float* w, const int32_t* slots,
+                              int32_t n_slots, void* out, void* stream);
+
+/*
+ * Preparation of queries and keys (Sec. 4: SiLU and unit length before the
+ * fast-weight net), with rotary positions, for the chunk calls and the delta
+ * calls.  Per row x of d elements, each step optional:
+ *   E2TTT_QK_SILU   s = x sigmoid(x)
+ *   E2TTT_QK_UNIT   y = s / sqrt(sum s^2 + eps)
+ *   rot > 0         the first rot (even) elements of y turn in pairs:
+ *                     z_a = rot_scale (y_a cos - y_b sin)
+ *                     z_b = rot_scale (y_b cos + y_a sin)
+ *                   pair p of rot / 2 turns by position * inv_freq[p]; it is
+ *                   (p, p + rot / 2), or (2 p, 2 p + 1) with
+ *                   E2TTT_QK_INTERLEAVED.  The other elements pass.
+ *   q [B][H][T][d], k [B][HK][T][d] io   (HK = 0: queries alone, k and k_out NULL)
+ *   inv_freq [rot / 2] f32   frequencies, as scaled for the context (with
+ *                   rot_scale its factor on the turned elements, else 1)
+ *   positions [B][T] int64   NULL: 0 .. T - 1; angles are formed in 64 bits
+ * Outputs may be the inputs themselves (same strides).  Strides as for the
+ * delta calls.  Supported: d <= 256, a multiple of 8, either io type.
+ */
+#define E2TTT_QK_SILU 0x1u
+#define E2TTT_QK_UNIT 0x2u
+#define E2TTT_QK_INTERLEAVED 0x4u
+
+typedef struct {
+  int32_t B, H, HK, T;  /* sequences, query heads, key heads, tokens */
+  int32_t d, rot;       /* head dim, elements that turn              */
+  int32_t io;           /* e2ttt_dtype                               */
+  uint32_t flags;       /* E2TTT_QK_*                                */
+  float eps;            /* > 0 with E2TTT_QK_UNIT                    */
+  float rot_scale;
+} e2ttt_qk_desc;
+
+typedef struct {
+  e2ttt_strides q, k, q_out, k_out;
+  e2ttt_strides d_q_out, d_k_out, dq, dk;
+} e2ttt_qk_strides;
+
+e2ttt_status e2ttt_qk_forward(const e2ttt_qk_desc* desc, const e2ttt_qk_strides* strides,
+                              const void* q, const void* k, const float* inv_freq,
+                              const int64_t* positions, void* q_out, void* k_out, void* stream);
+
+/* Gradients of q and k from those of the outputs.  q and k are the forward's
+ * inputs (not its outputs); without SILU and UNIT they are not read and may be
+ * NULL. */
+e2ttt_status e2ttt_qk_backward(const e2ttt_qk_desc* desc, const e2ttt_qk_strides* strides,
+                               const void* q, const void* k, const float* inv_freq,
+                               const int64_t* positions, const void* d_q_out,
+                               const void* d_k_out, void* dq, void* dk, void* stream);
+
 /* Static description of a status code. */
 const char* e2ttt_status_str(e2ttt_status status);
 

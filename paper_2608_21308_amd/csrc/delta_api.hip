@@ -1,0 +1,225 @@
+// C entry points of the gated delta rule: argument checks, the layout of
+// workspace and scratch, and the launches.
+#include <math.h>
+#include <string.h>
+
+#include "delta_common.h"
+#include "e2ttt.h"
+#include "strided.h"
+
+namespace e2ttt {
+namespace {
+
+e2ttt_status check_desc(const e2ttt_delta_desc* d) {
+  if (!d) return E2TTT_ERR_NULL_ARG;
+  if (d->B <= 0 || d->HK <= 0 || d->H <= 0 || d->T <= 0 || d->dk <= 0 || d->dv <= 0 ||
+      d->H % d->HK != 0 || !isfinite(d->scale))
+    return E2TTT_ERR_BAD_SHAPE;
+  if ((d->io != E2TTT_DT_F32 && d->io != E2TTT_DT_BF16) || d->dk % 8 || d->dv % 8 ||
+      d->dk > 128 || d->dv > 256 || d->T > (1 << 30))
+    return E2TTT_ERR_UNSUPPORTED;
+  // every launch numbers its workgroups in 31 bits
+  const double units = (double)d->B * d->H, nc = ((double)d->T + kDC - 1) / kDC;
+  if (units * 64 > 1e9 || units * nc > 1e9) return E2TTT_ERR_UNSUPPORTED;
+  return E2TTT_OK;
+}
+
+struct Plan {
+  bool bf;
+  long U, NC;
+  long nc_buf;                    // chunks per unit held at once
+  size_t o_gate, o_frag, o_state, o_w, o_u, bytes;       // workspace
+  size_t s_w, s_u, scratch;                              // backward scratch
+  long w_bytes, u_bytes;
+};
+
+size_t up(size_t x) { return (x + 255) & ~(size_t)255; }
+
+// Calls that do not save run in stretches of chunks whose gates and fragments
+// fit here: what the first kernel of a stretch writes, the second reads from
+// the 256 MB last-level cache.
+constexpr size_t kStretchBytes = (size_t)224 << 20;
+
+Plan plan(const e2ttt_delta_desc* d, bool save) {
+  Plan p{};
+  p.bf = d->io == E2TTT_DT_BF16;
+  p.U = (long)d->B * d->H;
+  p.NC = ((long)d->T + kDC - 1) / kDC;
+  const int dkp = delta_dkp(d->dk), dvp = delta_dvp(d->dv);
+  const size_t gate = kGateFloats * sizeof(float);
+  const size_t frag = 2 * (size_t)kTriBytes;
+  p.w_bytes = 4L * dkp * dvp;
+  p.u_bytes = 4L * kDC * dvp;
+  p.nc_buf = p.NC;
+  if (!save) {
+    const long fit = (long)(kStretchBytes / ((gate + frag) * (size_t)p.U));
+    p.nc_buf = fit < 1 ? 1 : fit < p.NC ? fit : p.NC;
+  }
+  const size_t cus = (size_t)p.U * p.nc_buf;
+  p.o_gate = 0;
+  p.o_frag = up(p.o_gate + cus * gate);
+  p.o_state = up(p.o_frag + cus * frag);
+  p.o_w = up(p.o_state + (p.nc_buf < p.NC ? (size_t)p.U * d->dk * d->dv * 4 : 0));
+  p.o_u = up(p.o_w + (save ? cus * p.w_bytes : 0));
+  p.bytes = up(p.o_u + (save ? cus * p.u_bytes : 0));
+  p.s_w = 0;
+  p.s_u = up((size_t)p.U * p.NC * p.w_bytes);
+  p.scratch = up(p.s_u + (size_t)p.U * p.NC * p.u_bytes);
+  return p;
+}
+
+struct Views {
+  e2ttt_strides q, k, v, out, eta, gam, d_out, dq, dk, dv, deta, dgam;
+};
+e2ttt_status check_views(const e2ttt_delta_desc* d, const e2ttt_delta_strides* s, bool bwd,
+                         bool gam, Views* o) {
+  const long elt = d->io == E2TTT_DT_BF16 ? 2 : 4;
+  const long B = d->B, HK = d->HK, H = d->H, T = d->T;
+  o->q = strides_of(s ? &s->q : nullptr, HK, T, d->dk);
+  o->k = strides_of(s ? &s->k : nullptr, HK, T, d->dk);
+  o->v = strides_of(s ? &s->v : nullptr, H, T, d->dv);
+  o->out = strides_of(s ? &s->out : nullptr, H, T, d->dv);
+  o->eta = strides_of(s ? &s->eta : nullptr, H, T, 1);
+  o->gam = strides_of(s ? &s->log_gamma : nullptr, H, T, 1);
+  o->d_out = strides_of(s ? &s->d_out : nullptr, H, T, d->dv);
+  o->dq = strides_of(s ? &s->dq : nullptr, HK, T, d->dk);
+  o->dk = strides_of(s ? &s->dk : nullptr, HK, T, d->dk);
+  o->dv = strides_of(s ? &s->dv : nullptr, H, T, d->dv);
+  o->deta = strides_of(s ? &s->d_eta : nullptr, H, T, 1);
+  o->dgam = strides_of(s ? &s->d_log_gamma : nullptr, H, T, 1);
+  bool ok = rows_ok(o->q, elt, true) && rows_ok(o->k, elt, true) && rows_ok(o->v, elt, true) &&
+            rows_ok(o->eta, 4, false) && (!gam || rows_ok(o->gam, 4, false));
+  if (!bwd)
+    ok = ok && rows_ok(o->out, elt, true) && disjoint(o->out, B, H, T, d->dv);
+  else
+    ok = ok && rows_ok(o->d_out, elt, true) && rows_ok(o->dq, elt, true) &&
+         rows_ok(o->dk, elt, true) && rows_ok(o->dv, elt, true) && rows_ok(o->deta, 4, false) &&
+         disjoint(o->dq, B, HK, T, d->dk) && disjoint(o->dk, B, HK, T, d->dk) &&
+         disjoint(o->dv, B, H, T, d->dv) && disjoint(o->deta, B, H, T, 1) &&
+         (!gam || (rows_ok(o->dgam, 4, false) && disjoint(o->dgam, B, H, T, 1)));
+  return ok ? E2TTT_OK : E2TTT_ERR_BAD_SHAPE;
+}
+
+void fill(DeltaArgs& a, const e2ttt_delta_desc* d, const Plan& p, char* ws) {
+  a.B = d->B; a.HK = d->HK; a.H = d->H; a.T = d->T;
+  a.dk = d->dk; a.dv = d->dv; a.dvp = delta_dvp(d->dv);
+  a.NC = (int)p.NC;
+  a.nc_buf = (int)p.nc_buf;
+  a.scale = d->scale;
+  a.gate = reinterpret_cast<float*>(ws + p.o_gate);
+  a.frag = ws + p.o_frag;
+  a.wst = reinterpret_cast<float*>(ws + p.o_w);
+  a.ust = reinterpret_cast<float*>(ws + p.o_u);
+}
+
+}  // namespace
+}  // namespace e2ttt
+
+using namespace e2ttt;
+
+extern "C" size_t e2ttt_delta_workspace_bytes(const e2ttt_delta_desc* desc, int save_for_backward) {
+  return check_desc(desc) == E2TTT_OK ? plan(desc, save_for_backward != 0).bytes : 0;
+}
+
+extern "C" size_t e2ttt_delta_scratch_bytes(const e2ttt_delta_desc* desc) {
+  return check_desc(desc) == E2TTT_OK ? plan(desc, true).scratch : 0;
+}
+
+extern "C" e2ttt_status e2ttt_delta_forward(const e2ttt_delta_desc* desc,
+                                            const e2ttt_delta_strides* strides, const void* q,
+                                            const void* k, const void* v, const float* eta,
+                                            const float* log_gamma, const int32_t* lengths,
+                                            const float* w_in, void* out, float* w_out,
+                                            void* workspace, size_t workspace_bytes,
+                                            int save_for_backward, void* stream) {
+  e2ttt_status st = check_desc(desc);
+  if (st != E2TTT_OK) return st;
+  if (!q || !k || !v || !eta || !out || !workspace) return E2TTT_ERR_NULL_ARG;
+  Views vw;
+  if ((st = check_views(desc, strides, false, log_gamma != nullptr, &vw)) != E2TTT_OK) return st;
+  if (misaligned(q) || misaligned(k) || misaligned(v) || misaligned(out) || misaligned(w_in) ||
+      misaligned(w_out) || misaligned(workspace))
+    return E2TTT_ERR_BAD_SHAPE;
+  const Plan p = plan(desc, save_for_backward != 0);
+  if (workspace_bytes < p.bytes) return E2TTT_ERR_WORKSPACE_TOO_SMALL;
+  char* ws = static_cast<char*>(workspace);
+  DeltaArgs a{};
+  fill(a, desc, p, ws);
+  a.q = view(q, vw.q); a.k = view(k, vw.k); a.v = view(v, vw.v); a.out = view(out, vw.out);
+  a.eta = view(eta, vw.eta); a.gam = view(log_gamma, vw.gam);
+  a.lengths = lengths;
+  float* carry = reinterpret_cast<float*>(ws + p.o_state);
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  for (long r0 = 0; r0 < p.NC; r0 += p.nc_buf) {
+    a.r0 = a.r_base = (int)r0;
+    a.r1 = (int)(r0 + p.nc_buf < p.NC ? r0 + p.nc_buf : p.NC);
+    a.w_in = r0 == 0 ? w_in : carry;
+    a.w_out = a.r1 == p.NC ? w_out : carry;
+    if (launch_delta_prep(a, p.bf, s) != hipSuccess ||
+        launch_delta_chain(a, p.bf, save_for_backward != 0, s) != hipSuccess)
+      return E2TTT_ERR_HIP;
+  }
+  return E2TTT_OK;
+}
+
+extern "C" e2ttt_status e2ttt_delta_backward(
+    const e2ttt_delta_desc* desc, const e2ttt_delta_strides* strides, const void* q, const void* k,
+    const void* v, const float* eta, const float* log_gamma, const int32_t* lengths,
+    const void* workspace, size_t workspace_bytes, const void* d_out, const float* d_w_out,
+    void* dq, void* dk, void* dv, float* d_eta, float* d_log_gamma, float* d_w_in, void* scratch,
+    size_t scratch_bytes, void* stream) {
+  e2ttt_status st = check_desc(desc);
+  if (st != E2TTT_OK) return st;
+  if (!q || !k || !v || !eta || !workspace || !d_out || !dq || !dk || !dv || !d_eta || !scratch)
+    return E2TTT_ERR_NULL_ARG;
+  if ((log_gamma == nullptr) != (d_log_gamma == nullptr)) return E2TTT_ERR_NULL_ARG;
+  Views vw;
+  if ((st = check_views(desc, strides, true, log_gamma != nullptr, &vw)) != E2TTT_OK) return st;
+  if (misaligned(q) || misaligned(k) || misaligned(v) || misaligned(d_out) || misaligned(dq) ||
+      misaligned(dk) || misaligned(dv) || misaligned(d_w_out) || misaligned(d_w_in) ||
+      misaligned(workspace) || misaligned(scratch))
+    return E2TTT_ERR_BAD_SHAPE;
+  const Plan p = plan(desc, true);
+  if (workspace_bytes < p.bytes || scratch_bytes < p.scratch) return E2TTT_ERR_WORKSPACE_TOO_SMALL;
+  DeltaArgs a{};
+  fill(a, desc, p, static_cast<char*>(const_cast<void*>(workspace)));
+  a.q = view(q, vw.q); a.k = view(k, vw.k); a.v = view(v, vw.v);
+  a.eta = view(eta, vw.eta); a.gam = view(log_gamma, vw.gam);
+  a.d_out = view(d_out, vw.d_out);
+  a.dq = view(dq, vw.dq); a.dkk = view(dk, vw.dk); a.dv_ = view(dv, vw.dv);
+  a.deta = view(d_eta, vw.deta); a.dgam = view(d_log_gamma, vw.dgam);
+  a.lengths = lengths;
+  a.d_w_out = d_w_out;
+  a.d_w_in = d_w_in;
+  a.dwst = reinterpret_cast<float*>(static_cast<char*>(scratch) + p.s_w);
+  a.yst = reinterpret_cast<float*>(static_cast<char*>(scratch) + p.s_u);
+  a.r0 = a.r_base = 0;
+  a.r1 = (int)p.NC;
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  if (launch_delta_chain_bwd(a, p.bf, s) != hipSuccess || launch_delta_grads(a, p.bf, s) != hipSuccess)
+    return E2TTT_ERR_HIP;
+  return E2TTT_OK;
+}
+
+extern "C" e2ttt_status e2ttt_delta_step(const e2ttt_delta_desc* desc,
+                                         const e2ttt_delta_strides* strides, const void* q,
+                                         const void* k, const void* v, const float* eta,
+                                         const float* log_gamma, float* w, const int32_t* slots,
+                                         int32_t n_slots, void* out, void* stream) {
+  e2ttt_status st = check_desc(desc);
+  if (st != E2TTT_OK) return st;
+  if (!q || !k || !v || !eta || !w || !out) return E2TTT_ERR_NULL_ARG;
+  if (n_slots <= 0 || (!slots && n_slots < desc->B)) return E2TTT_ERR_BAD_SHAPE;
+  Views vw;
+  if ((st = check_views(desc, strides, false, log_gamma != nullptr, &vw)) != E2TTT_OK) return st;
+  if (misaligned(q) || misaligned(k) || misaligned(v) || misaligned(out) || misaligned(w))
+    return E2TTT_ERR_BAD_SHAPE;
+  DeltaStepArgs a{};
+  a.q = view(q, vw.q); a.k = view(k, vw.k); a.v = view(v, vw.v); a.out = view(out, vw.out);
+  a.eta = view(eta, vw.eta); a.gam = view(log_gamma, vw.gam);
+  a.w = w; a.slots = slots; a.nslots = n_slots;
+  a.B = desc->B; a.HK = desc->HK; a.H = desc->H; a.T = desc->T;
+  a.dk = desc->dk; a.dv = desc->dv; a.scale = desc->scale;
+  return launch_delta_step(a, desc->io == E2TTT_DT_BF16, static_cast<hipStream_t>(stream)) == hipSuccess
+             ? E2TTT_OK : E2TTT_ERR_HIP;
+}

@@ -1,0 +1,353 @@
+// Shared pieces of the gated delta rule kernels (delta_*.hip).
+//
+// The rule, per unit (sequence, value head) and token, state W [dv][dk]:
+//   Wd = exp(g) W,  e = v - Wd k,  u = eta e,  W' = Wd + u k^T,  o = s W' q.
+// Over a chunk of 64 tokens with start state W_0, b_i = g_1 + .. + g_i,
+// G_i = exp(b_i), D_ij = exp(b_i - b_j) and M = strictly lower(D o K K^T):
+//   (I + diag(eta) M) U = diag(eta) R,       R = V - diag(G) K W_0^T
+//   O   = s diag(G) Q W_0^T + P U,           P = s lower(D o Q K^T)
+//   W_C = G_C W_0 + sum_j exp(b_C - b_j) u_j k_j^T
+// (unrolling W_i and collecting u_j; the system is unit lower triangular).
+// With T = (I + diag(eta) M)^-1 everything is a matrix product, T and P are
+// independent of the state (delta_prep.hip, every chunk at once), and the
+// columns of W^T (the value dimension) never meet: one wave carries 16 of
+// them through all chunks in its registers (delta_fwd.hip).
+//
+// Layouts.  MFMA tiles are 16x16; the accumulator of a tile holds, in lane
+// (g, c), rows 4 g + i (i = 0..3) of column c.  Token and key rows of tile m
+// are labelled
+//   lab(m, r) = 32 (m / 2) + 8 (r / 4) + 4 (m mod 2) + r mod 4,
+// so that the registers of tiles 2 a and 2 a + 1, joined, are eight
+// consecutive rows 32 a + 8 g .. + 7 of column c: the B operand of a product
+// that contracts over those rows.  A chain of products (K W^T -> T R -> P U ->
+// K^T U) then goes from accumulator to operand without leaving the lane.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include "e2ttt.h"
+#include "e2ttt_device.h"
+
+namespace e2ttt {
+
+constexpr int kDC = 64;           // tokens per chunk
+constexpr int kDeltaFrags = 6;    // 16x32 fragments of a lower triangular 64x64 matrix
+// Per chunk and unit: eta, eta G, s G, exp(b_C - b), then b as two floats
+// (b = bh + bl from a sum in 64 bits: differences of b keep their relative
+// accuracy however far the sum has gone), 64 each, and G_C.
+constexpr int kGateFloats = 6 * kDC + 16;
+enum { kGEta = 0, kGEtaG = kDC, kGsG = 2 * kDC, kGEnd = 3 * kDC, kGBh = 4 * kDC,
+       kGBl = 5 * kDC, kGC = 6 * kDC };
+
+// A token tensor [B][H][T][d] by its strides in elements (the last is 1).
+struct View {
+  const void* p;
+  long b, h, t;
+};
+
+struct DeltaArgs {
+  View q, k, v, eta, gam;     // gam.p nullable: no decay
+  View out;
+  View d_out, dq, dkk, dv_, deta, dgam;
+  const int* lengths;         // nullable
+  const float* w_in;          // nullable: zero
+  float* w_out;               // nullable
+  const float* d_w_out;       // nullable: zero
+  float* d_w_in;              // nullable
+  char* frag;                 // [chunk unit] T fragments, then P fragments (kTriBytes each)
+  float* gate;                // [chunk unit][kGateFloats]
+  float* wst;                 // [chunk unit][dvp][dkp] chunk-start states (saving)
+  float* ust;                 // [chunk unit][dvp][64] U^T (saving)
+  float* dwst;                // backward: chunk-end adjoint states, as wst
+  float* yst;                 // backward: Y^T, as ust
+  int B, HK, H, T, dk, dv, dvp;   // dvp: dv padded to a multiple of 32
+  int NC;                     // chunks of the whole call
+  int r0, r1;                 // chunks of this launch
+  int nc_buf;                 // chunks per unit that the buffers hold (index r - r_base)
+  int r_base;
+  float scale;
+};
+
+__device__ __forceinline__ int lab(int m, int r) {
+  return 32 * (m >> 1) + 8 * (r >> 2) + 4 * (m & 1) + (r & 3);
+}
+// Fragment (row tile m, 32-column block a <= m / 2) of a lower triangular matrix.
+__host__ __device__ constexpr int fidx(int m, int a) { return m < 2 ? m : 2 * (m - 1) + a; }
+
+// Operands.  X: a value of the io type, exact.  S: an fp32 value; with bf16 io
+// the sum of NT = 3 bf16 terms, each the rounding of what the ones before
+// leave, so that nothing is lost.  A product takes the terms whose combined
+// order is below N: with N = 3 it is an fp32 product (what is left out is
+// below 2^-24), used for all that reaches a state or a gate's gradient; with
+// N = 2 its error is at most 2^-17, far below the rounding of a bf16 output
+// (2^-9), used for what reaches such outputs only.  f32 io: fp32 MFMA.
+template <bool BF> struct DOp;
+
+template <> struct DOp<true> {
+  using E = __bf16;
+  static constexpr int NT = 3;
+  struct X { bf16x8 v; };
+  struct S { bf16x8 t[NT]; };
+  static __device__ __forceinline__ f32x4 m1(f32x4 acc, const bf16x8& a, const bf16x8& b) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, acc, 0, 0, 0);
+  }
+  static __device__ __forceinline__ f32x4 xx(f32x4 acc, const X& a, const X& b) {
+    return m1(acc, a.v, b.v);
+  }
+  template <int N>
+  static __device__ __forceinline__ f32x4 xs(f32x4 acc, const X& a, const S& b) {
+#pragma unroll
+    for (int i = N - 1; i >= 0; --i) acc = m1(acc, a.v, b.t[i]);
+    return acc;
+  }
+  template <int N>
+  static __device__ __forceinline__ f32x4 sx(f32x4 acc, const S& a, const X& b) {
+#pragma unroll
+    for (int i = N - 1; i >= 0; --i) acc = m1(acc, a.t[i], b.v);
+    return acc;
+  }
+  template <int N>
+  static __device__ __forceinline__ f32x4 ss(f32x4 acc, const S& a, const S& b) {
+#pragma unroll
+    for (int n = N - 1; n >= 0; --n)
+#pragma unroll
+      for (int i = 0; i <= n; ++i) acc = m1(acc, a.t[i], b.t[n - i]);
+    return acc;
+  }
+  template <int N>
+  static __device__ __forceinline__ S split(f32x4 x, f32x4 y) {
+    S s;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const bf16x8 r = {(__bf16)x[0], (__bf16)x[1], (__bf16)x[2], (__bf16)x[3],
+                        (__bf16)y[0], (__bf16)y[1], (__bf16)y[2], (__bf16)y[3]};
+      s.t[i] = r;
+      if (i + 1 < N) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          x[e] -= (float)r[e];
+          y[e] -= (float)r[4 + e];
+        }
+      }
+    }
+    return s;
+  }
+  static __device__ __forceinline__ X exact(f32x4 x, f32x4 y) {   // values of the io type
+    return X{bf16x8{(__bf16)x[0], (__bf16)x[1], (__bf16)x[2], (__bf16)x[3], (__bf16)y[0],
+                    (__bf16)y[1], (__bf16)y[2], (__bf16)y[3]}};
+  }
+};
+
+template <> struct DOp<false> {
+  using E = float;
+  static constexpr int NT = 1;
+  struct X { f32x4 a, b; };
+  using S = X;
+  static __device__ __forceinline__ f32x4 xx(f32x4 acc, const X& p, const X& q) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(p.a[e], q.a[e], acc, 0, 0, 0);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(p.b[e], q.b[e], acc, 0, 0, 0);
+    return acc;
+  }
+  template <int N>
+  static __device__ __forceinline__ f32x4 xs(f32x4 acc, const X& p, const X& q) { return xx(acc, p, q); }
+  template <int N>
+  static __device__ __forceinline__ f32x4 sx(f32x4 acc, const X& p, const X& q) { return xx(acc, p, q); }
+  template <int N>
+  static __device__ __forceinline__ f32x4 ss(f32x4 acc, const X& p, const X& q) { return xx(acc, p, q); }
+  template <int N>
+  static __device__ __forceinline__ S split(f32x4 x, f32x4 y) { return S{x, y}; }
+  static __device__ __forceinline__ X exact(f32x4 x, f32x4 y) { return X{x, y}; }
+};
+
+// A lower triangular 64x64 matrix in global memory: fp32 fragments, the two
+// halves of a lane's eight values at lane * 16 and 1024 + lane * 16.
+constexpr int kFragBytes = 2048;
+constexpr int kTriBytes = kDeltaFrags * kFragBytes;
+// The same in LDS as N terms: all fragments of a term, then of the next.
+template <bool BF> constexpr int tri_lds(int n) { return BF ? n * kDeltaFrags * 1024 : kTriBytes; }
+
+__device__ __forceinline__ void st_frag(char* base, int f, int lane, f32x4 x, f32x4 y) {
+  char* p = base + f * kFragBytes + lane * 16;
+  *reinterpret_cast<f32x4*>(p) = x;
+  *reinterpret_cast<f32x4*>(p + 1024) = y;
+}
+// One lane's part (slot: 64 fragment + lane) into LDS.
+template <bool BF, int N>
+__device__ __forceinline__ void put_frag(char* lds, int slot, f32x4 x, f32x4 y) {
+  if constexpr (BF) {
+    const auto s = DOp<true>::split<N>(x, y);
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      *reinterpret_cast<bf16x8*>(lds + (i * kDeltaFrags * 64 + slot) * 16) = s.t[i];
+  } else {
+    st_frag(lds, slot >> 6, slot & 63, x, y);
+  }
+}
+template <bool BF, int N>
+__device__ __forceinline__ typename DOp<BF>::S ld_frag(const char* lds, int f, int lane) {
+  typename DOp<BF>::S s;
+  if constexpr (BF) {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      s.t[i] = *reinterpret_cast<const bf16x8*>(lds + ((i * kDeltaFrags + f) * 64 + lane) * 16);
+  } else {
+    s.a = *reinterpret_cast<const f32x4*>(lds + f * kFragBytes + lane * 16);
+    s.b = *reinterpret_cast<const f32x4*>(lds + f * kFragBytes + 1024 + lane * 16);
+  }
+  return s;
+}
+
+// One transposing LDS read: within each group of 16 lanes, lane c receives
+// element c mod 4 of the quads addressed by lanes 4 r + c / 4, r = 0..3.
+__device__ __forceinline__ bf16x4 lds_tr4(const __bf16* p) {
+  typedef short s4 __attribute__((ext_vector_type(4)));
+  typedef __attribute__((address_space(3))) s4* lds_s4;
+  return __builtin_bit_cast(
+      bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4) const_cast<__bf16*>(p)));
+}
+__device__ __forceinline__ bf16x8 cat8(const bf16x4& a, const bf16x4& b) {
+  return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+
+// Fragment of the transpose of a lower triangular matrix in LDS: rows j =
+// lab(m, c), contraction over i = 32 a + 8 g .. + 7, a >= m / 2.  Element
+// (i, j) sits in fragment (2 a + (i / 4) mod 2, m / 2), lane group
+// (j mod 32) / 8, lane 4 g + i mod 4, slot j mod 8.
+template <bool BF, int N>
+__device__ __forceinline__ typename DOp<BF>::S ld_frag_t(const char* lds, int m, int a, int g,
+                                                          int c) {
+  typename DOp<BF>::S s;
+  if constexpr (BF) {
+    const int r = c >> 2, cq = c & 3;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      bf16x4 h[2];
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+        h[x] = lds_tr4(reinterpret_cast<const __bf16*>(lds) +
+                       ((i * kDeltaFrags + fidx(2 * a + x, m >> 1)) * 64 + 16 * cq + 4 * g + r) * 8 +
+                       4 * (m & 1));
+      s.t[i] = cat8(h[0], h[1]);
+    }
+  } else {
+    const int gj = c >> 2, sj = 4 * (m & 1) + (c & 3);   // lane group and slot of column j
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int at = (16 * gj + 4 * g + e) * 16 + (sj >> 2) * 1024 + (sj & 3) * 4;
+      s.a[e] = *reinterpret_cast<const float*>(lds + fidx(2 * a, m >> 1) * kFragBytes + at);
+      s.b[e] = *reinterpret_cast<const float*>(lds + fidx(2 * a + 1, m >> 1) * kFragBytes + at);
+    }
+  }
+  return s;
+}
+
+// A tile of rows of D elements of the io type in LDS, in 16-byte pieces;
+// piece p of a row lies at p XOR a function of the row, so that the 16 rows of
+// a fragment read (which differ in row bits 0, 1, 3, 4) touch different banks.
+template <bool BF, int D>
+struct LTile {
+  using E = typename DOp<BF>::E;
+  static constexpr int PE = 16 / (int)sizeof(E);     // elements of a piece
+  static constexpr int NP = D / PE;                  // pieces of a row
+  static __device__ __forceinline__ int at(int row, int p) {   // element index of a piece
+    const int f = ((row & 3) | ((row >> 1) & 12)) & (NP - 1);
+    return (row * NP + (p ^ f)) * PE;
+  }
+  // row `row`, columns 32 kt + 8 g .. + 7
+  static __device__ __forceinline__ typename DOp<BF>::X frag(const E* t, int row, int kt, int g) {
+    typename DOp<BF>::X x;
+    if constexpr (BF) {
+      x.v = *reinterpret_cast<const bf16x8*>(t + at(row, 4 * kt + g));
+    } else {
+      x.a = *reinterpret_cast<const f32x4*>(t + at(row, 8 * kt + 2 * g));
+      x.b = *reinterpret_cast<const f32x4*>(t + at(row, 8 * kt + 2 * g + 1));
+    }
+    return x;
+  }
+  // Rows 32 a + 8 g .. + 7 of one column: lab(m, c) or, natural, 16 m + c.
+  template <bool NAT = false>
+  static __device__ __forceinline__ typename DOp<BF>::X frag_t(const E* t, int m, int a, int g,
+                                                               int c) {
+    typename DOp<BF>::X x;
+    if constexpr (BF) {
+      const int row = 32 * a + 8 * g + (c >> 2);
+      const int p = NAT ? 2 * m + ((c & 3) >> 1) : 4 * (m >> 1) + (c & 3);
+      const int e = NAT ? 4 * (c & 1) : 4 * (m & 1);
+      x.v = cat8(lds_tr4(t + at(row, p) + e), lds_tr4(t + at(row + 4, p) + e));
+    } else {
+      const int col = NAT ? 16 * m + c : lab(m, c), p = col >> 2, e4 = col & 3;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        x.a[e] = t[at(32 * a + 8 * g + e, p) + e4];
+        x.b[e] = t[at(32 * a + 8 * g + 4 + e, p) + e4];
+      }
+    }
+    return x;
+  }
+};
+
+// The same from the terms of an S operand, each a tile `plane` elements on.
+template <bool BF, int D, bool NAT>
+__device__ __forceinline__ typename DOp<BF>::S terms_t(const typename DOp<BF>::E* t, int plane,
+                                                        int m, int g, int c) {
+  if constexpr (BF) {
+    typename DOp<BF>::S s;
+#pragma unroll
+    for (int i = 0; i < DOp<BF>::NT; ++i)
+      s.t[i] = LTile<BF, D>::template frag_t<NAT>(t + plane * i, m, 0, g, c).v;
+    return s;
+  } else {
+    return LTile<BF, D>::template frag_t<NAT>(t, m, 0, g, c);
+  }
+}
+// Eight fp32 values of such a tile's row (columns 8 p8 ..) into LDS as terms.
+template <bool BF, int D>
+__device__ __forceinline__ void put_terms(typename DOp<BF>::E* t, int plane, int row, int p8,
+                                          f32x4 x, f32x4 y) {
+  using L = LTile<BF, D>;
+  if constexpr (BF) {
+    const auto s = DOp<true>::split<DOp<true>::NT>(x, y);
+#pragma unroll
+    for (int i = 0; i < DOp<true>::NT; ++i)
+      *reinterpret_cast<bf16x8*>(t + plane * i + L::at(row, p8)) = s.t[i];
+  } else {
+    *reinterpret_cast<f32x4*>(t + L::at(row, 2 * p8)) = x;
+    *reinterpret_cast<f32x4*>(t + L::at(row, 2 * p8 + 1)) = y;
+  }
+}
+
+template <class E>
+__device__ __forceinline__ const E* row_of(const View& v, int b, int h, int t) {
+  return static_cast<const E*>(v.p) + (b * v.b + h * v.h + t * v.t);
+}
+template <class E>
+__device__ __forceinline__ E* row_of_w(const View& v, int b, int h, int t) {
+  return static_cast<E*>(const_cast<void*>(v.p)) + (b * v.b + h * v.h + t * v.t);
+}
+// Tokens of sequence b that the call takes.
+__device__ __forceinline__ int live_tokens(const DeltaArgs& a, int b) {
+  return a.lengths ? max(0, min(a.T, a.lengths[b])) : a.T;
+}
+
+struct DeltaStepArgs {
+  View q, k, v, eta, gam, out;
+  float* w;
+  const int* slots;      // nullable: sequence b at state b
+  int nslots;
+  int B, HK, H, T, dk, dv;
+  float scale;
+};
+
+// -------------------------------------------------------------- launchers
+hipError_t launch_delta_step(const DeltaStepArgs& a, bool bf, hipStream_t stream);
+hipError_t launch_delta_prep(const DeltaArgs& a, bool bf, hipStream_t stream);
+hipError_t launch_delta_chain(const DeltaArgs& a, bool bf, bool save, hipStream_t stream);
+hipError_t launch_delta_chain_bwd(const DeltaArgs& a, bool bf, hipStream_t stream);
+hipError_t launch_delta_grads(const DeltaArgs& a, bool bf, hipStream_t stream);
+// padded key dimension (32, 64 or 128) and value dimension (a multiple of 32)
+inline int delta_dkp(int dk) { return dk <= 32 ? 32 : dk <= 64 ? 64 : 128; }
+inline int delta_dvp(int dv) { return (dv + 31) & ~31; }
+
+}  // namespace e2ttt

@@ -1,0 +1,304 @@
+// Preparation of queries and keys (e2ttt_qk_forward / e2ttt_qk_backward): per
+// row x of d elements, each step optional,
+//   s = SiLU(x),   y = s / sqrt(sum s^2 + eps),
+//   z = y with its first `rot` elements turned: for pair p of channels (a, b),
+//       z_a = m (y_a cos - y_b sin),  z_b = m (y_b cos + y_a sin),
+//       angle = position * inv_freq[p],  m = rot_scale.
+// The backward turns dz back (the transposed map), then with r = 1 / sqrt(..)
+//   ds = r (dy - s r^2 (s . dy)),  dx = ds sigma(x) (1 + x (1 - sigma(x))).
+//
+// Bound by HBM: each element is read once (twice in the backward, with its
+// gradient) and written once.  An item is the two pieces of V elements that hold V whole
+// pairs (p and p + rot / 2 of a half layout, neighbours otherwise), so a pair
+// never leaves its lane; V is the widest that divides rot / 2 (16 bytes for
+// the usual head).  The lanes of a row sum by shuffles.  A group of lanes
+// keeps its angles' sines and cosines over several heads of a token.  Angles
+// are reduced in 64 bits: a far position times a frequency loses its fraction
+// of a turn in 32.
+#include <math.h>
+
+#include "delta_common.h"
+#include "e2ttt.h"
+#include "strided.h"
+
+namespace e2ttt {
+namespace {
+
+struct QkArgs {
+  View x[2], y[2], g[2];      // queries, keys: input, output (gradient of x), gradient of z
+  const float* inv_freq;
+  const int64_t* pos;         // nullable: 0 .. T - 1
+  int B, T, d, half;          // half: pairs that turn (rot / 2)
+  int nh[2];                  // heads of queries and keys
+  int hpg, nhg;               // heads of a group of lanes, groups of heads
+  int lanes;                  // lanes of a row (a power of two)
+  int tfast;                  // neighbouring groups: tokens (else heads)
+  float eps, m;
+};
+
+template <class E, int V> struct Piece { typedef __attribute__((ext_vector_type(V))) E T; };
+template <class E> struct Piece<E, 1> { typedef E T; };
+
+template <class E, int V>
+__device__ __forceinline__ void ld_piece(float (&o)[V], const E* p) {
+  const auto x = *reinterpret_cast<const typename Piece<E, V>::T*>(p);
+  if constexpr (V == 1) {
+    o[0] = (float)x;
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i) o[i] = (float)x[i];
+  }
+}
+template <class E, int V>
+__device__ __forceinline__ void st_piece(E* p, const float (&v)[V]) {
+  typename Piece<E, V>::T x;
+  if constexpr (V == 1) {
+    x = (E)v[0];
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i) x[i] = (E)v[i];
+  }
+  *reinterpret_cast<typename Piece<E, V>::T*>(p) = x;
+}
+
+// IPL: items of a lane.
+template <bool BF, int V, int IPL, bool BWD>
+__global__ void __launch_bounds__(256) qk_kernel(QkArgs a, unsigned flags) {
+  using E = typename DOp<BF>::E;
+  const long gid = ((long)blockIdx.x * 256 + threadIdx.x) / a.lanes;
+  const int l = threadIdx.x & (a.lanes - 1);
+  const long ntok = (long)a.B * a.T;
+  if (gid >= ntok * a.nhg) return;          // whole rows of lanes leave together
+  const long tok = a.tfast ? gid % ntok : gid / a.nhg;
+  const int hg = (int)(a.tfast ? gid / ntok : gid % a.nhg);
+  const int b = (int)(tok / a.T), t = (int)(tok % a.T);
+  const bool silu = flags & E2TTT_QK_SILU, unit = flags & E2TTT_QK_UNIT;
+  const bool inter = flags & E2TTT_QK_INTERLEAVED;
+  const int np = a.half / V;                // items that turn
+  const int ntail = (a.d - 2 * a.half) / V; // pieces that do not
+
+  int c0[IPL], c1[IPL];                     // first elements of an item's pieces (-1: none)
+  float co[IPL][V], si[IPL][V];
+#pragma unroll
+  for (int x = 0; x < IPL; ++x) {
+    const int it = l + x * a.lanes;
+    c0[x] = c1[x] = -1;
+    if (it < np) {
+      c0[x] = inter ? 2 * it * V : it * V;
+      c1[x] = inter ? c0[x] + V : c0[x] + a.half;
+      const double p = a.pos ? (double)a.pos[tok] : (double)t;
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        double turns = p * (double)a.inv_freq[it * V + i] * 0.15915494309189535;
+        turns -= rint(turns);
+        const float f = 2.0f * (float)turns;
+        co[x][i] = a.m * cospif(f);
+        si[x][i] = a.m * sinpif(f);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        co[x][i] = 1.0f;
+        si[x][i] = 0.0f;
+      }
+      const int q = 2 * (it - np);
+      if (q < ntail) c0[x] = 2 * a.half + q * V;
+      if (q + 1 < ntail) c1[x] = 2 * a.half + (q + 1) * V;
+    }
+  }
+
+  const int nh = a.nh[0] + a.nh[1];
+  for (int hh = hg * a.hpg; hh < min(nh, (hg + 1) * a.hpg); ++hh) {
+    const int s = hh >= a.nh[0], h = s ? hh - a.nh[0] : hh;
+    const E* xp = row_of<E>(a.x[s], b, h, t);
+    E* yp = row_of_w<E>(a.y[s], b, h, t);
+    float u[IPL][2][V], z[IPL][2][V];       // x, then SiLU(x); the gradient
+    float ss = 0.0f, sd = 0.0f;
+#pragma unroll
+    for (int x = 0; x < IPL; ++x)
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const int at = k ? c1[x] : c0[x];
+#pragma unroll
+        for (int i = 0; i < V; ++i) u[x][k][i] = z[x][k][i] = 0.0f;
+        if (at >= 0) {
+          if (!BWD || silu || unit) ld_piece<E, V>(u[x][k], xp + at);
+          if (BWD) ld_piece<E, V>(z[x][k], row_of<E>(a.g[s], b, h, t) + at);
+        }
+      }
+    float raw[IPL][2][V];
+#pragma unroll
+    for (int x = 0; x < IPL; ++x) {
+      if (BWD) {                            // back through the turn
+        if (l + x * a.lanes < np) {
+#pragma unroll
+          for (int i = 0; i < V; ++i) {
+            float& p = inter ? z[x][(2 * i) / V][(2 * i) % V] : z[x][0][i];
+            float& q = inter ? z[x][(2 * i + 1) / V][(2 * i + 1) % V] : z[x][1][i];
+            const float za = p, zb = q;
+            p = za * co[x][i] + zb * si[x][i];
+            q = zb * co[x][i] - za * si[x][i];
+          }
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          raw[x][k][i] = u[x][k][i];
+          if (silu) u[x][k][i] = u[x][k][i] / (1.0f + expf(-u[x][k][i]));
+          ss = fmaf(u[x][k][i], u[x][k][i], ss);
+          if (BWD) sd = fmaf(u[x][k][i], z[x][k][i], sd);
+        }
+    }
+    float r = 1.0f;
+    if (unit) {
+      for (int o = 1; o < a.lanes; o <<= 1) {
+        ss += __shfl_xor(ss, o);
+        if (BWD) sd += __shfl_xor(sd, o);
+      }
+      r = 1.0f / sqrtf(ss + a.eps);
+    }
+#pragma unroll
+    for (int x = 0; x < IPL; ++x) {
+      if (BWD) {
+        const float f = unit ? sd * r * r : 0.0f;
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+          for (int i = 0; i < V; ++i) {
+            float y = r * (z[x][k][i] - u[x][k][i] * f);
+            if (silu) {
+              const float sg = 1.0f / (1.0f + expf(-raw[x][k][i]));
+              y *= sg * (1.0f + raw[x][k][i] * (1.0f - sg));
+            }
+            u[x][k][i] = y;
+          }
+      } else {
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+          for (int i = 0; i < V; ++i) u[x][k][i] *= r;
+        if (l + x * a.lanes < np) {
+#pragma unroll
+          for (int i = 0; i < V; ++i) {
+            float& p = inter ? u[x][(2 * i) / V][(2 * i) % V] : u[x][0][i];
+            float& q = inter ? u[x][(2 * i + 1) / V][(2 * i + 1) % V] : u[x][1][i];
+            const float ya = p, yb = q;
+            p = ya * co[x][i] - yb * si[x][i];
+            q = yb * co[x][i] + ya * si[x][i];
+          }
+        }
+      }
+      if (c0[x] >= 0) st_piece<E, V>(yp + c0[x], u[x][0]);
+      if (c1[x] >= 0) st_piece<E, V>(yp + c1[x], u[x][1]);
+    }
+  }
+}
+
+template <bool BF, int V, bool BWD>
+hipError_t go(QkArgs a, unsigned flags, hipStream_t s) {
+  const int items = a.half / V + ((a.d - 2 * a.half) / V + 1) / 2;
+  a.lanes = 1;
+  while (a.lanes < items && a.lanes < 64) a.lanes *= 2;
+  const long rows = (long)a.B * a.T * (a.nh[0] + a.nh[1]);
+  // Several heads to a group of lanes (their angles are the same) as long as
+  // the card stays full: 256 CUs of 2048 lanes.
+  a.hpg = 1;
+  while (a.hpg < 8 && rows / (2 * a.hpg) * a.lanes >= 256L * 2048) a.hpg *= 2;
+  a.nhg = (a.nh[0] + a.nh[1] + a.hpg - 1) / a.hpg;
+  const long blocks = ((long)a.B * a.T * a.nhg * a.lanes + 255) / 256;
+  if (blocks > 0x7fffffffL) return hipErrorInvalidValue;
+  // (d <= 256: only single pairs to a piece can make more than 64 items)
+  constexpr int kMost = V == 1 ? 2 : 1;
+  if (items <= 64)
+    hipLaunchKernelGGL((qk_kernel<BF, V, 1, BWD>), dim3((unsigned)blocks), dim3(256), 0, s, a, flags);
+  else
+    hipLaunchKernelGGL((qk_kernel<BF, V, kMost, BWD>), dim3((unsigned)blocks), dim3(256), 0, s, a, flags);
+  return hipGetLastError();
+}
+
+template <bool BWD>
+hipError_t launch(const QkArgs& a, bool bf, unsigned flags, hipStream_t s) {
+  const int h = a.half;
+  if (bf && h % 8 == 0) return go<true, 8, BWD>(a, flags, s);
+  if (h % 4 == 0) return bf ? go<true, 4, BWD>(a, flags, s) : go<false, 4, BWD>(a, flags, s);
+  if (h % 2 == 0) return bf ? go<true, 2, BWD>(a, flags, s) : go<false, 2, BWD>(a, flags, s);
+  return bf ? go<true, 1, BWD>(a, flags, s) : go<false, 1, BWD>(a, flags, s);
+}
+
+constexpr unsigned kFlags = E2TTT_QK_SILU | E2TTT_QK_UNIT | E2TTT_QK_INTERLEAVED;
+
+e2ttt_status check_desc(const e2ttt_qk_desc* d) {
+  if (!d) return E2TTT_ERR_NULL_ARG;
+  if (d->B <= 0 || d->H <= 0 || d->HK < 0 || d->T <= 0 || d->d <= 0 || d->rot < 0 ||
+      d->rot > d->d || d->rot % 2)
+    return E2TTT_ERR_BAD_SHAPE;
+  if (!isfinite(d->rot_scale) || ((d->flags & E2TTT_QK_UNIT) && !(isfinite(d->eps) && d->eps > 0.0f)))
+    return E2TTT_ERR_BAD_SHAPE;
+  if ((d->io != E2TTT_DT_F32 && d->io != E2TTT_DT_BF16) || (d->flags & ~kFlags) || d->d % 8 ||
+      d->d > 256 || (double)d->B * d->T * ((double)d->H + d->HK) > 1e9)
+    return E2TTT_ERR_UNSUPPORTED;
+  return E2TTT_OK;
+}
+
+QkArgs args_of(const e2ttt_qk_desc* d, const float* inv_freq, const int64_t* pos) {
+  QkArgs a{};
+  a.B = d->B; a.T = d->T; a.d = d->d; a.half = d->rot / 2;
+  a.nh[0] = d->H; a.nh[1] = d->HK;
+  a.inv_freq = inv_freq; a.pos = pos;
+  a.eps = d->eps; a.m = d->rot_scale;
+  return a;
+}
+
+}  // namespace
+}  // namespace e2ttt
+
+using namespace e2ttt;
+
+extern "C" e2ttt_status e2ttt_qk_forward(const e2ttt_qk_desc* desc, const e2ttt_qk_strides* strides,
+                                         const void* q, const void* k, const float* inv_freq,
+                                         const int64_t* positions, void* q_out, void* k_out,
+                                         void* stream) {
+  e2ttt_status st = check_desc(desc);
+  if (st != E2TTT_OK) return st;
+  const bool ks = desc->HK > 0;
+  if (!q || !q_out || (ks && (!k || !k_out)) || (desc->rot && !inv_freq)) return E2TTT_ERR_NULL_ARG;
+  QkArgs a = args_of(desc, inv_freq, positions);
+  const RowSpec in{desc->B, desc->T, desc->d, desc->io};
+  if (!in.read(strides ? &strides->q : nullptr, q, desc->H, &a.x[0]) ||
+      !in.write(strides ? &strides->q_out : nullptr, q_out, desc->H, &a.y[0]) ||
+      (ks && (!in.read(strides ? &strides->k : nullptr, k, desc->HK, &a.x[1]) ||
+              !in.write(strides ? &strides->k_out : nullptr, k_out, desc->HK, &a.y[1]))))
+    return E2TTT_ERR_BAD_SHAPE;
+  a.tfast = a.x[0].t < a.x[0].h;
+  return launch<false>(a, desc->io == E2TTT_DT_BF16, desc->flags, static_cast<hipStream_t>(stream)) ==
+                 hipSuccess ? E2TTT_OK : E2TTT_ERR_HIP;
+}
+
+extern "C" e2ttt_status e2ttt_qk_backward(const e2ttt_qk_desc* desc,
+                                          const e2ttt_qk_strides* strides, const void* q,
+                                          const void* k, const float* inv_freq,
+                                          const int64_t* positions, const void* d_q_out,
+                                          const void* d_k_out, void* dq, void* dk, void* stream) {
+  e2ttt_status st = check_desc(desc);
+  if (st != E2TTT_OK) return st;
+  const bool ks = desc->HK > 0;
+  const bool need = desc->flags & (E2TTT_QK_SILU | E2TTT_QK_UNIT);   // x itself
+  if ((need && (!q || (ks && !k))) || !d_q_out || !dq || (ks && (!d_k_out || !dk)) ||
+      (desc->rot && !inv_freq))
+    return E2TTT_ERR_NULL_ARG;
+  QkArgs a = args_of(desc, inv_freq, positions);
+  const RowSpec in{desc->B, desc->T, desc->d, desc->io};
+  const bool ok =
+      (!need || in.read(strides ? &strides->q : nullptr, q, desc->H, &a.x[0])) &&
+      in.read(strides ? &strides->d_q_out : nullptr, d_q_out, desc->H, &a.g[0]) &&
+      in.write(strides ? &strides->dq : nullptr, dq, desc->H, &a.y[0]) &&
+      (!ks || ((!need || in.read(strides ? &strides->k : nullptr, k, desc->HK, &a.x[1])) &&
+               in.read(strides ? &strides->d_k_out : nullptr, d_k_out, desc->HK, &a.g[1]) &&
+               in.write(strides ? &strides->dk : nullptr, dk, desc->HK, &a.y[1])));
+  if (!ok) return E2TTT_ERR_BAD_SHAPE;
+  a.tfast = a.g[0].t < a.g[0].h;
+  return launch<true>(a, desc->io == E2TTT_DT_BF16, desc->flags, static_cast<hipStream_t>(stream)) ==
+                 hipSuccess ? E2TTT_OK : E2TTT_ERR_HIP;
+}

@@ -8,9 +8,10 @@ on a machine without the built library raises immediately.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 from dataclasses import dataclass
-from functools import cached_property
+from functools import cached_property, lru_cache
 
 import torch
 
@@ -25,6 +26,9 @@ FLAG_NO_RESIDUAL_LN = 1
 FLAG_CHUNK_AVERAGED = 2
 FLAG_LN_AFFINE = 4
 FLAG_POST_NORM = 8       # post-chunk L2 normalisation of the fast-weight rows (App. B.1)
+QK_SILU = 1              # steps of the query/key preparation
+QK_UNIT = 2
+QK_INTERLEAVED = 4
 
 STATUS = {0: "ok", 1: "null argument", 2: "bad shape", 3: "unsupported",
           4: "workspace too small", 5: "HIP error", 6: "device-side wait expired"}
@@ -34,7 +38,9 @@ EXPORTS = ("e2ttt_param_count", "e2ttt_workspace_bytes", "e2ttt_backward_scratch
            "e2ttt_chunk_forward", "e2ttt_chunk_backward", "e2ttt_chunk_coeffs",
            "e2ttt_apply", "e2ttt_gates_forward", "e2ttt_gates_backward", "e2ttt_wait_status",
            "e2ttt_chunk_forward_static", "e2ttt_chunk_forward_ln", "e2ttt_chunk_backward_ln",
-           "e2ttt_apply_ln", "e2ttt_status_str")
+           "e2ttt_apply_ln", "e2ttt_delta_workspace_bytes", "e2ttt_delta_scratch_bytes",
+           "e2ttt_delta_forward", "e2ttt_delta_backward", "e2ttt_delta_step",
+           "e2ttt_qk_forward", "e2ttt_qk_backward", "e2ttt_status_str")
 
 
 class E2TTTError(RuntimeError):
@@ -57,6 +63,29 @@ class GateParams(ctypes.Structure):
 
     def __init__(self, eta_base=0.01, alpha_base=0.1, tau=32.0):
         super().__init__(eta_base, alpha_base, tau)
+
+
+class Strides(ctypes.Structure):
+    _fields_ = [("b", ctypes.c_int64), ("h", ctypes.c_int64), ("t", ctypes.c_int64)]
+
+
+class DeltaDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("B", "HK", "H", "T", "dk", "dv", "io")]
+    _fields_ += [("scale", ctypes.c_float)]
+
+
+class DeltaStrides(ctypes.Structure):
+    _fields_ = [(n, Strides) for n in ("q", "k", "v", "out", "eta", "log_gamma", "d_out", "dq",
+                                       "dk", "dv", "d_eta", "d_log_gamma")]
+
+
+class QKDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("B", "H", "HK", "T", "d", "rot", "io")]
+    _fields_ += [("flags", ctypes.c_uint32), ("eps", ctypes.c_float), ("rot_scale", ctypes.c_float)]
+
+
+class QKStrides(ctypes.Structure):
+    _fields_ = [(n, Strides) for n in ("q", "k", "q_out", "k_out", "d_q_out", "d_k_out", "dq", "dk")]
 
 
 _lib = None
@@ -102,6 +131,22 @@ def load():
     lib.e2ttt_chunk_backward_ln.restype = i
     lib.e2ttt_apply_ln.argtypes = [dp] + [vp] * 6
     lib.e2ttt_apply_ln.restype = i
+    dd, ds = ctypes.POINTER(DeltaDesc), ctypes.POINTER(DeltaStrides)
+    lib.e2ttt_delta_workspace_bytes.argtypes = [dd, i]
+    lib.e2ttt_delta_workspace_bytes.restype = sz
+    lib.e2ttt_delta_scratch_bytes.argtypes = [dd]
+    lib.e2ttt_delta_scratch_bytes.restype = sz
+    lib.e2ttt_delta_forward.argtypes = [dd, ds] + [vp] * 10 + [sz, i, vp]
+    lib.e2ttt_delta_forward.restype = i
+    lib.e2ttt_delta_backward.argtypes = [dd, ds] + [vp] * 7 + [sz] + [vp] * 9 + [sz, vp]
+    lib.e2ttt_delta_backward.restype = i
+    lib.e2ttt_delta_step.argtypes = [dd, ds] + [vp] * 7 + [ctypes.c_int32, vp, vp]
+    lib.e2ttt_delta_step.restype = i
+    qd, qs = ctypes.POINTER(QKDesc), ctypes.POINTER(QKStrides)
+    lib.e2ttt_qk_forward.argtypes = [qd, qs] + [vp] * 7
+    lib.e2ttt_qk_forward.restype = i
+    lib.e2ttt_qk_backward.argtypes = [qd, qs] + [vp] * 9
+    lib.e2ttt_qk_backward.restype = i
     lib.e2ttt_status_str.argtypes = [i]
     lib.e2ttt_status_str.restype = ctypes.c_char_p
     _lib = lib
@@ -473,3 +518,384 @@ class GatesFunction(torch.autograd.Function):
         g_eta, g_beta, g_alpha = gates_backward(ctx.params, l_eta, l_beta, l_alpha, d_eta,
                                                 d_beta, d_gamma)
         return None, g_eta, g_beta, g_alpha
+
+
+# ------------------------------------------------- gated delta rule, queries and keys
+def _strided(name, t, shape, dtype, device):
+    """Guard of the delta and qk calls before any launch: a device tensor of this
+    shape and type on `device`, contiguous in its last dimension.  Its strides
+    (None: C order)."""
+    if not isinstance(t, torch.Tensor):
+        raise ValueError("%s must be a tensor" % name)
+    if t.dtype is not dtype or t.shape != shape:
+        raise ValueError("%s: expected %s of %s, got %s of %s"
+                         % (name, tuple(shape), dtype, tuple(t.shape), t.dtype))
+    if not t.is_cuda:
+        raise ValueError("%s must be a device tensor" % name)
+    if t.get_device() != device:
+        raise ValueError("%s is on %s, expected cuda:%d" % (name, t.device, device))
+    if t.is_contiguous():
+        return None
+    st = t.stride()
+    if len(st) == 4 and st[3] != 1 and shape[3] != 1:
+        raise ValueError("%s must be contiguous in its last dimension" % name)
+    return tuple(s if n > 1 else 0 for s, n in zip(st[:3], shape))
+
+
+def _plain(name, t, shape, dtype, device):
+    """The same for a contiguous tensor (None passes)."""
+    if t is not None and _strided(name, t, shape, dtype, device) is not None:
+        raise ValueError("%s must be contiguous" % name)
+
+
+@lru_cache(maxsize=256)
+def _strides_ref(kind, *given):
+    """The strides argument for (name, shape, strides) triples; None where all are in C order."""
+    if all(st is None for _, _, st in given):
+        return None
+    s = kind()
+    for name, shape, st in given:
+        if st is None:
+            _, h, t = shape[:3]
+            inner = shape[3] if len(shape) == 4 else 1
+            st = (h * t * inner, t * inner, inner)
+        setattr(s, name, Strides(*st))
+    return ctypes.byref(s)
+
+
+def _on_device(f):
+    """The library works on the current device: make it that of the first tensor."""
+    def call(cfg, q, *args, **kw):
+        if not isinstance(q, torch.Tensor) or not q.is_cuda:
+            raise ValueError("q must be a device tensor")
+        if q.get_device() == _current_device():
+            return f(cfg, q, *args, **kw)
+        with torch.cuda.device(q.device):
+            return f(cfg, q, *args, **kw)
+    call.__name__, call.__doc__, call.__wrapped__ = f.__name__, f.__doc__, f
+    return call
+
+
+def _as_rows(g):
+    """A gradient as the library takes it: rows contiguous and on 16 bytes."""
+    if g.stride(-1) != 1 or g.data_ptr() % 16 or any(
+            s * g.element_size() % 16 for s, n in zip(g.stride()[:3], g.shape) if n > 1):
+        return g.contiguous()
+    return g
+
+
+@dataclass(frozen=True)
+class DeltaConfig:
+    """Gated delta rule: H value heads share HK key heads; o_t = scale W_t q_t."""
+    B: int
+    HK: int
+    H: int
+    T: int
+    dk: int
+    dv: int
+    io: int = DT_BF16
+    scale: float = 1.0
+
+    def desc(self) -> DeltaDesc:
+        return DeltaDesc(self.B, self.HK, self.H, self.T, self.dk, self.dv, self.io, self.scale)
+
+    @cached_property
+    def _call(self):
+        """The descriptor by reference, the io type and the tensors' shapes."""
+        return (ctypes.byref(self.desc()), torch.bfloat16 if self.io == DT_BF16 else torch.float32,
+                torch.Size((self.B, self.HK, self.T, self.dk)),
+                torch.Size((self.B, self.H, self.T, self.dv)), torch.Size((self.B, self.H, self.T)),
+                torch.Size((self.B, self.H, self.dv, self.dk)))
+
+    def __getstate__(self):
+        return {n: v for n, v in self.__dict__.items() if n != "_call"}
+
+
+def delta_workspace_bytes(cfg: DeltaConfig, save_for_backward: bool) -> int:
+    return int(load().e2ttt_delta_workspace_bytes(cfg._call[0], int(bool(save_for_backward))))
+
+
+def delta_scratch_bytes(cfg: DeltaConfig) -> int:
+    return int(load().e2ttt_delta_scratch_bytes(cfg._call[0]))
+
+
+def alloc_delta_workspace(cfg: DeltaConfig, save_for_backward: bool, device="cuda"):
+    n = delta_workspace_bytes(cfg, save_for_backward)
+    if n == 0:
+        raise E2TTTError(3, "e2ttt_delta_workspace_bytes")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def _buffer(name, t, device):
+    if t is not None:
+        _plain(name, t, t.shape, torch.uint8, device)
+
+
+@_on_device
+def delta_forward(cfg: DeltaConfig, q, k, v, eta, log_gamma=None, w_in=None, *, lengths=None,
+                  out=None, w_out=None, workspace=None, save_for_backward=False):
+    """Runs e2ttt_delta_forward on the current stream: the gated delta rule over
+    q, k [B, HK, T, dk], v [B, H, T, dv] (any strides with a contiguous last
+    dimension, such as a transposed [B, T, H, d]), eta and log_gamma [B, H, T]
+    (log_gamma None: no decay), from w_in [B, H, dv, dk] (None: zero), over the
+    first lengths [B] (int32) tokens of each sequence.  Returns (out, w_out,
+    workspace); out has v's order in memory."""
+    d, io, s_k, s_v, s_g, s_w = cfg._call
+    dev, f32 = q.get_device(), torch.float32
+    given = [("q", s_k, _strided("q", q, s_k, io, dev)), ("k", s_k, _strided("k", k, s_k, io, dev)),
+             ("v", s_v, _strided("v", v, s_v, io, dev)),
+             ("eta", s_g, _strided("eta", eta, s_g, f32, dev))]
+    if log_gamma is not None:
+        given.append(("log_gamma", s_g, _strided("log_gamma", log_gamma, s_g, f32, dev)))
+    _plain("w_in", w_in, s_w, f32, dev)
+    _plain("w_out", w_out, s_w, f32, dev)
+    _plain("lengths", lengths, s_g[:1], torch.int32, dev)
+    _buffer("workspace", workspace, dev)
+    if out is None:
+        out = torch.empty_like(v)
+    given.append(("out", s_v, _strided("out", out, s_v, io, dev)))
+    if w_out is None:
+        w_out = torch.empty(s_w, dtype=f32, device=q.device)
+    if workspace is None:
+        workspace = alloc_delta_workspace(cfg, save_for_backward, q.device)
+    st = load().e2ttt_delta_forward(d, _strides_ref(DeltaStrides, *given), _ptr(q), _ptr(k), _ptr(v),
+                                    _ptr(eta), _ptr(log_gamma), _ptr(lengths), _ptr(w_in), _ptr(out),
+                                    _ptr(w_out), _ptr(workspace), workspace.numel(),
+                                    int(bool(save_for_backward)), _stream())
+    _check(st, "e2ttt_delta_forward")
+    return out, w_out, workspace
+
+
+@_on_device
+def delta_backward(cfg: DeltaConfig, q, k, v, eta, log_gamma, workspace, d_out, d_w_out=None, *,
+                   lengths=None, grads=None, scratch=None):
+    """Runs e2ttt_delta_backward with the workspace of a saving delta_forward;
+    returns a dict of gradients (dq, dk, dv, d_eta, d_log_gamma, d_w_in)."""
+    d, io, s_k, s_v, s_g, s_w = cfg._call
+    dev, f32 = q.get_device(), torch.float32
+    if grads is None:
+        grads = dict(dq=torch.empty_like(q), dk=torch.empty_like(k), dv=torch.empty_like(v),
+                     d_eta=torch.empty_like(eta),
+                     d_log_gamma=None if log_gamma is None else torch.empty_like(log_gamma),
+                     d_w_in=torch.empty(s_w, dtype=f32, device=q.device))
+    g = grads
+    given = [("q", s_k, _strided("q", q, s_k, io, dev)), ("k", s_k, _strided("k", k, s_k, io, dev)),
+             ("v", s_v, _strided("v", v, s_v, io, dev)),
+             ("eta", s_g, _strided("eta", eta, s_g, f32, dev)),
+             ("d_out", s_v, _strided("d_out", d_out, s_v, io, dev)),
+             ("dq", s_k, _strided("dq", g["dq"], s_k, io, dev)),
+             ("dk", s_k, _strided("dk", g["dk"], s_k, io, dev)),
+             ("dv", s_v, _strided("dv", g["dv"], s_v, io, dev)),
+             ("d_eta", s_g, _strided("d_eta", g["d_eta"], s_g, f32, dev))]
+    if log_gamma is not None:
+        given += [("log_gamma", s_g, _strided("log_gamma", log_gamma, s_g, f32, dev)),
+                  ("d_log_gamma", s_g, _strided("d_log_gamma", g["d_log_gamma"], s_g, f32, dev))]
+    _plain("d_w_out", d_w_out, s_w, f32, dev)
+    _plain("d_w_in", g.get("d_w_in"), s_w, f32, dev)
+    _plain("lengths", lengths, s_g[:1], torch.int32, dev)
+    _buffer("workspace", workspace, dev)
+    _buffer("scratch", scratch, dev)
+    if scratch is None:
+        scratch = torch.empty(delta_scratch_bytes(cfg), dtype=torch.uint8, device=q.device)
+    st = load().e2ttt_delta_backward(
+        d, _strides_ref(DeltaStrides, *given), _ptr(q), _ptr(k), _ptr(v), _ptr(eta), _ptr(log_gamma),
+        _ptr(lengths), _ptr(workspace), workspace.numel(), _ptr(d_out), _ptr(d_w_out), _ptr(g["dq"]),
+        _ptr(g["dk"]), _ptr(g["dv"]), _ptr(g["d_eta"]), _ptr(g.get("d_log_gamma")),
+        _ptr(g.get("d_w_in")), _ptr(scratch), scratch.numel(), _stream())
+    _check(st, "e2ttt_delta_backward")
+    return grads
+
+
+@_on_device
+def delta_step(cfg: DeltaConfig, q, k, v, eta, log_gamma, w, *, slots=None, out=None):
+    """Runs e2ttt_delta_step on the current stream: the cfg.T arriving tokens of
+    every sequence, on states w [N, H, dv, dk] that are updated in place.
+    Sequence b is at state slots[b] (int32 device tensor; None: at state b, N >=
+    B); slots outside 0..N-1 are skipped (zero outputs), rows with the same slot
+    are taken in order."""
+    d, io, s_k, s_v, s_g, s_w = cfg._call
+    dev, f32 = q.get_device(), torch.float32
+    given = [("q", s_k, _strided("q", q, s_k, io, dev)), ("k", s_k, _strided("k", k, s_k, io, dev)),
+             ("v", s_v, _strided("v", v, s_v, io, dev)),
+             ("eta", s_g, _strided("eta", eta, s_g, f32, dev))]
+    if log_gamma is not None:
+        given.append(("log_gamma", s_g, _strided("log_gamma", log_gamma, s_g, f32, dev)))
+    if not isinstance(w, torch.Tensor) or w.dim() != 4 or w.shape[0] < 1:
+        raise ValueError("w must be a tensor [N, H, dv, dk] of states")
+    _plain("w", w, w.shape[:1] + s_w[1:], f32, dev)
+    _plain("slots", slots, s_g[:1], torch.int32, dev)
+    if out is None:
+        out = torch.empty_like(v)
+    given.append(("out", s_v, _strided("out", out, s_v, io, dev)))
+    st = load().e2ttt_delta_step(d, _strides_ref(DeltaStrides, *given), _ptr(q), _ptr(k), _ptr(v),
+                                 _ptr(eta), _ptr(log_gamma), _ptr(w), _ptr(slots), w.shape[0],
+                                 _ptr(out), _stream())
+    _check(st, "e2ttt_delta_step")
+    return out
+
+
+class DeltaFunction(torch.autograd.Function):
+    """Autograd wrapper of the gated delta rule: (out, w_out) of (cfg, q, k, v,
+    eta, log_gamma, w_in, lengths); the forward saves the workspace."""
+
+    @staticmethod
+    def forward(ctx, cfg, q, k, v, eta, log_gamma=None, w_in=None, lengths=None):
+        out, w_out, ws = delta_forward(cfg, q, k, v, eta, log_gamma, w_in, lengths=lengths,
+                                       save_for_backward=True)
+        ctx.cfg, ctx.has_w = cfg, w_in is not None
+        ctx.save_for_backward(q, k, v, eta, log_gamma, lengths, ws)
+        ctx.set_materialize_grads(False)
+        return out, w_out
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, d_out, d_w_out):
+        q, k, v, eta, log_gamma, lengths, ws = ctx.saved_tensors
+        if d_out is None:
+            d_out = torch.zeros_like(v)
+        g = delta_backward(ctx.cfg, q, k, v, eta, log_gamma, ws, _as_rows(d_out),
+                           None if d_w_out is None else d_w_out.contiguous(), lengths=lengths)
+        return (None, g["dq"], g["dk"], g["dv"], g["d_eta"], g["d_log_gamma"],
+                g["d_w_in"] if ctx.has_w else None, None)
+
+
+@dataclass(frozen=True)
+class QKConfig:
+    """Query/key preparation: H query heads and HK key heads (0: queries alone)
+    of dim d; the first `rot` elements turn; flags QK_*."""
+    B: int
+    H: int
+    HK: int
+    T: int
+    d: int
+    rot: int
+    io: int = DT_BF16
+    flags: int = QK_SILU | QK_UNIT
+    eps: float = 1e-6
+    rot_scale: float = 1.0
+
+    def desc(self) -> QKDesc:
+        return QKDesc(self.B, self.H, self.HK, self.T, self.d, self.rot, self.io, self.flags, self.eps,
+                      self.rot_scale)
+
+    @cached_property
+    def _call(self):
+        return (ctypes.byref(self.desc()), torch.bfloat16 if self.io == DT_BF16 else torch.float32,
+                torch.Size((self.B, self.H, self.T, self.d)),
+                torch.Size((self.B, self.HK, self.T, self.d)), torch.Size((self.B, self.T)),
+                torch.Size((self.rot // 2,)))
+
+    def __getstate__(self):
+        return {n: v for n, v in self.__dict__.items() if n != "_call"}
+
+
+def rotary_frequencies(rot, base=10000.0, factor=1.0, original=None, fast=32.0, slow=1.0,
+                       device="cuda"):
+    """(inv_freq [rot / 2] float32, rot_scale) of rotary positions at `base`.
+
+    factor > 1 stretches them to a context that many times the trained one:
+    without `original` every frequency is divided by it (position
+    interpolation); with `original`, the trained length, by parts (the YaRN
+    paper): a pair that makes more than `fast` turns over the trained length
+    keeps its frequency, one below `slow` turns is divided by factor, between
+    them a linear ramp in the pair's index, and rot_scale = 0.1 ln(factor) + 1."""
+    if rot < 0 or rot % 2 or not (base > 1.0 and factor >= 1.0):
+        raise ValueError("rot is even and not negative, base > 1, factor >= 1")
+    p = torch.arange(0, rot, 2, dtype=torch.float64)
+    f = base ** (-p / max(rot, 1))
+    scale = 1.0
+    if factor > 1.0 and original is None:
+        f = f / factor
+    elif factor > 1.0:
+        if not (original > 0 and fast > slow > 0):
+            raise ValueError("original > 0, fast > slow > 0")
+
+        def pair(turns):     # the (fractional) pair that makes so many turns over `original`
+            return rot * math.log(original / (2.0 * math.pi * turns)) / (2.0 * math.log(base))
+
+        lo, hi = max(math.floor(pair(fast)), 0), min(math.ceil(pair(slow)), rot - 1)
+        ramp = ((p / 2.0 - lo) / max(hi - lo, 1e-3)).clamp(0.0, 1.0)
+        f = f / factor * ramp + f * (1.0 - ramp)
+        scale = 0.1 * math.log(factor) + 1.0
+    return f.float().to(device), scale
+
+
+def _qk_common(cfg, dev, inv_freq, positions):
+    _, _, _, _, s_p, s_f = cfg._call
+    if cfg.rot and inv_freq is None:
+        raise ValueError("inv_freq must be given where rot > 0")
+    _plain("inv_freq", inv_freq, s_f, torch.float32, dev)
+    _plain("positions", positions, s_p, torch.int64, dev)
+
+
+@_on_device
+def qk_forward(cfg: QKConfig, q, k, inv_freq=None, positions=None, *, out=None):
+    """Runs e2ttt_qk_forward on the current stream: q [B, H, T, d] and k [B, HK,
+    T, d] (None where HK = 0) prepared for the state rules; positions [B, T]
+    int64 (None: 0 .. T - 1).  `out`: optional (q, k) tensors to write into,
+    which may be the inputs.  Returns (q', k')."""
+    d, io, s_q, s_k, _, _ = cfg._call
+    dev = q.get_device()
+    if (k is None) != (cfg.HK == 0):
+        raise ValueError("k is given where HK > 0, and only there")
+    _qk_common(cfg, dev, inv_freq, positions)
+    qo, ko = out if out is not None else (torch.empty_like(q), None if k is None else torch.empty_like(k))
+    given = [("q", s_q, _strided("q", q, s_q, io, dev)), ("q_out", s_q, _strided("out", qo, s_q, io, dev))]
+    if k is not None:
+        given += [("k", s_k, _strided("k", k, s_k, io, dev)),
+                  ("k_out", s_k, _strided("out", ko, s_k, io, dev))]
+    st = load().e2ttt_qk_forward(d, _strides_ref(QKStrides, *given), _ptr(q), _ptr(k), _ptr(inv_freq),
+                                 _ptr(positions), _ptr(qo), _ptr(ko) if k is not None else None,
+                                 _stream())
+    _check(st, "e2ttt_qk_forward")
+    return qo, ko
+
+
+@_on_device
+def qk_backward(cfg: QKConfig, d_q_out, d_k_out, q=None, k=None, inv_freq=None, positions=None, *,
+                out=None):
+    """Gradients (dq, dk) of qk_forward's inputs q, k from those of its outputs
+    (q and k are not needed without QK_SILU and QK_UNIT)."""
+    d, io, s_q, s_k, _, _ = cfg._call
+    dev, need = d_q_out.get_device(), bool(cfg.flags & (QK_SILU | QK_UNIT))
+    if (d_k_out is None) != (cfg.HK == 0):
+        raise ValueError("d_k_out is given where HK > 0, and only there")
+    _qk_common(cfg, dev, inv_freq, positions)
+    dq, dk = out if out is not None else (
+        torch.empty_like(d_q_out), None if d_k_out is None else torch.empty_like(d_k_out))
+    given = [("d_q_out", s_q, _strided("d_q_out", d_q_out, s_q, io, dev)),
+             ("dq", s_q, _strided("out", dq, s_q, io, dev))]
+    if need:
+        given.append(("q", s_q, _strided("q", q, s_q, io, dev)))
+    if d_k_out is not None:
+        given += [("d_k_out", s_k, _strided("d_k_out", d_k_out, s_k, io, dev)),
+                  ("dk", s_k, _strided("out", dk, s_k, io, dev))]
+        if need:
+            given.append(("k", s_k, _strided("k", k, s_k, io, dev)))
+    st = load().e2ttt_qk_backward(d, _strides_ref(QKStrides, *given), _ptr(q) if need else None,
+                                  _ptr(k) if need else None, _ptr(inv_freq), _ptr(positions),
+                                  _ptr(d_q_out), _ptr(d_k_out), _ptr(dq),
+                                  _ptr(dk) if d_k_out is not None else None, _stream())
+    _check(st, "e2ttt_qk_backward")
+    return dq, dk
+
+
+class QKFunction(torch.autograd.Function):
+    """Autograd wrapper of the query/key preparation: (q', k') of (cfg, q, k,
+    inv_freq, positions)."""
+
+    @staticmethod
+    def forward(ctx, cfg, q, k, inv_freq=None, positions=None):
+        qo, ko = qk_forward(cfg, q, k, inv_freq, positions)
+        ctx.cfg = cfg
+        need = cfg.flags & (QK_SILU | QK_UNIT)
+        ctx.save_for_backward(q if need else None, k if need else None, inv_freq, positions)
+        return qo, ko
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, d_q, d_k):
+        q, k, inv_freq, positions = ctx.saved_tensors
+        dq, dk = qk_backward(ctx.cfg, _as_rows(d_q), None if d_k is None else _as_rows(d_k), q, k,
+                             inv_freq, positions)
+        return None, dq, dk, None, None
