@@ -17,6 +17,12 @@ HIPCC_FLAGS = [
     "-Wno-unused-command-line-argument",
 ]
 
+# Flags of single files.  The delta rule's kernels live on MFMA results that the
+# vector units take up at once: kept out of the accumulation registers, they need
+# no moves (a sixth of the chain's instructions).
+FILE_FLAGS = {n: ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]
+              for n in ("delta_prep.hip", "delta_fwd.hip", "delta_bwd.hip", "delta_grads.hip")}
+
 
 def sources():
     return sorted(glob.glob(os.path.join(CSRC, "*.hip")))
@@ -46,7 +52,8 @@ def build(verbose: bool = False, extra: list[str] | None = None) -> str:
     jobs = []
     for src in sources():
         obj = os.path.join(objdir, os.path.basename(src)[:-4] + ".o")
-        jobs.append((src, obj, [hipcc, *flags, *inc, "-c", src, "-o", obj]))
+        own = FILE_FLAGS.get(os.path.basename(src), [])
+        jobs.append((src, obj, [hipcc, *flags, *own, *inc, "-c", src, "-o", obj]))
     workers = max(1, min(len(jobs), int(os.environ.get("MAX_JOBS", "0")) or (os.cpu_count() or 1)))
     with ThreadPoolExecutor(max_workers=workers) as ex:
         for f in [ex.submit(_run, cmd, verbose) for _, _, cmd in jobs]:

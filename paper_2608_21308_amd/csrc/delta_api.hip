@@ -27,6 +27,7 @@ e2ttt_status check_desc(const e2ttt_delta_desc* d) {
 struct Plan {
   bool bf;
   long U, NC;
+  int pterms;
   long nc_buf;                    // chunks per unit held at once
   size_t o_gate, o_frag, o_state, o_w, o_u, bytes;       // workspace
   size_t s_w, s_u, scratch;                              // backward scratch
@@ -47,7 +48,8 @@ Plan plan(const e2ttt_delta_desc* d, bool save) {
   p.NC = ((long)d->T + kDC - 1) / kDC;
   const int dkp = delta_dkp(d->dk), dvp = delta_dvp(d->dv);
   const size_t gate = kGateFloats * sizeof(float);
-  const size_t frag = 2 * (size_t)kTriBytes;
+  p.pterms = save ? 3 : 2;
+  const size_t frag = tri_bytes(p.bf, 3) + tri_bytes(p.bf, p.pterms);
   p.w_bytes = 4L * dkp * dvp;
   p.u_bytes = 4L * kDC * dvp;
   p.nc_buf = p.NC;
@@ -108,6 +110,7 @@ void fill(DeltaArgs& a, const e2ttt_delta_desc* d, const Plan& p, char* ws) {
   a.scale = d->scale;
   a.gate = reinterpret_cast<float*>(ws + p.o_gate);
   a.frag = ws + p.o_frag;
+  a.pterms = p.pterms;
   a.wst = reinterpret_cast<float*>(ws + p.o_w);
   a.ust = reinterpret_cast<float*>(ws + p.o_u);
 }

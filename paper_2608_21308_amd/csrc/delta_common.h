@@ -32,12 +32,13 @@ namespace e2ttt {
 
 constexpr int kDC = 64;           // tokens per chunk
 constexpr int kDeltaFrags = 6;    // 16x32 fragments of a lower triangular 64x64 matrix
-// Per chunk and unit: eta, eta G, s G, exp(b_C - b), then b as two floats
-// (b = bh + bl from a sum in 64 bits: differences of b keep their relative
-// accuracy however far the sum has gone), 64 each, and G_C.
+// Per chunk and unit: eta, eta G, s G, exp(b_C - b), 64 each, G_C (16 times),
+// then b as two floats (b = bh + bl from a sum in 64 bits: differences of b keep
+// their relative accuracy however far the sum has gone).
 constexpr int kGateFloats = 6 * kDC + 16;
-enum { kGEta = 0, kGEtaG = kDC, kGsG = 2 * kDC, kGEnd = 3 * kDC, kGBh = 4 * kDC,
-       kGBl = 5 * kDC, kGC = 6 * kDC };
+enum { kGEta = 0, kGEtaG = kDC, kGsG = 2 * kDC, kGEnd = 3 * kDC, kGC = 4 * kDC,
+       kGBh = 4 * kDC + 16, kGBl = 5 * kDC + 16 };
+constexpr int kGateChain = 4 * kDC + 16;   // the part that the chains read
 
 // A token tensor [B][H][T][d] by its strides in elements (the last is 1).
 struct View {
@@ -54,10 +55,11 @@ struct DeltaArgs {
   float* w_out;               // nullable
   const float* d_w_out;       // nullable: zero
   float* d_w_in;              // nullable
-  char* frag;                 // [chunk unit] T fragments, then P fragments (kTriBytes each)
+  char* frag;                 // [chunk unit] T in three terms, then P in pterms
+  int pterms;                 // two (not saving), or three
   float* gate;                // [chunk unit][kGateFloats]
-  float* wst;                 // [chunk unit][dvp][dkp] chunk-start states (saving)
-  float* ust;                 // [chunk unit][dvp][64] U^T (saving)
+  float* wst;                 // [chunk unit][dvp x dkp] chunk-start states (saving), in lane order
+  float* ust;                 // [chunk unit][dvp x 64] U^T (saving), in lane order
   float* dwst;                // backward: chunk-end adjoint states, as wst
   float* yst;                 // backward: Y^T, as ust
   int B, HK, H, T, dk, dv, dvp;   // dvp: dv padded to a multiple of 32
@@ -75,12 +77,13 @@ __device__ __forceinline__ int lab(int m, int r) {
 __host__ __device__ constexpr int fidx(int m, int a) { return m < 2 ? m : 2 * (m - 1) + a; }
 
 // Operands.  X: a value of the io type, exact.  S: an fp32 value; with bf16 io
-// the sum of NT = 3 bf16 terms, each the rounding of what the ones before
-// leave, so that nothing is lost.  A product takes the terms whose combined
-// order is below N: with N = 3 it is an fp32 product (what is left out is
-// below 2^-24), used for all that reaches a state or a gate's gradient; with
-// N = 2 its error is at most 2^-17, far below the rounding of a bf16 output
-// (2^-9), used for what reaches such outputs only.  f32 io: fp32 MFMA.
+// the sum of NT = 3 bf16 terms, each the upper half of the word that the ones
+// before leave: 8 bits each, 24 in all, so that nothing is lost.  A product
+// takes the terms whose combined order is below N: with N = 3 it is an fp32
+// product (what is left out is of the order 2^-24), used for all that reaches
+// a state or a gate's gradient; with N = 2 its error is at most 2^-15, far
+// below the rounding of a bf16 output (2^-9), used for what reaches such
+// outputs only.  f32 io: fp32 MFMA.
 template <bool BF> struct DOp;
 
 template <> struct DOp<true> {
@@ -116,25 +119,43 @@ template <> struct DOp<true> {
   }
   template <int N>
   static __device__ __forceinline__ S split(f32x4 x, f32x4 y) {
+    typedef __attribute__((ext_vector_type(4))) unsigned u4;
     S s;
+    float v[8];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      v[e] = x[e];
+      v[4 + e] = y[e];
+    }
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const bf16x8 r = {(__bf16)x[0], (__bf16)x[1], (__bf16)x[2], (__bf16)x[3],
-                        (__bf16)y[0], (__bf16)y[1], (__bf16)y[2], (__bf16)y[3]};
-      s.t[i] = r;
+      u4 p;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)   // the upper halves of a pair of words
+        p[e] = __builtin_amdgcn_perm(__float_as_uint(v[2 * e + 1]), __float_as_uint(v[2 * e]),
+                                     0x07060302u);
+      s.t[i] = __builtin_bit_cast(bf16x8, p);
       if (i + 1 < N) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          x[e] -= (float)r[e];
-          y[e] -= (float)r[4 + e];
-        }
+        for (int e = 0; e < 8; ++e)
+          v[e] -= __uint_as_float(__float_as_uint(v[e]) & 0xffff0000u);
       }
     }
     return s;
   }
-  static __device__ __forceinline__ X exact(f32x4 x, f32x4 y) {   // values of the io type
-    return X{bf16x8{(__bf16)x[0], (__bf16)x[1], (__bf16)x[2], (__bf16)x[3], (__bf16)y[0],
-                    (__bf16)y[1], (__bf16)y[2], (__bf16)y[3]}};
+  static __device__ __forceinline__ void sum(const S& s, f32x4& x, f32x4& y) {   // of all terms
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      x[e] = ((float)s.t[2][e] + (float)s.t[1][e]) + (float)s.t[0][e];
+      y[e] = ((float)s.t[2][4 + e] + (float)s.t[1][4 + e]) + (float)s.t[0][4 + e];
+    }
+  }
+  static __device__ __forceinline__ void values(const X& p, f32x4& x, f32x4& y) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      x[e] = (float)p.v[e];
+      y[e] = (float)p.v[4 + e];
+    }
   }
 };
 
@@ -143,6 +164,10 @@ template <> struct DOp<false> {
   static constexpr int NT = 1;
   struct X { f32x4 a, b; };
   using S = X;
+  static __device__ __forceinline__ void sum(const S& p, f32x4& x, f32x4& y) {
+    x = p.a;
+    y = p.b;
+  }
   static __device__ __forceinline__ f32x4 xx(f32x4 acc, const X& p, const X& q) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(p.a[e], q.a[e], acc, 0, 0, 0);
@@ -158,31 +183,30 @@ template <> struct DOp<false> {
   static __device__ __forceinline__ f32x4 ss(f32x4 acc, const X& p, const X& q) { return xx(acc, p, q); }
   template <int N>
   static __device__ __forceinline__ S split(f32x4 x, f32x4 y) { return S{x, y}; }
-  static __device__ __forceinline__ X exact(f32x4 x, f32x4 y) { return X{x, y}; }
+  static __device__ __forceinline__ void values(const X& p, f32x4& x, f32x4& y) {
+    x = p.a;
+    y = p.b;
+  }
 };
 
-// A lower triangular 64x64 matrix in global memory: fp32 fragments, the two
-// halves of a lane's eight values at lane * 16 and 1024 + lane * 16.
-constexpr int kFragBytes = 2048;
-constexpr int kTriBytes = kDeltaFrags * kFragBytes;
-// The same in LDS as N terms: all fragments of a term, then of the next.
-template <bool BF> constexpr int tri_lds(int n) { return BF ? n * kDeltaFrags * 1024 : kTriBytes; }
-
-__device__ __forceinline__ void st_frag(char* base, int f, int lane, f32x4 x, f32x4 y) {
-  char* p = base + f * kFragBytes + lane * 16;
-  *reinterpret_cast<f32x4*>(p) = x;
-  *reinterpret_cast<f32x4*>(p + 1024) = y;
+// A lower triangular 64x64 matrix as the fragments of N terms, in global
+// memory and in LDS: a lane's 16 bytes of a fragment at lane * 16, the
+// fragments of a term together (f32 io: the two halves of a fragment's fp32
+// values at lane * 16 and 1024 + lane * 16).
+__host__ __device__ constexpr int tri_bytes(bool bf, int n) {
+  return bf ? n * kDeltaFrags * 1024 : kDeltaFrags * 2048;
 }
-// One lane's part (slot: 64 fragment + lane) into LDS.
+// One lane's part of fragment f.
 template <bool BF, int N>
-__device__ __forceinline__ void put_frag(char* lds, int slot, f32x4 x, f32x4 y) {
+__device__ __forceinline__ void put_frag(char* p, int f, int lane, f32x4 x, f32x4 y) {
   if constexpr (BF) {
     const auto s = DOp<true>::split<N>(x, y);
 #pragma unroll
     for (int i = 0; i < N; ++i)
-      *reinterpret_cast<bf16x8*>(lds + (i * kDeltaFrags * 64 + slot) * 16) = s.t[i];
+      *reinterpret_cast<bf16x8*>(p + ((i * kDeltaFrags + f) * 64 + lane) * 16) = s.t[i];
   } else {
-    st_frag(lds, slot >> 6, slot & 63, x, y);
+    *reinterpret_cast<f32x4*>(p + f * 2048 + lane * 16) = x;
+    *reinterpret_cast<f32x4*>(p + f * 2048 + 1024 + lane * 16) = y;
   }
 }
 template <bool BF, int N>
@@ -193,10 +217,21 @@ __device__ __forceinline__ typename DOp<BF>::S ld_frag(const char* lds, int f, i
     for (int i = 0; i < N; ++i)
       s.t[i] = *reinterpret_cast<const bf16x8*>(lds + ((i * kDeltaFrags + f) * 64 + lane) * 16);
   } else {
-    s.a = *reinterpret_cast<const f32x4*>(lds + f * kFragBytes + lane * 16);
-    s.b = *reinterpret_cast<const f32x4*>(lds + f * kFragBytes + 1024 + lane * 16);
+    s.a = *reinterpret_cast<const f32x4*>(lds + f * 2048 + lane * 16);
+    s.b = *reinterpret_cast<const f32x4*>(lds + f * 2048 + 1024 + lane * 16);
   }
   return s;
+}
+
+// What a chain leaves for the gradients, in the order of its lanes: per 16
+// columns and 32 rows, the lanes' first four values, then their second (row
+// 16 tile + c, columns 32 blk + 8 g ..; a wave writes whole lines).
+__device__ __forceinline__ long lane_at(int tile, int blk, int nblk, int lane) {
+  return ((long)(tile * nblk + blk) * 2 * 64 + lane) * 4;
+}
+__device__ __forceinline__ void st_lane(float* p, f32x4 x, f32x4 y) {
+  *reinterpret_cast<f32x4*>(p) = x;
+  *reinterpret_cast<f32x4*>(p + 256) = y;
 }
 
 // One transposing LDS read: within each group of 16 lanes, lane c receives
@@ -236,8 +271,8 @@ __device__ __forceinline__ typename DOp<BF>::S ld_frag_t(const char* lds, int m,
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const int at = (16 * gj + 4 * g + e) * 16 + (sj >> 2) * 1024 + (sj & 3) * 4;
-      s.a[e] = *reinterpret_cast<const float*>(lds + fidx(2 * a, m >> 1) * kFragBytes + at);
-      s.b[e] = *reinterpret_cast<const float*>(lds + fidx(2 * a + 1, m >> 1) * kFragBytes + at);
+      s.a[e] = *reinterpret_cast<const float*>(lds + fidx(2 * a, m >> 1) * 2048 + at);
+      s.b[e] = *reinterpret_cast<const float*>(lds + fidx(2 * a + 1, m >> 1) * 2048 + at);
     }
   }
   return s;

@@ -44,7 +44,7 @@ __global__ void __launch_bounds__(512) delta_grads_kernel(DeltaArgs a) {
   constexpr int MG = 8 / CTS, MR = 4 / MG;              // row groups, row tiles of a wave
   constexpr int WP = 32 * DK, UP = 32 * kDC;            // elements of a term's block
   constexpr int kStage = (2 * NT * WP + 2 * NT * UP + kDC * 32) * (int)sizeof(E);
-  constexpr int kBuf = kStage > 2 * tri_lds<BF>(2) ? kStage : 2 * tri_lds<BF>(2);
+  constexpr int kBuf = kStage > 2 * tri_bytes(BF, 2) ? kStage : 2 * tri_bytes(BF, 2);
   __shared__ __align__(16) E ks[kDC * DK];
   __shared__ __align__(16) E qs[kDC * DK];
   __shared__ __align__(16) char buf[kBuf];              // value blocks, then A and N
@@ -61,7 +61,7 @@ __global__ void __launch_bounds__(512) delta_grads_kernel(DeltaArgs a) {
   E* ys = us + NT * UP;
   E* dos = ys + NT * UP;
   char* as = buf;
-  char* ns = buf + tri_lds<BF>(2);
+  char* ns = buf + tri_bytes(BF, 2);
 
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, g = lane >> 4, c = lane & 15;
   const int nr = a.r1 - a.r0, rep = a.H / a.HK;
@@ -123,21 +123,24 @@ __global__ void __launch_bounds__(512) delta_grads_kernel(DeltaArgs a) {
       const float* dwg = a.dwst + (cu * a.dvp + v0) * DK;
       const float* ug = a.ust + (cu * a.dvp + v0) * kDC;
       const float* yg = a.yst + (cu * a.dvp + v0) * kDC;
-      for (int p = tid; p < PW; p += NTH) {
-        const f32x4 x0 = *reinterpret_cast<const f32x4*>(w0g + 8 * p);
-        const f32x4 x1 = *reinterpret_cast<const f32x4*>(w0g + 8 * p + 4);
-        const f32x4 y0 = *reinterpret_cast<const f32x4*>(dwg + 8 * p);
-        const f32x4 y1 = *reinterpret_cast<const f32x4*>(dwg + 8 * p + 4);
-        put_terms<BF, DK>(w0s, WP, p / (DK / 8), p % (DK / 8), x0, x1);
-        put_terms<BF, DK>(dws, WP, p / (DK / 8), p % (DK / 8), y0, y1);
+      for (int p = tid; p < PW; p += NTH) {  // a wave takes 16 rows x 32 columns
+        const int tile = p / (64 * KT), kt = (p >> 6) % KT;
+        const long at = lane_at(tile, kt, KT, lane);
+        const f32x4 x0 = *reinterpret_cast<const f32x4*>(w0g + at);
+        const f32x4 x1 = *reinterpret_cast<const f32x4*>(w0g + at + 256);
+        const f32x4 y0 = *reinterpret_cast<const f32x4*>(dwg + at);
+        const f32x4 y1 = *reinterpret_cast<const f32x4*>(dwg + at + 256);
+        put_terms<BF, DK>(w0s, WP, 16 * tile + c, 4 * kt + g, x0, x1);
+        put_terms<BF, DK>(dws, WP, 16 * tile + c, 4 * kt + g, y0, y1);
 #pragma unroll
         for (int e = 0; e < 4; ++e) wdot = fmaf(x0[e], y0[e], fmaf(x1[e], y1[e], wdot));
       }
       for (int p = tid; p < 2 * PU; p += NTH) {
-        const int s = p >= PU, pp = p - s * PU;
-        const float* src = (s ? yg : ug) + 8 * pp;
-        put_terms<BF, kDC>(s ? ys : us, UP, pp / 8, pp % 8, *reinterpret_cast<const f32x4*>(src),
-                           *reinterpret_cast<const f32x4*>(src + 4));
+        const int s = p >= PU, tile = (p >> 7) & 1, x = (p >> 6) & 1;
+        const float* src = (s ? yg : ug) + lane_at(tile, x, 2, lane);
+        put_terms<BF, kDC>(s ? ys : us, UP, 16 * tile + c, 4 * x + g,
+                           *reinterpret_cast<const f32x4*>(src),
+                           *reinterpret_cast<const f32x4*>(src + 256));
       }
       for (int p = tid; p < PO; p += NTH) {
         const int row = p / LV::NP, col = v0 + (p % LV::NP) * LV::PE;
@@ -160,6 +163,13 @@ __global__ void __launch_bounds__(512) delta_grads_kernel(DeltaArgs a) {
       if (low) {
         const auto doi = LV::frag(dos, i, 0, g);
         const auto yi = terms_t<BF, kDC, false>(ys, UP, rt, g, c);
+        if (xb == 0 && t0 + i < a.T && v0 + 8 * g < a.dv) {   // dV = eta Y, eight channels a lane
+          f32x4 y0, y1;
+          O::sum(yi, y0, y1);
+          E* p = row_of_w<E>(a.dv_, b, h, t0 + i) + v0 + 8 * g;
+          IoT<BF>::st4(p, y0 * gl[kGEta + i]);
+          IoT<BF>::st4(p + 4, y1 * gl[kGEta + i]);
+        }
 #pragma unroll
         for (int y = 0; y < 2; ++y) {
           const auto uj = terms_t<BF, kDC, false>(us, UP, 2 * xb + y, g, c);
@@ -200,8 +210,8 @@ __global__ void __launch_bounds__(512) delta_grads_kernel(DeltaArgs a) {
         if (c == 0) *reinterpret_cast<f32x4*>(&scol[rt][32 * xb + 8 * g + 4 * y]) = pair;
       }
       if (low) {
-        put_frag<BF, 2>(as, fidx(rt, xb) * 64 + lane, pa[0], pa[1]);
-        put_frag<BF, 2>(ns, fidx(rt, xb) * 64 + lane, pn[0], pn[1]);
+        put_frag<BF, 2>(as, fidx(rt, xb), lane, pa[0], pa[1]);
+        put_frag<BF, 2>(ns, fidx(rt, xb), lane, pn[0], pn[1]);
       }
       rx += __shfl_xor(rx, 16);
       rx += __shfl_xor(rx, 32);
@@ -279,10 +289,11 @@ __global__ void __launch_bounds__(512) delta_grads_kernel(DeltaArgs a) {
       float de = syu[t] / eta;
       if (live && !(fabsf(eta) >= kMinEta)) {
         // eta (near) zero: Y_i . e_i by its definition
-        const float* yp = a.yst + cu * a.dvp * kDC + t;
+        const float* yp = a.yst + cu * a.dvp * kDC + (t & 4) * 64 + (t & 3);
         const E* vp = row_of<E>(a.v, b, h, t0 + t);
         float yv = 0.0f;
-        for (int n = 0; n < a.dv; ++n) yv = fmaf(yp[(long)n * kDC], (float)vp[n], yv);
+        for (int n = 0; n < a.dv; ++n)
+          yv = fmaf(yp[lane_at(n >> 4, t >> 5, 2, 16 * ((t >> 3) & 3) + (n & 15))], (float)vp[n], yv);
         de = yv - expf(gl[kGBh + t]) * sr - (sx[1][0][t] + sx[1][1][t]);
       }
       // sums over tokens at and after t, and before t

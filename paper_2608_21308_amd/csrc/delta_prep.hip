@@ -120,7 +120,7 @@ __global__ void __launch_bounds__(256) delta_prep_kernel(DeltaArgs a) {
   }
   __syncthreads();
 
-  char* frag = a.frag + cu * 2 * kTriBytes;
+  char* frag = a.frag + cu * (tri_bytes(BF, 3) + tri_bytes(BF, a.pterms));
   const float bhi = gl[kGBh + i], bli = gl[kGBl + i], eta = gl[kGEta + i];
 #pragma unroll
   for (int x = 0; x < 2; ++x) {
@@ -138,14 +138,17 @@ __global__ void __launch_bounds__(256) delta_prep_kernel(DeltaArgs a) {
         }
         *reinterpret_cast<f32x4*>(am + i * LDT + 32 * x + 8 * g + 4 * y) = m4;
       }
-      st_frag(frag + kTriBytes, fidx(w, x), lane, p[0], p[1]);
+      if (a.pterms == 3)
+        put_frag<BF, 3>(frag + tri_bytes(BF, 3), fidx(w, x), lane, p[0], p[1]);
+      else
+        put_frag<BF, 2>(frag + tri_bytes(BF, 3), fidx(w, x), lane, p[0], p[1]);
     }
   }
   if (w == 0) {
     float* go = a.gate + cu * kGateFloats;
 #pragma unroll
     for (int x = 0; x < 6; ++x) go[64 * x + lane] = gl[64 * x + lane];
-    if (lane < 16) go[kGC + lane] = gl[kGC + lane];
+    if (lane < 16) go[6 * 64 + lane] = gl[6 * 64 + lane];
   }
   __syncthreads();
 
@@ -196,8 +199,8 @@ __global__ void __launch_bounds__(256) delta_prep_kernel(DeltaArgs a) {
   for (int x = 0; x < 2; ++x) {
     if (x < na) {
       const float* p = tm + i * LDT + 32 * x + 8 * g;
-      st_frag(frag, fidx(w, x), lane, *reinterpret_cast<const f32x4*>(p),
-              *reinterpret_cast<const f32x4*>(p + 4));
+      put_frag<BF, 3>(frag, fidx(w, x), lane, *reinterpret_cast<const f32x4*>(p),
+                      *reinterpret_cast<const f32x4*>(p + 4));
     }
   }
 }

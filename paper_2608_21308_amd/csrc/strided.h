@@ -13,14 +13,15 @@ inline e2ttt_strides strides_of(const e2ttt_strides* given, long H, long T, long
   if (given) return *given;
   return e2ttt_strides{H * T * inner, T * inner, inner};
 }
-// Strides in range; with `vec` every row starts on 16 bytes (as its tensor does).
+// Strides in range (the rows of a 64-token chunk are addressed in 32 bits);
+// with `vec` every row starts on 16 bytes (as its tensor does).
 inline bool rows_ok(const e2ttt_strides& s, long elt, bool vec) {
   const int64_t lim = (int64_t)1 << 46;
   for (int64_t x : {s.b, s.h, s.t}) {
     if (x < 0 || x > lim) return false;
     if (vec && (x * elt) % 16) return false;
   }
-  return true;
+  return s.t <= ((int64_t)1 << 23);
 }
 // No two elements of a written tensor share memory: taken by rising stride,
 // each dimension (of more than one) starts behind all that the ones before span.
