@@ -1,7 +1,8 @@
 // C entry points of the gated delta rule: argument checks, the layout of
 // workspace and scratch, and the launches.
 #include <math.h>
-#include <string.h>
+
+#include <algorithm>
 
 #include "delta_common.h"
 #include "e2ttt.h"
@@ -29,8 +30,9 @@ struct Plan {
   long U, NC;
   int pterms;
   long nc_buf;                    // chunks per unit held at once
-  size_t o_gate, o_frag, o_state, o_w, o_u, bytes;       // workspace
-  size_t s_w, s_u, scratch;                              // backward scratch
+  long nseg, seglen;              // segments of a stretch
+  size_t o_gate, o_frag, o_state, o_segs, o_segb, o_segf, o_w, o_u, bytes;   // workspace
+  size_t s_w, s_u, s_segs, s_segb, scratch;              // backward scratch
   long w_bytes, u_bytes;
 };
 
@@ -40,6 +42,18 @@ size_t up(size_t x) { return (x + 255) & ~(size_t)255; }
 // fit here: what the first kernel of a stretch writes, the second reads from
 // the 256 MB last-level cache.
 constexpr size_t kStretchBytes = (size_t)224 << 20;
+
+// Segments that `nch` chunks of U units run as (1: none).  A wave holds 16 value
+// channels of a unit, and the card takes 2048 such waves at once.  Segments
+// cost a pass over dv + dk channels ahead of the one over dv: four gain
+// nothing (128 units of 64, 64 chunks: 339 us against 285), eight halve the time
+// (32 units of 128, 32 chunks: 125 us against 186).  A segment of fewer than 4
+// chunks is not worth its joining.
+long segments(const e2ttt_delta_desc* d, long U, long nch) {
+  const long waves = U * (delta_dvp(d->dv) / 16);
+  const long n = std::min(2048 / waves, nch / 4);
+  return n < 6 ? 1 : n;
+}
 
 Plan plan(const e2ttt_delta_desc* d, bool save) {
   Plan p{};
@@ -55,18 +69,28 @@ Plan plan(const e2ttt_delta_desc* d, bool save) {
   p.nc_buf = p.NC;
   if (!save) {
     const long fit = (long)(kStretchBytes / ((gate + frag) * (size_t)p.U));
-    p.nc_buf = fit < 1 ? 1 : fit < p.NC ? fit : p.NC;
+    const long n = fit < 1 ? p.NC : (p.NC + fit - 1) / fit;   // stretches of equal length
+    p.nc_buf = (p.NC + n - 1) / n;
   }
   const size_t cus = (size_t)p.U * p.nc_buf;
   p.o_gate = 0;
   p.o_frag = up(p.o_gate + cus * gate);
+  p.nseg = segments(d, p.U, p.nc_buf);
+  p.seglen = (p.nc_buf + p.nseg - 1) / p.nseg;
+  p.nseg = (p.nc_buf + p.seglen - 1) / p.seglen;
+  const size_t segs = p.nseg > 1 ? (size_t)p.U * p.nseg : 0;
   p.o_state = up(p.o_frag + cus * frag);
-  p.o_w = up(p.o_state + (p.nc_buf < p.NC ? (size_t)p.U * d->dk * d->dv * 4 : 0));
+  p.o_segs = up(p.o_state + (p.nc_buf < p.NC ? (size_t)p.U * d->dk * d->dv * 4 : 0));
+  p.o_segb = up(p.o_segs + segs * p.w_bytes);
+  p.o_segf = up(p.o_segb + segs * p.w_bytes);
+  p.o_w = up(p.o_segf + segs * 2 * dkp * dkp * 4);
   p.o_u = up(p.o_w + (save ? cus * p.w_bytes : 0));
   p.bytes = up(p.o_u + (save ? cus * p.u_bytes : 0));
   p.s_w = 0;
   p.s_u = up((size_t)p.U * p.NC * p.w_bytes);
-  p.scratch = up(p.s_u + (size_t)p.U * p.NC * p.u_bytes);
+  p.s_segs = up(p.s_u + (size_t)p.U * p.NC * p.u_bytes);
+  p.s_segb = up(p.s_segs + segs * p.w_bytes);
+  p.scratch = up(p.s_segb + segs * p.w_bytes);
   return p;
 }
 
@@ -111,6 +135,11 @@ void fill(DeltaArgs& a, const e2ttt_delta_desc* d, const Plan& p, char* ws) {
   a.gate = reinterpret_cast<float*>(ws + p.o_gate);
   a.frag = ws + p.o_frag;
   a.pterms = p.pterms;
+  a.segs = reinterpret_cast<float*>(ws + p.o_segs);
+  a.segb = reinterpret_cast<float*>(ws + p.o_segb);
+  a.segf = reinterpret_cast<float*>(ws + p.o_segf);
+  a.seglen = (int)p.seglen;
+  a.nseg = (int)p.nseg;
   a.wst = reinterpret_cast<float*>(ws + p.o_w);
   a.ust = reinterpret_cast<float*>(ws + p.o_u);
 }
@@ -158,8 +187,12 @@ extern "C" e2ttt_status e2ttt_delta_forward(const e2ttt_delta_desc* desc,
     a.r1 = (int)(r0 + p.nc_buf < p.NC ? r0 + p.nc_buf : p.NC);
     a.w_in = r0 == 0 ? w_in : carry;
     a.w_out = a.r1 == p.NC ? w_out : carry;
-    if (launch_delta_prep(a, p.bf, s) != hipSuccess ||
-        launch_delta_chain(a, p.bf, save_for_backward != 0, s) != hipSuccess)
+    a.nseg = (a.r1 - a.r0 + a.seglen - 1) / a.seglen;    // (the last stretch may be shorter)
+    if (launch_delta_prep(a, p.bf, s) != hipSuccess) return E2TTT_ERR_HIP;
+    if (a.nseg > 1 && (launch_delta_chain(a, p.bf, false, true, s) != hipSuccess ||
+                       launch_delta_join(a, false, s) != hipSuccess))
+      return E2TTT_ERR_HIP;
+    if (launch_delta_chain(a, p.bf, save_for_backward != 0, false, s) != hipSuccess)
       return E2TTT_ERR_HIP;
   }
   return E2TTT_OK;
@@ -196,10 +229,16 @@ extern "C" e2ttt_status e2ttt_delta_backward(
   a.d_w_in = d_w_in;
   a.dwst = reinterpret_cast<float*>(static_cast<char*>(scratch) + p.s_w);
   a.yst = reinterpret_cast<float*>(static_cast<char*>(scratch) + p.s_u);
+  a.segs = reinterpret_cast<float*>(static_cast<char*>(scratch) + p.s_segs);
+  a.segb = reinterpret_cast<float*>(static_cast<char*>(scratch) + p.s_segb);
   a.r0 = a.r_base = 0;
   a.r1 = (int)p.NC;
   const hipStream_t s = static_cast<hipStream_t>(stream);
-  if (launch_delta_chain_bwd(a, p.bf, s) != hipSuccess || launch_delta_grads(a, p.bf, s) != hipSuccess)
+  if (a.nseg > 1 && (launch_delta_chain_bwd(a, p.bf, true, s) != hipSuccess ||
+                     launch_delta_join(a, true, s) != hipSuccess))
+    return E2TTT_ERR_HIP;
+  if (launch_delta_chain_bwd(a, p.bf, false, s) != hipSuccess ||
+      launch_delta_grads(a, p.bf, s) != hipSuccess)
     return E2TTT_ERR_HIP;
   return E2TTT_OK;
 }

@@ -6,14 +6,18 @@
 //   dW_0 = G_C dW + sum_i s G_i dO_i q_i^T - sum_i eta_i G_i Y_i k_i^T.
 // As in the forward, a wave owns 16 columns of dW^T and carries them in its
 // accumulators; dW at every chunk end and Y are left for the gradients that
-// sum over the value dimension (delta_grads.hip).
+// sum over the value dimension (delta_grads.hip).  Long chains of few units run
+// as segments (delta_fwd.hip): a segment with the transition F takes the
+// adjoint at its end to dW F^T + B at its start.
 #include "delta_common.h"
 
 namespace e2ttt {
 namespace {
 
-template <bool BF, int DK, int NW>
-__global__ void __launch_bounds__(64 * NW, DK <= 64 ? 2 : 1) delta_bwd_kernel(DeltaArgs a, int nsl) {
+// STATE: only the adjoint at every segment's start, from zero at its end.
+template <bool BF, int DK, int NW, bool STATE>
+__global__ void __launch_bounds__(64 * NW, NW == 8 || DK <= 64 ? 2 : 1)
+delta_bwd_kernel(DeltaArgs a, int nsl) {
   using O = DOp<BF>;
   using E = typename O::E;
   using L = LTile<BF, DK>;
@@ -31,15 +35,20 @@ __global__ void __launch_bounds__(64 * NW, DK <= 64 ? 2 : 1) delta_bwd_kernel(De
   __shared__ __align__(16) float gl[kGateChain];
 
   const char* ps = ts + tri_bytes(BF, 3);
-  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, g = lane >> 4, c = lane & 15;
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, c = lane & 15;
+  const int w = wave_id();
   const long U = (long)a.B * a.H;
   const long blk = blockIdx.x;
-  const long u = (blk / (8 * nsl)) * 8 + blk % 8;
-  if (u >= U) return;
+  const long us = (blk / (8 * nsl)) * 8 + blk % 8;       // (unit, segment)
+  if (us >= U * a.nseg) return;
+  const long u = us / a.nseg;
+  const int seg = (int)(us % a.nseg);
+  if (STATE && seg == 0) return;
+  const int r0 = a.r0 + seg * a.seglen, r1 = min(a.r1, r0 + a.seglen);
   const int sl = (int)((blk / 8) % nsl);
   const int b = (int)(u / a.H), h = (int)(u % a.H), hk = h / (a.H / a.HK);
   const int nlive = live_tokens(a, b);
-  const int sc0 = sl * NW * 16, col = sc0 + 16 * w + c;
+  const int sc0 = sl * NW * 16, col = sc0 + 16 * w + c, tile = sl * NW + w;
   const int krow = tid / L::NP, kcol = (tid % L::NP) * L::PE;
   const int vrow = tid / LV::NP, vcol = (tid % LV::NP) * LV::PE;
   const bool kok = kcol < a.dk, vok = sc0 + vcol < a.dv;
@@ -50,8 +59,14 @@ __global__ void __launch_bounds__(64 * NW, DK <= 64 ? 2 : 1) delta_bwd_kernel(De
   for (int m = 0; m < MT; ++m) {
     const int kc = lab(m, 4 * g);
     st[m] = zero4();
-    if (a.d_w_out && col < a.dv && kc < a.dk)
+    if constexpr (STATE) continue;
+    if (seg < a.nseg - 1) {
+      if (col < a.dvp)
+        st[m] = *reinterpret_cast<const f32x4*>(a.segs + us * a.dvp * DK +
+                                                lane_at(tile, m / 2, KT, lane) + 256 * (m & 1));
+    } else if (a.d_w_out && col < a.dv && kc < a.dk) {
       st[m] = *reinterpret_cast<const f32x4*>(a.d_w_out + (u * a.dv + col) * a.dk + kc);
+    }
   }
 
   u32x4 rk[PK], rq[PK], rv[PV];
@@ -86,9 +101,9 @@ __global__ void __launch_bounds__(64 * NW, DK <= 64 ? 2 : 1) delta_bwd_kernel(De
     if (tid < kGateChain / 4)
       rg = *reinterpret_cast<const f32x4*>(a.gate + cu * kGateFloats + 4 * tid);
   };
-  if (a.r0 < a.r1) fetch(a.r1 - 1);
+  if (r0 < r1) fetch(r1 - 1);
 
-  for (int r = a.r1 - 1; r >= a.r0; --r) {
+  for (int r = r1 - 1; r >= r0; --r) {
     const long cu = u * a.nc_buf + (r - a.r_base);
     __syncthreads();
 #pragma unroll
@@ -105,14 +120,14 @@ __global__ void __launch_bounds__(64 * NW, DK <= 64 ? 2 : 1) delta_bwd_kernel(De
       reinterpret_cast<u32x4*>(ts)[min(tid + x * NTH, NF - 1)] = rf[x];
     if (tid < kGateChain / 4) *reinterpret_cast<f32x4*>(gl + 4 * tid) = rg;
     __syncthreads();
-    if (r > a.r0) fetch(r - 1);
+    if (r > r0) fetch(r - 1);
 
     typename O::S sb[KT];
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt) {
       sb[kt] = O::template split<3>(st[2 * kt], st[2 * kt + 1]);
-      if (col < a.dvp)
-        st_lane(a.dwst + cu * a.dvp * DK + lane_at(sl * NW + w, kt, KT, lane), st[2 * kt],
+      if (!STATE && col < a.dvp)
+        st_lane(a.dwst + cu * a.dvp * DK + lane_at(tile, kt, KT, lane), st[2 * kt],
                 st[2 * kt + 1]);
     }
     f32x4 xa[4];
@@ -160,8 +175,8 @@ __global__ void __launch_bounds__(64 * NW, DK <= 64 ? 2 : 1) delta_bwd_kernel(De
     }
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
-      if (col < a.dvp)
-        st_lane(a.yst + cu * a.dvp * kDC + lane_at(sl * NW + w, x, 2, lane), xa[2 * x],
+      if (!STATE && col < a.dvp)
+        st_lane(a.yst + cu * a.dvp * kDC + lane_at(tile, x, 2, lane), xa[2 * x],
                 xa[2 * x + 1]);
       const float* gp = gl + kGEtaG + 32 * x + 8 * g;
       rb[x] = O::template split<3>(xa[2 * x] * -*reinterpret_cast<const f32x4*>(gp),
@@ -174,7 +189,15 @@ __global__ void __launch_bounds__(64 * NW, DK <= 64 ? 2 : 1) delta_bwd_kernel(De
         st[m] = O::template xs<3>(st[m], L::template frag_t<false>(ks, m, x, g, c), rb[x]);
   }
 
-  if (a.d_w_in) {
+  if constexpr (STATE) {
+    if (col < a.dvp) {
+#pragma unroll
+      for (int kt = 0; kt < KT; ++kt)
+        st_lane(a.segb + us * a.dvp * DK + lane_at(tile, kt, KT, lane), st[2 * kt], st[2 * kt + 1]);
+    }
+    return;
+  }
+  if (a.d_w_in && seg == 0) {
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
       const int kc = lab(m, 4 * g);
@@ -185,26 +208,29 @@ __global__ void __launch_bounds__(64 * NW, DK <= 64 ? 2 : 1) delta_bwd_kernel(De
 }
 
 template <bool BF, int DK, int NW>
-hipError_t go(const DeltaArgs& a, hipStream_t s) {
+hipError_t go(const DeltaArgs& a, bool state, hipStream_t s) {
   const int nsl = (a.dvp + 16 * NW - 1) / (16 * NW);
-  const long u8 = ((long)a.B * a.H + 7) / 8 * 8;
-  hipLaunchKernelGGL((delta_bwd_kernel<BF, DK, NW>), dim3((unsigned)(u8 * nsl)), dim3(64 * NW), 0, s,
-                     a, nsl);
+  const long u8 = ((long)a.B * a.H * a.nseg + 7) / 8 * 8;
+  const dim3 grid((unsigned)(u8 * nsl)), blk(64 * NW);
+  if (state)
+    hipLaunchKernelGGL((delta_bwd_kernel<BF, DK, NW, true>), grid, blk, 0, s, a, nsl);
+  else
+    hipLaunchKernelGGL((delta_bwd_kernel<BF, DK, NW, false>), grid, blk, 0, s, a, nsl);
   return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_delta_chain_bwd(const DeltaArgs& a, bool bf, hipStream_t s) {
+hipError_t launch_delta_chain_bwd(const DeltaArgs& a, bool bf, bool state, hipStream_t s) {
   const int dkp = delta_dkp(a.dk);
   if (bf) {
-    if (dkp == 32) return go<true, 32, 2>(a, s);
-    if (dkp == 64) return go<true, 64, 4>(a, s);
-    return go<true, 128, 4>(a, s);
+    if (dkp == 32) return go<true, 32, 2>(a, state, s);
+    if (dkp == 64) return go<true, 64, 4>(a, state, s);
+    return go<true, 128, 8>(a, state, s);
   }
-  if (dkp == 32) return go<false, 32, 2>(a, s);
-  if (dkp == 64) return go<false, 64, 4>(a, s);
-  return go<false, 128, 4>(a, s);
+  if (dkp == 32) return go<false, 32, 2>(a, state, s);
+  if (dkp == 64) return go<false, 64, 4>(a, state, s);
+  return go<false, 128, 4>(a, state, s);
 }
 
 }  // namespace e2ttt

@@ -65,10 +65,22 @@ struct DeltaArgs {
   int B, HK, H, T, dk, dv, dvp;   // dvp: dv padded to a multiple of 32
   int NC;                     // chunks of the whole call
   int r0, r1;                 // chunks of this launch
+  // The launch's chunks in nseg segments of seglen (the last may be shorter):
+  int nseg, seglen;
+  float* segs;                // [unit][nseg] what the segments start (backward: end) from, in lane
+                              // order (dvp x dkp); entry 0 (the last) is w_in (d_w_out)
+  float* segb;                // [unit][nseg] what they make of a zero state, in lane order
+  float* segf;                // [unit][nseg] their transitions F (W -> W F): rows in lane order
+                              // (dkp x dkp), then the transpose in C order
   int nc_buf;                 // chunks per unit that the buffers hold (index r - r_base)
   int r_base;
   float scale;
 };
+
+// The wave's number in its workgroup, in a scalar register.
+__device__ __forceinline__ int wave_id() {
+  return __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+}
 
 __device__ __forceinline__ int lab(int m, int r) {
   return 32 * (m >> 1) + 8 * (r >> 2) + 4 * (m & 1) + (r & 3);
@@ -378,8 +390,12 @@ struct DeltaStepArgs {
 // -------------------------------------------------------------- launchers
 hipError_t launch_delta_step(const DeltaStepArgs& a, bool bf, hipStream_t stream);
 hipError_t launch_delta_prep(const DeltaArgs& a, bool bf, hipStream_t stream);
-hipError_t launch_delta_chain(const DeltaArgs& a, bool bf, bool save, hipStream_t stream);
-hipError_t launch_delta_chain_bwd(const DeltaArgs& a, bool bf, hipStream_t stream);
+// The chain over every segment from its start (end) state: `state`, only what
+// the segments make of a zero state and their transitions.
+hipError_t launch_delta_chain(const DeltaArgs& a, bool bf, bool save, bool state, hipStream_t stream);
+hipError_t launch_delta_chain_bwd(const DeltaArgs& a, bool bf, bool state, hipStream_t stream);
+// The segments' start states from their parts, one after the other.
+hipError_t launch_delta_join(const DeltaArgs& a, bool bwd, hipStream_t stream);
 hipError_t launch_delta_grads(const DeltaArgs& a, bool bf, hipStream_t stream);
 // padded key dimension (32, 64 or 128) and value dimension (a multiple of 32)
 inline int delta_dkp(int dk) { return dk <= 32 ? 32 : dk <= 64 ? 64 : 128; }

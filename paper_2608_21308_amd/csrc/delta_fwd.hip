@@ -12,13 +12,24 @@
 // is formed transposed (operands exchanged), so that a lane holds four
 // neighbouring channels of a token and stores them at once.  The next chunk's
 // global loads are issued before the current one's products.
+//
+// A chain is as long as its sequence, and few units leave most of the card
+// idle.  The chunks then run as segments: what a segment makes of a state is
+// W -> W F + B, so a first pass takes B (the columns above from zero) and F
+// (dk more columns, from the unit matrix, with V = 0) of every segment at
+// once, delta_join.hip forms the states that the segments start from, and
+// this pass runs them all at once.
 #include "delta_common.h"
 
 namespace e2ttt {
 namespace {
 
-template <bool BF, int DK, int NW, bool SAVE>
-__global__ void __launch_bounds__(64 * NW, DK <= 64 ? 2 : 1) delta_fwd_kernel(DeltaArgs a, int nsl) {
+enum { kPlain = 0, kSave = 1, kState = 2 };
+
+template <bool BF, int DK, int NW, int MODE>
+__global__ void __launch_bounds__(64 * NW, NW == 8 || DK <= 64 ? 2 : 1)
+delta_fwd_kernel(DeltaArgs a, int nsl) {
+  constexpr bool SAVE = MODE == kSave, OUT = MODE != kState;
   using O = DOp<BF>;
   using E = typename O::E;
   using L = LTile<BF, DK>;
@@ -26,28 +37,35 @@ __global__ void __launch_bounds__(64 * NW, DK <= 64 ? 2 : 1) delta_fwd_kernel(De
   constexpr int NTH = 64 * NW, KT = DK / 32, MT = DK / 16;
   constexpr int PK = kDC * L::NP / NTH;                 // a thread's pieces of K (Q) rows
   constexpr int PV = kDC * LV::NP / NTH;                // and of V rows
-  constexpr int NF = (tri_bytes(BF, 3) + tri_bytes(BF, 2)) / 16;   // pieces of T and P
+  constexpr int NF = (tri_bytes(BF, 3) + (OUT ? tri_bytes(BF, 2) : 0)) / 16;   // pieces of T and P
   constexpr int PF = (NF + NTH - 1) / NTH;
   static_assert(kDC * L::NP % NTH == 0 && NTH % L::NP == 0 && NTH % LV::NP == 0,
                 "whole rounds of pieces");
   __shared__ __align__(16) E ks[kDC * DK];
-  __shared__ __align__(16) E qs[kDC * DK];
+  __shared__ __align__(16) E qs[OUT ? kDC * DK : 8];
   __shared__ __align__(16) E vs[kDC * 16 * NW];
   __shared__ __align__(16) char ts[16 * NF];             // T, then P
   __shared__ __align__(16) float gl[kGateChain];
 
   const char* ps = ts + tri_bytes(BF, 3);
-  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, g = lane >> 4, c = lane & 15;
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, c = lane & 15;
+  const int w = wave_id();
   // the slices of a unit go to one XCD (workgroups are dealt to the eight in turn)
   const long U = (long)a.B * a.H;
   const long blk = blockIdx.x;
-  const long u = (blk / (8 * nsl)) * 8 + blk % 8;
-  if (u >= U) return;
+  const long us = (blk / (8 * nsl)) * 8 + blk % 8;       // (unit, segment)
+  if (us >= U * a.nseg) return;
+  const long u = us / a.nseg;
+  const int seg = (int)(us % a.nseg);
+  const int r0 = a.r0 + seg * a.seglen, r1 = min(a.r1, r0 + a.seglen);
   const int sl = (int)((blk / 8) % nsl);
+  // (nothing starts behind the last segment; the backward wants its transition)
+  if (MODE == kState && seg == a.nseg - 1 && (a.pterms == 2 || (sl + 1) * NW <= a.dvp / 16)) return;
   const int b = (int)(u / a.H), h = (int)(u % a.H), hk = h / (a.H / a.HK);
   const int nlive = live_tokens(a, b);
   const int sc0 = sl * NW * 16;                          // the workgroup's first column
   const int col = sc0 + 16 * w + c;                      // the lane's
+  const int tile = sl * NW + w, nvt = a.dvp / 16;        // the wave's tile: of B, or behind them of F
   // thread offsets within a chunk (32 bits: rows are at most 2^23 elements apart)
   const int krow = tid / L::NP, kcol = (tid % L::NP) * L::PE;
   const int vrow = tid / LV::NP, vcol = (tid % LV::NP) * LV::PE;
@@ -59,8 +77,16 @@ __global__ void __launch_bounds__(64 * NW, DK <= 64 ? 2 : 1) delta_fwd_kernel(De
   for (int m = 0; m < MT; ++m) {
     const int kc = lab(m, 4 * g);
     st[m] = zero4();
-    if (a.w_in && col < a.dv && kc < a.dk)
+    if constexpr (MODE == kState) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) st[m][e] = 16 * (tile - nvt) + c == kc + e ? 1.0f : 0.0f;
+    } else if (seg > 0) {
+      if (col < a.dvp)
+        st[m] = *reinterpret_cast<const f32x4*>(a.segs + us * a.dvp * DK +
+                                                lane_at(tile, m / 2, KT, lane) + 256 * (m & 1));
+    } else if (a.w_in && col < a.dv && kc < a.dk) {
       st[m] = *reinterpret_cast<const f32x4*>(a.w_in + (u * a.dv + col) * a.dk + kc);
+    }
   }
 
   u32x4 rk[PK], rq[PK], rv[PV];
@@ -78,7 +104,7 @@ __global__ void __launch_bounds__(64 * NW, DK <= 64 ? 2 : 1) delta_fwd_kernel(De
       rk[x] = rq[x] = u32x4{0, 0, 0, 0};
       if (kok && row < nt) {
         rk[x] = *reinterpret_cast<const u32x4*>(kp + row * kst);
-        rq[x] = *reinterpret_cast<const u32x4*>(qp + row * qst);
+        if constexpr (OUT) rq[x] = *reinterpret_cast<const u32x4*>(qp + row * qst);
       }
     }
 #pragma unroll
@@ -95,9 +121,9 @@ __global__ void __launch_bounds__(64 * NW, DK <= 64 ? 2 : 1) delta_fwd_kernel(De
     if (tid < kGateChain / 4)
       rg = *reinterpret_cast<const f32x4*>(a.gate + cu * kGateFloats + 4 * tid);
   };
-  if (a.r0 < a.r1) fetch(a.r0);
+  if (r0 < r1) fetch(r0);
 
-  for (int r = a.r0; r < a.r1; ++r) {
+  for (int r = r0; r < r1; ++r) {
     const int t0 = r * kDC;
     const long cu = u * a.nc_buf + (r - a.r_base);
     __syncthreads();
@@ -105,7 +131,7 @@ __global__ void __launch_bounds__(64 * NW, DK <= 64 ? 2 : 1) delta_fwd_kernel(De
     for (int x = 0; x < PK; ++x) {
       const int at = L::at(krow + x * (NTH / L::NP), tid % L::NP);
       *reinterpret_cast<u32x4*>(ks + at) = rk[x];
-      *reinterpret_cast<u32x4*>(qs + at) = rq[x];
+      if constexpr (OUT) *reinterpret_cast<u32x4*>(qs + at) = rq[x];
     }
 #pragma unroll
     for (int x = 0; x < PV; ++x)
@@ -115,7 +141,7 @@ __global__ void __launch_bounds__(64 * NW, DK <= 64 ? 2 : 1) delta_fwd_kernel(De
       reinterpret_cast<u32x4*>(ts)[min(tid + x * NTH, NF - 1)] = rf[x];
     if (tid < kGateChain / 4) *reinterpret_cast<f32x4*>(gl + 4 * tid) = rg;
     __syncthreads();
-    if (r + 1 < a.r1) fetch(r + 1);
+    if (r + 1 < r1) fetch(r + 1);
 
     typename O::S sb[KT];
 #pragma unroll
@@ -160,6 +186,7 @@ __global__ void __launch_bounds__(64 * NW, DK <= 64 ? 2 : 1) delta_fwd_kernel(De
       for (int x = 0; x <= m / 2; ++x)
         xa[m] = O::template ss<3>(xa[m], ld_frag<BF, 3>(ts, fidx(m, x), lane), rb[x]);
     }
+    if constexpr (OUT) {
 #pragma unroll
     for (int m = 0; m < 4; ++m) {
       oa[m] = zero4();
@@ -168,10 +195,11 @@ __global__ void __launch_bounds__(64 * NW, DK <= 64 ? 2 : 1) delta_fwd_kernel(De
         oa[m] = O::template sx<2>(oa[m], sb[kt], L::frag(qs, lab(m, c), kt, g));
       oa[m] = oa[m] * gl[kGsG + lab(m, c)];
     }
+    }
     typename O::S ub[2];
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
-      ub[x] = O::template split<2>(xa[2 * x], xa[2 * x + 1]);
+      if constexpr (OUT) ub[x] = O::template split<2>(xa[2 * x], xa[2 * x + 1]);
       if constexpr (SAVE) {
         if (col < a.dvp)
           st_lane(a.ust + cu * a.dvp * kDC + lane_at(sl * NW + w, x, 2, lane), xa[2 * x],
@@ -193,6 +221,7 @@ __global__ void __launch_bounds__(64 * NW, DK <= 64 ? 2 : 1) delta_fwd_kernel(De
       for (int x = 0; x < 2; ++x)
         st[m] = O::template xs<3>(st[m], L::template frag_t<false>(ks, m, x, g, c), ue[x]);
     }
+    if constexpr (OUT) {
     E* op = row_of_w<E>(a.out, b, h, t0) + sc0 + 16 * w + 4 * g;
 #pragma unroll
     for (int m = 0; m < 4; ++m) {
@@ -202,9 +231,28 @@ __global__ void __launch_bounds__(64 * NW, DK <= 64 ? 2 : 1) delta_fwd_kernel(De
       if (sc0 + 16 * w + 4 * g < a.dv && t0 + lab(m, c) < a.T)
         IoT<BF>::st4(op + lab(m, c) * ost, oa[m]);
     }
+    }
   }
 
-  if (a.w_out) {
+  if constexpr (MODE == kState) {
+    if (tile < nvt) {
+#pragma unroll
+      for (int kt = 0; kt < KT; ++kt)
+        st_lane(a.segb + us * a.dvp * DK + lane_at(tile, kt, KT, lane), st[2 * kt], st[2 * kt + 1]);
+    } else if (tile < nvt + MT) {
+      float* f = a.segf + us * 2 * DK * DK;
+      const int row = 16 * (tile - nvt) + c;
+#pragma unroll
+      for (int kt = 0; kt < KT; ++kt)
+        st_lane(f + lane_at(tile - nvt, kt, KT, lane), st[2 * kt], st[2 * kt + 1]);
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) f[DK * DK + (lab(m, 4 * g) + e) * DK + row] = st[m][e];
+    }
+    return;
+  }
+  if (a.w_out && seg == a.nseg - 1) {
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
       const int kc = lab(m, 4 * g);
@@ -215,29 +263,31 @@ __global__ void __launch_bounds__(64 * NW, DK <= 64 ? 2 : 1) delta_fwd_kernel(De
 }
 
 template <bool BF, int DK, int NW>
-hipError_t go(const DeltaArgs& a, bool save, hipStream_t s) {
-  const int nsl = (delta_dvp(a.dv) + 16 * NW - 1) / (16 * NW);
-  const long u8 = ((long)a.B * a.H + 7) / 8 * 8;
+hipError_t go(const DeltaArgs& a, bool save, bool state, hipStream_t s) {
+  const int tiles = a.dvp / 16 + (state ? DK / 16 : 0), nsl = (tiles + NW - 1) / NW;
+  const long u8 = ((long)a.B * a.H * a.nseg + 7) / 8 * 8;
   const dim3 grid((unsigned)(u8 * nsl)), blk(64 * NW);
-  if (save)
-    hipLaunchKernelGGL((delta_fwd_kernel<BF, DK, NW, true>), grid, blk, 0, s, a, nsl);
+  if (state)
+    hipLaunchKernelGGL((delta_fwd_kernel<BF, DK, NW, kState>), grid, blk, 0, s, a, nsl);
+  else if (save)
+    hipLaunchKernelGGL((delta_fwd_kernel<BF, DK, NW, kSave>), grid, blk, 0, s, a, nsl);
   else
-    hipLaunchKernelGGL((delta_fwd_kernel<BF, DK, NW, false>), grid, blk, 0, s, a, nsl);
+    hipLaunchKernelGGL((delta_fwd_kernel<BF, DK, NW, kPlain>), grid, blk, 0, s, a, nsl);
   return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_delta_chain(const DeltaArgs& a, bool bf, bool save, hipStream_t s) {
+hipError_t launch_delta_chain(const DeltaArgs& a, bool bf, bool save, bool state, hipStream_t s) {
   const int dkp = delta_dkp(a.dk);
   if (bf) {
-    if (dkp == 32) return go<true, 32, 2>(a, save, s);
-    if (dkp == 64) return go<true, 64, 4>(a, save, s);
-    return go<true, 128, 4>(a, save, s);
+    if (dkp == 32) return go<true, 32, 2>(a, save, state, s);
+    if (dkp == 64) return go<true, 64, 4>(a, save, state, s);
+    return go<true, 128, 8>(a, save, state, s);
   }
-  if (dkp == 32) return go<false, 32, 2>(a, save, s);
-  if (dkp == 64) return go<false, 64, 4>(a, save, s);
-  return go<false, 128, 4>(a, save, s);
+  if (dkp == 32) return go<false, 32, 2>(a, save, state, s);
+  if (dkp == 64) return go<false, 64, 4>(a, save, state, s);
+  return go<false, 128, 4>(a, save, state, s);
 }
 
 }  // namespace e2ttt

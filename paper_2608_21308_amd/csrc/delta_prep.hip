@@ -56,7 +56,8 @@ __global__ void __launch_bounds__(256) delta_prep_kernel(DeltaArgs a) {
   __shared__ float gl[kGateFloats];
   __shared__ float am[kDC * LDT];   // diag(eta) M
   __shared__ float tm[kDC * LDT];   // its unit lower inverse
-  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, g = lane >> 4, c = lane & 15;
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, c = lane & 15;
+  const int w = wave_id();
   const int nr = a.r1 - a.r0;
   const long u = blockIdx.x / nr;
   const int r = a.r0 + (int)(blockIdx.x % nr);

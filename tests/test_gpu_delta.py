@@ -73,7 +73,7 @@ def check(x, d, c, io, layout="bhtd", lengths=None, use_d_w=True, tag=""):
     cfg = e2ttt.DeltaConfig(B, HK, H, T, dk, dv, e2ttt.DT_BF16 if io == "bf16" else e2ttt.DT_F32, scale)
     print("delta", c, io, layout, tag, flush=True)
     t, td = to_dev(x, io, layout), to_dev(d, io, layout)
-    ln = None if lengths is None else torch.tensor(lengths, dtype=torch.int32)
+    ln = None if lengths is None else torch.as_tensor(lengths).to(torch.int32)
     lg = None if ln is None else ln.cuda()
     out, w_out, ws = e2ttt.delta_forward(cfg, t["q"], t["k"], t["v"], t["eta"], t["log_gamma"],
                                          t["w_in"], lengths=lg, save_for_backward=True)
@@ -314,6 +314,17 @@ def test_state_in_place_and_in_stretches(monkeypatch):
         o, _, _ = e2ttt.delta_forward(cfg2, *[a[:, :, sl] for a in (q, k, v, eta, lg)], w2, w_out=w2)
         parts.append(o)
     assert torch.equal(torch.cat(parts, 2), out) and torch.equal(w2, w_out)
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+@pytest.mark.parametrize("c,lengths", [((1, 1, 1, 1500, 64, 64), None), ((2, 1, 2, 1030, 128, 72), (1030, 700)),
+                                       ((1, 2, 2, 801, 16, 40), None), ((2, 1, 1, 900, 72, 128), (0, 64))])
+def test_segments(c, lengths, io):
+    """Long chains of few units, which run as segments: forward and backward against the
+    recurrence, and a decay slow enough that the first segment's state reaches the last."""
+    x, d = make(*c, io, seed=31, rate=0.003)
+    check(x, d, c, io, "bthd" if c[0] == 1 else "bhtd",
+          lengths=None if lengths is None else torch.tensor(lengths))
 
 
 def test_graph_replays_and_streams():
