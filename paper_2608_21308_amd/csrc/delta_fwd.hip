@@ -143,24 +143,24 @@ delta_fwd_kernel(DeltaArgs a, int nsl) {
     __syncthreads();
     if (r + 1 < r1) fetch(r + 1);
 
+    // X, per 32 columns of the state
     typename O::S sb[KT];
+    f32x4 xa[4], oa[4], ua[4];
+#pragma unroll
+    for (int m = 0; m < 4; ++m) xa[m] = oa[m] = ua[m] = zero4();
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt) {
       sb[kt] = O::template split<3>(st[2 * kt], st[2 * kt + 1]);
       if constexpr (SAVE) {
         if (col < a.dvp)
-          st_lane(a.wst + cu * a.dvp * DK + lane_at(sl * NW + w, kt, KT, lane), st[2 * kt],
-                  st[2 * kt + 1]);
+          st_lane(a.wst + cu * a.dvp * DK + lane_at(tile, kt, KT, lane), st[2 * kt], st[2 * kt + 1]);
       }
-    }
-    f32x4 xa[4], oa[4];
 #pragma unroll
-    for (int m = 0; m < 4; ++m) {
-      xa[m] = zero4();
-#pragma unroll
-      for (int kt = 0; kt < KT; ++kt)
+      for (int m = 0; m < 4; ++m)
         xa[m] = O::template xs<3>(xa[m], L::frag(ks, lab(m, c), kt, g), sb[kt]);
     }
+    // R, and while it is formed the state's part of O
+    typename O::S rb[2], ub[2], ue[2];
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
       f32x4 v0, v1;
@@ -175,50 +175,38 @@ delta_fwd_kernel(DeltaArgs a, int nsl) {
         xa[2 * x][e] = fmaf(-h0[e], xa[2 * x][e], e0[e] * v0[e]);
         xa[2 * x + 1][e] = fmaf(-h1[e], xa[2 * x + 1][e], e1[e] * v1[e]);
       }
-    }
-    typename O::S rb[2];
+      rb[x] = O::template split<3>(xa[2 * x], xa[2 * x + 1]);
+      if constexpr (OUT) {
 #pragma unroll
-    for (int x = 0; x < 2; ++x) rb[x] = O::template split<3>(xa[2 * x], xa[2 * x + 1]);
+        for (int m = 2 * x; m < 2 * x + 2; ++m) {
 #pragma unroll
-    for (int m = 0; m < 4; ++m) {
-      xa[m] = zero4();
-#pragma unroll
-      for (int x = 0; x <= m / 2; ++x)
-        xa[m] = O::template ss<3>(xa[m], ld_frag<BF, 3>(ts, fidx(m, x), lane), rb[x]);
-    }
-    if constexpr (OUT) {
-#pragma unroll
-    for (int m = 0; m < 4; ++m) {
-      oa[m] = zero4();
-#pragma unroll
-      for (int kt = 0; kt < KT; ++kt)
-        oa[m] = O::template sx<2>(oa[m], sb[kt], L::frag(qs, lab(m, c), kt, g));
-      oa[m] = oa[m] * gl[kGsG + lab(m, c)];
-    }
-    }
-    typename O::S ub[2];
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      if constexpr (OUT) ub[x] = O::template split<2>(xa[2 * x], xa[2 * x + 1]);
-      if constexpr (SAVE) {
-        if (col < a.dvp)
-          st_lane(a.ust + cu * a.dvp * kDC + lane_at(sl * NW + w, x, 2, lane), xa[2 * x],
-                  xa[2 * x + 1]);
+          for (int kt = 0; kt < KT; ++kt)
+            oa[m] = O::template sx<2>(oa[m], sb[kt], L::frag(qs, lab(m, c), kt, g));
+          oa[m] = oa[m] * gl[kGsG + lab(m, c)];
+        }
       }
     }
-    typename O::S ue[2];
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      const f32x4 n0 = *reinterpret_cast<const f32x4*>(gl + kGEnd + 32 * x + 8 * g);
-      const f32x4 n1 = *reinterpret_cast<const f32x4*>(gl + kGEnd + 32 * x + 8 * g + 4);
-      ue[x] = O::template split<3>(xa[2 * x] * n0, xa[2 * x + 1] * n1);
-    }
+    // U, half by half; the first half's use overlaps the second's products
     const float gC = gl[kGC];
 #pragma unroll
-    for (int m = 0; m < MT; ++m) {
-      st[m] = st[m] * gC;
+    for (int m = 0; m < MT; ++m) st[m] = st[m] * gC;
 #pragma unroll
-      for (int x = 0; x < 2; ++x)
+    for (int x = 0; x < 2; ++x) {
+#pragma unroll
+      for (int m = 2 * x; m < 2 * x + 2; ++m)
+#pragma unroll
+        for (int y = 0; y <= x; ++y)
+          ua[m] = O::template ss<3>(ua[m], ld_frag<BF, 3>(ts, fidx(m, y), lane), rb[y]);
+      if constexpr (SAVE) {
+        if (col < a.dvp)
+          st_lane(a.ust + cu * a.dvp * kDC + lane_at(tile, x, 2, lane), ua[2 * x], ua[2 * x + 1]);
+      }
+      const f32x4 n0 = *reinterpret_cast<const f32x4*>(gl + kGEnd + 32 * x + 8 * g);
+      const f32x4 n1 = *reinterpret_cast<const f32x4*>(gl + kGEnd + 32 * x + 8 * g + 4);
+      ue[x] = O::template split<3>(ua[2 * x] * n0, ua[2 * x + 1] * n1);
+      if constexpr (OUT) ub[x] = O::template split<2>(ua[2 * x], ua[2 * x + 1]);
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
         st[m] = O::template xs<3>(st[m], L::template frag_t<false>(ks, m, x, g, c), ue[x]);
     }
     if constexpr (OUT) {

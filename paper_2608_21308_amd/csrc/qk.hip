@@ -61,6 +61,32 @@ __device__ __forceinline__ void st_piece(E* p, const float (&v)[V]) {
   *reinterpret_cast<typename Piece<E, V>::T*>(p) = x;
 }
 
+// sigma(x) by the hardware's exponential and reciprocal (an ulp each; the
+// rounding of x log2 e costs |x| 2^-24 of e^-x, below 2^-24 of x sigma(x)'s
+// largest values).
+__device__ __forceinline__ float sigma(float x) {
+  return rcp_f(1.0f + __builtin_amdgcn_exp2f(-1.44269504f * x));
+}
+
+// m times cosine and sine of 2 pi t, |t| <= 1/2: Taylor's series to x^9 around
+// the nearest quarter turn (|x| <= pi / 4, remainder below 2^-28).
+__device__ __forceinline__ void turn(float t, float m, float& co, float& si) {
+  const float q = rintf(4.0f * t);
+  const float x = fmaf(-0.25f, q, t) * 6.283185307f, x2 = x * x;
+  float s = fmaf(x2, 2.7557319e-6f, -1.9841270e-4f);
+  s = fmaf(x2, s, 8.3333333e-3f);
+  s = fmaf(x2, s, -1.6666667e-1f);
+  s = m * fmaf(x * x2, s, x);
+  float c = fmaf(x2, 2.4801587e-5f, -1.3888889e-3f);
+  c = fmaf(x2, c, 4.1666667e-2f);
+  c = fmaf(x2, c, -0.5f);
+  c = m * fmaf(x2, c, 1.0f);
+  const int n = (int)q;                     // -2 .. 2 quarter turns
+  const float a = n & 1 ? s : c, b = n & 1 ? c : s;
+  co = (n + 1) & 2 ? -a : a;
+  si = n & 2 ? -b : b;
+}
+
 // IPL: items of a lane.
 template <bool BF, int V, int IPL, bool BWD>
 __global__ void __launch_bounds__(256) qk_kernel(QkArgs a, unsigned flags) {
@@ -91,9 +117,7 @@ __global__ void __launch_bounds__(256) qk_kernel(QkArgs a, unsigned flags) {
       for (int i = 0; i < V; ++i) {
         double turns = p * (double)a.inv_freq[it * V + i] * 0.15915494309189535;
         turns -= rint(turns);
-        const float f = 2.0f * (float)turns;
-        co[x][i] = a.m * cospif(f);
-        si[x][i] = a.m * sinpif(f);
+        turn((float)turns, a.m, co[x][i], si[x][i]);
       }
     } else {
 #pragma unroll
@@ -146,7 +170,7 @@ __global__ void __launch_bounds__(256) qk_kernel(QkArgs a, unsigned flags) {
 #pragma unroll
         for (int i = 0; i < V; ++i) {
           raw[x][k][i] = u[x][k][i];
-          if (silu) u[x][k][i] = u[x][k][i] / (1.0f + expf(-u[x][k][i]));
+          if (silu) u[x][k][i] *= sigma(u[x][k][i]);
           ss = fmaf(u[x][k][i], u[x][k][i], ss);
           if (BWD) sd = fmaf(u[x][k][i], z[x][k][i], sd);
         }
@@ -157,7 +181,7 @@ __global__ void __launch_bounds__(256) qk_kernel(QkArgs a, unsigned flags) {
         ss += __shfl_xor(ss, o);
         if (BWD) sd += __shfl_xor(sd, o);
       }
-      r = 1.0f / sqrtf(ss + a.eps);
+      r = rsq_f(ss + a.eps);
     }
 #pragma unroll
     for (int x = 0; x < IPL; ++x) {
@@ -169,7 +193,7 @@ __global__ void __launch_bounds__(256) qk_kernel(QkArgs a, unsigned flags) {
           for (int i = 0; i < V; ++i) {
             float y = r * (z[x][k][i] - u[x][k][i] * f);
             if (silu) {
-              const float sg = 1.0f / (1.0f + expf(-raw[x][k][i]));
+              const float sg = sigma(raw[x][k][i]);
               y *= sg * (1.0f + raw[x][k][i] * (1.0f - sg));
             }
             u[x][k][i] = y;
