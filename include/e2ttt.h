@@ -389,8 +389,8 @@ typedef struct {
 
 /* Bytes of `workspace` for e2ttt_delta_forward and of `scratch` for
  * e2ttt_delta_backward (0 for a bad descriptor).  Without save_for_backward at
- * most about 224 MiB and one state per unit (more only where a single chunk of
- * every unit needs it); with it the workspace keeps, per unit and chunk, the
+ * most 704 MiB and one state per unit (more only where a single chunk of every
+ * unit needs it); with it the workspace keeps, per unit and chunk, the
  * chunk-start state and what the backward reuses, and must be passed to
  * e2ttt_delta_backward untouched. */
 size_t e2ttt_delta_workspace_bytes(const e2ttt_delta_desc* desc, int save_for_backward);

@@ -29,7 +29,8 @@ struct Plan {
   bool bf;
   long U, NC;
   int pterms;
-  long nc_buf;                    // chunks per unit held at once
+  long stretch;                   // chunks of a launch
+  long nc_buf;                    // chunks whose gates and fragments are held (all, saving)
   long nseg, seglen;              // segments of a stretch
   size_t o_gate, o_frag, o_state, o_segs, o_segb, o_segf, o_w, o_u, bytes;   // workspace
   size_t s_w, s_u, s_segs, s_segb, scratch;              // backward scratch
@@ -38,21 +39,25 @@ struct Plan {
 
 size_t up(size_t x) { return (x + 255) & ~(size_t)255; }
 
-// Calls that do not save run in stretches of chunks whose gates and fragments
-// fit here: what the first kernel of a stretch writes, the second reads from
-// the 256 MB last-level cache.
-constexpr size_t kStretchBytes = (size_t)224 << 20;
+// Gates and fragments of this many bytes are formed and used at a time.  What
+// one launch writes the next reads from the 256 MB last-level cache while it
+// is well below that (512 units of 64, 16 chunks: 222 us with 128 MB, 263 at
+// once); segments want long stretches instead, which they divide (16 units of
+// 128, 512 chunks: 795 us at once, 927 in four).
+constexpr size_t kCacheBytes = (size_t)128 << 20, kStretchBytes = (size_t)512 << 20;
 
 // Segments that `nch` chunks of U units run as (1: none).  A wave holds 16 value
 // channels of a unit, and the card takes 2048 such waves at once.  Segments
-// cost a pass over dv + dk channels ahead of the one over dv: four gain
-// nothing (128 units of 64, 64 chunks: 339 us against 285), eight halve the time
-// (32 units of 128, 32 chunks: 125 us against 186).  A segment of fewer than 4
-// chunks is not worth its joining.
+// cost a pass over dv + dk channels ahead of the one over dv: where the card has
+// room for four only they lose (128 units of 64, 64 chunks: 375 us against
+// 319), at eight they halve the time (32 units of 128, 32 chunks: 125 us
+// against 195).  n of them take (nch / n) (t_state + t_chain) + n t_join, about
+// 5 us and 1 us: least at n = sqrt(5 nch).
+long room(const e2ttt_delta_desc* d, long U) { return 2048 / (U * (delta_dvp(d->dv) / 16)); }
 long segments(const e2ttt_delta_desc* d, long U, long nch) {
-  const long waves = U * (delta_dvp(d->dv) / 16);
-  const long n = std::min(2048 / waves, nch / 4);
-  return n < 6 ? 1 : n;
+  const long most = room(d, U);
+  const long n = std::min(std::min(most, nch / 2), (long)sqrt(5.0 * nch));
+  return most < 6 || n < 3 ? 1 : n;
 }
 
 Plan plan(const e2ttt_delta_desc* d, bool save) {
@@ -66,21 +71,22 @@ Plan plan(const e2ttt_delta_desc* d, bool save) {
   const size_t frag = tri_bytes(p.bf, 3) + tri_bytes(p.bf, p.pterms);
   p.w_bytes = 4L * dkp * dvp;
   p.u_bytes = 4L * kDC * dvp;
-  p.nc_buf = p.NC;
-  if (!save) {
-    const long fit = (long)(kStretchBytes / ((gate + frag) * (size_t)p.U));
-    const long n = fit < 1 ? p.NC : (p.NC + fit - 1) / fit;   // stretches of equal length
-    p.nc_buf = (p.NC + n - 1) / n;
-  }
+  const size_t each = (gate + frag) * (size_t)p.U;
+  p.nseg = segments(d, p.U, p.NC);
+  const long fit = (long)((room(d, p.U) < 2 ? kCacheBytes : kStretchBytes) / each);
+  const long n = fit < 1 ? p.NC : (p.NC + fit - 1) / fit;       // stretches of equal length
+  p.stretch = (p.NC + n - 1) / n;
+  if (save && room(d, p.U) >= 2) p.stretch = p.NC;
+  p.nc_buf = save ? p.NC : p.stretch;
+  if (p.nseg > 1) p.nseg = std::min(p.nseg, segments(d, p.U, p.stretch));
+  p.seglen = (p.stretch + p.nseg - 1) / p.nseg;
+  p.nseg = (p.stretch + p.seglen - 1) / p.seglen;
   const size_t cus = (size_t)p.U * p.nc_buf;
   p.o_gate = 0;
   p.o_frag = up(p.o_gate + cus * gate);
-  p.nseg = segments(d, p.U, p.nc_buf);
-  p.seglen = (p.nc_buf + p.nseg - 1) / p.nseg;
-  p.nseg = (p.nc_buf + p.seglen - 1) / p.seglen;
   const size_t segs = p.nseg > 1 ? (size_t)p.U * p.nseg : 0;
   p.o_state = up(p.o_frag + cus * frag);
-  p.o_segs = up(p.o_state + (p.nc_buf < p.NC ? (size_t)p.U * d->dk * d->dv * 4 : 0));
+  p.o_segs = up(p.o_state + (p.stretch < p.NC ? (size_t)p.U * d->dk * d->dv * 4 : 0));
   p.o_segb = up(p.o_segs + segs * p.w_bytes);
   p.o_segf = up(p.o_segb + segs * p.w_bytes);
   p.o_w = up(p.o_segf + segs * 2 * dkp * dkp * 4);
@@ -139,7 +145,6 @@ void fill(DeltaArgs& a, const e2ttt_delta_desc* d, const Plan& p, char* ws) {
   a.segb = reinterpret_cast<float*>(ws + p.o_segb);
   a.segf = reinterpret_cast<float*>(ws + p.o_segf);
   a.seglen = (int)p.seglen;
-  a.nseg = (int)p.nseg;
   a.wst = reinterpret_cast<float*>(ws + p.o_w);
   a.ust = reinterpret_cast<float*>(ws + p.o_u);
 }
@@ -182,9 +187,10 @@ extern "C" e2ttt_status e2ttt_delta_forward(const e2ttt_delta_desc* desc,
   a.lengths = lengths;
   float* carry = reinterpret_cast<float*>(ws + p.o_state);
   const hipStream_t s = static_cast<hipStream_t>(stream);
-  for (long r0 = 0; r0 < p.NC; r0 += p.nc_buf) {
-    a.r0 = a.r_base = (int)r0;
-    a.r1 = (int)(r0 + p.nc_buf < p.NC ? r0 + p.nc_buf : p.NC);
+  for (long r0 = 0; r0 < p.NC; r0 += p.stretch) {
+    a.r0 = (int)r0;
+    a.r_base = save_for_backward ? 0 : (int)r0;
+    a.r1 = (int)std::min(r0 + p.stretch, p.NC);
     a.w_in = r0 == 0 ? w_in : carry;
     a.w_out = a.r1 == p.NC ? w_out : carry;
     a.nseg = (a.r1 - a.r0 + a.seglen - 1) / a.seglen;    // (the last stretch may be shorter)
@@ -233,6 +239,8 @@ extern "C" e2ttt_status e2ttt_delta_backward(
   a.segb = reinterpret_cast<float*>(static_cast<char*>(scratch) + p.s_segb);
   a.r0 = a.r_base = 0;
   a.r1 = (int)p.NC;
+  if (p.stretch < p.NC) a.seglen = (int)p.NC;   // (no segments)
+  a.nseg = (int)((p.NC + a.seglen - 1) / a.seglen);
   const hipStream_t s = static_cast<hipStream_t>(stream);
   if (a.nseg > 1 && (launch_delta_chain_bwd(a, p.bf, true, s) != hipSuccess ||
                      launch_delta_join(a, true, s) != hipSuccess))

@@ -85,6 +85,14 @@ __device__ __forceinline__ int wave_id() {
 __device__ __forceinline__ int lab(int m, int r) {
   return 32 * (m >> 1) + 8 * (r >> 2) + 4 * (m & 1) + (r & 3);
 }
+// exp(x) of a finite x: the hardware's power of two at x log2 e rounded, times
+// 1 + ln 2 times what the rounding left (2^-23 relative).
+__device__ __forceinline__ float exp_finite(float x) {
+  const float h = x * 1.44269504f;
+  const float l = fmaf(x, 1.44269504f, -h) + x * 1.92596299e-8f;
+  const float p = __builtin_amdgcn_exp2f(h);
+  return fmaf(p, l * 0.693147181f, p);
+}
 // Fragment (row tile m, 32-column block a <= m / 2) of a lower triangular matrix.
 __host__ __device__ constexpr int fidx(int m, int a) { return m < 2 ? m : 2 * (m - 1) + a; }
 

@@ -262,7 +262,7 @@ __global__ void __launch_bounds__(64 * NWV, 2) delta_grads_kernel(DeltaArgs a) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int j = j0 + e;
-          const float d = j <= i ? expf((bhi - bhj[e]) + (bli - blj[e])) : 0.0f;
+          const float d = j <= i ? exp_finite((bhi - bhj[e]) + (bli - blj[e])) : 0.0f;
           const float dy = j < i ? d * yu[n][y][e] : 0.0f;
           pa[y][e] = a.scale * (d * du[n][y][e]);
           pn[y][e] = -eta_i * dy;

@@ -16,7 +16,15 @@ namespace {
 
 constexpr int LDT = kDC + 4;   // row of the 64x64 fp32 arrays in LDS
 
-// C += A[ar.., ak..] B[bk.., bc..], 16x16 blocks of row-major LDS arrays;
+// LDS written and read by the same wave completes in order; this only keeps the
+// compiler from exchanging the two.
+__device__ __forceinline__ void wave_lds_order() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// C += A[ar.., ak..] B[bk.., bc..], 16x16 blocks of a row-major LDS array;
 // contraction index of slot (g, i) is 4 g + i.
 __device__ __forceinline__ f32x4 blk_a(const float* m, int r0, int k0, int g, int c) {
   return *reinterpret_cast<const f32x4*>(m + (r0 + c) * LDT + k0 + 4 * g);
@@ -53,9 +61,9 @@ template <bool BF, int DK>
 __global__ void __launch_bounds__(256) delta_prep_kernel(DeltaArgs a) {
   using O = DOp<BF>;
   using E = typename O::E;
-  __shared__ float gl[kGateFloats];
-  __shared__ float am[kDC * LDT];   // diag(eta) M
-  __shared__ float tm[kDC * LDT];   // its unit lower inverse
+  __shared__ __align__(16) float gl[kGateFloats];
+  // diag(eta) M, block by block replaced by the unit lower inverse
+  __shared__ __align__(16) float am[kDC * LDT];
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, c = lane & 15;
   const int w = wave_id();
   const int nr = a.r1 - a.r0;
@@ -88,7 +96,6 @@ __global__ void __launch_bounds__(256) delta_prep_kernel(DeltaArgs a) {
     gl[kGBl + lane] = (float)(s - (double)bh);
     if (lane < 16) gl[kGC + lane] = expf((float)last);
   }
-  for (int x = tid; x < kDC * LDT; x += 256) tm[x] = am[x] = 0.0f;
 
   // rows of the products: i = lab(w, c) (columns of the MFMA tile), columns
   // j = lab(m, .) of tile m (its rows)
@@ -129,15 +136,18 @@ __global__ void __launch_bounds__(256) delta_prep_kernel(DeltaArgs a) {
       f32x4 p[2];
 #pragma unroll
       for (int y = 0; y < 2; ++y) {
+        const int j0 = 32 * x + 8 * g + 4 * y;
+        const f32x4 bhj = *reinterpret_cast<const f32x4*>(gl + kGBh + j0);
+        const f32x4 blj = *reinterpret_cast<const f32x4*>(gl + kGBl + j0);
         f32x4 m4;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const int j = 32 * x + 8 * g + 4 * y + e;
-          const float d = expf((bhi - gl[kGBh + j]) + (bli - gl[kGBl + j]));
+          const int j = j0 + e;
+          const float d = exp_finite((bhi - bhj[e]) + (bli - blj[e]));
           m4[e] = j < i ? eta * (d * kk[2 * x + y][e]) : 0.0f;
           p[y][e] = j <= i ? a.scale * (d * qk[2 * x + y][e]) : 0.0f;
         }
-        *reinterpret_cast<f32x4*>(am + i * LDT + 32 * x + 8 * g + 4 * y) = m4;
+        *reinterpret_cast<f32x4*>(am + i * LDT + j0) = m4;
       }
       if (a.pterms == 3)
         put_frag<BF, 3>(frag + tri_bytes(BF, 3), fidx(w, x), lane, p[0], p[1]);
@@ -155,27 +165,29 @@ __global__ void __launch_bounds__(256) delta_prep_kernel(DeltaArgs a) {
 
   // diagonal block w: column c of its inverse by substitution
   {
-    const int o = 16 * w;
+    float* d = am + 16 * w * LDT + 16 * w;
     float x[16];
 #pragma unroll
     for (int i1 = 0; i1 < 16; ++i1) {
       float s = i1 == c ? 1.0f : 0.0f;
 #pragma unroll
-      for (int l = 0; l < i1; ++l) s = fmaf(-am[(o + i1) * LDT + o + l], x[l], s);
+      for (int l = 0; l < i1; ++l) s = fmaf(-d[i1 * LDT + l], x[l], s);
       x[i1] = s;
     }
+    wave_lds_order();                   // (the block is read by this wave alone)
     if (g == 0) {
 #pragma unroll
-      for (int i1 = 0; i1 < 16; ++i1) tm[(o + i1) * LDT + o + c] = x[i1];
+      for (int i1 = 0; i1 < 16; ++i1) d[i1 * LDT + c] = x[i1];
     }
   }
   __syncthreads();
-  if (w < 2) {   // 16x16 blocks (1, 0) and (3, 2)
+  if (w < 2) {   // 16x16 blocks (1, 0) and (3, 2), each read by its wave alone
     const int o = 32 * w;
-    f32x4 z = mm16(zero4(), blk_a(am, o + 16, o, g, c), blk_b(tm, o, o, g, c));
-    z = mm16(zero4(), blk_a(tm, o + 16, o + 16, g, c), z);
+    f32x4 z = mm16(zero4(), blk_a(am, o + 16, o, g, c), blk_b(am, o, o, g, c));
+    z = mm16(zero4(), blk_a(am, o + 16, o + 16, g, c), z);
+    wave_lds_order();
 #pragma unroll
-    for (int e = 0; e < 4; ++e) tm[(o + 16 + 4 * g + e) * LDT + o + c] = -z[e];
+    for (int e = 0; e < 4; ++e) am[(o + 16 + 4 * g + e) * LDT + o + c] = -z[e];
   }
   __syncthreads();
   {              // the 32x32 block below: wave w its block (w / 2, w mod 2)
@@ -188,18 +200,19 @@ __global__ void __launch_bounds__(256) delta_prep_kernel(DeltaArgs a) {
 #pragma unroll
         for (int y = 0; y < 2; ++y)
           if (y >= ct)
-            z = mm16(z, blk_a(am, 32 + 16 * x, 16 * y, g, c), blk_b(tm, 16 * y, 16 * ct, g, c));
-        acc = mm16(acc, blk_a(tm, 32 + 16 * rt, 32 + 16 * x, g, c), z);
+            z = mm16(z, blk_a(am, 32 + 16 * x, 16 * y, g, c), blk_b(am, 16 * y, 16 * ct, g, c));
+        acc = mm16(acc, blk_a(am, 32 + 16 * rt, 32 + 16 * x, g, c), z);
       }
     }
+    __syncthreads();                    // every wave has read the block
 #pragma unroll
-    for (int e = 0; e < 4; ++e) tm[(32 + 16 * rt + 4 * g + e) * LDT + 16 * ct + c] = -acc[e];
+    for (int e = 0; e < 4; ++e) am[(32 + 16 * rt + 4 * g + e) * LDT + 16 * ct + c] = -acc[e];
   }
   __syncthreads();
 #pragma unroll
   for (int x = 0; x < 2; ++x) {
     if (x < na) {
-      const float* p = tm + i * LDT + 32 * x + 8 * g;
+      const float* p = am + i * LDT + 32 * x + 8 * g;
       put_frag<BF, 3>(frag, fidx(w, x), lane, *reinterpret_cast<const f32x4*>(p),
                       *reinterpret_cast<const f32x4*>(p + 4));
     }

@@ -31,7 +31,7 @@ struct QkArgs {
   int B, T, d, half;          // half: pairs that turn (rot / 2)
   int nh[2];                  // heads of queries and keys
   int hpg, nhg;               // heads of a group of lanes, groups of heads
-  int lanes;                  // lanes of a row (a power of two)
+  int lanes, llanes;          // lanes of a row (a power of two), its logarithm
   int tfast;                  // neighbouring groups: tokens (else heads)
   float eps, m;
 };
@@ -40,8 +40,7 @@ template <class E, int V> struct Piece { typedef __attribute__((ext_vector_type(
 template <class E> struct Piece<E, 1> { typedef E T; };
 
 template <class E, int V>
-__device__ __forceinline__ void ld_piece(float (&o)[V], const E* p) {
-  const auto x = *reinterpret_cast<const typename Piece<E, V>::T*>(p);
+__device__ __forceinline__ void widen(float (&o)[V], const typename Piece<E, V>::T& x) {
   if constexpr (V == 1) {
     o[0] = (float)x;
   } else {
@@ -58,7 +57,18 @@ __device__ __forceinline__ void st_piece(E* p, const float (&v)[V]) {
 #pragma unroll
     for (int i = 0; i < V; ++i) x[i] = (E)v[i];
   }
-  *reinterpret_cast<typename Piece<E, V>::T*>(p) = x;
+  __builtin_nontemporal_store(x, reinterpret_cast<typename Piece<E, V>::T*>(p));
+}
+
+// Sum over the lanes of a row (a power of two, neighbours).
+__device__ __forceinline__ float row_sum(float v, int lanes) {
+  if (lanes > 1) v += dpp_f<0xB1>(v);    // quad_perm [1,0,3,2]
+  if (lanes > 2) v += dpp_f<0x4E>(v);    // quad_perm [2,3,0,1]
+  if (lanes > 4) v += dpp_f<0x141>(v);   // row_half_mirror
+  if (lanes > 8) v += dpp_f<0x140>(v);   // row_mirror
+  if (lanes > 16) v += __shfl_xor(v, 16);
+  if (lanes > 32) v += __shfl_xor(v, 32);
+  return v;
 }
 
 // sigma(x) by the hardware's exponential and reciprocal (an ulp each; the
@@ -87,19 +97,30 @@ __device__ __forceinline__ void turn(float t, float m, float& co, float& si) {
   si = n & 2 ? -b : b;
 }
 
+// The pair (a, b) of index i in an item's two pieces.
+template <bool INTER, int V>
+__device__ __forceinline__ float& first_of(float (&u)[2][V], int i) {
+  return INTER ? u[(2 * i) / V][(2 * i) % V] : u[0][i];
+}
+template <bool INTER, int V>
+__device__ __forceinline__ float& second_of(float (&u)[2][V], int i) {
+  return INTER ? u[(2 * i + 1) / V][(2 * i + 1) % V] : u[1][i];
+}
+
 // IPL: items of a lane.
-template <bool BF, int V, int IPL, bool BWD>
+template <bool BF, int V, int IPL, bool BWD, bool INTER>
 __global__ void __launch_bounds__(256) qk_kernel(QkArgs a, unsigned flags) {
   using E = typename DOp<BF>::E;
-  const long gid = ((long)blockIdx.x * 256 + threadIdx.x) / a.lanes;
+  using P = typename Piece<E, V>::T;
+  // (at most 10^9 rows: 32 bits)
+  const unsigned gid = blockIdx.x * (256u >> a.llanes) + (threadIdx.x >> a.llanes);
   const int l = threadIdx.x & (a.lanes - 1);
-  const long ntok = (long)a.B * a.T;
+  const unsigned ntok = (unsigned)a.B * a.T;
   if (gid >= ntok * a.nhg) return;          // whole rows of lanes leave together
-  const long tok = a.tfast ? gid % ntok : gid / a.nhg;
+  const unsigned tok = a.tfast ? gid % ntok : gid / a.nhg;
   const int hg = (int)(a.tfast ? gid / ntok : gid % a.nhg);
-  const int b = (int)(tok / a.T), t = (int)(tok % a.T);
+  const int b = (int)(tok / (unsigned)a.T), t = (int)(tok - (unsigned)b * a.T);
   const bool silu = flags & E2TTT_QK_SILU, unit = flags & E2TTT_QK_UNIT;
-  const bool inter = flags & E2TTT_QK_INTERLEAVED;
   const int np = a.half / V;                // items that turn
   const int ntail = (a.d - 2 * a.half) / V; // pieces that do not
 
@@ -109,9 +130,14 @@ __global__ void __launch_bounds__(256) qk_kernel(QkArgs a, unsigned flags) {
   for (int x = 0; x < IPL; ++x) {
     const int it = l + x * a.lanes;
     c0[x] = c1[x] = -1;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      co[x][i] = 1.0f;
+      si[x][i] = 0.0f;
+    }
     if (it < np) {
-      c0[x] = inter ? 2 * it * V : it * V;
-      c1[x] = inter ? c0[x] + V : c0[x] + a.half;
+      c0[x] = INTER ? 2 * it * V : it * V;
+      c1[x] = INTER ? c0[x] + V : c0[x] + a.half;
       const double p = a.pos ? (double)a.pos[tok] : (double)t;
 #pragma unroll
       for (int i = 0; i < V; ++i) {
@@ -120,98 +146,113 @@ __global__ void __launch_bounds__(256) qk_kernel(QkArgs a, unsigned flags) {
         turn((float)turns, a.m, co[x][i], si[x][i]);
       }
     } else {
-#pragma unroll
-      for (int i = 0; i < V; ++i) {
-        co[x][i] = 1.0f;
-        si[x][i] = 0.0f;
-      }
       const int q = 2 * (it - np);
       if (q < ntail) c0[x] = 2 * a.half + q * V;
       if (q + 1 < ntail) c1[x] = 2 * a.half + (q + 1) * V;
     }
   }
 
-  const int nh = a.nh[0] + a.nh[1];
-  for (int hh = hg * a.hpg; hh < min(nh, (hg + 1) * a.hpg); ++hh) {
-    const int s = hh >= a.nh[0], h = s ? hh - a.nh[0] : hh;
-    const E* xp = row_of<E>(a.x[s], b, h, t);
-    E* yp = row_of_w<E>(a.y[s], b, h, t);
-    float u[IPL][2][V], z[IPL][2][V];       // x, then SiLU(x); the gradient
-    float ss = 0.0f, sd = 0.0f;
+  // rows of this token: queries, then keys
+  const E* xb[2] = {row_of<E>(a.x[0], b, 0, t), row_of<E>(a.x[1], b, 0, t)};
+  const E* gb[2] = {row_of<E>(a.g[0], b, 0, t), row_of<E>(a.g[1], b, 0, t)};
+  E* yb[2] = {row_of_w<E>(a.y[0], b, 0, t), row_of_w<E>(a.y[1], b, 0, t)};
+  const bool need = !BWD || silu || unit;
+  P rx[IPL][2], rg[IPL][2];                 // the next row, as it lies in memory
+  auto load = [&](int hh) {
+    const bool s = hh >= a.nh[0];
+    const long h = s ? hh - a.nh[0] : hh;
+    const E* xp = (s ? xb[1] : xb[0]) + h * (s ? a.x[1].h : a.x[0].h);
+    const E* gp = (s ? gb[1] : gb[0]) + h * (s ? a.g[1].h : a.g[0].h);
 #pragma unroll
     for (int x = 0; x < IPL; ++x)
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
         const int at = k ? c1[x] : c0[x];
-#pragma unroll
-        for (int i = 0; i < V; ++i) u[x][k][i] = z[x][k][i] = 0.0f;
+        rx[x][k] = rg[x][k] = P{};
         if (at >= 0) {
-          if (!BWD || silu || unit) ld_piece<E, V>(u[x][k], xp + at);
-          if (BWD) ld_piece<E, V>(z[x][k], row_of<E>(a.g[s], b, h, t) + at);
+          if (need) rx[x][k] = *reinterpret_cast<const P*>(xp + at);
+          if (BWD) rg[x][k] = *reinterpret_cast<const P*>(gp + at);
         }
       }
-    float raw[IPL][2][V];
+  };
+  const int h1 = min(a.nh[0] + a.nh[1], (hg + 1) * a.hpg);
+  load(hg * a.hpg);
+  for (int hh = hg * a.hpg; hh < h1; ++hh) {
+    float u[IPL][2][V], z[IPL][2][V], raw[IPL][2][V];
 #pragma unroll
-    for (int x = 0; x < IPL; ++x) {
-      if (BWD) {                            // back through the turn
+    for (int x = 0; x < IPL; ++x)
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        widen<E, V>(u[x][k], rx[x][k]);
+        if (BWD) widen<E, V>(z[x][k], rg[x][k]);
+      }
+    if (hh + 1 < h1) load(hh + 1);
+    if (BWD) {                              // back through the turn
+#pragma unroll
+      for (int x = 0; x < IPL; ++x)
         if (l + x * a.lanes < np) {
 #pragma unroll
           for (int i = 0; i < V; ++i) {
-            float& p = inter ? z[x][(2 * i) / V][(2 * i) % V] : z[x][0][i];
-            float& q = inter ? z[x][(2 * i + 1) / V][(2 * i + 1) % V] : z[x][1][i];
+            float &p = first_of<INTER, V>(z[x], i), &q = second_of<INTER, V>(z[x], i);
             const float za = p, zb = q;
             p = za * co[x][i] + zb * si[x][i];
             q = zb * co[x][i] - za * si[x][i];
           }
         }
-      }
+    }
+    if (silu) {
+#pragma unroll
+      for (int x = 0; x < IPL; ++x)
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+          for (int i = 0; i < V; ++i) {
+            const float sg = sigma(u[x][k][i]);
+            if (BWD) raw[x][k][i] = sg * fmaf(u[x][k][i], 1.0f - sg, 1.0f);   // the derivative
+            u[x][k][i] *= sg;
+          }
+    }
+    float r = 1.0f, f = 0.0f;
+    if (unit) {
+      float ss = 0.0f, sd = 0.0f;
+#pragma unroll
+      for (int x = 0; x < IPL; ++x)
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+          for (int i = 0; i < V; ++i) {
+            ss = fmaf(u[x][k][i], u[x][k][i], ss);
+            if (BWD) sd = fmaf(u[x][k][i], z[x][k][i], sd);
+          }
+      r = rsq_f(row_sum(ss, a.lanes) + a.eps);
+      if (BWD) f = row_sum(sd, a.lanes) * r * r;
+    }
+#pragma unroll
+    for (int x = 0; x < IPL; ++x)
 #pragma unroll
       for (int k = 0; k < 2; ++k)
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-          raw[x][k][i] = u[x][k][i];
-          if (silu) u[x][k][i] *= sigma(u[x][k][i]);
-          ss = fmaf(u[x][k][i], u[x][k][i], ss);
-          if (BWD) sd = fmaf(u[x][k][i], z[x][k][i], sd);
-        }
+        for (int i = 0; i < V; ++i) u[x][k][i] = BWD ? r * fmaf(-f, u[x][k][i], z[x][k][i]) : r * u[x][k][i];
+    if (BWD && silu) {
+#pragma unroll
+      for (int x = 0; x < IPL; ++x)
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+          for (int i = 0; i < V; ++i) u[x][k][i] *= raw[x][k][i];
     }
-    float r = 1.0f;
-    if (unit) {
-      for (int o = 1; o < a.lanes; o <<= 1) {
-        ss += __shfl_xor(ss, o);
-        if (BWD) sd += __shfl_xor(sd, o);
-      }
-      r = rsq_f(ss + a.eps);
-    }
+    const bool s = hh >= a.nh[0];
+    const long h = s ? hh - a.nh[0] : hh;
+    E* yp = (s ? yb[1] : yb[0]) + h * (s ? a.y[1].h : a.y[0].h);
 #pragma unroll
     for (int x = 0; x < IPL; ++x) {
-      if (BWD) {
-        const float f = unit ? sd * r * r : 0.0f;
+      if (!BWD && l + x * a.lanes < np) {
 #pragma unroll
-        for (int k = 0; k < 2; ++k)
-#pragma unroll
-          for (int i = 0; i < V; ++i) {
-            float y = r * (z[x][k][i] - u[x][k][i] * f);
-            if (silu) {
-              const float sg = sigma(raw[x][k][i]);
-              y *= sg * (1.0f + raw[x][k][i] * (1.0f - sg));
-            }
-            u[x][k][i] = y;
-          }
-      } else {
-#pragma unroll
-        for (int k = 0; k < 2; ++k)
-#pragma unroll
-          for (int i = 0; i < V; ++i) u[x][k][i] *= r;
-        if (l + x * a.lanes < np) {
-#pragma unroll
-          for (int i = 0; i < V; ++i) {
-            float& p = inter ? u[x][(2 * i) / V][(2 * i) % V] : u[x][0][i];
-            float& q = inter ? u[x][(2 * i + 1) / V][(2 * i + 1) % V] : u[x][1][i];
-            const float ya = p, yb = q;
-            p = ya * co[x][i] - yb * si[x][i];
-            q = yb * co[x][i] + ya * si[x][i];
-          }
+        for (int i = 0; i < V; ++i) {
+          float &p = first_of<INTER, V>(u[x], i), &q = second_of<INTER, V>(u[x], i);
+          const float ya = p, yb_ = q;
+          p = ya * co[x][i] - yb_ * si[x][i];
+          q = yb_ * co[x][i] + ya * si[x][i];
         }
       }
       if (c0[x] >= 0) st_piece<E, V>(yp + c0[x], u[x][0]);
@@ -223,8 +264,9 @@ __global__ void __launch_bounds__(256) qk_kernel(QkArgs a, unsigned flags) {
 template <bool BF, int V, bool BWD>
 hipError_t go(QkArgs a, unsigned flags, hipStream_t s) {
   const int items = a.half / V + ((a.d - 2 * a.half) / V + 1) / 2;
-  a.lanes = 1;
-  while (a.lanes < items && a.lanes < 64) a.lanes *= 2;
+  a.llanes = 0;
+  while ((1 << a.llanes) < items && a.llanes < 6) ++a.llanes;
+  a.lanes = 1 << a.llanes;
   const long rows = (long)a.B * a.T * (a.nh[0] + a.nh[1]);
   // Several heads to a group of lanes (their angles are the same) as long as
   // the card stays full: 256 CUs of 2048 lanes.
@@ -235,10 +277,15 @@ hipError_t go(QkArgs a, unsigned flags, hipStream_t s) {
   if (blocks > 0x7fffffffL) return hipErrorInvalidValue;
   // (d <= 256: only single pairs to a piece can make more than 64 items)
   constexpr int kMost = V == 1 ? 2 : 1;
-  if (items <= 64)
-    hipLaunchKernelGGL((qk_kernel<BF, V, 1, BWD>), dim3((unsigned)blocks), dim3(256), 0, s, a, flags);
-  else
-    hipLaunchKernelGGL((qk_kernel<BF, V, kMost, BWD>), dim3((unsigned)blocks), dim3(256), 0, s, a, flags);
+  const dim3 grid((unsigned)blocks), blk(256);
+  const bool inter = flags & E2TTT_QK_INTERLEAVED;
+  if (items > 64) {
+    if (inter) hipLaunchKernelGGL((qk_kernel<BF, V, kMost, BWD, true>), grid, blk, 0, s, a, flags);
+    else hipLaunchKernelGGL((qk_kernel<BF, V, kMost, BWD, false>), grid, blk, 0, s, a, flags);
+  } else {
+    if (inter) hipLaunchKernelGGL((qk_kernel<BF, V, 1, BWD, true>), grid, blk, 0, s, a, flags);
+    else hipLaunchKernelGGL((qk_kernel<BF, V, 1, BWD, false>), grid, blk, 0, s, a, flags);
+  }
   return hipGetLastError();
 }
 

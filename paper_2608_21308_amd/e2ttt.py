@@ -544,15 +544,16 @@ def _strided(name, t, shape, dtype, device):
 
 def _plain(name, t, shape, dtype, device):
     """The same for a contiguous tensor (None passes)."""
-    if t is not None and _strided(name, t, shape, dtype, device) is not None:
+    if t is None or (type(t) in _TENSORS and t.dtype is dtype and t.shape == shape and
+                     t.is_contiguous() and t.get_device() == device):
+        return
+    if _strided(name, t, shape, dtype, device) is not None:
         raise ValueError("%s must be contiguous" % name)
 
 
 @lru_cache(maxsize=256)
-def _strides_ref(kind, *given):
-    """The strides argument for (name, shape, strides) triples; None where all are in C order."""
-    if all(st is None for _, _, st in given):
-        return None
+def _strides_ref(kind, given):
+    """The strides argument for (name, shape, strides) triples."""
     s = kind()
     for name, shape, st in given:
         if st is None:
@@ -563,11 +564,26 @@ def _strides_ref(kind, *given):
     return ctypes.byref(s)
 
 
+def _layout(kind, device, *given):
+    """Checks (name, tensor, shape, dtype) and gives the call's strides argument
+    (None: every tensor in C order, found at the price that a call of a few
+    microseconds can afford)."""
+    for _, t, shape, dtype in given:
+        if not (type(t) in _TENSORS and t.dtype is dtype and t.shape == shape and
+                t.is_contiguous() and t.get_device() == device):
+            break
+    else:
+        return None
+    st = tuple((name, shape, _strided(name, t, shape, dtype, device))
+               for name, t, shape, dtype in given)
+    return _strides_ref(kind, st) if any(x[2] is not None for x in st) else None
+
+
 def _on_device(f):
     """The library works on the current device: make it that of the first tensor."""
     def call(cfg, q, *args, **kw):
-        if not isinstance(q, torch.Tensor) or not q.is_cuda:
-            raise ValueError("q must be a device tensor")
+        if not isinstance(q, torch.Tensor) or q.get_device() < 0:
+            raise ValueError("the first tensor must be a device tensor")
         if q.get_device() == _current_device():
             return f(cfg, q, *args, **kw)
         with torch.cuda.device(q.device):
@@ -642,26 +658,23 @@ def delta_forward(cfg: DeltaConfig, q, k, v, eta, log_gamma=None, w_in=None, *, 
     workspace); out has v's order in memory."""
     d, io, s_k, s_v, s_g, s_w = cfg._call
     dev, f32 = q.get_device(), torch.float32
-    given = [("q", s_k, _strided("q", q, s_k, io, dev)), ("k", s_k, _strided("k", k, s_k, io, dev)),
-             ("v", s_v, _strided("v", v, s_v, io, dev)),
-             ("eta", s_g, _strided("eta", eta, s_g, f32, dev))]
-    if log_gamma is not None:
-        given.append(("log_gamma", s_g, _strided("log_gamma", log_gamma, s_g, f32, dev)))
+    if out is None:
+        out = torch.empty_like(v)
+    st = _layout(DeltaStrides, dev, ("q", q, s_k, io), ("k", k, s_k, io), ("v", v, s_v, io),
+                 ("out", out, s_v, io), ("eta", eta, s_g, f32),
+                 *(() if log_gamma is None else (("log_gamma", log_gamma, s_g, f32),)))
     _plain("w_in", w_in, s_w, f32, dev)
     _plain("w_out", w_out, s_w, f32, dev)
     _plain("lengths", lengths, s_g[:1], torch.int32, dev)
     _buffer("workspace", workspace, dev)
-    if out is None:
-        out = torch.empty_like(v)
-    given.append(("out", s_v, _strided("out", out, s_v, io, dev)))
     if w_out is None:
         w_out = torch.empty(s_w, dtype=f32, device=q.device)
     if workspace is None:
         workspace = alloc_delta_workspace(cfg, save_for_backward, q.device)
-    st = load().e2ttt_delta_forward(d, _strides_ref(DeltaStrides, *given), _ptr(q), _ptr(k), _ptr(v),
-                                    _ptr(eta), _ptr(log_gamma), _ptr(lengths), _ptr(w_in), _ptr(out),
-                                    _ptr(w_out), _ptr(workspace), workspace.numel(),
-                                    int(bool(save_for_backward)), _stream())
+    st = (_lib or load()).e2ttt_delta_forward(
+        d, st, q.data_ptr(), k.data_ptr(), v.data_ptr(), eta.data_ptr(), _ptr(log_gamma),
+        _ptr(lengths), _ptr(w_in), out.data_ptr(), w_out.data_ptr(), workspace.data_ptr(),
+        workspace.numel(), int(bool(save_for_backward)), _stream())
     _check(st, "e2ttt_delta_forward")
     return out, w_out, workspace
 
@@ -679,17 +692,11 @@ def delta_backward(cfg: DeltaConfig, q, k, v, eta, log_gamma, workspace, d_out, 
                      d_log_gamma=None if log_gamma is None else torch.empty_like(log_gamma),
                      d_w_in=torch.empty(s_w, dtype=f32, device=q.device))
     g = grads
-    given = [("q", s_k, _strided("q", q, s_k, io, dev)), ("k", s_k, _strided("k", k, s_k, io, dev)),
-             ("v", s_v, _strided("v", v, s_v, io, dev)),
-             ("eta", s_g, _strided("eta", eta, s_g, f32, dev)),
-             ("d_out", s_v, _strided("d_out", d_out, s_v, io, dev)),
-             ("dq", s_k, _strided("dq", g["dq"], s_k, io, dev)),
-             ("dk", s_k, _strided("dk", g["dk"], s_k, io, dev)),
-             ("dv", s_v, _strided("dv", g["dv"], s_v, io, dev)),
-             ("d_eta", s_g, _strided("d_eta", g["d_eta"], s_g, f32, dev))]
-    if log_gamma is not None:
-        given += [("log_gamma", s_g, _strided("log_gamma", log_gamma, s_g, f32, dev)),
-                  ("d_log_gamma", s_g, _strided("d_log_gamma", g["d_log_gamma"], s_g, f32, dev))]
+    st = _layout(DeltaStrides, dev, ("q", q, s_k, io), ("k", k, s_k, io), ("v", v, s_v, io),
+                 ("d_out", d_out, s_v, io), ("dq", g["dq"], s_k, io), ("dk", g["dk"], s_k, io),
+                 ("dv", g["dv"], s_v, io), ("eta", eta, s_g, f32), ("d_eta", g["d_eta"], s_g, f32),
+                 *(() if log_gamma is None else (("log_gamma", log_gamma, s_g, f32),
+                                                 ("d_log_gamma", g["d_log_gamma"], s_g, f32))))
     _plain("d_w_out", d_w_out, s_w, f32, dev)
     _plain("d_w_in", g.get("d_w_in"), s_w, f32, dev)
     _plain("lengths", lengths, s_g[:1], torch.int32, dev)
@@ -697,8 +704,8 @@ def delta_backward(cfg: DeltaConfig, q, k, v, eta, log_gamma, workspace, d_out, 
     _buffer("scratch", scratch, dev)
     if scratch is None:
         scratch = torch.empty(delta_scratch_bytes(cfg), dtype=torch.uint8, device=q.device)
-    st = load().e2ttt_delta_backward(
-        d, _strides_ref(DeltaStrides, *given), _ptr(q), _ptr(k), _ptr(v), _ptr(eta), _ptr(log_gamma),
+    st = (_lib or load()).e2ttt_delta_backward(
+        d, st, _ptr(q), _ptr(k), _ptr(v), _ptr(eta), _ptr(log_gamma),
         _ptr(lengths), _ptr(workspace), workspace.numel(), _ptr(d_out), _ptr(d_w_out), _ptr(g["dq"]),
         _ptr(g["dk"]), _ptr(g["dv"]), _ptr(g["d_eta"]), _ptr(g.get("d_log_gamma")),
         _ptr(g.get("d_w_in")), _ptr(scratch), scratch.numel(), _stream())
@@ -715,21 +722,19 @@ def delta_step(cfg: DeltaConfig, q, k, v, eta, log_gamma, w, *, slots=None, out=
     are taken in order."""
     d, io, s_k, s_v, s_g, s_w = cfg._call
     dev, f32 = q.get_device(), torch.float32
-    given = [("q", s_k, _strided("q", q, s_k, io, dev)), ("k", s_k, _strided("k", k, s_k, io, dev)),
-             ("v", s_v, _strided("v", v, s_v, io, dev)),
-             ("eta", s_g, _strided("eta", eta, s_g, f32, dev))]
-    if log_gamma is not None:
-        given.append(("log_gamma", s_g, _strided("log_gamma", log_gamma, s_g, f32, dev)))
     if not isinstance(w, torch.Tensor) or w.dim() != 4 or w.shape[0] < 1:
         raise ValueError("w must be a tensor [N, H, dv, dk] of states")
-    _plain("w", w, w.shape[:1] + s_w[1:], f32, dev)
-    _plain("slots", slots, s_g[:1], torch.int32, dev)
     if out is None:
         out = torch.empty_like(v)
-    given.append(("out", s_v, _strided("out", out, s_v, io, dev)))
-    st = load().e2ttt_delta_step(d, _strides_ref(DeltaStrides, *given), _ptr(q), _ptr(k), _ptr(v),
-                                 _ptr(eta), _ptr(log_gamma), _ptr(w), _ptr(slots), w.shape[0],
-                                 _ptr(out), _stream())
+    st = _layout(DeltaStrides, dev, ("q", q, s_k, io), ("k", k, s_k, io), ("v", v, s_v, io),
+                 ("out", out, s_v, io), ("eta", eta, s_g, f32),
+                 *(() if log_gamma is None else (("log_gamma", log_gamma, s_g, f32),)))
+    n = w.shape[0]
+    _plain("w", w, (n, *s_w[1:]), f32, dev)
+    _plain("slots", slots, s_g[:1], torch.int32, dev)
+    st = (_lib or load()).e2ttt_delta_step(
+        d, st, q.data_ptr(), k.data_ptr(), v.data_ptr(), eta.data_ptr(), _ptr(log_gamma),
+        w.data_ptr(), _ptr(slots), n, out.data_ptr(), _stream())
     _check(st, "e2ttt_delta_step")
     return out
 
@@ -821,7 +826,7 @@ def rotary_frequencies(rot, base=10000.0, factor=1.0, original=None, fast=32.0, 
 
 
 def _qk_common(cfg, dev, inv_freq, positions):
-    _, _, _, _, s_p, s_f = cfg._call
+    s_p, s_f = cfg._call[4:]
     if cfg.rot and inv_freq is None:
         raise ValueError("inv_freq must be given where rot > 0")
     _plain("inv_freq", inv_freq, s_f, torch.float32, dev)
@@ -840,13 +845,11 @@ def qk_forward(cfg: QKConfig, q, k, inv_freq=None, positions=None, *, out=None):
         raise ValueError("k is given where HK > 0, and only there")
     _qk_common(cfg, dev, inv_freq, positions)
     qo, ko = out if out is not None else (torch.empty_like(q), None if k is None else torch.empty_like(k))
-    given = [("q", s_q, _strided("q", q, s_q, io, dev)), ("q_out", s_q, _strided("out", qo, s_q, io, dev))]
-    if k is not None:
-        given += [("k", s_k, _strided("k", k, s_k, io, dev)),
-                  ("k_out", s_k, _strided("out", ko, s_k, io, dev))]
-    st = load().e2ttt_qk_forward(d, _strides_ref(QKStrides, *given), _ptr(q), _ptr(k), _ptr(inv_freq),
-                                 _ptr(positions), _ptr(qo), _ptr(ko) if k is not None else None,
-                                 _stream())
+    st = _layout(QKStrides, dev, ("q", q, s_q, io), ("q_out", qo, s_q, io),
+                 *(() if k is None else (("k", k, s_k, io), ("k_out", ko, s_k, io))))
+    st = (_lib or load()).e2ttt_qk_forward(
+        d, st, q.data_ptr(), _ptr(k), _ptr(inv_freq), _ptr(positions), qo.data_ptr(),
+        None if k is None else ko.data_ptr(), _stream())
     _check(st, "e2ttt_qk_forward")
     return qo, ko
 
@@ -863,19 +866,14 @@ def qk_backward(cfg: QKConfig, d_q_out, d_k_out, q=None, k=None, inv_freq=None, 
     _qk_common(cfg, dev, inv_freq, positions)
     dq, dk = out if out is not None else (
         torch.empty_like(d_q_out), None if d_k_out is None else torch.empty_like(d_k_out))
-    given = [("d_q_out", s_q, _strided("d_q_out", d_q_out, s_q, io, dev)),
-             ("dq", s_q, _strided("out", dq, s_q, io, dev))]
-    if need:
-        given.append(("q", s_q, _strided("q", q, s_q, io, dev)))
-    if d_k_out is not None:
-        given += [("d_k_out", s_k, _strided("d_k_out", d_k_out, s_k, io, dev)),
-                  ("dk", s_k, _strided("out", dk, s_k, io, dev))]
-        if need:
-            given.append(("k", s_k, _strided("k", k, s_k, io, dev)))
-    st = load().e2ttt_qk_backward(d, _strides_ref(QKStrides, *given), _ptr(q) if need else None,
-                                  _ptr(k) if need else None, _ptr(inv_freq), _ptr(positions),
-                                  _ptr(d_q_out), _ptr(d_k_out), _ptr(dq),
-                                  _ptr(dk) if d_k_out is not None else None, _stream())
+    st = _layout(QKStrides, dev, ("d_q_out", d_q_out, s_q, io), ("dq", dq, s_q, io),
+                 *((("q", q, s_q, io),) if need else ()),
+                 *(() if d_k_out is None else (("d_k_out", d_k_out, s_k, io), ("dk", dk, s_k, io))),
+                 *((("k", k, s_k, io),) if need and d_k_out is not None else ()))
+    st = (_lib or load()).e2ttt_qk_backward(
+        d, st, _ptr(q) if need else None, _ptr(k) if need else None, _ptr(inv_freq),
+        _ptr(positions), d_q_out.data_ptr(), _ptr(d_k_out), dq.data_ptr(),
+        None if d_k_out is None else dk.data_ptr(), _stream())
     _check(st, "e2ttt_qk_backward")
     return dq, dk
 

@@ -88,9 +88,11 @@ def test_null_alignment_and_sizes(lib):
 
 def test_workspace_without_saving_is_bounded(lib):
     short = ddesc(B=1, HK=16, H=16, T=64, dk=128, dv=128)
-    long = ddesc(B=1, HK=16, H=16, T=1 << 20, dk=128, dv=128)
-    state = 16 * 128 * 128 * 4
-    assert lib.e2ttt_delta_workspace_bytes(ctypes.byref(long), 0) <= (224 << 20) + state + 4096
+    for kw in (dict(B=1, HK=16, H=16), dict(B=1, HK=1, H=1), dict(B=16, HK=16, H=16),
+               dict(B=1, HK=1, H=2, dv=32)):
+        long = ddesc(**dict(dict(T=1 << 20, dk=128, dv=128), **kw))
+        state = long.B * long.H * long.dk * long.dv * 4
+        assert lib.e2ttt_delta_workspace_bytes(ctypes.byref(long), 0) <= (704 << 20) + state, kw
     assert lib.e2ttt_delta_workspace_bytes(ctypes.byref(short), 0) < 1 << 20
     # saving: a state and an update per chunk and unit
     assert lib.e2ttt_delta_workspace_bytes(ctypes.byref(short), 1) >= 16 * (128 * 128 + 128 * 64) * 4

@@ -291,29 +291,42 @@ def test_prefill_then_steps_equal_one_prefill():
     close("w", w, w_out.double().cpu(), "f32")
 
 
-def test_state_in_place_and_in_stretches(monkeypatch):
-    """w_out may be w_in, and a call whose fragments pass the stretch bound carries its state
-    over several launches: equal, bit for bit, to the calls of its parts."""
-    B, HK, H, dk, dv = 8, 8, 32, 16, 16
-    T = 64 * 48
-    cfg = e2ttt.DeltaConfig(B, HK, H, T, dk, dv, e2ttt.DT_BF16, 1.0)
+def test_state_in_place_and_in_stretches():
+    """w_out may be w_in, and a call of so many units that its chunks are taken in stretches
+    carries its state over several launches: equal, bit for bit, to the calls of its parts;
+    and saving for the backward in stretches gives what it gives in one."""
+    B, HK, H, dk, dv = 64, 8, 32, 16, 16
+    T = 64 * 5
+    io = e2ttt.DT_BF16
+    cfg = e2ttt.DeltaConfig(B, HK, H, T, dk, dv, io, 1.0)
     one_chunk = e2ttt.delta_workspace_bytes(e2ttt.DeltaConfig(B, HK, H, 64, dk, dv), False)
-    assert e2ttt.delta_workspace_bytes(cfg, False) < 48 * one_chunk        # several stretches
+    assert e2ttt.delta_workspace_bytes(cfg, False) < 4 * one_chunk        # several stretches
     g = torch.Generator(device="cuda").manual_seed(5)
     rn = lambda *s: torch.randn(*s, device="cuda", generator=g)
     unit = lambda x: (x / x.norm(dim=-1, keepdim=True)).bfloat16()
     q, k, v = unit(rn(B, HK, T, dk)), unit(rn(B, HK, T, dk)), rn(B, H, T, dv).bfloat16()
     eta, lg, w = torch.sigmoid(rn(B, H, T)), -torch.rand(B, H, T, device="cuda", generator=g), rn(B, H, dv, dk)
     out, w_out, _ = e2ttt.delta_forward(cfg, q, k, v, eta, lg, w)
-    half = T // 2
-    cfg2 = e2ttt.DeltaConfig(B, HK, H, half, dk, dv, e2ttt.DT_BF16, 1.0)
     w2 = w.clone()
     parts = []
-    for i in range(2):
-        sl = slice(i * half, (i + 1) * half)
+    for sl in (slice(0, 128), slice(128, T)):
+        n = sl.stop - sl.start
+        cfg2 = e2ttt.DeltaConfig(B, HK, H, n, dk, dv, io, 1.0)
         o, _, _ = e2ttt.delta_forward(cfg2, *[a[:, :, sl] for a in (q, k, v, eta, lg)], w2, w_out=w2)
         parts.append(o)
     assert torch.equal(torch.cat(parts, 2), out) and torch.equal(w2, w_out)
+    o2, w3, ws = e2ttt.delta_forward(cfg, q, k, v, eta, lg, w, save_for_backward=True)
+    assert torch.equal(o2, out) and torch.equal(w3, w_out)
+    d_out = rn(B, H, T, dv).bfloat16()
+    gr = e2ttt.delta_backward(cfg, q, k, v, eta, lg, ws, d_out)
+    # the first sequence alone (a call of few units, in segments), to fp32 and bf16 rounding
+    few = e2ttt.DeltaConfig(1, HK, H, T, dk, dv, io, 1.0)
+    one = [a[:1].contiguous() for a in (q, k, v, eta, lg)]
+    _, _, ws1 = e2ttt.delta_forward(few, *one, w[:1].contiguous(), save_for_backward=True)
+    g1 = e2ttt.delta_backward(few, *one, ws1, d_out[:1].contiguous())
+    for n, io_n in (("dq", "bf16"), ("dk", "bf16"), ("dv", "bf16"), ("d_eta", "f32"),
+                    ("d_log_gamma", "f32"), ("d_w_in", "f32")):
+        close(n, gr[n][:1], g1[n].double().cpu(), io_n)
 
 
 @pytest.mark.parametrize("io", ["bf16", "f32"])
