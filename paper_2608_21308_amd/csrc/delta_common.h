@@ -71,7 +71,7 @@ struct DeltaArgs {
                               // order (dvp x dkp); entry 0 (the last) is w_in (d_w_out)
   float* segb;                // [unit][nseg] what they make of a zero state, in lane order
   float* segf;                // [unit][nseg] their transitions F (W -> W F): rows in lane order
-                              // (dkp x dkp), then the transpose in C order
+                              // (dkp x dkp), then the transpose as row operands (operand_at)
   int nc_buf;                 // chunks per unit that the buffers hold (index r - r_base)
   int r_base;
   float scale;
@@ -248,6 +248,13 @@ __device__ __forceinline__ typename DOp<BF>::S ld_frag(const char* lds, int f, i
 // 16 tile + c, columns 32 blk + 8 g ..; a wave writes whole lines).
 __device__ __forceinline__ long lane_at(int tile, int blk, int nblk, int lane) {
   return ((long)(tile * nblk + blk) * 2 * 64 + lane) * 4;
+}
+// Element (row, column) of a matrix kept as the row operands of a product, rows
+// labelled by lab(): per row tile and 32 columns as lane_at.
+__device__ __forceinline__ int operand_at(int row, int col, int nblk) {
+  const int m = 2 * (row >> 5) + ((row >> 2) & 1), c = 4 * ((row >> 3) & 3) + (row & 3);
+  return (((m * nblk + (col >> 5)) * 2 + ((col >> 2) & 1)) * 64 + 16 * ((col >> 3) & 3) + c) * 4 +
+         (col & 3);
 }
 __device__ __forceinline__ void st_lane(float* p, f32x4 x, f32x4 y) {
   *reinterpret_cast<f32x4*>(p) = x;

@@ -236,7 +236,7 @@ delta_fwd_kernel(DeltaArgs a, int nsl) {
 #pragma unroll
       for (int m = 0; m < MT; ++m)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) f[DK * DK + (lab(m, 4 * g) + e) * DK + row] = st[m][e];
+        for (int e = 0; e < 4; ++e) f[DK * DK + operand_at(lab(m, 4 * g) + e, row, KT)] = st[m][e];
     }
     return;
   }

@@ -4,8 +4,7 @@
 //
 // One workgroup per unit and 16 rows of W (columns of W^T), a wave per 16 rows
 // of W^T, so that a step is dk / 32 products of fp32 accuracy a wave; the state
-// goes round through LDS, and the next F is on its way meanwhile.  A step takes
-// about a microsecond, a few for a call.
+// goes round through LDS, and the next two F are on their way meanwhile.
 #include "delta_common.h"
 
 namespace e2ttt {
@@ -14,59 +13,71 @@ namespace {
 template <int DK, bool BWD>
 __global__ void __launch_bounds__(4 * DK) delta_join_kernel(DeltaArgs a) {
   using O = DOp<true>;     // (fp32 products by bf16 terms, whatever the io type)
-  constexpr int KT = DK / 32, LD = DK + 4;
-  __shared__ __align__(16) float ws[2][16 * LD];
+  constexpr int KT = DK / 32, LD = DK + 8;
+  __shared__ __align__(16) __bf16 ws[2][3][16 * LD];      // the state's rows, in three terms
   const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
   const int w = wave_id();
   const int nvt = a.dvp / 16;
-  const long u = blockIdx.x / nvt;
-  const int tile = (int)(blockIdx.x % nvt);
+  // the tiles of a unit, which read the same F, go to one XCD
+  const long u = (blockIdx.x / (8 * nvt)) * 8 + blockIdx.x % 8;
+  if (u >= (long)a.B * a.H) return;
+  const int tile = (int)(blockIdx.x / 8 % nvt);
   const int row = 16 * tile + c, kc = lab(w, 4 * g);     // the lane's row of W, its columns kc ..
   const int first = BWD ? a.nseg - 1 : 0, step = BWD ? -1 : 1;
   const float* from = BWD ? a.d_w_out : a.w_in;
   f32x4 st = zero4();
   if (from && row < a.dv && kc < a.dk)
     st = *reinterpret_cast<const f32x4*>(from + (u * a.dv + row) * a.dk + kc);
-  f32x4 f[KT][2], bb;
-  auto fetch = [&](int p) {
+  f32x4 f[2][KT][2], bb[2];                              // two steps' operands under way
+  auto fetch = [&](int p, f32x4 (&f)[KT][2], f32x4& bb) {
     const float* fp = a.segf + (u * a.nseg + p) * 2 * DK * DK;
     const int r = lab(w, c);                             // row of the operand
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt) {
-      // F^T (forward): row r, columns 32 kt + 8 g ..; F (backward) in lane order
+      // row r, columns 32 kt + 8 g .. of F^T (forward), F (backward)
       const float* q = BWD ? fp + lane_at(r >> 4, kt, KT, 16 * g + (r & 15))
-                           : fp + DK * DK + r * DK + 32 * kt + 8 * g;
+                           : fp + DK * DK + lane_at(w, kt, KT, lane);
       f[kt][0] = *reinterpret_cast<const f32x4*>(q);
-      f[kt][1] = *reinterpret_cast<const f32x4*>(q + (BWD ? 256 : 4));
+      f[kt][1] = *reinterpret_cast<const f32x4*>(q + 256);
     }
     bb = *reinterpret_cast<const f32x4*>(a.segb + (u * a.nseg + p) * a.dvp * DK +
                                          lane_at(tile, w >> 1, KT, lane) + 256 * (w & 1));
   };
-  fetch(first);
-  for (int i = 0; i + 1 < a.nseg; ++i) {
+  auto one = [&](int i, f32x4 (&f)[KT][2], f32x4& bb) {
     const int p = first + step * i;
-    float* s = ws[i & 1];
-    *reinterpret_cast<f32x4*>(s + c * LD + kc) = st;
+    const O::S own = O::split<3>(st, zero4());
+#pragma unroll
+    for (int t = 0; t < 3; ++t)
+      *reinterpret_cast<bf16x4*>(&ws[i & 1][t][c * LD + kc]) =
+          __builtin_shufflevector(own.t[t], own.t[t], 0, 1, 2, 3);
     __syncthreads();                                     // (the other buffer is read until the next)
     st = bb;
     O::S fa[KT];
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt) fa[kt] = O::split<3>(f[kt][0], f[kt][1]);
-    if (i + 2 < a.nseg) fetch(p + step);
+    if (i + 3 < a.nseg) fetch(p + 2 * step, f, bb);
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt) {
-      const float* q = s + c * LD + 32 * kt + 8 * g;
-      st = O::ss<3>(st, fa[kt], O::split<3>(*reinterpret_cast<const f32x4*>(q),
-                                            *reinterpret_cast<const f32x4*>(q + 4)));
+      O::S sb;
+#pragma unroll
+      for (int t = 0; t < 3; ++t)
+        sb.t[t] = *reinterpret_cast<const bf16x8*>(&ws[i & 1][t][c * LD + 32 * kt + 8 * g]);
+      st = O::ss<3>(st, fa[kt], sb);
     }
     *reinterpret_cast<f32x4*>(a.segs + (u * a.nseg + p + step) * a.dvp * DK +
                               lane_at(tile, w >> 1, KT, lane) + 256 * (w & 1)) = st;
+  };
+  fetch(first, f[0], bb[0]);
+  if (a.nseg > 2) fetch(first + step, f[1], bb[1]);
+  for (int i = 0; i + 1 < a.nseg; i += 2) {
+    one(i, f[0], bb[0]);
+    if (i + 2 < a.nseg) one(i + 1, f[1], bb[1]);
   }
 }
 
 template <bool BWD>
 hipError_t go(const DeltaArgs& a, hipStream_t s) {
-  const dim3 grid((unsigned)((long)a.B * a.H * (a.dvp / 16)));
+  const dim3 grid((unsigned)(((long)a.B * a.H + 7) / 8 * 8 * (a.dvp / 16)));
   switch (delta_dkp(a.dk)) {
     case 32: hipLaunchKernelGGL((delta_join_kernel<32, BWD>), grid, dim3(128), 0, s, a); break;
     case 64: hipLaunchKernelGGL((delta_join_kernel<64, BWD>), grid, dim3(256), 0, s, a); break;

@@ -58,7 +58,7 @@ __device__ __forceinline__ typename DOp<BF>::X ld_row(const typename DOp<BF>::E*
 }
 
 template <bool BF, int DK>
-__global__ void __launch_bounds__(256) delta_prep_kernel(DeltaArgs a) {
+__global__ void __launch_bounds__(256, 4) delta_prep_kernel(DeltaArgs a) {
   using O = DOp<BF>;
   using E = typename O::E;
   __shared__ __align__(16) float gl[kGateFloats];

@@ -26,31 +26,44 @@ __global__ void __launch_bounds__(256) delta_step_kernel(DeltaStepArgs a, int nb
   constexpr int LPR = DK >= 64 ? 8 : 4;     // lanes of a row
   constexpr int NQ = DK / (4 * LPR);        // float4 pieces of a row in a lane
   constexpr int RW = 64 / LPR;              // rows of a set in a wave
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  typedef __attribute__((ext_vector_type(4))) E Q;
+  const int lane = threadIdx.x & 63, w = wave_id();
   const long bh = blockIdx.x / nblk;
   const int b = (int)(bh / a.H), h = (int)(bh % a.H), hk = h / (a.H / a.HK);
   const int row0 = ((int)(blockIdx.x % nblk) * 4 + w) * RW * RS + lane / LPR;
   const int l = lane % LPR;
 
+  // a token's operands, on their way one token ahead
+  Q rk[NQ], rq[NQ];
+  E rv[RS];
+  float re, rg;
+  auto load = [&](int bb, int t) {
+    const E* kp = row_of<E>(a.k, bb, hk, t);
+    const E* qp = row_of<E>(a.q, bb, hk, t);
+    const E* vp = row_of<E>(a.v, bb, h, t);
+#pragma unroll
+    for (int j = 0; j < NQ; ++j) {
+      const int col = 4 * (j * LPR + l);
+      rk[j] = rq[j] = Q{};
+      if (col < a.dk) {
+        rk[j] = *reinterpret_cast<const Q*>(kp + col);
+        rq[j] = *reinterpret_cast<const Q*>(qp + col);
+      }
+    }
+#pragma unroll
+    for (int x = 0; x < RS; ++x) rv[x] = row0 + x * RW < a.dv ? vp[row0 + x * RW] : (E)0.0f;
+    re = *row_of<float>(a.eta, bb, h, t);
+    rg = a.gam.p ? *row_of<float>(a.gam, bb, h, t) : 0.0f;
+  };
+  load(b, 0);
+
   long slot = b;
-  bool mine = true, more = false;
+  bool more = false;
   if (a.slots) {
     // requests that share a slot are taken in the order of their rows by the
     // workgroups of the first of them
     const int s = a.slots[b];
     slot = s;
-    if (s >= 0 && s < a.nslots) {
-      unsigned long before = 0, after = 0;
-      for (int x = 0; x < a.B; x += 64) {
-        const int y = x + lane;
-        const bool eq = y < a.B && a.slots[y] == s;
-        before |= __ballot(eq && y < b);
-        after |= __ballot(eq && y > b);
-      }
-      mine = before == 0;
-      more = after != 0;
-    }
-    if (!mine) return;
     if (s < 0 || s >= a.nslots) {           // no state: zero outputs
       for (int t = 0; t < a.T; ++t)
 #pragma unroll
@@ -59,6 +72,15 @@ __global__ void __launch_bounds__(256) delta_step_kernel(DeltaStepArgs a, int nb
             row_of_w<E>(a.out, b, h, t)[row0 + x * RW] = (E)0.0f;
       return;
     }
+    unsigned long before = 0, after = 0;
+    for (int x = 0; x < a.B; x += 64) {
+      const int y = x + lane;
+      const bool eq = y < a.B && a.slots[y] == s;
+      before |= __ballot(eq && y < b);
+      after |= __ballot(eq && y > b);
+    }
+    if (before) return;
+    more = after != 0;
   }
 
   float* wp = a.w + (slot * a.H + h) * (long)a.dv * a.dk;
@@ -73,38 +95,27 @@ __global__ void __launch_bounds__(256) delta_step_kernel(DeltaStepArgs a, int nb
         st[x][j] = *reinterpret_cast<const f32x4*>(wp + (long)row * a.dk + col);
     }
 
-  for (int bb = b; bb < a.B; ++bb) {
-    if (bb != b && a.slots[bb] != (int)slot) continue;
+  for (int bb = b;;) {
+    int nb = a.B;                           // the next row of the batch at this slot
+    if (more)
+      for (nb = bb + 1; nb < a.B && a.slots[nb] != (int)slot;) ++nb;
     for (int t = 0; t < a.T; ++t) {
-      const E* kp = row_of<E>(a.k, bb, hk, t);
-      const E* qp = row_of<E>(a.q, bb, hk, t);
-      const E* vp = row_of<E>(a.v, bb, h, t);
       f32x4 kv[NQ], qv[NQ];
       float vv[RS];
 #pragma unroll
-      for (int j = 0; j < NQ; ++j) {
-        const int col = 4 * (j * LPR + l);
-        kv[j] = qv[j] = zero4();
-        if (col < a.dk) {
-          if constexpr (BF) {
-            const bf16x4 x = *reinterpret_cast<const bf16x4*>(kp + col);
-            const bf16x4 y = *reinterpret_cast<const bf16x4*>(qp + col);
+      for (int j = 0; j < NQ; ++j)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              kv[j][e] = (float)x[e];
-              qv[j][e] = (float)y[e];
-            }
-          } else {
-            kv[j] = *reinterpret_cast<const f32x4*>(kp + col);
-            qv[j] = *reinterpret_cast<const f32x4*>(qp + col);
-          }
+        for (int e = 0; e < 4; ++e) {
+          kv[j][e] = (float)rk[j][e];
+          qv[j][e] = (float)rq[j][e];
         }
-      }
 #pragma unroll
-      for (int x = 0; x < RS; ++x)
-        vv[x] = row0 + x * RW < a.dv ? (float)vp[row0 + x * RW] : 0.0f;
-      const float eta = *row_of<float>(a.eta, bb, h, t);
-      const float gm = a.gam.p ? expf(*row_of<float>(a.gam, bb, h, t)) : 1.0f;
+      for (int x = 0; x < RS; ++x) vv[x] = (float)rv[x];
+      const float eta = re, gm = a.gam.p ? expf(rg) : 1.0f;
+      if (t + 1 < a.T)
+        load(bb, t + 1);
+      else if (nb < a.B)
+        load(nb, 0);
 #pragma unroll
       for (int x = 0; x < RS; ++x) {
         float d = 0.0f;
@@ -129,7 +140,8 @@ __global__ void __launch_bounds__(256) delta_step_kernel(DeltaStepArgs a, int nb
         if (l == 0 && row < a.dv) row_of_w<E>(a.out, bb, h, t)[row] = (E)(a.scale * o);
       }
     }
-    if (!more) break;
+    if (nb >= a.B) break;
+    bb = nb;
   }
 #pragma unroll
   for (int x = 0; x < RS; ++x)
@@ -137,7 +149,7 @@ __global__ void __launch_bounds__(256) delta_step_kernel(DeltaStepArgs a, int nb
     for (int j = 0; j < NQ; ++j) {
       const int row = row0 + x * RW, col = 4 * (j * LPR + l);
       if (row < a.dv && col < a.dk)
-        *reinterpret_cast<f32x4*>(wp + (long)row * a.dk + col) = st[x][j];
+        st_stream(reinterpret_cast<f32x4*>(wp + (long)row * a.dk + col), st[x][j]);
     }
 }
 
@@ -154,8 +166,8 @@ template <bool BF>
 hipError_t pick(const DeltaStepArgs& a, hipStream_t s) {
   if (a.dk <= 16) return go<BF, 16, 1>(a, s);
   if (a.dk <= 32) return go<BF, 32, 1>(a, s);
-  if (a.dk <= 64) return go<BF, 64, 2>(a, s);
-  return go<BF, 128, 2>(a, s);
+  if (a.dk <= 64) return go<BF, 64, 2>(a, s);   // (two rows of 256 bytes a lane, one of 512)
+  return go<BF, 128, 1>(a, s);
 }
 
 }  // namespace

@@ -544,8 +544,7 @@ def _strided(name, t, shape, dtype, device):
 
 def _plain(name, t, shape, dtype, device):
     """The same for a contiguous tensor (None passes)."""
-    if t is None or (type(t) in _TENSORS and t.dtype is dtype and t.shape == shape and
-                     t.is_contiguous() and t.get_device() == device):
+    if t is None or _flat(t, shape, dtype, device):
         return
     if _strided(name, t, shape, dtype, device) is not None:
         raise ValueError("%s must be contiguous" % name)
@@ -564,13 +563,18 @@ def _strides_ref(kind, given):
     return ctypes.byref(s)
 
 
+def _flat(t, shape, dtype, device):
+    """Whether t passes _strided's checks as a tensor in C order."""
+    return (type(t) in _TENSORS and t.dtype is dtype and t.get_device() == device and
+            t.shape == shape and t.is_contiguous())
+
+
 def _layout(kind, device, *given):
     """Checks (name, tensor, shape, dtype) and gives the call's strides argument
     (None: every tensor in C order, found at the price that a call of a few
     microseconds can afford)."""
     for _, t, shape, dtype in given:
-        if not (type(t) in _TENSORS and t.dtype is dtype and t.shape == shape and
-                t.is_contiguous() and t.get_device() == device):
+        if not _flat(t, shape, dtype, device):
             break
     else:
         return None
@@ -579,12 +583,16 @@ def _layout(kind, device, *given):
     return _strides_ref(kind, st) if any(x[2] is not None for x in st) else None
 
 
+def _device_of(t):
+    if not isinstance(t, torch.Tensor) or t.get_device() < 0:
+        raise ValueError("the first tensor must be a device tensor")
+    return t.get_device()
+
+
 def _on_device(f):
     """The library works on the current device: make it that of the first tensor."""
     def call(cfg, q, *args, **kw):
-        if not isinstance(q, torch.Tensor) or q.get_device() < 0:
-            raise ValueError("the first tensor must be a device tensor")
-        if q.get_device() == _current_device():
+        if _device_of(q) == _current_device():
             return f(cfg, q, *args, **kw)
         with torch.cuda.device(q.device):
             return f(cfg, q, *args, **kw)
@@ -713,29 +721,40 @@ def delta_backward(cfg: DeltaConfig, q, k, v, eta, log_gamma, workspace, d_out, 
     return grads
 
 
-@_on_device
 def delta_step(cfg: DeltaConfig, q, k, v, eta, log_gamma, w, *, slots=None, out=None):
     """Runs e2ttt_delta_step on the current stream: the cfg.T arriving tokens of
     every sequence, on states w [N, H, dv, dk] that are updated in place.
     Sequence b is at state slots[b] (int32 device tensor; None: at state b, N >=
     B); slots outside 0..N-1 are skipped (zero outputs), rows with the same slot
     are taken in order."""
+    dev = _device_of(q)
+    if dev != _current_device():
+        with torch.cuda.device(dev):
+            return delta_step(cfg, q, k, v, eta, log_gamma, w, slots=slots, out=out)
     d, io, s_k, s_v, s_g, s_w = cfg._call
-    dev, f32 = q.get_device(), torch.float32
+    f32 = torch.float32
     if not isinstance(w, torch.Tensor) or w.dim() != 4 or w.shape[0] < 1:
         raise ValueError("w must be a tensor [N, H, dv, dk] of states")
     if out is None:
         out = torch.empty_like(v)
-    st = _layout(DeltaStrides, dev, ("q", q, s_k, io), ("k", k, s_k, io), ("v", v, s_v, io),
-                 ("out", out, s_v, io), ("eta", eta, s_g, f32),
-                 *(() if log_gamma is None else (("log_gamma", log_gamma, s_g, f32),)))
     n = w.shape[0]
+    if (_flat(q, s_k, io, dev) and _flat(k, s_k, io, dev) and _flat(v, s_v, io, dev) and
+            _flat(out, s_v, io, dev) and _flat(eta, s_g, f32, dev) and
+            (log_gamma is None or _flat(log_gamma, s_g, f32, dev))):
+        st = None        # (_layout's answer, for a call of a few microseconds)
+    else:
+        st = _layout(DeltaStrides, dev, ("q", q, s_k, io), ("k", k, s_k, io), ("v", v, s_v, io),
+                     ("out", out, s_v, io), ("eta", eta, s_g, f32),
+                     *(() if log_gamma is None else (("log_gamma", log_gamma, s_g, f32),)))
     _plain("w", w, (n, *s_w[1:]), f32, dev)
-    _plain("slots", slots, s_g[:1], torch.int32, dev)
+    if slots is not None:
+        _plain("slots", slots, s_g[:1], torch.int32, dev)
     st = (_lib or load()).e2ttt_delta_step(
-        d, st, q.data_ptr(), k.data_ptr(), v.data_ptr(), eta.data_ptr(), _ptr(log_gamma),
-        w.data_ptr(), _ptr(slots), n, out.data_ptr(), _stream())
-    _check(st, "e2ttt_delta_step")
+        d, st, q.data_ptr(), k.data_ptr(), v.data_ptr(), eta.data_ptr(),
+        None if log_gamma is None else log_gamma.data_ptr(), w.data_ptr(),
+        None if slots is None else slots.data_ptr(), n, out.data_ptr(), _stream())
+    if st:
+        _check(st, "e2ttt_delta_step")
     return out
 
 
@@ -833,24 +852,36 @@ def _qk_common(cfg, dev, inv_freq, positions):
     _plain("positions", positions, s_p, torch.int64, dev)
 
 
-@_on_device
 def qk_forward(cfg: QKConfig, q, k, inv_freq=None, positions=None, *, out=None):
     """Runs e2ttt_qk_forward on the current stream: q [B, H, T, d] and k [B, HK,
     T, d] (None where HK = 0) prepared for the state rules; positions [B, T]
     int64 (None: 0 .. T - 1).  `out`: optional (q, k) tensors to write into,
     which may be the inputs.  Returns (q', k')."""
+    dev = _device_of(q)
+    if dev != _current_device():
+        with torch.cuda.device(dev):
+            return qk_forward(cfg, q, k, inv_freq, positions, out=out)
     d, io, s_q, s_k, _, _ = cfg._call
-    dev = q.get_device()
     if (k is None) != (cfg.HK == 0):
         raise ValueError("k is given where HK > 0, and only there")
     _qk_common(cfg, dev, inv_freq, positions)
-    qo, ko = out if out is not None else (torch.empty_like(q), None if k is None else torch.empty_like(k))
-    st = _layout(QKStrides, dev, ("q", q, s_q, io), ("q_out", qo, s_q, io),
-                 *(() if k is None else (("k", k, s_k, io), ("k_out", ko, s_k, io))))
+    if out is not None:
+        qo, ko = out
+    else:
+        qo, ko = torch.empty_like(q), None if k is None else torch.empty_like(k)
+    if (_flat(q, s_q, io, dev) and _flat(qo, s_q, io, dev) and
+            (k is None or (_flat(k, s_k, io, dev) and _flat(ko, s_k, io, dev)))):
+        st = None        # (_layout's answer, for a call of a few microseconds)
+    else:
+        st = _layout(QKStrides, dev, ("q", q, s_q, io), ("q_out", qo, s_q, io),
+                     *(() if k is None else (("k", k, s_k, io), ("k_out", ko, s_k, io))))
     st = (_lib or load()).e2ttt_qk_forward(
-        d, st, q.data_ptr(), _ptr(k), _ptr(inv_freq), _ptr(positions), qo.data_ptr(),
+        d, st, q.data_ptr(), None if k is None else k.data_ptr(),
+        None if inv_freq is None else inv_freq.data_ptr(),
+        None if positions is None else positions.data_ptr(), qo.data_ptr(),
         None if k is None else ko.data_ptr(), _stream())
-    _check(st, "e2ttt_qk_forward")
+    if st:
+        _check(st, "e2ttt_qk_forward")
     return qo, ko
 
 
