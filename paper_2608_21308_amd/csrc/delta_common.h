@@ -210,11 +210,17 @@ template <> struct DOp<false> {
 };
 
 // A lower triangular 64x64 matrix as the fragments of N terms, in global
-// memory and in LDS: a lane's 16 bytes of a fragment at lane * 16, the
+// memory and in LDS: 16 bytes a lane and fragment (in the order of frag_slot), the
 // fragments of a term together (f32 io: the two halves of a fragment's fp32
 // values at lane * 16 and 1024 + lane * 16).
 __host__ __device__ constexpr int tri_bytes(bool bf, int n) {
   return bf ? n * kDeltaFrags * 1024 : kDeltaFrags * 2048;
+}
+// Lane l's 16 bytes of a term lie at slot l XOR 4 x, x = 0, 3, 1, 2 for lane
+// groups 0 .. 3: the sixteen lanes of a transposing read (four rows of four lane
+// groups) and those that a 16-byte read serves together (LTile) meet all banks.
+__device__ __forceinline__ int frag_slot(int lane) {
+  return lane ^ ((lane >> 3) & 4) ^ ((lane & 16) ? 12 : 0);
 }
 // One lane's part of fragment f.
 template <bool BF, int N>
@@ -223,7 +229,7 @@ __device__ __forceinline__ void put_frag(char* p, int f, int lane, f32x4 x, f32x
     const auto s = DOp<true>::split<N>(x, y);
 #pragma unroll
     for (int i = 0; i < N; ++i)
-      *reinterpret_cast<bf16x8*>(p + ((i * kDeltaFrags + f) * 64 + lane) * 16) = s.t[i];
+      *reinterpret_cast<bf16x8*>(p + ((i * kDeltaFrags + f) * 64 + frag_slot(lane)) * 16) = s.t[i];
   } else {
     *reinterpret_cast<f32x4*>(p + f * 2048 + lane * 16) = x;
     *reinterpret_cast<f32x4*>(p + f * 2048 + 1024 + lane * 16) = y;
@@ -235,7 +241,7 @@ __device__ __forceinline__ typename DOp<BF>::S ld_frag(const char* lds, int f, i
   if constexpr (BF) {
 #pragma unroll
     for (int i = 0; i < N; ++i)
-      s.t[i] = *reinterpret_cast<const bf16x8*>(lds + ((i * kDeltaFrags + f) * 64 + lane) * 16);
+      s.t[i] = *reinterpret_cast<const bf16x8*>(lds + ((i * kDeltaFrags + f) * 64 + frag_slot(lane)) * 16);
   } else {
     s.a = *reinterpret_cast<const f32x4*>(lds + f * 2048 + lane * 16);
     s.b = *reinterpret_cast<const f32x4*>(lds + f * 2048 + 1024 + lane * 16);
@@ -289,7 +295,7 @@ __device__ __forceinline__ typename DOp<BF>::S ld_frag_t(const char* lds, int m,
 #pragma unroll
       for (int x = 0; x < 2; ++x)
         h[x] = lds_tr4(reinterpret_cast<const __bf16*>(lds) +
-                       ((i * kDeltaFrags + fidx(2 * a + x, m >> 1)) * 64 + 16 * cq + 4 * g + r) * 8 +
+                       ((i * kDeltaFrags + fidx(2 * a + x, m >> 1)) * 64 + frag_slot(16 * cq + 4 * g + r)) * 8 +
                        4 * (m & 1));
       s.t[i] = cat8(h[0], h[1]);
     }
@@ -305,16 +311,25 @@ __device__ __forceinline__ typename DOp<BF>::S ld_frag_t(const char* lds, int m,
   return s;
 }
 
-// A tile of rows of D elements of the io type in LDS, in 16-byte pieces;
-// piece p of a row lies at p XOR a function of the row, so that the 16 rows of
-// a fragment read (which differ in row bits 0, 1, 3, 4) touch different banks.
+// A tile of rows of D elements of the io type in LDS, in 16-byte pieces; piece
+// p of a row lies at p XOR a function of the row's low bits b0 .. b4.  A 16-byte
+// read serves lanes 0-3, 12-15, 20-27 together, then 4-11, 16-19, 28-31, and so
+// on; an 8-byte transposing read a group of 16.  With bf16 the function spreads
+// over the 256 bytes of the banks the rows of a fragment read (b0, b1, b3, b4
+// differ; the lane groups 0 and 1, 2 and 3 ask for neighbouring pieces), the four
+// rows (b0, b1) of a transposing read.  (b2 stays out: the rows 4 on that such a
+// read goes on to are then a constant away.)  fp32 fragments are two pieces,
+// which takes another one.
 template <bool BF, int D>
 struct LTile {
   using E = typename DOp<BF>::E;
   static constexpr int PE = 16 / (int)sizeof(E);     // elements of a piece
   static constexpr int NP = D / PE;                  // pieces of a row
   static __device__ __forceinline__ int at(int row, int p) {   // element index of a piece
-    const int f = ((row & 3) | ((row >> 1) & 12)) & (NP - 1);
+    if constexpr (!BF) return (row * NP + (p ^ (((row & 3) | ((row >> 1) & 12)) & (NP - 1)))) * PE;
+    // (rows of 64 and 128 bytes: b0 and b1, b0 move the bank by themselves)
+    const int up = NP >= 16 ? (row & 3) << 2 : NP == 8 ? (row & 2) << 1 : 0;
+    const int b4 = (row >> 4) & 1, f = up | (((row >> 2) & 2) ^ (3 * b4));
     return (row * NP + (p ^ f)) * PE;
   }
   // row `row`, columns 32 kt + 8 g .. + 7
