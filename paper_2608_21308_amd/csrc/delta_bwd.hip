@@ -132,12 +132,14 @@ delta_bwd_kernel(DeltaArgs a, int nsl) {
     }
     f32x4 xa[4];
 #pragma unroll
-    for (int m = 0; m < 4; ++m) {
-      xa[m] = zero4();
+    for (int m = 0; m < 4; m += 2) {
+      xa[m] = xa[m + 1] = zero4();
 #pragma unroll
       for (int kt = 0; kt < KT; ++kt)
-        xa[m] = O::template xs<3>(xa[m], L::frag(ks, lab(m, c), kt, g), sb[kt]);
+        O::template xs2<3>(xa[m], L::frag(ks, lab(m, c), kt, g), sb[kt], xa[m + 1],
+                           L::frag(ks, lab(m + 1, c), kt, g), sb[kt]);
       xa[m] = xa[m] * *reinterpret_cast<const f32x4*>(gl + kGEnd + lab(m, 4 * g));
+      xa[m + 1] = xa[m + 1] * *reinterpret_cast<const f32x4*>(gl + kGEnd + lab(m + 1, 4 * g));
     }
     typename O::X dob[2];           // dO as an operand
     typename O::S gb[2];            // s G dO
@@ -151,27 +153,31 @@ delta_bwd_kernel(DeltaArgs a, int nsl) {
           d1 * *reinterpret_cast<const f32x4*>(gl + kGsG + 32 * x + 8 * g + 4));
     }
 #pragma unroll
-    for (int m = 0; m < 4; ++m)
+    for (int m = 0; m < 4; m += 2)
 #pragma unroll
       for (int x = m / 2; x < 2; ++x)
-        xa[m] = O::template sx<3>(xa[m], ld_frag_t<BF, 3>(ps, m, x, g, c), dob[x]);
+        O::template sx2<3>(xa[m], ld_frag_t<BF, 3>(ps, m, x, g, c), dob[x], xa[m + 1],
+                           ld_frag_t<BF, 3>(ps, m + 1, x, g, c), dob[x]);
     typename O::S rb[2];
 #pragma unroll
     for (int x = 0; x < 2; ++x) rb[x] = O::template split<3>(xa[2 * x], xa[2 * x + 1]);
     const float gC = gl[kGC];
 #pragma unroll
-    for (int m = 0; m < MT; ++m) {  // (needs nothing of Y: fills the waits of its products)
+    for (int m = 0; m < MT; m += 2) {  // (needs nothing of Y: fills the waits of its products)
       st[m] = st[m] * gC;
+      st[m + 1] = st[m + 1] * gC;
 #pragma unroll
       for (int x = 0; x < 2; ++x)
-        st[m] = O::template xs<3>(st[m], L::template frag_t<false>(qs, m, x, g, c), gb[x]);
+        O::template xs2<3>(st[m], L::template frag_t<false>(qs, m, x, g, c), gb[x], st[m + 1],
+                           L::template frag_t<false>(qs, m + 1, x, g, c), gb[x]);
     }
 #pragma unroll
-    for (int m = 0; m < 4; ++m) {
-      xa[m] = zero4();
+    for (int m = 0; m < 4; m += 2) {
+      xa[m] = xa[m + 1] = zero4();
 #pragma unroll
       for (int x = m / 2; x < 2; ++x)
-        xa[m] = O::template ss<3>(xa[m], ld_frag_t<BF, 3>(ts, m, x, g, c), rb[x]);
+        O::template ss2<3>(xa[m], ld_frag_t<BF, 3>(ts, m, x, g, c), rb[x], xa[m + 1],
+                           ld_frag_t<BF, 3>(ts, m + 1, x, g, c), rb[x]);
     }
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
@@ -183,10 +189,11 @@ delta_bwd_kernel(DeltaArgs a, int nsl) {
                                    xa[2 * x + 1] * -*reinterpret_cast<const f32x4*>(gp + 4));
     }
 #pragma unroll
-    for (int m = 0; m < MT; ++m)
+    for (int m = 0; m < MT; m += 2)
 #pragma unroll
       for (int x = 0; x < 2; ++x)
-        st[m] = O::template xs<3>(st[m], L::template frag_t<false>(ks, m, x, g, c), rb[x]);
+        O::template xs2<3>(st[m], L::template frag_t<false>(ks, m, x, g, c), rb[x], st[m + 1],
+                           L::template frag_t<false>(ks, m + 1, x, g, c), rb[x]);
   }
 
   if constexpr (STATE) {

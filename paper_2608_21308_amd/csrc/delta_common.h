@@ -137,6 +137,37 @@ template <> struct DOp<true> {
       for (int i = 0; i <= n; ++i) acc = m1(acc, a.t[i], b.t[n - i]);
     return acc;
   }
+  // Two products at once, issued in turn: an MFMA waits for the one before it
+  // on the same accumulator twice as long as for the matrix unit.
+  template <int N>
+  static __device__ __forceinline__ void xs2(f32x4& c0, const X& a0, const S& b0, f32x4& c1,
+                                             const X& a1, const S& b1) {
+#pragma unroll
+    for (int i = N - 1; i >= 0; --i) {
+      c0 = m1(c0, a0.v, b0.t[i]);
+      c1 = m1(c1, a1.v, b1.t[i]);
+    }
+  }
+  template <int N>
+  static __device__ __forceinline__ void sx2(f32x4& c0, const S& a0, const X& b0, f32x4& c1,
+                                             const S& a1, const X& b1) {
+#pragma unroll
+    for (int i = N - 1; i >= 0; --i) {
+      c0 = m1(c0, a0.t[i], b0.v);
+      c1 = m1(c1, a1.t[i], b1.v);
+    }
+  }
+  template <int N>
+  static __device__ __forceinline__ void ss2(f32x4& c0, const S& a0, const S& b0, f32x4& c1,
+                                             const S& a1, const S& b1) {
+#pragma unroll
+    for (int n = N - 1; n >= 0; --n)
+#pragma unroll
+      for (int i = 0; i <= n; ++i) {
+        c0 = m1(c0, a0.t[i], b0.t[n - i]);
+        c1 = m1(c1, a1.t[i], b1.t[n - i]);
+      }
+  }
   template <int N>
   static __device__ __forceinline__ S split(f32x4 x, f32x4 y) {
     typedef __attribute__((ext_vector_type(4))) unsigned u4;
@@ -201,6 +232,30 @@ template <> struct DOp<false> {
   static __device__ __forceinline__ f32x4 sx(f32x4 acc, const X& p, const X& q) { return xx(acc, p, q); }
   template <int N>
   static __device__ __forceinline__ f32x4 ss(f32x4 acc, const X& p, const X& q) { return xx(acc, p, q); }
+  template <int N>
+  static __device__ __forceinline__ void ss2(f32x4& c0, const X& a0, const X& b0, f32x4& c1,
+                                             const X& a1, const X& b1) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      c0 = __builtin_amdgcn_mfma_f32_16x16x4f32(a0.a[e], b0.a[e], c0, 0, 0, 0);
+      c1 = __builtin_amdgcn_mfma_f32_16x16x4f32(a1.a[e], b1.a[e], c1, 0, 0, 0);
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      c0 = __builtin_amdgcn_mfma_f32_16x16x4f32(a0.b[e], b0.b[e], c0, 0, 0, 0);
+      c1 = __builtin_amdgcn_mfma_f32_16x16x4f32(a1.b[e], b1.b[e], c1, 0, 0, 0);
+    }
+  }
+  template <int N>
+  static __device__ __forceinline__ void xs2(f32x4& c0, const X& a0, const X& b0, f32x4& c1,
+                                             const X& a1, const X& b1) {
+    ss2<N>(c0, a0, b0, c1, a1, b1);
+  }
+  template <int N>
+  static __device__ __forceinline__ void sx2(f32x4& c0, const X& a0, const X& b0, f32x4& c1,
+                                             const X& a1, const X& b1) {
+    ss2<N>(c0, a0, b0, c1, a1, b1);
+  }
   template <int N>
   static __device__ __forceinline__ S split(f32x4 x, f32x4 y) { return S{x, y}; }
   static __device__ __forceinline__ void values(const X& p, f32x4& x, f32x4& y) {

@@ -156,8 +156,9 @@ delta_fwd_kernel(DeltaArgs a, int nsl) {
           st_lane(a.wst + cu * a.dvp * DK + lane_at(tile, kt, KT, lane), st[2 * kt], st[2 * kt + 1]);
       }
 #pragma unroll
-      for (int m = 0; m < 4; ++m)
-        xa[m] = O::template xs<3>(xa[m], L::frag(ks, lab(m, c), kt, g), sb[kt]);
+      for (int m = 0; m < 4; m += 2)
+        O::template xs2<3>(xa[m], L::frag(ks, lab(m, c), kt, g), sb[kt], xa[m + 1],
+                           L::frag(ks, lab(m + 1, c), kt, g), sb[kt]);
     }
     // R, and while it is formed the state's part of O
     typename O::S rb[2], ub[2], ue[2];
@@ -178,12 +179,11 @@ delta_fwd_kernel(DeltaArgs a, int nsl) {
       rb[x] = O::template split<3>(xa[2 * x], xa[2 * x + 1]);
       if constexpr (OUT) {
 #pragma unroll
-        for (int m = 2 * x; m < 2 * x + 2; ++m) {
-#pragma unroll
-          for (int kt = 0; kt < KT; ++kt)
-            oa[m] = O::template sx<2>(oa[m], sb[kt], L::frag(qs, lab(m, c), kt, g));
-          oa[m] = oa[m] * gl[kGsG + lab(m, c)];
-        }
+        for (int kt = 0; kt < KT; ++kt)
+          O::template sx2<2>(oa[2 * x], sb[kt], L::frag(qs, lab(2 * x, c), kt, g), oa[2 * x + 1],
+                             sb[kt], L::frag(qs, lab(2 * x + 1, c), kt, g));
+        oa[2 * x] = oa[2 * x] * gl[kGsG + lab(2 * x, c)];
+        oa[2 * x + 1] = oa[2 * x + 1] * gl[kGsG + lab(2 * x + 1, c)];
       }
     }
     // U, half by half; the first half's use overlaps the second's products
@@ -193,10 +193,9 @@ delta_fwd_kernel(DeltaArgs a, int nsl) {
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
 #pragma unroll
-      for (int m = 2 * x; m < 2 * x + 2; ++m)
-#pragma unroll
-        for (int y = 0; y <= x; ++y)
-          ua[m] = O::template ss<3>(ua[m], ld_frag<BF, 3>(ts, fidx(m, y), lane), rb[y]);
+      for (int y = 0; y <= x; ++y)
+        O::template ss2<3>(ua[2 * x], ld_frag<BF, 3>(ts, fidx(2 * x, y), lane), rb[y], ua[2 * x + 1],
+                           ld_frag<BF, 3>(ts, fidx(2 * x + 1, y), lane), rb[y]);
       if constexpr (SAVE) {
         if (col < a.dvp)
           st_lane(a.ust + cu * a.dvp * kDC + lane_at(tile, x, 2, lane), ua[2 * x], ua[2 * x + 1]);
@@ -206,16 +205,20 @@ delta_fwd_kernel(DeltaArgs a, int nsl) {
       ue[x] = O::template split<3>(ua[2 * x] * n0, ua[2 * x + 1] * n1);
       if constexpr (OUT) ub[x] = O::template split<2>(ua[2 * x], ua[2 * x + 1]);
 #pragma unroll
-      for (int m = 0; m < MT; ++m)
-        st[m] = O::template xs<3>(st[m], L::template frag_t<false>(ks, m, x, g, c), ue[x]);
+      for (int m = 0; m < MT; m += 2)
+        O::template xs2<3>(st[m], L::template frag_t<false>(ks, m, x, g, c), ue[x], st[m + 1],
+                           L::template frag_t<false>(ks, m + 1, x, g, c), ue[x]);
     }
     if constexpr (OUT) {
     E* op = row_of_w<E>(a.out, b, h, t0) + sc0 + 16 * w + 4 * g;
 #pragma unroll
     for (int m = 0; m < 4; ++m) {
+      if (m % 2 == 0) {
 #pragma unroll
-      for (int x = 0; x <= m / 2; ++x)
-        oa[m] = O::template ss<2>(oa[m], ub[x], ld_frag<BF, 2>(ps, fidx(m, x), lane));
+        for (int x = 0; x <= m / 2; ++x)
+          O::template ss2<2>(oa[m], ub[x], ld_frag<BF, 2>(ps, fidx(m, x), lane), oa[m + 1], ub[x],
+                             ld_frag<BF, 2>(ps, fidx(m + 1, x), lane));
+      }
       if (sc0 + 16 * w + 4 * g < a.dv && t0 + lab(m, c) < a.T)
         IoT<BF>::st4(op + lab(m, c) * ost, oa[m]);
     }

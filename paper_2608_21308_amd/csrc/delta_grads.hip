@@ -40,7 +40,8 @@ __device__ __forceinline__ float sum16x8(f32x4 x, f32x4 y, int c) {
   return row16_reduce_scatter8(v, c);
 }
 
-template <bool BF, int DK, int NWV>
+// ONE: a value head to a key head, whose sums then need no registers ahead.
+template <bool BF, int DK, int NWV, bool ONE>
 __global__ void __launch_bounds__(64 * NWV, 2) delta_grads_kernel(DeltaArgs a) {
   using O = DOp<BF>;
   using E = typename O::E;
@@ -80,7 +81,7 @@ __global__ void __launch_bounds__(64 * NWV, 2) delta_grads_kernel(DeltaArgs a) {
 
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, c = lane & 15;
   const int w = wave_id();
-  const int nr = a.r1 - a.r0, rep = a.H / a.HK;
+  const int nr = a.r1 - a.r0, rep = ONE ? 1 : a.H / a.HK;
   const long bh = blockIdx.x / nr;
   const int r = a.r0 + (int)(blockIdx.x % nr);
   const int b = (int)(bh / a.HK), hk = (int)(bh % a.HK);
@@ -194,7 +195,7 @@ __global__ void __launch_bounds__(64 * NWV, 2) delta_grads_kernel(DeltaArgs a) {
       __syncthreads();
       if (v0 + 32 < a.dvp)
         fetch(h, cu, v0 + 32);
-      else if (hv + 1 < rep)
+      else if (!ONE && hv + 1 < rep)
         fetch(h + 1, cu + a.nc_buf, 0);
       {
         const auto wf = terms_t<BF, DK, true>(w0s, WP, ct, g, c);
@@ -229,6 +230,10 @@ __global__ void __launch_bounds__(64 * NWV, 2) delta_grads_kernel(DeltaArgs a) {
       }
     }
     __syncthreads();                         // the value blocks are done: buf holds A and N
+    if (ONE) {
+#pragma unroll
+      for (int m = 0; m < MR; ++m) dq[m] = dk[m] = zero4();
+    }
 
     // 64x64 terms of row i, columns j = 32 xb + 8 g + 4 y + e
     {
@@ -400,8 +405,11 @@ __global__ void __launch_bounds__(64 * NWV, 2) delta_grads_kernel(DeltaArgs a) {
 
 template <bool BF, int DK, int NWV>
 hipError_t go(const DeltaArgs& a, hipStream_t s) {
-  hipLaunchKernelGGL((delta_grads_kernel<BF, DK, NWV>),
-                     dim3((unsigned)((long)a.B * a.HK * (a.r1 - a.r0))), dim3(64 * NWV), 0, s, a);
+  const dim3 grid((unsigned)((long)a.B * a.HK * (a.r1 - a.r0))), blk(64 * NWV);
+  if (a.H == a.HK)
+    hipLaunchKernelGGL((delta_grads_kernel<BF, DK, NWV, true>), grid, blk, 0, s, a);
+  else
+    hipLaunchKernelGGL((delta_grads_kernel<BF, DK, NWV, false>), grid, blk, 0, s, a);
   return hipGetLastError();
 }
 
