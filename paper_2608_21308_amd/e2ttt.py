@@ -602,6 +602,8 @@ def _on_device(f):
 
 def _as_rows(g):
     """A gradient as the library takes it: rows contiguous and on 16 bytes."""
+    if g.is_contiguous() and g.data_ptr() % 16 == 0:
+        return g
     if g.stride(-1) != 1 or g.data_ptr() % 16 or any(
             s * g.element_size() % 16 for s, n in zip(g.stride()[:3], g.shape) if n > 1):
         return g.contiguous()
@@ -636,11 +638,11 @@ class DeltaConfig:
 
 
 def delta_workspace_bytes(cfg: DeltaConfig, save_for_backward: bool) -> int:
-    return int(load().e2ttt_delta_workspace_bytes(cfg._call[0], int(bool(save_for_backward))))
+    return int((_lib or load()).e2ttt_delta_workspace_bytes(cfg._call[0], int(bool(save_for_backward))))
 
 
 def delta_scratch_bytes(cfg: DeltaConfig) -> int:
-    return int(load().e2ttt_delta_scratch_bytes(cfg._call[0]))
+    return int((_lib or load()).e2ttt_delta_scratch_bytes(cfg._call[0]))
 
 
 def alloc_delta_workspace(cfg: DeltaConfig, save_for_backward: bool, device="cuda"):
@@ -687,19 +689,36 @@ def delta_forward(cfg: DeltaConfig, q, k, v, eta, log_gamma=None, w_in=None, *, 
     return out, w_out, workspace
 
 
+def _new_grads(cfg, q, k, v, eta, log_gamma):
+    return dict(dq=torch.empty_like(q), dk=torch.empty_like(k), dv=torch.empty_like(v),
+                d_eta=torch.empty_like(eta),
+                d_log_gamma=None if log_gamma is None else torch.empty_like(log_gamma),
+                d_w_in=torch.empty(cfg._call[5], dtype=torch.float32, device=q.device))
+
+
+def _run_delta_backward(cfg, st, q, k, v, eta, log_gamma, workspace, d_out, d_w_out, lengths, g,
+                        scratch):
+    """The library's call on checked tensors (st: their strides argument)."""
+    if scratch is None:
+        scratch = torch.empty(delta_scratch_bytes(cfg), dtype=torch.uint8, device=q.device)
+    st = (_lib or load()).e2ttt_delta_backward(
+        cfg._call[0], st, q.data_ptr(), k.data_ptr(), v.data_ptr(), eta.data_ptr(), _ptr(log_gamma),
+        _ptr(lengths), workspace.data_ptr(), workspace.numel(), d_out.data_ptr(), _ptr(d_w_out),
+        g["dq"].data_ptr(), g["dk"].data_ptr(), g["dv"].data_ptr(), g["d_eta"].data_ptr(),
+        _ptr(g.get("d_log_gamma")), _ptr(g.get("d_w_in")), scratch.data_ptr(), scratch.numel(),
+        _stream())
+    _check(st, "e2ttt_delta_backward")
+    return g
+
+
 @_on_device
 def delta_backward(cfg: DeltaConfig, q, k, v, eta, log_gamma, workspace, d_out, d_w_out=None, *,
                    lengths=None, grads=None, scratch=None):
     """Runs e2ttt_delta_backward with the workspace of a saving delta_forward;
     returns a dict of gradients (dq, dk, dv, d_eta, d_log_gamma, d_w_in)."""
-    d, io, s_k, s_v, s_g, s_w = cfg._call
+    _, io, s_k, s_v, s_g, s_w = cfg._call
     dev, f32 = q.get_device(), torch.float32
-    if grads is None:
-        grads = dict(dq=torch.empty_like(q), dk=torch.empty_like(k), dv=torch.empty_like(v),
-                     d_eta=torch.empty_like(eta),
-                     d_log_gamma=None if log_gamma is None else torch.empty_like(log_gamma),
-                     d_w_in=torch.empty(s_w, dtype=f32, device=q.device))
-    g = grads
+    g = grads = _new_grads(cfg, q, k, v, eta, log_gamma) if grads is None else grads
     st = _layout(DeltaStrides, dev, ("q", q, s_k, io), ("k", k, s_k, io), ("v", v, s_v, io),
                  ("d_out", d_out, s_v, io), ("dq", g["dq"], s_k, io), ("dk", g["dk"], s_k, io),
                  ("dv", g["dv"], s_v, io), ("eta", eta, s_g, f32), ("d_eta", g["d_eta"], s_g, f32),
@@ -710,15 +729,8 @@ def delta_backward(cfg: DeltaConfig, q, k, v, eta, log_gamma, workspace, d_out, 
     _plain("lengths", lengths, s_g[:1], torch.int32, dev)
     _buffer("workspace", workspace, dev)
     _buffer("scratch", scratch, dev)
-    if scratch is None:
-        scratch = torch.empty(delta_scratch_bytes(cfg), dtype=torch.uint8, device=q.device)
-    st = (_lib or load()).e2ttt_delta_backward(
-        d, st, _ptr(q), _ptr(k), _ptr(v), _ptr(eta), _ptr(log_gamma),
-        _ptr(lengths), _ptr(workspace), workspace.numel(), _ptr(d_out), _ptr(d_w_out), _ptr(g["dq"]),
-        _ptr(g["dk"]), _ptr(g["dv"]), _ptr(g["d_eta"]), _ptr(g.get("d_log_gamma")),
-        _ptr(g.get("d_w_in")), _ptr(scratch), scratch.numel(), _stream())
-    _check(st, "e2ttt_delta_backward")
-    return grads
+    return _run_delta_backward(cfg, st, q, k, v, eta, log_gamma, workspace, d_out, d_w_out, lengths,
+                               grads, scratch)
 
 
 def delta_step(cfg: DeltaConfig, q, k, v, eta, log_gamma, w, *, slots=None, out=None):
@@ -767,20 +779,41 @@ class DeltaFunction(torch.autograd.Function):
         out, w_out, ws = delta_forward(cfg, q, k, v, eta, log_gamma, w_in, lengths=lengths,
                                        save_for_backward=True)
         ctx.cfg, ctx.has_w = cfg, w_in is not None
+        ctx.flat = (q.is_contiguous() and k.is_contiguous() and v.is_contiguous() and
+                    eta.is_contiguous() and (log_gamma is None or log_gamma.is_contiguous()))
         ctx.save_for_backward(q, k, v, eta, log_gamma, lengths, ws)
         ctx.set_materialize_grads(False)
         return out, w_out
 
     @staticmethod
-    @torch.autograd.function.once_differentiable
     def backward(ctx, d_out, d_w_out):
-        q, k, v, eta, log_gamma, lengths, ws = ctx.saved_tensors
-        if d_out is None:
-            d_out = torch.zeros_like(v)
-        g = delta_backward(ctx.cfg, q, k, v, eta, log_gamma, ws, _as_rows(d_out),
-                           None if d_w_out is None else d_w_out.contiguous(), lengths=lengths)
-        return (None, g["dq"], g["dk"], g["dv"], g["d_eta"], g["d_log_gamma"],
-                g["d_w_in"] if ctx.has_w else None, None)
+        return _once(_delta_grads, ctx, d_out, d_w_out)
+
+
+def _once(f, ctx, *grads):
+    """f's gradients, which do not have gradients themselves."""
+    if torch.is_grad_enabled():      # a graph of the backward is asked for
+        f = torch.autograd.function.once_differentiable(f)
+    return f(ctx, *grads)
+
+
+def _delta_grads(ctx, d_out, d_w_out):
+    cfg = ctx.cfg
+    q, k, v, eta, log_gamma, lengths, ws = ctx.saved_tensors
+    d_out = torch.zeros_like(v) if d_out is None else _as_rows(d_out)
+    if d_w_out is not None:
+        d_w_out = d_w_out.contiguous()
+    _, io, _, s_v, _, s_w = cfg._call
+    dev = q.get_device()
+    if (ctx.flat and dev == _current_device() and _flat(d_out, s_v, io, dev) and
+            (d_w_out is None or _flat(d_w_out, s_w, torch.float32, dev))):
+        # (the rest was checked by the forward, and new gradients lie as their tensors do)
+        g = _run_delta_backward(cfg, None, q, k, v, eta, log_gamma, ws, d_out, d_w_out, lengths,
+                                _new_grads(cfg, q, k, v, eta, log_gamma), None)
+    else:
+        g = delta_backward(cfg, q, k, v, eta, log_gamma, ws, d_out, d_w_out, lengths=lengths)
+    return (None, g["dq"], g["dk"], g["dv"], g["d_eta"], g["d_log_gamma"],
+            g["d_w_in"] if ctx.has_w else None, None)
 
 
 @dataclass(frozen=True)
@@ -885,12 +918,20 @@ def qk_forward(cfg: QKConfig, q, k, inv_freq=None, positions=None, *, out=None):
     return qo, ko
 
 
+def _run_qk_backward(cfg, st, d_q_out, d_k_out, q, k, inv_freq, positions, dq, dk):
+    st = (_lib or load()).e2ttt_qk_backward(
+        cfg._call[0], st, _ptr(q), _ptr(k), _ptr(inv_freq), _ptr(positions), d_q_out.data_ptr(),
+        _ptr(d_k_out), dq.data_ptr(), None if d_k_out is None else dk.data_ptr(), _stream())
+    _check(st, "e2ttt_qk_backward")
+    return dq, dk
+
+
 @_on_device
 def qk_backward(cfg: QKConfig, d_q_out, d_k_out, q=None, k=None, inv_freq=None, positions=None, *,
                 out=None):
     """Gradients (dq, dk) of qk_forward's inputs q, k from those of its outputs
     (q and k are not needed without QK_SILU and QK_UNIT)."""
-    d, io, s_q, s_k, _, _ = cfg._call
+    _, io, s_q, s_k, _, _ = cfg._call
     dev, need = d_q_out.get_device(), bool(cfg.flags & (QK_SILU | QK_UNIT))
     if (d_k_out is None) != (cfg.HK == 0):
         raise ValueError("d_k_out is given where HK > 0, and only there")
@@ -901,12 +942,8 @@ def qk_backward(cfg: QKConfig, d_q_out, d_k_out, q=None, k=None, inv_freq=None, 
                  *((("q", q, s_q, io),) if need else ()),
                  *(() if d_k_out is None else (("d_k_out", d_k_out, s_k, io), ("dk", dk, s_k, io))),
                  *((("k", k, s_k, io),) if need and d_k_out is not None else ()))
-    st = (_lib or load()).e2ttt_qk_backward(
-        d, st, _ptr(q) if need else None, _ptr(k) if need else None, _ptr(inv_freq),
-        _ptr(positions), d_q_out.data_ptr(), _ptr(d_k_out), dq.data_ptr(),
-        None if d_k_out is None else dk.data_ptr(), _stream())
-    _check(st, "e2ttt_qk_backward")
-    return dq, dk
+    return _run_qk_backward(cfg, st, d_q_out, d_k_out, q if need else None, k if need else None,
+                            inv_freq, positions, dq, dk)
 
 
 class QKFunction(torch.autograd.Function):
@@ -922,9 +959,22 @@ class QKFunction(torch.autograd.Function):
         return qo, ko
 
     @staticmethod
-    @torch.autograd.function.once_differentiable
     def backward(ctx, d_q, d_k):
-        q, k, inv_freq, positions = ctx.saved_tensors
-        dq, dk = qk_backward(ctx.cfg, _as_rows(d_q), None if d_k is None else _as_rows(d_k), q, k,
-                             inv_freq, positions)
-        return None, dq, dk, None, None
+        return _once(_qk_grads, ctx, d_q, d_k)
+
+
+def _qk_grads(ctx, d_q, d_k):
+    cfg = ctx.cfg
+    q, k, inv_freq, positions = ctx.saved_tensors
+    d_q, d_k = _as_rows(d_q), None if d_k is None else _as_rows(d_k)
+    _, io, s_q, s_k, _, _ = cfg._call
+    dev = d_q.get_device()
+    if (dev == _current_device() and _flat(d_q, s_q, io, dev) and
+            (d_k is None or _flat(d_k, s_k, io, dev)) and (q is None or q.is_contiguous()) and
+            (k is None or k.is_contiguous())):
+        # (the rest was checked by the forward)
+        dq, dk = _run_qk_backward(cfg, None, d_q, d_k, q, k, inv_freq, positions,
+                                  torch.empty_like(d_q), None if d_k is None else torch.empty_like(d_k))
+    else:
+        dq, dk = qk_backward(cfg, d_q, d_k, q, k, inv_freq, positions)
+    return None, dq, dk, None, None
