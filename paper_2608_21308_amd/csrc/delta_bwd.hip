@@ -60,7 +60,7 @@ delta_bwd_kernel(DeltaArgs a, int nsl) {
     const int kc = lab(m, 4 * g);
     st[m] = zero4();
     if constexpr (STATE) continue;
-    if (seg < a.nseg - 1) {
+    if (a.nseg > 1) {
       if (col < a.dvp)
         st[m] = *reinterpret_cast<const f32x4*>(a.segs + us * a.dvp * DK +
                                                 lane_at(tile, m / 2, KT, lane) + 256 * (m & 1));

@@ -68,7 +68,7 @@ struct DeltaArgs {
   // The launch's chunks in nseg segments of seglen (the last may be shorter):
   int nseg, seglen;
   float* segs;                // [unit][nseg] what the segments start (backward: end) from, in lane
-                              // order (dvp x dkp); entry 0 (the last) is w_in (d_w_out)
+                              // order (dvp x dkp)
   float* segb;                // [unit][nseg] what they make of a zero state, in lane order
   float* segf;                // [unit][nseg] their transitions F (W -> W F): rows in lane order
                               // (dkp x dkp), then the transpose as row operands (operand_at)

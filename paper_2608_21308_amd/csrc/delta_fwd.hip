@@ -80,7 +80,7 @@ delta_fwd_kernel(DeltaArgs a, int nsl) {
     if constexpr (MODE == kState) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) st[m][e] = 16 * (tile - nvt) + c == kc + e ? 1.0f : 0.0f;
-    } else if (seg > 0) {
+    } else if (a.nseg > 1) {
       if (col < a.dvp)
         st[m] = *reinterpret_cast<const f32x4*>(a.segs + us * a.dvp * DK +
                                                 lane_at(tile, m / 2, KT, lane) + 256 * (m & 1));

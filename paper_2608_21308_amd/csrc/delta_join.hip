@@ -67,6 +67,10 @@ __global__ void __launch_bounds__(4 * DK) delta_join_kernel(DeltaArgs a) {
     *reinterpret_cast<f32x4*>(a.segs + (u * a.nseg + p + step) * a.dvp * DK +
                               lane_at(tile, w >> 1, KT, lane) + 256 * (w & 1)) = st;
   };
+  // (the first state too, from where every segment then reads: the launch that
+  // reads them writes the last one's result, which may lie where `from` does)
+  *reinterpret_cast<f32x4*>(a.segs + (u * a.nseg + first) * a.dvp * DK +
+                            lane_at(tile, w >> 1, KT, lane) + 256 * (w & 1)) = st;
   fetch(first, f[0], bb[0]);
   if (a.nseg > 2) fetch(first + step, f[1], bb[1]);
   for (int i = 0; i + 1 < a.nseg; i += 2) {

@@ -340,6 +340,48 @@ def test_segments(c, lengths, io):
           lengths=None if lengths is None else torch.tensor(lengths))
 
 
+def test_segments_in_place_and_in_stretches():
+    """w_out = w_in where the call runs in segments, and a sequence of several stretches, each
+    in segments, that carries its state from one to the next: bit for bit the separate calls."""
+    c = (1, 1, 2, 2000, 64, 64)
+    x, _ = make(*c, "bf16", seed=37, rate=0.01)
+    t = to_dev(x, "bf16")
+    cfg = e2ttt.DeltaConfig(*c, e2ttt.DT_BF16, 1.0)
+    names = ("q", "k", "v", "eta", "log_gamma")
+    out, w_out, _ = e2ttt.delta_forward(cfg, *[t[n] for n in names], t["w_in"])
+    for _ in range(8):
+        w = t["w_in"].clone()
+        o, _, _ = e2ttt.delta_forward(cfg, *[t[n] for n in names], w, w_out=w)
+        assert torch.equal(o, out) and torch.equal(w, w_out)
+    B, H, T, d = 1, 16, 64 * 1100, 64         # more fragments than a stretch holds
+    cfg = e2ttt.DeltaConfig(B, H, H, T, d, d, e2ttt.DT_BF16, 1.0)
+    each = e2ttt.delta_workspace_bytes(e2ttt.DeltaConfig(B, H, H, 64, d, d), False)
+    assert e2ttt.delta_workspace_bytes(cfg, False) < 900 * each
+    g = torch.Generator(device="cuda").manual_seed(3)
+    rn = lambda *s: torch.randn(*s, device="cuda", generator=g)
+    unit = lambda x: (x / x.norm(dim=-1, keepdim=True)).bfloat16()
+    a = [unit(rn(B, H, T, d)), unit(rn(B, H, T, d)), rn(B, H, T, d).bfloat16(),
+         torch.sigmoid(rn(B, H, T)), -0.001 * torch.rand(B, H, T, device="cuda", generator=g)]
+    w = rn(B, H, d, d)
+    out, w_out, _ = e2ttt.delta_forward(cfg, *a, w)
+    n = 64 * 550
+    half = e2ttt.DeltaConfig(B, H, H, n, d, d, e2ttt.DT_BF16, 1.0)
+    o1, w1, _ = e2ttt.delta_forward(half, *[y[:, :, :n] for y in a], w)
+    o2, w2, _ = e2ttt.delta_forward(half, *[y[:, :, n:] for y in a], w1)
+    assert torch.equal(torch.cat([o1, o2], 2), out) and torch.equal(w2, w_out)
+
+
+def test_no_second_derivatives():
+    c = (1, 1, 1, 10, 16, 16)
+    x, _ = make(*c, "f32", seed=41)
+    t = {n: a.requires_grad_(True) for n, a in to_dev(x, "f32").items()}
+    cfg = e2ttt.DeltaConfig(*c, e2ttt.DT_F32, 1.0)
+    out, _ = e2ttt.DeltaFunction.apply(cfg, *[t[n] for n in ("q", "k", "v", "eta", "log_gamma", "w_in")])
+    (dq,) = torch.autograd.grad(out.sum(), t["q"], create_graph=True)
+    with pytest.raises(RuntimeError):
+        dq.sum().backward()
+
+
 def test_graph_replays_and_streams():
     """A training step captured as a graph and replayed equals the eager one, with eager work
     between the replays; and the calls on another stream equal those on the default one."""
