@@ -6,9 +6,9 @@
 // Wave w forms rows lab(w, .) of K K^T and Q K^T by MFMA with operands
 // straight from global memory (each chunk's rows are read by one workgroup,
 // 16 bytes a lane), transposed, so that the accumulators are already in the
-// order of the fragments to be written.  The inverse is taken in fp32: each
-// wave inverts one 16x16 diagonal block by substitution, and the blocks below
-// follow from -Y^-1 Z X^-1 at sizes 16 and 32 with fp32 MFMA.
+// order of the fragments to be written.  The inverse is taken in fp32 by blocks
+// of doubling size, each wave a 16x16 diagonal block and then its share of the
+// blocks below, with fp32 MFMA.
 #include "delta_common.h"
 
 namespace e2ttt {
@@ -39,6 +39,18 @@ __device__ __forceinline__ f32x4 mm16(f32x4 acc, f32x4 a, f32x4 b) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i], b[i], acc, 0, 0, 0);
   return acc;
+}
+
+__device__ __forceinline__ void mm16_2(f32x4& x, f32x4 a, f32x4 b, f32x4& y, f32x4 c, f32x4 d) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i], b[i], x, 0, 0, 0);
+    y = __builtin_amdgcn_mfma_f32_16x16x4f32(c[i], d[i], y, 0, 0, 0);
+  }
+}
+// Whether (r, c) lies in the lower left h x h block of a diagonal 2h x 2h block.
+__device__ __forceinline__ bool below(int r, int c, int h) {
+  return ((r ^ c) & (15 & ~(h - 1))) == h && (r & h);
 }
 
 template <bool BF>
@@ -163,22 +175,37 @@ __global__ void __launch_bounds__(256, 4) delta_prep_kernel(DeltaArgs a) {
   }
   __syncthreads();
 
-  // diagonal block w: column c of its inverse by substitution
+  // diagonal block w: its inverse by blocks of doubling size h (the inverse of
+  // [[X, 0], [Z, Y]] has -Y^-1 Z X^-1 below its diagonal blocks).  T and its
+  // transpose are kept in accumulator order, in which each is also the other's
+  // row operand.
   {
     float* d = am + 16 * w * LDT + 16 * w;
-    float x[16];
+    const f32x4 ar = blk_a(d, 0, 0, g, c), ac = blk_b(d, 0, 0, g, c);   // rows c; columns c
+    f32x4 t, u;                         // T, T^T: rows 4 g + e of column c
 #pragma unroll
-    for (int i1 = 0; i1 < 16; ++i1) {
-      float s = i1 == c ? 1.0f : 0.0f;
+    for (int e = 0; e < 4; ++e) {
+      const int r = 4 * g + e;
+      t[e] = r == c ? 1.0f : below(r, c, 1) ? -ac[e] : 0.0f;
+      u[e] = r == c ? 1.0f : below(c, r, 1) ? -ar[e] : 0.0f;
+    }
 #pragma unroll
-      for (int l = 0; l < i1; ++l) s = fmaf(-d[i1 * LDT + l], x[l], s);
-      x[i1] = s;
+    for (int h = 2; h < 16; h *= 2) {
+      f32x4 mr, mc, z, y;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int r = 4 * g + e;
+        mr[e] = below(c, r, h) ? -ar[e] : 0.0f;
+        mc[e] = below(r, c, h) ? -ac[e] : 0.0f;
+      }
+      z = y = zero4();
+      mm16_2(z, mr, t, y, mc, u);
+      const f32x4 t0 = t, u0 = u;
+      mm16_2(t, u0, z, u, t0, y);
     }
     wave_lds_order();                   // (the block is read by this wave alone)
-    if (g == 0) {
 #pragma unroll
-      for (int i1 = 0; i1 < 16; ++i1) d[i1 * LDT + c] = x[i1];
-    }
+    for (int e = 0; e < 4; ++e) d[(4 * g + e) * LDT + c] = t[e];
   }
   __syncthreads();
   if (w < 2) {   // 16x16 blocks (1, 0) and (3, 2), each read by its wave alone
