@@ -47,17 +47,20 @@ size_t up(size_t x) { return (x + 255) & ~(size_t)255; }
 constexpr size_t kCacheBytes = (size_t)128 << 20, kStretchBytes = (size_t)512 << 20;
 
 // Segments that `nch` chunks of U units run as (1: none).  A wave holds 16 value
-// channels of a unit, and the card takes 2048 such waves at once.  Segments
-// cost a pass over dv + dk channels ahead of the one over dv: where the card has
-// room for four only they lose (128 units of 64, 64 chunks: 375 us against
-// 319), at eight they halve the time (32 units of 128, 32 chunks: 125 us
-// against 195).  n of them take (nch / n) (t_state + t_chain) + n t_join, about
-// 5 us and 1 us: least at n = sqrt(5 nch).
+// channels of a unit, and the card takes 2048 such waves at once (`room`: how
+// many times the units fit).  Segments cost a pass over dv + dk channels ahead of
+// the one over dv, so they pay where the units' own workgroups leave more than
+// two thirds of the 256 CUs idle (64 units, 32 chunks: a training step of 128 x 128
+// 588 us against 700, of 32 x 64 233 against 251) and not beyond (128 units of
+// 64 x 64, 64 chunks: 371 us against 315; a step of 128 of 32 x 32: 312 against
+// 289).  n of them take (nch / n) (t_state + t_chain) + n t_join, about 5 us and
+// 1 us: least at n = sqrt(5 nch).
 long room(const e2ttt_delta_desc* d, long U) { return 2048 / (U * (delta_dvp(d->dv) / 16)); }
 long segments(const e2ttt_delta_desc* d, long U, long nch) {
-  const long most = room(d, U);
-  const long n = std::min(std::min(most, nch / 2), (long)sqrt(5.0 * nch));
-  return most < 6 || n < 3 ? 1 : n;
+  const int nw = delta_dkp(d->dk) > 64 ? 8 : 4;
+  const long groups = U * ((delta_dvp(d->dv) / 16 + nw - 1) / nw);
+  const long n = std::min(std::min(room(d, U), nch / 2), (long)sqrt(5.0 * nch));
+  return groups > 80 || n < 3 ? 1 : n;
 }
 
 Plan plan(const e2ttt_delta_desc* d, bool save) {

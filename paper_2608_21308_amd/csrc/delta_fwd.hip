@@ -274,6 +274,11 @@ hipError_t launch_delta_chain(const DeltaArgs& a, bool bf, bool save, bool state
   if (bf) {
     if (dkp == 32) return go<true, 32, 2>(a, save, state, s);
     if (dkp == 64) return go<true, 64, 4>(a, save, state, s);
+    // eight waves share a staged chunk (256 units of 128, 16 chunks: 197 us, with
+    // four 236); four where eight would leave half of the 256 CUs idle (128 units,
+    // 32 chunks: 235 us, with eight 270)
+    const long tiles = a.dvp / 16 + (state ? 8 : 0);
+    if ((long)a.B * a.H * a.nseg * ((tiles + 7) / 8) <= 128) return go<true, 128, 4>(a, save, state, s);
     return go<true, 128, 8>(a, save, state, s);
   }
   if (dkp == 32) return go<false, 32, 2>(a, save, state, s);
