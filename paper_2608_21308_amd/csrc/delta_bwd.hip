@@ -44,10 +44,11 @@ delta_bwd_kernel(DeltaArgs a, int nsl) {
   const long u = us / a.nseg;
   const int seg = (int)(us % a.nseg);
   if (STATE && seg == 0) return;
-  const int r0 = a.r0 + seg * a.seglen, r1 = min(a.r1, r0 + a.seglen);
   const int sl = (int)((blk / 8) % nsl);
   const int b = (int)(u / a.H), h = (int)(u % a.H), hk = h / (a.H / a.HK);
   const int nlive = live_tokens(a, b);
+  const int r0 = a.r0 + seg * a.seglen;                  // (up to the sequence's last chunk)
+  const int r1 = min(min(a.r1, r0 + a.seglen), (nlive + kDC - 1) / kDC);
   const int sc0 = sl * NW * 16, col = sc0 + 16 * w + c, tile = sl * NW + w;
   const int krow = tid / L::NP, kcol = (tid % L::NP) * L::PE;
   const int vrow = tid / LV::NP, vcol = (tid % LV::NP) * LV::PE;

@@ -63,6 +63,7 @@ delta_fwd_kernel(DeltaArgs a, int nsl) {
   if (MODE == kState && seg == a.nseg - 1 && (a.pterms == 2 || (sl + 1) * NW <= a.dvp / 16)) return;
   const int b = (int)(u / a.H), h = (int)(u % a.H), hk = h / (a.H / a.HK);
   const int nlive = live_tokens(a, b);
+  const int rl = min(r1, (nlive + kDC - 1) / kDC);       // chunks up to the sequence's end (zeros behind)
   const int sc0 = sl * NW * 16;                          // the workgroup's first column
   const int col = sc0 + 16 * w + c;                      // the lane's
   const int tile = sl * NW + w, nvt = a.dvp / 16;        // the wave's tile: of B, or behind them of F
@@ -121,9 +122,9 @@ delta_fwd_kernel(DeltaArgs a, int nsl) {
     if (tid < kGateChain / 4)
       rg = *reinterpret_cast<const f32x4*>(a.gate + cu * kGateFloats + 4 * tid);
   };
-  if (r0 < r1) fetch(r0);
+  if (r0 < rl) fetch(r0);
 
-  for (int r = r0; r < r1; ++r) {
+  for (int r = r0; r < rl; ++r) {
     const int t0 = r * kDC;
     const long cu = u * a.nc_buf + (r - a.r_base);
     __syncthreads();
@@ -141,7 +142,7 @@ delta_fwd_kernel(DeltaArgs a, int nsl) {
       reinterpret_cast<u32x4*>(ts)[min(tid + x * NTH, NF - 1)] = rf[x];
     if (tid < kGateChain / 4) *reinterpret_cast<f32x4*>(gl + 4 * tid) = rg;
     __syncthreads();
-    if (r + 1 < r1) fetch(r + 1);
+    if (r + 1 < rl) fetch(r + 1);
 
     // X, per 32 columns of the state
     typename O::S sb[KT];
@@ -219,12 +220,18 @@ delta_fwd_kernel(DeltaArgs a, int nsl) {
           O::template ss2<2>(oa[m], ub[x], ld_frag<BF, 2>(ps, fidx(m, x), lane), oa[m + 1], ub[x],
                              ld_frag<BF, 2>(ps, fidx(m + 1, x), lane));
       }
-      if (sc0 + 16 * w + 4 * g < a.dv && t0 + lab(m, c) < a.T)
+      if (sc0 + 16 * w + 4 * g < a.dv && t0 + lab(m, c) < nlive)
         IoT<BF>::st4(op + lab(m, c) * ost, oa[m]);
     }
     }
   }
 
+  if constexpr (OUT) {
+    const int t1 = (int)min((long)r1 * kDC, (long)a.T);
+    for (int t = max(r0 * kDC, nlive) + vrow; t < t1; t += NTH / LV::NP)
+      if (vok)
+        *reinterpret_cast<u32x4*>(row_of_w<E>(a.out, b, h, t) + sc0 + vcol) = u32x4{0, 0, 0, 0};
+  }
   if constexpr (MODE == kState) {
     if (tile < nvt) {
 #pragma unroll

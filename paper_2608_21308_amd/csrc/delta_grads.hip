@@ -88,6 +88,26 @@ __global__ void __launch_bounds__(64 * NWV, 2) delta_grads_kernel(DeltaArgs a) {
   const int t0 = r * kDC, nt = min(kDC, max(0, live_tokens(a, b) - t0));
   const int kst = (int)a.k.t, qst = (int)a.q.t, gst = (int)a.d_out.t, ost = (int)a.dv_.t;
 
+  if (nt < kDC) {                            // behind the sequence: zeros
+    const int rows = min(kDC, a.T - t0);
+    auto clear = [&](const View& v, int h, int d) {
+      const int np = d / L::PE;
+      for (int p = tid; p < (rows - nt) * np; p += NTH)
+        *reinterpret_cast<u32x4*>(row_of_w<E>(v, b, h, t0 + nt + p / np) + p % np * L::PE) =
+            u32x4{0, 0, 0, 0};
+    };
+    clear(a.dq, hk, a.dk);
+    clear(a.dkk, hk, a.dk);
+    for (int h = hk * rep; h < (hk + 1) * rep; ++h) {
+      clear(a.dv_, h, a.dv);
+      if (tid >= nt && tid < rows) {
+        *row_of_w<float>(a.deta, b, h, t0 + tid) = 0.0f;
+        if (a.dgam.p) *row_of_w<float>(a.dgam, b, h, t0 + tid) = 0.0f;
+      }
+    }
+    if (nt == 0) return;
+  }
+
   // the next value block on its way: v0 of value head h (chunk unit cu)
   f32x4 rw[PW][4], ru[PU][2];
   u32x4 ro[PO];
@@ -210,7 +230,7 @@ __global__ void __launch_bounds__(64 * NWV, 2) delta_grads_kernel(DeltaArgs a) {
       {
         const auto doi = LV::frag(dos, i, 0, g);
         const auto yi = terms_t<BF, kDC, false>(ys, UP, rt, g, c);
-        if (xb0 == 0 && t0 + i < a.T && v0 + 8 * g < a.dv) {   // dV = eta Y, eight channels a lane
+        if (xb0 == 0 && i < nt && v0 + 8 * g < a.dv) {   // dV = eta Y, eight channels a lane
           f32x4 y0, y1;
           O::sum(yi, y0, y1);
           E* p = row_of_w<E>(a.dv_, b, h, t0) + i * ost + v0 + 8 * g;
@@ -378,11 +398,11 @@ __global__ void __launch_bounds__(64 * NWV, 2) delta_grads_kernel(DeltaArgs a) {
         if (lane >= o) p += y;
         if (lane + o < 64) q += z;
       }
-      if (t0 + t < a.T) {
-        *row_of_w<float>(a.deta, b, h, t0 + t) = live ? de : 0.0f;
+      if (live) {
+        *row_of_w<float>(a.deta, b, h, t0 + t) = de;
         if (a.dgam.p)
           *row_of_w<float>(a.dgam, b, h, t0 + t) =
-              live ? (float)(q + (p - upto) + (double)gl[kGC] * dot) : 0.0f;
+              (float)(q + (p - upto) + (double)gl[kGC] * dot);
       }
     }
   }
@@ -396,7 +416,7 @@ __global__ void __launch_bounds__(64 * NWV, 2) delta_grads_kernel(DeltaArgs a) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const int t = lab(m0 + m, 4 * g) + e;
-      if (t0 + t < a.T && col < a.dk) {
+      if (t < nt && col < a.dk) {
         dqp[t * dqst + col] = (E)dq[m][e];
         dkp[t * dkst + col] = (E)dk[m][e];
       }

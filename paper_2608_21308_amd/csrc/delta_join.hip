@@ -23,6 +23,7 @@ __global__ void __launch_bounds__(4 * DK) delta_join_kernel(DeltaArgs a) {
   if (u >= (long)a.B * a.H) return;
   const int tile = (int)(blockIdx.x / 8 % nvt);
   const int row = 16 * tile + c, kc = lab(w, 4 * g);     // the lane's row of W, its columns kc ..
+  const int live = live_tokens(a, (int)(u / a.H));       // (segments behind it leave the state)
   const int first = BWD ? a.nseg - 1 : 0, step = BWD ? -1 : 1;
   const float* from = BWD ? a.d_w_out : a.w_in;
   f32x4 st = zero4();
@@ -51,6 +52,7 @@ __global__ void __launch_bounds__(4 * DK) delta_join_kernel(DeltaArgs a) {
       *reinterpret_cast<bf16x4*>(&ws[i & 1][t][c * LD + kc]) =
           __builtin_shufflevector(own.t[t], own.t[t], 0, 1, 2, 3);
     __syncthreads();                                     // (the other buffer is read until the next)
+    const f32x4 was = st;
     st = bb;
     O::S fa[KT];
 #pragma unroll
@@ -64,6 +66,7 @@ __global__ void __launch_bounds__(4 * DK) delta_join_kernel(DeltaArgs a) {
         sb.t[t] = *reinterpret_cast<const bf16x8*>(&ws[i & 1][t][c * LD + 32 * kt + 8 * g]);
       st = O::ss<3>(st, fa[kt], sb);
     }
+    if ((long)(a.r0 + p * a.seglen) * kDC >= live) st = was;
     *reinterpret_cast<f32x4*>(a.segs + (u * a.nseg + p + step) * a.dvp * DK +
                               lane_at(tile, w >> 1, KT, lane) + 256 * (w & 1)) = st;
   };

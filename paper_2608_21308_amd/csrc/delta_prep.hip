@@ -84,6 +84,7 @@ __global__ void __launch_bounds__(256, 4) delta_prep_kernel(DeltaArgs a) {
   const int b = (int)(u / a.H), h = (int)(u % a.H), hk = h / (a.H / a.HK);
   const int t0 = r * kDC, nt = min(kDC, max(0, live_tokens(a, b) - t0));
   const long cu = u * a.nc_buf + (r - a.r_base);
+  if (nt == 0) return;              // (no kernel reads anything of such a chunk)
 
   if (w == 0) {
     const bool ok = lane < nt;

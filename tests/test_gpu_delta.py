@@ -425,3 +425,45 @@ def test_graph_replays_and_streams():
         step()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(everything(), ref)), i
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+@pytest.mark.parametrize("c,lengths", [((3, 1, 2, 200, 64, 64), (70, 0, 130)),
+                                       ((2, 1, 1, 1500, 32, 40), (600, 0))])
+def test_nothing_behind_a_sequence(c, lengths, io):
+    """Tokens behind a sequence's end have zero outputs and gradients whatever its live tokens
+    and its state hold, and an empty sequence keeps its state as it is."""
+    x, d = make(*c, io, seed=53)
+    x["v"][0, :, 3, 5] = float("nan")
+    x["k"][0, :, 40, 2] = float("inf")
+    x["w_in"][1, 0, 1, 2] = float("inf")
+    cfg = e2ttt.DeltaConfig(*c, e2ttt.DT_BF16 if io == "bf16" else e2ttt.DT_F32, 0.125)
+    t, td = to_dev(x, io), to_dev(d, io)
+    names = ("q", "k", "v", "eta", "log_gamma")
+    ln = torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    for save in (True, False):
+        out = torch.full_like(t["v"], float("nan"))
+        _, w_out, ws = e2ttt.delta_forward(cfg, *[t[n] for n in names], t["w_in"], lengths=ln, out=out,
+                                           save_for_backward=save)
+        for b, n in enumerate(lengths):
+            assert (out[b, :, n:] == 0).all(), (save, b)
+        assert torch.equal(w_out[1], t["w_in"][1])
+        if not save:
+            continue
+        g = {n: torch.full_like(a, float("nan")) for n, a in
+             (("dq", t["q"]), ("dk", t["k"]), ("dv", t["v"]), ("d_eta", t["eta"]),
+              ("d_log_gamma", t["eta"]), ("d_w_in", t["w_in"]))}
+        e2ttt.delta_backward(cfg, *[t[n] for n in names], ws, td["d_out"], td["d_w_out"], lengths=ln,
+                             grads=g)
+        for n, a in g.items():
+            for b, k in enumerate(lengths):
+                if n != "d_w_in":
+                    assert (a[b, :, k:] == 0).all(), (n, b)
+        assert torch.equal(g["d_w_in"][1], td["d_w_out"][1])
+    if len(lengths) == 3:          # the sequences with finite values are as they would be alone
+        x["v"][0] = 0
+        x["k"][0] = 0
+        ref, rw, _ = deltaref.delta_grads({n: a[2:] for n, a in x.items()}, 0.125, d["d_out"][2:],
+                                          d["d_w_out"][2:], torch.tensor(lengths[2:]))
+        close("out", out[2:], ref, io)
+        close("w_out", w_out[2:], rw, "f32")
