@@ -355,17 +355,19 @@ e2ttt_status e2ttt_apply_ln(const e2ttt_desc* desc, const float* ln_weight, cons
  * contiguous.  Token tensors and gates may have any non-negative strides
  * (e2ttt_delta_strides, in elements; the last dimension is contiguous), for
  * example those of a projection's [B][T][H][d]; strides NULL means C order.
- * Rows of the io type start on 16 bytes, and elements of a written tensor do
- * not overlap (else E2TTT_ERR_BAD_SHAPE).
+ * Rows of the io type start on 16 bytes, tokens are at most 2^23 elements
+ * apart, and elements of a written tensor do not overlap (else
+ * E2TTT_ERR_BAD_SHAPE).
  * lengths [B] int32 (device; NULL: all T): tokens of sequence b at and after
  * lengths[b] (clamped to 0..T) are not read and do not touch the state; their
  * outputs and gradients are written as zero.
- * Supported: dk <= 128 and dv <= 256, multiples of 8, either io type, T >= 1
- * (else E2TTT_ERR_UNSUPPORTED).
+ * Supported: dk <= 128 and dv <= 256, multiples of 8, either io type, T >= 1,
+ * B H up to 1.9 million units (more of dv <= 64) and 10^9 chunks of 64 tokens,
+ * 7.8 million to train (else E2TTT_ERR_UNSUPPORTED).
  *
  * Precision: fp32 throughout (with bf16 tensors, fp32 values enter the matrix
  * products as sums of three bf16 numbers, which lose nothing, or of two, to
- * 2^-17, where only a bf16 output follows).  Within a chunk of 64 tokens
+ * 2^-13 at the worst, where only a bf16 output follows).  Within a chunk of 64 tokens
  * (0..63, 64..127, ...) a token with a non-finite value may make the outputs
  * of its whole chunk non-finite, as it does those after it.
  */
@@ -445,7 +447,8 @@ e2ttt_status e2ttt_delta_step(const e2ttt_delta_desc* desc, const e2ttt_delta_st
  *                   rot_scale its factor on the turned elements, else 1)
  *   positions [B][T] int64   NULL: 0 .. T - 1; angles are formed in 64 bits
  * Outputs may be the inputs themselves (same strides).  Strides as for the
- * delta calls.  Supported: d <= 256, a multiple of 8, either io type.
+ * delta calls.  Supported: d <= 256, a multiple of 8, either io type, 10^9
+ * rows, fewer where rot / 2 is odd (32 d threads' worth; E2TTT_ERR_UNSUPPORTED).
  */
 #define E2TTT_QK_SILU 0x1u
 #define E2TTT_QK_UNIT 0x2u

@@ -11,7 +11,7 @@
 namespace e2ttt {
 namespace {
 
-e2ttt_status check_desc(const e2ttt_delta_desc* d) {
+e2ttt_status check_desc(const e2ttt_delta_desc* d, bool save) {
   if (!d) return E2TTT_ERR_NULL_ARG;
   if (d->B <= 0 || d->HK <= 0 || d->H <= 0 || d->T <= 0 || d->dk <= 0 || d->dv <= 0 ||
       d->H % d->HK != 0 || !isfinite(d->scale))
@@ -19,9 +19,12 @@ e2ttt_status check_desc(const e2ttt_delta_desc* d) {
   if ((d->io != E2TTT_DT_F32 && d->io != E2TTT_DT_BF16) || d->dk % 8 || d->dv % 8 ||
       d->dk > 128 || d->dv > 256 || d->T > (1 << 30))
     return E2TTT_ERR_UNSUPPORTED;
-  // every launch numbers its workgroups in 31 bits
+  // a launch numbers its threads in 32 bits: at most 8 dvp (512) to a unit, and
+  // where it takes every chunk at once 512 to a chunk
   const double units = (double)d->B * d->H, nc = ((double)d->T + kDC - 1) / kDC;
-  if (units * 64 > 1e9 || units * nc > 1e9) return E2TTT_ERR_UNSUPPORTED;
+  if (units * std::max(512, 8 * delta_dvp(d->dv)) > 4e9 || units * nc > 1e9 ||
+      (save && units * nc * 512 > 4e9))
+    return E2TTT_ERR_UNSUPPORTED;
   return E2TTT_OK;
 }
 
@@ -158,11 +161,12 @@ void fill(DeltaArgs& a, const e2ttt_delta_desc* d, const Plan& p, char* ws) {
 using namespace e2ttt;
 
 extern "C" size_t e2ttt_delta_workspace_bytes(const e2ttt_delta_desc* desc, int save_for_backward) {
-  return check_desc(desc) == E2TTT_OK ? plan(desc, save_for_backward != 0).bytes : 0;
+  const bool save = save_for_backward != 0;
+  return check_desc(desc, save) == E2TTT_OK ? plan(desc, save).bytes : 0;
 }
 
 extern "C" size_t e2ttt_delta_scratch_bytes(const e2ttt_delta_desc* desc) {
-  return check_desc(desc) == E2TTT_OK ? plan(desc, true).scratch : 0;
+  return check_desc(desc, true) == E2TTT_OK ? plan(desc, true).scratch : 0;
 }
 
 extern "C" e2ttt_status e2ttt_delta_forward(const e2ttt_delta_desc* desc,
@@ -172,7 +176,7 @@ extern "C" e2ttt_status e2ttt_delta_forward(const e2ttt_delta_desc* desc,
                                             const float* w_in, void* out, float* w_out,
                                             void* workspace, size_t workspace_bytes,
                                             int save_for_backward, void* stream) {
-  e2ttt_status st = check_desc(desc);
+  e2ttt_status st = check_desc(desc, save_for_backward != 0);
   if (st != E2TTT_OK) return st;
   if (!q || !k || !v || !eta || !out || !workspace) return E2TTT_ERR_NULL_ARG;
   Views vw;
@@ -213,7 +217,7 @@ extern "C" e2ttt_status e2ttt_delta_backward(
     const void* workspace, size_t workspace_bytes, const void* d_out, const float* d_w_out,
     void* dq, void* dk, void* dv, float* d_eta, float* d_log_gamma, float* d_w_in, void* scratch,
     size_t scratch_bytes, void* stream) {
-  e2ttt_status st = check_desc(desc);
+  e2ttt_status st = check_desc(desc, true);
   if (st != E2TTT_OK) return st;
   if (!q || !k || !v || !eta || !workspace || !d_out || !dq || !dk || !dv || !d_eta || !scratch)
     return E2TTT_ERR_NULL_ARG;
@@ -259,7 +263,7 @@ extern "C" e2ttt_status e2ttt_delta_step(const e2ttt_delta_desc* desc,
                                          const void* k, const void* v, const float* eta,
                                          const float* log_gamma, float* w, const int32_t* slots,
                                          int32_t n_slots, void* out, void* stream) {
-  e2ttt_status st = check_desc(desc);
+  e2ttt_status st = check_desc(desc, false);
   if (st != E2TTT_OK) return st;
   if (!q || !k || !v || !eta || !w || !out) return E2TTT_ERR_NULL_ARG;
   if (n_slots <= 0 || (!slots && n_slots < desc->B)) return E2TTT_ERR_BAD_SHAPE;

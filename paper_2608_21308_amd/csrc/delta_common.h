@@ -101,9 +101,9 @@ __host__ __device__ constexpr int fidx(int m, int a) { return m < 2 ? m : 2 * (m
 // before leave: 8 bits each, 24 in all, so that nothing is lost.  A product
 // takes the terms whose combined order is below N: with N = 3 it is an fp32
 // product (what is left out is of the order 2^-24), used for all that reaches
-// a state or a gate's gradient; with N = 2 its error is at most 2^-15, far
-// below the rounding of a bf16 output (2^-9), used for what reaches such
-// outputs only.  f32 io: fp32 MFMA.
+// a state or a gate's gradient; with N = 2 its error is at most 2^-15 (2^-13 of
+// two S operands), far below the rounding of a bf16 output (2^-9), used for what
+// reaches such outputs only.  f32 io: fp32 MFMA.
 template <bool BF> struct DOp;
 
 template <> struct DOp<true> {

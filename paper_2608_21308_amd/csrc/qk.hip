@@ -261,25 +261,36 @@ __global__ void __launch_bounds__(256) qk_kernel(QkArgs a, unsigned flags) {
   }
 }
 
+// The widest pieces of a head, the lanes of a row, and how many heads a group
+// of lanes takes.
+struct Shape {
+  int v, items, llanes, hpg, nhg;
+  long blocks;
+};
+Shape shape_of(const e2ttt_qk_desc* d) {
+  Shape s;
+  const int h = d->rot / 2;
+  s.v = d->io == E2TTT_DT_BF16 && h % 8 == 0 ? 8 : h % 4 == 0 ? 4 : h % 2 == 0 ? 2 : 1;
+  s.items = h / s.v + ((d->d - 2 * h) / s.v + 1) / 2;
+  s.llanes = 0;
+  while ((1 << s.llanes) < s.items && s.llanes < 6) ++s.llanes;
+  // Several heads to a group (their angles are the same) as long as the card
+  // stays full: 256 CUs of 2048 lanes.
+  const long tokens = (long)d->B * d->T, heads = (long)d->H + d->HK;
+  s.hpg = 1;
+  while (s.hpg < 8 && ((tokens * heads / (2 * s.hpg)) << s.llanes) >= 256L * 2048) s.hpg *= 2;
+  s.nhg = (int)((heads + s.hpg - 1) / s.hpg);
+  s.blocks = (((tokens * s.nhg) << s.llanes) + 255) / 256;
+  return s;
+}
+
 template <bool BF, int V, bool BWD>
-hipError_t go(QkArgs a, unsigned flags, hipStream_t s) {
-  const int items = a.half / V + ((a.d - 2 * a.half) / V + 1) / 2;
-  a.llanes = 0;
-  while ((1 << a.llanes) < items && a.llanes < 6) ++a.llanes;
-  a.lanes = 1 << a.llanes;
-  const long rows = (long)a.B * a.T * (a.nh[0] + a.nh[1]);
-  // Several heads to a group of lanes (their angles are the same) as long as
-  // the card stays full: 256 CUs of 2048 lanes.
-  a.hpg = 1;
-  while (a.hpg < 8 && rows / (2 * a.hpg) * a.lanes >= 256L * 2048) a.hpg *= 2;
-  a.nhg = (a.nh[0] + a.nh[1] + a.hpg - 1) / a.hpg;
-  const long blocks = ((long)a.B * a.T * a.nhg * a.lanes + 255) / 256;
-  if (blocks > 0x7fffffffL) return hipErrorInvalidValue;
+hipError_t go(const QkArgs& a, const Shape& sh, unsigned flags, hipStream_t s) {
   // (d <= 256: only single pairs to a piece can make more than 64 items)
   constexpr int kMost = V == 1 ? 2 : 1;
-  const dim3 grid((unsigned)blocks), blk(256);
+  const dim3 grid((unsigned)sh.blocks), blk(256);
   const bool inter = flags & E2TTT_QK_INTERLEAVED;
-  if (items > 64) {
+  if (sh.items > 64) {
     if (inter) hipLaunchKernelGGL((qk_kernel<BF, V, kMost, BWD, true>), grid, blk, 0, s, a, flags);
     else hipLaunchKernelGGL((qk_kernel<BF, V, kMost, BWD, false>), grid, blk, 0, s, a, flags);
   } else {
@@ -290,12 +301,17 @@ hipError_t go(QkArgs a, unsigned flags, hipStream_t s) {
 }
 
 template <bool BWD>
-hipError_t launch(const QkArgs& a, bool bf, unsigned flags, hipStream_t s) {
-  const int h = a.half;
-  if (bf && h % 8 == 0) return go<true, 8, BWD>(a, flags, s);
-  if (h % 4 == 0) return bf ? go<true, 4, BWD>(a, flags, s) : go<false, 4, BWD>(a, flags, s);
-  if (h % 2 == 0) return bf ? go<true, 2, BWD>(a, flags, s) : go<false, 2, BWD>(a, flags, s);
-  return bf ? go<true, 1, BWD>(a, flags, s) : go<false, 1, BWD>(a, flags, s);
+e2ttt_status launch(const QkArgs& a, const e2ttt_qk_desc* d, void* stream) {
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  const bool bf = d->io == E2TTT_DT_BF16;
+  const unsigned f = d->flags;
+  const Shape sh = shape_of(d);
+  hipError_t e;
+  if (sh.v == 8) e = go<true, 8, BWD>(a, sh, f, s);
+  else if (sh.v == 4) e = bf ? go<true, 4, BWD>(a, sh, f, s) : go<false, 4, BWD>(a, sh, f, s);
+  else if (sh.v == 2) e = bf ? go<true, 2, BWD>(a, sh, f, s) : go<false, 2, BWD>(a, sh, f, s);
+  else e = bf ? go<true, 1, BWD>(a, sh, f, s) : go<false, 1, BWD>(a, sh, f, s);
+  return e == hipSuccess ? E2TTT_OK : E2TTT_ERR_HIP;
 }
 
 constexpr unsigned kFlags = E2TTT_QK_SILU | E2TTT_QK_UNIT | E2TTT_QK_INTERLEAVED;
@@ -310,7 +326,8 @@ e2ttt_status check_desc(const e2ttt_qk_desc* d) {
   if ((d->io != E2TTT_DT_F32 && d->io != E2TTT_DT_BF16) || (d->flags & ~kFlags) || d->d % 8 ||
       d->d > 256 || (double)d->B * d->T * ((double)d->H + d->HK) > 1e9)
     return E2TTT_ERR_UNSUPPORTED;
-  return E2TTT_OK;
+  // (a launch numbers its threads in 32 bits)
+  return shape_of(d).blocks > 0xffffff ? E2TTT_ERR_UNSUPPORTED : E2TTT_OK;
 }
 
 QkArgs args_of(const e2ttt_qk_desc* d, const float* inv_freq, const int64_t* pos) {
@@ -319,6 +336,9 @@ QkArgs args_of(const e2ttt_qk_desc* d, const float* inv_freq, const int64_t* pos
   a.nh[0] = d->H; a.nh[1] = d->HK;
   a.inv_freq = inv_freq; a.pos = pos;
   a.eps = d->eps; a.m = d->rot_scale;
+  const Shape s = shape_of(d);
+  a.llanes = s.llanes; a.lanes = 1 << s.llanes;
+  a.hpg = s.hpg; a.nhg = s.nhg;
   return a;
 }
 
@@ -343,8 +363,7 @@ extern "C" e2ttt_status e2ttt_qk_forward(const e2ttt_qk_desc* desc, const e2ttt_
               !in.write(strides ? &strides->k_out : nullptr, k_out, desc->HK, &a.y[1]))))
     return E2TTT_ERR_BAD_SHAPE;
   a.tfast = a.x[0].t < a.x[0].h;
-  return launch<false>(a, desc->io == E2TTT_DT_BF16, desc->flags, static_cast<hipStream_t>(stream)) ==
-                 hipSuccess ? E2TTT_OK : E2TTT_ERR_HIP;
+  return launch<false>(a, desc, stream);
 }
 
 extern "C" e2ttt_status e2ttt_qk_backward(const e2ttt_qk_desc* desc,
@@ -370,6 +389,5 @@ extern "C" e2ttt_status e2ttt_qk_backward(const e2ttt_qk_desc* desc,
                in.write(strides ? &strides->dk : nullptr, dk, desc->HK, &a.y[1])));
   if (!ok) return E2TTT_ERR_BAD_SHAPE;
   a.tfast = a.g[0].t < a.g[0].h;
-  return launch<true>(a, desc->io == E2TTT_DT_BF16, desc->flags, static_cast<hipStream_t>(stream)) ==
-                 hipSuccess ? E2TTT_OK : E2TTT_ERR_HIP;
+  return launch<true>(a, desc, stream);
 }

@@ -601,10 +601,11 @@ def _on_device(f):
 
 
 def _as_rows(g):
-    """A gradient as the library takes it: rows contiguous and on 16 bytes."""
+    """A gradient as the library takes it: rows contiguous, on 16 bytes and at
+    most 2^23 elements apart."""
     if g.is_contiguous() and g.data_ptr() % 16 == 0:
         return g
-    if g.stride(-1) != 1 or g.data_ptr() % 16 or any(
+    if g.stride(-1) != 1 or g.stride(2) > 1 << 23 or g.data_ptr() % 16 or any(
             s * g.element_size() % 16 for s, n in zip(g.stride()[:3], g.shape) if n > 1):
         return g.contiguous()
     return g

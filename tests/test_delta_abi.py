@@ -195,3 +195,16 @@ def test_rotary_frequencies():
                 dict(rot=64, factor=2.0, original=-1)):
         with pytest.raises(ValueError):
             e2ttt.rotary_frequencies(device="cpu", **bad)
+
+
+def test_launches_of_more_than_32_bits_of_threads(lib):
+    def size(save, **kw):
+        return lib.e2ttt_delta_workspace_bytes(ctypes.byref(ddesc(**kw)), save)
+
+    assert size(0, B=1 << 21, HK=1, H=1, dv=64) > 0
+    assert size(0, B=1 << 21, HK=1, H=1, dv=256) == 0
+    big = dict(B=1, HK=1024, H=1024, T=1 << 20)
+    assert size(0, **big) > 0 and size(1, **big) == 0
+    assert lib.e2ttt_delta_scratch_bytes(ctypes.byref(ddesc(**big))) == 0
+    assert calls(lib, ddesc(**big))[1] == 3
+    assert qcalls(lib, qdesc(B=1 << 14, T=1 << 14, H=1, HK=0, rot=2)) == (3, 3)
