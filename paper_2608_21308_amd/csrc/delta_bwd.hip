@@ -15,8 +15,10 @@ namespace e2ttt {
 namespace {
 
 // STATE: only the adjoint at every segment's start, from zero at its end.
+// (f32 io: one wave a SIMD, as in the forward: a step of 256 units of 64, 16
+// chunks, 592 us against 693.)
 template <bool BF, int DK, int NW, bool STATE>
-__global__ void __launch_bounds__(64 * NW, NW == 8 || DK <= 64 ? 2 : 1)
+__global__ void __launch_bounds__(64 * NW, BF && (NW == 8 || DK <= 64) ? 2 : 1)
 delta_bwd_kernel(DeltaArgs a, int nsl) {
   using O = DOp<BF>;
   using E = typename O::E;
