@@ -57,13 +57,15 @@ constexpr size_t kCacheBytes = (size_t)128 << 20, kStretchBytes = (size_t)512 <<
 // 588 us against 700, of 32 x 64 233 against 251) and not beyond (128 units of
 // 64 x 64, 64 chunks: 371 us against 315; a step of 128 of 32 x 32: 312 against
 // 289).  n of them take (nch / n) (t_state + t_chain) + n t_join, about 5 us and
-// 1 us: least at n = sqrt(5 nch).
+// 1 us: least at n = sqrt(5 nch).  They begin at 8 chunks with bf16 (32 units of
+// 64: 37 us either way, at 6 chunks 34 against 31), at 6 with the slower fp32
+// products (8 units of 64: 41 us against 49).
 long room(const e2ttt_delta_desc* d, long U) { return 2048 / (U * (delta_dvp(d->dv) / 16)); }
 long segments(const e2ttt_delta_desc* d, long U, long nch) {
   const int nw = delta_dkp(d->dk) > 64 ? 8 : 4;
   const long groups = U * ((delta_dvp(d->dv) / 16 + nw - 1) / nw);
   const long n = std::min(std::min(room(d, U), nch / 2), (long)sqrt(5.0 * nch));
-  return groups > 80 || n < 3 ? 1 : n;
+  return groups > 80 || n < 3 || nch < (d->io == E2TTT_DT_BF16 ? 8 : 6) ? 1 : n;
 }
 
 Plan plan(const e2ttt_delta_desc* d, bool save) {
