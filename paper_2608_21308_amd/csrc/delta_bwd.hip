@@ -9,17 +9,22 @@
 // sum over the value dimension (delta_grads.hip).  Long chains of few units run
 // as segments (delta_fwd.hip): a segment with the transition F takes the
 // adjoint at its end to dW F^T + B at its start.
-#include "delta_common.h"
+#include "delta_grads.h"
 
 namespace e2ttt {
 namespace {
 
-// STATE: only the adjoint at every segment's start, from zero at its end.
-// (f32 io: one wave a SIMD, as in the forward: a step of 256 units of 64, 16
-// chunks, 592 us against 693.)
+// LDS of a workgroup (offsets in bytes).
 template <bool BF, int DK, int NW, bool STATE>
-__global__ void __launch_bounds__(64 * NW, BF && (NW == 8 || DK <= 64) ? 2 : 1)
-delta_bwd_kernel(DeltaArgs a, int nsl) {
+struct BwdLds {
+  static constexpr int e = (int)sizeof(typename DOp<BF>::E), ks = kDC * DK * e;
+  static constexpr int qs = ks, vs = qs + (ks), ts = vs + kDC * 16 * NW * e;
+  static constexpr int gl = ts + 2 * tri_bytes(BF, 3), bytes = gl + kGateChain * 4;
+};
+
+// STATE: only the adjoint at every segment's start, from zero at its end.
+template <bool BF, int DK, int NW, bool STATE>
+__device__ __forceinline__ void bwd_chain(const DeltaArgs& a, int nsl, long blk, char* lds) {
   using O = DOp<BF>;
   using E = typename O::E;
   using L = LTile<BF, DK>;
@@ -30,17 +35,17 @@ delta_bwd_kernel(DeltaArgs a, int nsl) {
   constexpr int PF = (NF + NTH - 1) / NTH;
   static_assert(kDC * L::NP % NTH == 0 && NTH % L::NP == 0 && NTH % LV::NP == 0,
                 "whole rounds of pieces");
-  __shared__ __align__(16) E ks[kDC * DK];
-  __shared__ __align__(16) E qs[kDC * DK];
-  __shared__ __align__(16) E vs[kDC * 16 * NW];          // dO rows
-  __shared__ __align__(16) char ts[16 * NF];             // T, then P
-  __shared__ __align__(16) float gl[kGateChain];
+  using M = BwdLds<BF, DK, NW, STATE>;
+  E* ks = reinterpret_cast<E*>(lds);
+  E* qs = reinterpret_cast<E*>(lds + M::qs);
+  E* vs = reinterpret_cast<E*>(lds + M::vs);             // dO rows
+  char* ts = lds + M::ts;                                // T, then P
+  float* gl = reinterpret_cast<float*>(lds + M::gl);
 
   const char* ps = ts + tri_bytes(BF, 3);
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, c = lane & 15;
   const int w = wave_id();
   const long U = (long)a.B * a.H;
-  const long blk = blockIdx.x;
   const long us = (blk / (8 * nsl)) * 8 + blk % 8;       // (unit, segment)
   if (us >= U * a.nseg) return;
   const long u = us / a.nseg;
@@ -217,6 +222,15 @@ delta_bwd_kernel(DeltaArgs a, int nsl) {
   }
 }
 
+// (f32 io: one wave a SIMD, as in the forward: a step of 256 units of 64, 16
+// chunks, 592 us against 693.)
+template <bool BF, int DK, int NW, bool STATE>
+__global__ void __launch_bounds__(64 * NW, BF && (NW == 8 || DK <= 64) ? 2 : 1)
+delta_bwd_kernel(DeltaArgs a, int nsl) {
+  __shared__ __align__(16) char lds[BwdLds<BF, DK, NW, STATE>::bytes];
+  bwd_chain<BF, DK, NW, STATE>(a, nsl, blockIdx.x, lds);
+}
+
 template <bool BF, int DK, int NW>
 hipError_t go(const DeltaArgs& a, bool state, hipStream_t s) {
   const int nsl = (a.dvp + 16 * NW - 1) / (16 * NW);
@@ -229,7 +243,31 @@ hipError_t go(const DeltaArgs& a, bool state, hipStream_t s) {
   return hipGetLastError();
 }
 
+// The first `nchain` workgroups run the chain, those behind them form the
+// gradients of the ng chunks from g0 on, which the launch before has passed.
+template <bool ONE>
+__global__ void __launch_bounds__(256, 2)
+delta_bwd_grads_kernel(DeltaArgs a, int nsl, int nchain, int g0, int ng) {
+  constexpr int kChain = BwdLds<true, 64, 4, false>::bytes, kGrads = GradsLds<true, 64, 4>::bytes;
+  __shared__ __align__(16) char lds[kChain > kGrads ? kChain : kGrads];
+  if ((int)blockIdx.x < nchain)
+    bwd_chain<true, 64, 4, false>(a, nsl, blockIdx.x, lds);
+  else
+    grads_chunk<true, 64, 4, ONE>(a, g0, ng, blockIdx.x - nchain, lds);
+}
+
 }  // namespace
+
+hipError_t launch_delta_chain_bwd_grads(const DeltaArgs& a, int g0, int ng, hipStream_t s) {
+  const int nsl = (a.dvp + 63) / 64;
+  const long nchain = ((long)a.B * a.H + 7) / 8 * 8 * nsl;
+  const dim3 grid((unsigned)(nchain + (long)a.B * a.HK * ng)), blk(256);
+  if (a.H == a.HK)
+    hipLaunchKernelGGL((delta_bwd_grads_kernel<true>), grid, blk, 0, s, a, nsl, (int)nchain, g0, ng);
+  else
+    hipLaunchKernelGGL((delta_bwd_grads_kernel<false>), grid, blk, 0, s, a, nsl, (int)nchain, g0, ng);
+  return hipGetLastError();
+}
 
 hipError_t launch_delta_chain_bwd(const DeltaArgs& a, bool bf, bool state, hipStream_t s) {
   const int dkp = delta_dkp(a.dk);

@@ -479,6 +479,10 @@ hipError_t launch_delta_prep(const DeltaArgs& a, bool bf, hipStream_t stream);
 // the segments make of a zero state and their transitions.
 hipError_t launch_delta_chain(const DeltaArgs& a, bool bf, bool save, bool state, hipStream_t stream);
 hipError_t launch_delta_chain_bwd(const DeltaArgs& a, bool bf, bool state, hipStream_t stream);
+// bf16, dk in 33..64, no segments: the chain over r0 .. r1 - 1 beside the preparation
+// of the np chunks from p0 on, or the gradients of the ng from g0 on.
+hipError_t launch_delta_chain_prep(const DeltaArgs& a, bool save, int p0, int np, hipStream_t stream);
+hipError_t launch_delta_chain_bwd_grads(const DeltaArgs& a, int g0, int ng, hipStream_t stream);
 // The segments' start states from their parts, one after the other.
 hipError_t launch_delta_join(const DeltaArgs& a, bool bwd, hipStream_t stream);
 hipError_t launch_delta_grads(const DeltaArgs& a, bool bf, hipStream_t stream);

@@ -18,19 +18,26 @@
 // W -> W F + B, so a first pass takes B (the columns above from zero) and F
 // (dk more columns, from the unit matrix, with V = 0) of every segment at
 // once, delta_join.hip forms the states that the segments start from, and
-// this pass runs them all at once.
-#include "delta_common.h"
+// this pass runs them all at once.  Some more units leave CUs idle whose own
+// chains segments would not shorten: there the launch takes a part of the chain
+// beside the preparation of the next (delta_api.hip holds the rules of both).
+#include "delta_prep.h"
 
 namespace e2ttt {
 namespace {
 
 enum { kPlain = 0, kSave = 1, kState = 2 };
 
-// (f32 io: one wave a SIMD, as 256 registers would spill some 40: 256 units of 64,
-// 16 chunks, 187 us against 262)
+// LDS of a workgroup (offsets in bytes).
 template <bool BF, int DK, int NW, int MODE>
-__global__ void __launch_bounds__(64 * NW, BF && (NW == 8 || DK <= 64) ? 2 : 1)
-delta_fwd_kernel(DeltaArgs a, int nsl) {
+struct FwdLds {
+  static constexpr int e = (int)sizeof(typename DOp<BF>::E), ks = kDC * DK * e;
+  static constexpr int qs = ks, vs = qs + (MODE != kState ? ks : 0), ts = vs + kDC * 16 * NW * e;
+  static constexpr int gl = ts + tri_bytes(BF, 3) + (MODE != kState ? tri_bytes(BF, 2) : 0), bytes = gl + kGateChain * 4;
+};
+
+template <bool BF, int DK, int NW, int MODE>
+__device__ __forceinline__ void fwd_chain(const DeltaArgs& a, int nsl, long blk, char* lds) {
   constexpr bool SAVE = MODE == kSave, OUT = MODE != kState;
   using O = DOp<BF>;
   using E = typename O::E;
@@ -43,18 +50,18 @@ delta_fwd_kernel(DeltaArgs a, int nsl) {
   constexpr int PF = (NF + NTH - 1) / NTH;
   static_assert(kDC * L::NP % NTH == 0 && NTH % L::NP == 0 && NTH % LV::NP == 0,
                 "whole rounds of pieces");
-  __shared__ __align__(16) E ks[kDC * DK];
-  __shared__ __align__(16) E qs[OUT ? kDC * DK : 8];
-  __shared__ __align__(16) E vs[kDC * 16 * NW];
-  __shared__ __align__(16) char ts[16 * NF];             // T, then P
-  __shared__ __align__(16) float gl[kGateChain];
+  using M = FwdLds<BF, DK, NW, MODE>;
+  E* ks = reinterpret_cast<E*>(lds);
+  E* qs = reinterpret_cast<E*>(lds + M::qs);
+  E* vs = reinterpret_cast<E*>(lds + M::vs);
+  char* ts = lds + M::ts;                                // T, then P
+  float* gl = reinterpret_cast<float*>(lds + M::gl);
 
   const char* ps = ts + tri_bytes(BF, 3);
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, c = lane & 15;
   const int w = wave_id();
   // the slices of a unit go to one XCD (workgroups are dealt to the eight in turn)
   const long U = (long)a.B * a.H;
-  const long blk = blockIdx.x;
   const long us = (blk / (8 * nsl)) * 8 + blk % 8;       // (unit, segment)
   if (us >= U * a.nseg) return;
   const long u = us / a.nseg;
@@ -262,6 +269,15 @@ delta_fwd_kernel(DeltaArgs a, int nsl) {
   }
 }
 
+// (f32 io: one wave a SIMD, as 256 registers would spill some 40: 256 units of 64,
+// 16 chunks, 187 us against 262)
+template <bool BF, int DK, int NW, int MODE>
+__global__ void __launch_bounds__(64 * NW, BF && (NW == 8 || DK <= 64) ? 2 : 1)
+delta_fwd_kernel(DeltaArgs a, int nsl) {
+  __shared__ __align__(16) char lds[FwdLds<BF, DK, NW, MODE>::bytes];
+  fwd_chain<BF, DK, NW, MODE>(a, nsl, blockIdx.x, lds);
+}
+
 template <bool BF, int DK, int NW>
 hipError_t go(const DeltaArgs& a, bool save, bool state, hipStream_t s) {
   const int tiles = a.dvp / 16 + (state ? DK / 16 : 0), nsl = (tiles + NW - 1) / NW;
@@ -276,7 +292,31 @@ hipError_t go(const DeltaArgs& a, bool save, bool state, hipStream_t s) {
   return hipGetLastError();
 }
 
+// The first `nchain` workgroups run the chain, those behind them prepare the np
+// chunks from p0 on, which the next launch takes.
+template <int MODE>
+__global__ void __launch_bounds__(256, 2)
+delta_fwd_prep_kernel(DeltaArgs a, int nsl, int nchain, int p0, int np) {
+  constexpr int kChain = FwdLds<true, 64, 4, MODE>::bytes;
+  __shared__ __align__(16) char lds[kChain > kPrepLds ? kChain : kPrepLds];
+  if ((int)blockIdx.x < nchain)
+    fwd_chain<true, 64, 4, MODE>(a, nsl, blockIdx.x, lds);
+  else
+    prep_chunk<true, 64>(a, p0, np, blockIdx.x - nchain, lds);
+}
+
 }  // namespace
+
+hipError_t launch_delta_chain_prep(const DeltaArgs& a, bool save, int p0, int np, hipStream_t s) {
+  const int nsl = (a.dvp + 63) / 64;
+  const long units = (long)a.B * a.H, nchain = (units + 7) / 8 * 8 * nsl;
+  const dim3 grid((unsigned)(nchain + units * np)), blk(256);
+  if (save)
+    hipLaunchKernelGGL((delta_fwd_prep_kernel<kSave>), grid, blk, 0, s, a, nsl, (int)nchain, p0, np);
+  else
+    hipLaunchKernelGGL((delta_fwd_prep_kernel<kPlain>), grid, blk, 0, s, a, nsl, (int)nchain, p0, np);
+  return hipGetLastError();
+}
 
 hipError_t launch_delta_chain(const DeltaArgs& a, bool bf, bool save, bool state, hipStream_t s) {
   const int dkp = delta_dkp(a.dk);

@@ -467,3 +467,33 @@ def test_nothing_behind_a_sequence(c, lengths, io):
                                           d["d_w_out"][2:], torch.tensor(lengths[2:]))
         close("out", out[2:], ref, io)
         close("w_out", w_out[2:], rw, "f32")
+
+
+@pytest.mark.parametrize("c,lengths", [((7, 4, 12, 2100, 40, 24), (2100, 0, 1, 700, 1024, 1025, 2099)),
+                                       ((6, 16, 16, 2049, 64, 8), None)])
+@pytest.mark.parametrize("layout", ["bhtd", "bthd"])
+def test_parts(c, lengths, layout):
+    """Units that half fill the card, over long sequences: the chain in parts."""
+    x, d = make(*c, "bf16", seed=61)
+    B, HK, H, T, dk, dv = c
+    cfg = e2ttt.DeltaConfig(*c, e2ttt.DT_BF16, 0.125)
+    t, td = to_dev(x, "bf16", layout), to_dev(d, "bf16", layout)
+    names = ("q", "k", "v", "eta", "log_gamma")
+    ln = None if lengths is None else torch.tensor(lengths, dtype=torch.int32)
+    lg = None if ln is None else ln.cuda()
+    out, w_out, ws = e2ttt.delta_forward(cfg, *[t[n] for n in names], t["w_in"], lengths=lg,
+                                         save_for_backward=True)
+    g = e2ttt.delta_backward(cfg, *[t[n] for n in names], ws, td["d_out"], td["d_w_out"], lengths=lg)
+    w = t["w_in"].clone()
+    out2, _, _ = e2ttt.delta_forward(cfg, *[t[n] for n in names], w, lengths=lg, w_out=w)
+    torch.cuda.synchronize()
+    assert torch.equal(out, out2) and torch.equal(w_out, w)
+    for b in (0, 3, 5):            # (the sequences do not meet)
+        ro, rw, rg = deltaref.delta_grads({n: a[b:b + 1] for n, a in x.items()}, 0.125, d["d_out"][b:b + 1],
+                                          d["d_w_out"][b:b + 1], None if ln is None else ln[b:b + 1])
+        close("out", out[b:b + 1], ro, "bf16")
+        close("w_out", w_out[b:b + 1], rw, "f32")
+        for n, m, y in (("q", "dq", "bf16"), ("k", "dk", "bf16"), ("v", "dv", "bf16"),
+                        ("eta", "d_eta", "f32"), ("log_gamma", "d_log_gamma", "f32"),
+                        ("w_in", "d_w_in", "f32")):
+            close(m, g[m][b:b + 1], rg[n], y)
