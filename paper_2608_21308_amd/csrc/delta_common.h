@@ -373,9 +373,10 @@ __device__ __forceinline__ typename DOp<BF>::S ld_frag_t(const char* lds, int m,
 // over the 256 bytes of the banks the rows of a fragment read (b0, b1, b3, b4
 // differ; the lane groups 0 and 1, 2 and 3 ask for neighbouring pieces), the four
 // rows (b0, b1) of a transposing read.  (b2 stays out: the rows 4 on that such a
-// read goes on to are then a constant away.)  fp32 fragments are two pieces,
-// which takes another one.
-template <bool BF, int D>
+// read goes on to are then a constant away; with COLS it is in, for tiles that
+// are written by columns, sixteen rows of a piece at a time.)  fp32 fragments are
+// two pieces, which takes another one.
+template <bool BF, int D, bool COLS = false>
 struct LTile {
   using E = typename DOp<BF>::E;
   static constexpr int PE = 16 / (int)sizeof(E);     // elements of a piece
@@ -385,7 +386,7 @@ struct LTile {
     // (rows of 64 and 128 bytes: b0 and b1, b0 move the bank by themselves)
     const int up = NP >= 16 ? (row & 3) << 2 : NP == 8 ? (row & 2) << 1 : 0;
     const int b4 = (row >> 4) & 1, f = up | (((row >> 2) & 2) ^ (3 * b4));
-    return (row * NP + (p ^ f)) * PE;
+    return (row * NP + (p ^ f ^ (COLS ? (row >> 2) & 1 : 0))) * PE;
   }
   // row `row`, columns 32 kt + 8 g .. + 7
   static __device__ __forceinline__ typename DOp<BF>::X frag(const E* t, int row, int kt, int g) {
@@ -428,17 +429,17 @@ __device__ __forceinline__ typename DOp<BF>::S terms_t(const typename DOp<BF>::E
     typename DOp<BF>::S s;
 #pragma unroll
     for (int i = 0; i < DOp<BF>::NT; ++i)
-      s.t[i] = LTile<BF, D>::template frag_t<NAT>(t + plane * i, m, 0, g, c).v;
+      s.t[i] = LTile<BF, D, true>::template frag_t<NAT>(t + plane * i, m, 0, g, c).v;
     return s;
   } else {
-    return LTile<BF, D>::template frag_t<NAT>(t, m, 0, g, c);
+    return LTile<BF, D, true>::template frag_t<NAT>(t, m, 0, g, c);
   }
 }
 // Eight fp32 values of such a tile's row (columns 8 p8 ..) into LDS as terms.
 template <bool BF, int D>
 __device__ __forceinline__ void put_terms(typename DOp<BF>::E* t, int plane, int row, int p8,
                                           f32x4 x, f32x4 y) {
-  using L = LTile<BF, D>;
+  using L = LTile<BF, D, true>;
   if constexpr (BF) {
     const auto s = DOp<true>::split<DOp<true>::NT>(x, y);
 #pragma unroll

@@ -63,7 +63,6 @@ __device__ __forceinline__ void grads_chunk(const DeltaArgs& a, int c0, int nr, 
   using E = typename O::E;
   using L = LTile<BF, DK>;      // K, Q rows; states
   using LV = LTile<BF, 32>;     // dO rows of a value block
-  using LU = LTile<BF, kDC>;    // U^T, Y^T
   constexpr int NT = O::NT, KT = DK / 32, NTH = 64 * NWV;
   constexpr int CTS = DK / 16;                          // column tiles
   constexpr int MG = NWV / CTS, MR = 4 / MG;            // row groups, row tiles of a wave
