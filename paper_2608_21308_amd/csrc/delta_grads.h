@@ -20,6 +20,11 @@
 // lab(w mod 4, .), with eight waves one of the two 32-column blocks.  Four
 // waves up to DK = 64, so that two workgroups share a CU and one computes while
 // the other waits; eight, and one workgroup a CU, at 128.
+//
+// 16384 chunks of dk = dv = 64 (112 KB each) take 580 us, 3.2 TB/s: the waves wait
+// for 40 % of it, for the next block and for each other, and issue vector
+// instructions for half, a third of them to split fp32 values into terms (the
+// registers and the 77 KB of LDS leave two workgroups a CU).  8192 of 128: 790 us.
 #pragma once
 
 #include "delta_common.h"

@@ -4,7 +4,8 @@
 //
 // One workgroup per unit and 16 rows of W (columns of W^T), a wave per 16 rows
 // of W^T, so that a step is dk / 32 products of fp32 accuracy a wave; the state
-// goes round through LDS, and the next two F are on their way meanwhile.
+// goes round through LDS, and the next two F are on their way meanwhile.  Bound
+// by that round: 1 us a segment at dk = 64, 2 us at 128 (backward 3).
 #include "delta_common.h"
 
 namespace e2ttt {

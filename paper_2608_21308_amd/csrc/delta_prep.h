@@ -9,6 +9,10 @@
 // order of the fragments to be written.  The inverse is taken in fp32 by blocks
 // of doubling size, each wave a 16x16 diagonal block and then its share of the
 // blocks below, with fp32 MFMA.
+//
+// Near HBM's rate: 16384 chunks of dk = 64 (16 KB read and 38 KB written each)
+// take 215 us, 4.1 TB/s where a large copy reaches 5.2; vector and matrix units
+// are busy for two thirds of it.
 #pragma once
 
 #include "delta_common.h"

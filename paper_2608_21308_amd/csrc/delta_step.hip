@@ -6,6 +6,9 @@
 // the state is dealt out by rows: LPR lanes hold a row as float4 pieces (a wave
 // reads whole rows of 64 / LPR channels per load) and sum their partial dots
 // by DPP.  A wave takes RS row sets, all loaded before the first is used.
+// 128 sequences of 32 heads of 128 x 128: 540 MB in 90 us, 6 TB/s (a part still
+// lies in the last-level cache; a large copy reaches 5.2); 8 sequences of 16
+// heads of 64 x 64: 4.8 us, which is the launch.
 #include "delta_common.h"
 
 namespace e2ttt {
