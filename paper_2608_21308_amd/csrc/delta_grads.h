@@ -185,7 +185,7 @@ __device__ __forceinline__ void grads_chunk(const DeltaArgs& a, int c0, int nr, 
   __syncthreads();
 
   const int rt = w & 3, xb0 = NB == 1 ? w >> 2 : 0;    // row tile, (first) block of the 64x64 products
-  const int ct = w % CTS, m0 = (w / CTS) * MR;   // column tile, first row tile of the 64xDK ones
+  const int ct = w % CTS, m0 = MG == 1 ? 0 : (w / CTS) * MR;   // column tile, first row tile of the 64xDK ones
   f32x4 dq[MR], dk[MR];
 #pragma unroll
   for (int m = 0; m < MR; ++m) dq[m] = dk[m] = zero4();
@@ -236,36 +236,46 @@ __device__ __forceinline__ void grads_chunk(const DeltaArgs& a, int c0, int nr, 
         fetch(h, cu, v0 + 32);
       else if (!ONE && hv + 1 < rep)
         fetch(h + 1, cu + a.nc_buf, 0);
-      {
+      auto products = [&](int m, const auto& wf, const auto& df, const auto& um) {
+        ow[m] = O::template xs<3>(ow[m], LV::frag(dos, lab(m0 + m, c), 0, g), wf);
+        yw[m] = O::template ss<3>(yw[m], terms_t<BF, kDC, false>(ys, UP, m0 + m, g, c), wf);
+        uw[m] = O::template ss<3>(uw[m], um, df);
+      };
+      if constexpr (MR < 4) {
+        const auto wf = terms_t<BF, DK, true>(w0s, WP, ct, g, c);
+        const auto df = terms_t<BF, DK, true>(dws, WP, ct, g, c);
+#pragma unroll
+        for (int m = 0; m < MR; ++m) products(m, wf, df, terms_t<BF, kDC, false>(us, UP, m0 + m, g, c));
+      }
+      const auto doi = LV::frag(dos, i, 0, g);
+      const auto yi = terms_t<BF, kDC, false>(ys, UP, rt, g, c);
+      if (xb0 == 0 && i < nt && v0 + 8 * g < a.dv) {          // dV = eta Y, eight channels a lane
+        f32x4 y0, y1;
+        O::sum(yi, y0, y1);
+        E* p = row_of_w<E>(a.dv_, b, h, t0) + i * ost + v0 + 8 * g;
+        IoT<BF>::st4(p, y0 * gl[kGEta + i]);
+        IoT<BF>::st4(p + 4, y1 * gl[kGEta + i]);
+      }
+      auto pairs = [&](int n, int y, const auto& uj) {
+        du[n][y] = O::template sx<3>(du[n][y], uj, doi);
+        yu[n][y] = O::template ss<3>(yu[n][y], uj, yi);
+      };
+      if constexpr (MR < 4) {
+#pragma unroll
+        for (int n = 0; n < NB; ++n)
+          if (xb0 + n <= rt / 2) {
+            pairs(n, 0, terms_t<BF, kDC, false>(us, UP, 2 * (xb0 + n), g, c));
+            pairs(n, 1, terms_t<BF, kDC, false>(us, UP, 2 * (xb0 + n) + 1, g, c));
+          }
+      } else {                               // (both take every row tile of U: read once)
         const auto wf = terms_t<BF, DK, true>(w0s, WP, ct, g, c);
         const auto df = terms_t<BF, DK, true>(dws, WP, ct, g, c);
 #pragma unroll
         for (int m = 0; m < MR; ++m) {
-          ow[m] = O::template xs<3>(ow[m], LV::frag(dos, lab(m0 + m, c), 0, g), wf);
-          yw[m] = O::template ss<3>(yw[m], terms_t<BF, kDC, false>(ys, UP, m0 + m, g, c), wf);
-          uw[m] = O::template ss<3>(uw[m], terms_t<BF, kDC, false>(us, UP, m0 + m, g, c), df);
+          const auto um = terms_t<BF, kDC, false>(us, UP, m, g, c);
+          products(m, wf, df, um);
+          if (m / 2 <= rt / 2 && (NB == 2 || m / 2 == xb0)) pairs(NB == 2 ? m / 2 : 0, m % 2, um);
         }
-      }
-      {
-        const auto doi = LV::frag(dos, i, 0, g);
-        const auto yi = terms_t<BF, kDC, false>(ys, UP, rt, g, c);
-        if (xb0 == 0 && i < nt && v0 + 8 * g < a.dv) {   // dV = eta Y, eight channels a lane
-          f32x4 y0, y1;
-          O::sum(yi, y0, y1);
-          E* p = row_of_w<E>(a.dv_, b, h, t0) + i * ost + v0 + 8 * g;
-          IoT<BF>::st4(p, y0 * gl[kGEta + i]);
-          IoT<BF>::st4(p + 4, y1 * gl[kGEta + i]);
-        }
-#pragma unroll
-        for (int n = 0; n < NB; ++n)
-          if (xb0 + n <= rt / 2) {
-#pragma unroll
-            for (int y = 0; y < 2; ++y) {
-              const auto uj = terms_t<BF, kDC, false>(us, UP, 2 * (xb0 + n) + y, g, c);
-              du[n][y] = O::template sx<3>(du[n][y], uj, doi);
-              yu[n][y] = O::template ss<3>(yu[n][y], uj, yi);
-            }
-          }
       }
     }
     __syncthreads();                         // the value blocks are done: buf holds A and N
