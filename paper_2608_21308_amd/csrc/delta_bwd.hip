@@ -30,6 +30,7 @@ __device__ __forceinline__ void bwd_chain(const DeltaArgs& a, int nsl, long blk,
   using E = typename O::E;
   using L = LTile<BF, DK>;
   using LV = LTile<BF, 16 * NW>;
+  constexpr unsigned ES = sizeof(E);
   constexpr int NTH = 64 * NW, KT = DK / 32, MT = DK / 16;
   constexpr int PK = kDC * L::NP / NTH, PV = kDC * LV::NP / NTH;
   constexpr int NF = (tri_bytes(BF, 3) + tri_bytes(BF, 3)) / 16;   // pieces of T and P
@@ -49,15 +50,16 @@ __device__ __forceinline__ void bwd_chain(const DeltaArgs& a, int nsl, long blk,
   const long U = (long)a.B * a.H;
   const long us = (blk / (8 * nsl)) * 8 + blk % 8;       // (unit, segment)
   if (us >= U * a.nseg) return;
-  const long u = us / a.nseg;
-  const int seg = (int)(us % a.nseg);
+  const int u = __builtin_amdgcn_readfirstlane((int)(us / a.nseg));
+  const int seg = __builtin_amdgcn_readfirstlane((int)(us % a.nseg));
   if (STATE && seg == 0) return;
   const int sl = (int)((blk / 8) % nsl);
-  const int b = (int)(u / a.H), h = (int)(u % a.H), hk = h / (a.H / a.HK);
+  const int b = u / a.H, h = u % a.H, hk = h / (a.H / a.HK);
   const int nlive = live_tokens(a, b);
   const int r0 = a.r0 + seg * a.seglen;                  // (up to the sequence's last chunk)
   const int r1 = min(min(a.r1, r0 + a.seglen), (nlive + kDC - 1) / kDC);
   const int sc0 = sl * NW * 16, col = sc0 + 16 * w + c, tile = sl * NW + w;
+  const unsigned sat = tile < a.dvp / 16 ? 0 : kNowhere;   // (no stores behind the value channels)
   const int krow = tid / L::NP, kcol = (tid % L::NP) * L::PE;
   const int vrow = tid / LV::NP, vcol = (tid % LV::NP) * LV::PE;
   const bool kok = kcol < a.dk, vok = sc0 + vcol < a.dv;
@@ -74,47 +76,38 @@ __device__ __forceinline__ void bwd_chain(const DeltaArgs& a, int nsl, long blk,
         st[m] = *reinterpret_cast<const f32x4*>(a.segs + us * a.dvp * DK +
                                                 lane_at(tile, m / 2, KT, lane) + 256 * (m & 1));
     } else if (a.d_w_out && col < a.dv && kc < a.dk) {
-      st[m] = *reinterpret_cast<const f32x4*>(a.d_w_out + (u * a.dv + col) * a.dk + kc);
+      st[m] = *reinterpret_cast<const f32x4*>(a.d_w_out + ((long)u * a.dv + col) * a.dk + kc);
     }
   }
 
   u32x4 rk[PK], rq[PK], rv[PV];
-  u32x4 rf[PF];
-  f32x4 rg;
+  u32x4 rf[PF], rg;
+  // byte offsets within a chunk
+  const unsigned kat = (unsigned)(krow * kst + kcol) * ES, qat = (unsigned)(krow * qst + kcol) * ES;
+  const unsigned vat = (unsigned)(vrow * vst + vcol) * ES;
   auto fetch = [&](int r) {
     const int t0 = r * kDC, nt = nlive - t0;
-    const long cu = u * a.nc_buf + (r - a.r_base);
-    const E* kp = row_of<E>(a.k, b, hk, t0) + kcol;
-    const E* qp = row_of<E>(a.q, b, hk, t0) + kcol;
-    const E* vp = row_of<E>(a.d_out, b, h, t0) + sc0 + vcol;
+    const long cu = (long)u * a.nc_buf + (r - a.r_base);
+    const Buf kb = buf_of(row_of<E>(a.k, b, hk, t0)), qb = buf_of(row_of<E>(a.q, b, hk, t0));
+    const Buf vb = buf_of(row_of<E>(a.d_out, b, h, t0) + sc0);
 #pragma unroll
     for (int x = 0; x < PK; ++x) {
       const int row = krow + x * (NTH / L::NP);
-      rk[x] = rq[x] = u32x4{0, 0, 0, 0};
-      if (kok && row < nt) {
-        rk[x] = *reinterpret_cast<const u32x4*>(kp + row * kst);
-        rq[x] = *reinterpret_cast<const u32x4*>(qp + row * qst);
-      }
+      const unsigned no = kok && row < nt ? 0 : kNowhere;
+      rk[x] = buf_ld(kb, (kat + (unsigned)(x * (NTH / L::NP) * kst) * ES) | no);
+      rq[x] = buf_ld(qb, (qat + (unsigned)(x * (NTH / L::NP) * qst) * ES) | no);
     }
 #pragma unroll
     for (int x = 0; x < PV; ++x) {
-      const int row = vrow + x * (NTH / LV::NP);
-      rv[x] = u32x4{0, 0, 0, 0};
-      if (vok && row < nt) rv[x] = *reinterpret_cast<const u32x4*>(vp + row * vst);
+      const unsigned no = vok && vrow + x * (NTH / LV::NP) < nt ? 0 : kNowhere;
+      rv[x] = buf_ld(vb, (vat + (unsigned)(x * (NTH / LV::NP) * vst) * ES) | no);
     }
-    const u32x4* f = reinterpret_cast<const u32x4*>(
-        a.frag + cu * (tri_bytes(BF, 3) + tri_bytes(BF, a.pterms)));
+    const Buf fb = buf_of(a.frag + cu * (tri_bytes(BF, 3) + tri_bytes(BF, a.pterms)));
 #pragma unroll
-    for (int x = 0; x < PF; ++x)
-      rf[x] = f[min(tid + x * NTH, NF - 1)];             // (the last piece by several)
-    if (tid < kGateChain / 4)
-      rg = *reinterpret_cast<const f32x4*>(a.gate + cu * kGateFloats + 4 * tid);
+    for (int x = 0; x < PF; ++x) rf[x] = buf_ld(fb, 16 * min(tid + x * NTH, NF - 1));   // (the last piece by several)
+    rg = buf_ld(buf_of(a.gate + cu * kGateFloats), 16 * min(tid, kGateChain / 4 - 1));
   };
-  if (r0 < r1) fetch(r1 - 1);
-
-  for (int r = r1 - 1; r >= r0; --r) {
-    const long cu = u * a.nc_buf + (r - a.r_base);
-    __syncthreads();
+  auto stage = [&]() {
 #pragma unroll
     for (int x = 0; x < PK; ++x) {
       const int at = L::at(krow + x * (NTH / L::NP), tid % L::NP);
@@ -127,17 +120,28 @@ __device__ __forceinline__ void bwd_chain(const DeltaArgs& a, int nsl, long blk,
 #pragma unroll
     for (int x = 0; x < PF; ++x)
       reinterpret_cast<u32x4*>(ts)[min(tid + x * NTH, NF - 1)] = rf[x];
-    if (tid < kGateChain / 4) *reinterpret_cast<f32x4*>(gl + 4 * tid) = rg;
+    if (tid < kGateChain / 4) *reinterpret_cast<u32x4*>(gl + 4 * tid) = rg;
+  };
+  if (r0 < r1) {
+    fetch(r1 - 1);
+    stage();
+  }
+
+  for (int r = r1 - 1; r >= r0; --r) {
+    const long cu = (long)u * a.nc_buf + (r - a.r_base);
     __syncthreads();
     if (r > r0) fetch(r - 1);
 
+    const Buf wb = buf_of(a.dwst + cu * a.dvp * DK), yb = buf_of(a.yst + cu * a.dvp * kDC);
     typename O::S sb[KT];
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt) {
       sb[kt] = O::template split<3>(st[2 * kt], st[2 * kt + 1]);
-      if (!STATE && col < a.dvp)
-        st_lane(a.dwst + cu * a.dvp * DK + lane_at(tile, kt, KT, lane), st[2 * kt],
-                st[2 * kt + 1]);
+      if constexpr (!STATE) {
+        const unsigned at = sat + 4 * (unsigned)lane_at(tile, kt, KT, lane);
+        buf_st(wb, at, st[2 * kt]);
+        buf_st(wb, at + 1024, st[2 * kt + 1]);
+      }
     }
     f32x4 xa[4];
 #pragma unroll
@@ -190,9 +194,11 @@ __device__ __forceinline__ void bwd_chain(const DeltaArgs& a, int nsl, long blk,
     }
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
-      if (!STATE && col < a.dvp)
-        st_lane(a.yst + cu * a.dvp * kDC + lane_at(tile, x, 2, lane), xa[2 * x],
-                xa[2 * x + 1]);
+      if constexpr (!STATE) {
+        const unsigned at = sat + 4 * (unsigned)lane_at(tile, x, 2, lane);
+        buf_st(yb, at, xa[2 * x]);
+        buf_st(yb, at + 1024, xa[2 * x + 1]);
+      }
       const float* gp = gl + kGEtaG + 32 * x + 8 * g;
       rb[x] = O::template split<3>(xa[2 * x] * -*reinterpret_cast<const f32x4*>(gp),
                                    xa[2 * x + 1] * -*reinterpret_cast<const f32x4*>(gp + 4));
@@ -203,6 +209,10 @@ __device__ __forceinline__ void bwd_chain(const DeltaArgs& a, int nsl, long blk,
       for (int x = 0; x < 2; ++x)
         O::template xs2<3>(st[m], L::template frag_t<false>(ks, m, x, g, c), rb[x], st[m + 1],
                            L::template frag_t<false>(ks, m + 1, x, g, c), rb[x]);
+    if (r > r0) {
+      __syncthreads();                       // (the chunk in LDS is done with)
+      stage();
+    }
   }
 
   if constexpr (STATE) {
@@ -218,7 +228,7 @@ __device__ __forceinline__ void bwd_chain(const DeltaArgs& a, int nsl, long blk,
     for (int m = 0; m < MT; ++m) {
       const int kc = lab(m, 4 * g);
       if (col < a.dv && kc < a.dk)
-        *reinterpret_cast<f32x4*>(a.d_w_in + (u * a.dv + col) * a.dk + kc) = st[m];
+        *reinterpret_cast<f32x4*>(a.d_w_in + ((long)u * a.dv + col) * a.dk + kc) = st[m];
     }
   }
 }

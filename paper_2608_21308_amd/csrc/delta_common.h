@@ -464,6 +464,33 @@ __device__ __forceinline__ int live_tokens(const DeltaArgs& a, int b) {
   return a.lengths ? max(0, min(a.T, a.lengths[b])) : a.T;
 }
 
+// Memory from a uniform address on, addressed by byte offsets of 31 bits; an
+// access at kNowhere or behind it is dropped (reads zero).  A masked lane then
+// needs no branch, and without branches between them the compiler knows how many
+// stores are younger than a load: waiting for it does not wait for them.
+typedef __amdgpu_buffer_rsrc_t Buf;
+constexpr unsigned kNowhere = 0x80000000u;
+__device__ __forceinline__ Buf buf_of(const void* p) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, 0x7fffffff, 0x00020000);
+}
+__device__ __forceinline__ u32x4 buf_ld(Buf b, unsigned at) {
+  return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(b, (int)at, 0, 0));
+}
+__device__ __forceinline__ void buf_st(Buf b, unsigned at, f32x4 x) {
+  __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, x), b, (int)at, 0, 0);
+}
+// Four neighbouring values of the io type, streaming.
+template <bool BF>
+__device__ __forceinline__ void buf_st_io(Buf b, unsigned at, f32x4 x) {
+  typedef __attribute__((ext_vector_type(2))) unsigned u32x2;
+  if constexpr (BF)
+    __builtin_amdgcn_raw_buffer_store_b64(
+        __builtin_bit_cast(u32x2, bf16x4{(__bf16)x[0], (__bf16)x[1], (__bf16)x[2], (__bf16)x[3]}), b,
+        (int)at, 0, 2);
+  else
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, x), b, (int)at, 0, 2);
+}
+
 struct DeltaStepArgs {
   View q, k, v, eta, gam, out;
   float* w;

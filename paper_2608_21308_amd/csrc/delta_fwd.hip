@@ -48,6 +48,7 @@ __device__ __forceinline__ void fwd_chain(const DeltaArgs& a, int nsl, long blk,
   using E = typename O::E;
   using L = LTile<BF, DK>;
   using LV = LTile<BF, 16 * NW>;
+  constexpr unsigned ES = sizeof(E);
   constexpr int NTH = 64 * NW, KT = DK / 32, MT = DK / 16;
   constexpr int PK = kDC * L::NP / NTH;                 // a thread's pieces of K (Q) rows
   constexpr int PV = kDC * LV::NP / NTH;                // and of V rows
@@ -69,18 +70,19 @@ __device__ __forceinline__ void fwd_chain(const DeltaArgs& a, int nsl, long blk,
   const long U = (long)a.B * a.H;
   const long us = (blk / (8 * nsl)) * 8 + blk % 8;       // (unit, segment)
   if (us >= U * a.nseg) return;
-  const long u = us / a.nseg;
-  const int seg = (int)(us % a.nseg);
+  const int u = __builtin_amdgcn_readfirstlane((int)(us / a.nseg));
+  const int seg = __builtin_amdgcn_readfirstlane((int)(us % a.nseg));
   const int r0 = a.r0 + seg * a.seglen, r1 = min(a.r1, r0 + a.seglen);
   const int sl = (int)((blk / 8) % nsl);
   // (nothing starts behind the last segment; the backward wants its transition)
   if (MODE == kState && seg == a.nseg - 1 && (a.pterms == 2 || (sl + 1) * NW <= a.dvp / 16)) return;
-  const int b = (int)(u / a.H), h = (int)(u % a.H), hk = h / (a.H / a.HK);
+  const int b = u / a.H, h = u % a.H, hk = h / (a.H / a.HK);
   const int nlive = live_tokens(a, b);
   const int rl = min(r1, (nlive + kDC - 1) / kDC);       // chunks up to the sequence's end (zeros behind)
   const int sc0 = sl * NW * 16;                          // the workgroup's first column
   const int col = sc0 + 16 * w + c;                      // the lane's
   const int tile = sl * NW + w, nvt = a.dvp / 16;        // the wave's tile: of B, or behind them of F
+  const unsigned sat = tile < a.dvp / 16 ? 0 : kNowhere;   // (no stores behind the value channels)
   // thread offsets within a chunk (32 bits: rows are at most 2^23 elements apart)
   const int krow = tid / L::NP, kcol = (tid % L::NP) * L::PE;
   const int vrow = tid / LV::NP, vcol = (tid % LV::NP) * LV::PE;
@@ -100,48 +102,38 @@ __device__ __forceinline__ void fwd_chain(const DeltaArgs& a, int nsl, long blk,
         st[m] = *reinterpret_cast<const f32x4*>(a.segs + us * a.dvp * DK +
                                                 lane_at(tile, m / 2, KT, lane) + 256 * (m & 1));
     } else if (a.w_in && col < a.dv && kc < a.dk) {
-      st[m] = *reinterpret_cast<const f32x4*>(a.w_in + (u * a.dv + col) * a.dk + kc);
+      st[m] = *reinterpret_cast<const f32x4*>(a.w_in + ((long)u * a.dv + col) * a.dk + kc);
     }
   }
 
   u32x4 rk[PK], rq[PK], rv[PV];
-  u32x4 rf[PF];
-  f32x4 rg;
+  u32x4 rf[PF], rg;
+  // byte offsets within a chunk
+  const unsigned kat = (unsigned)(krow * kst + kcol) * ES, qat = (unsigned)(krow * qst + kcol) * ES;
+  const unsigned vat = (unsigned)(vrow * vst + vcol) * ES;
   auto fetch = [&](int r) {
     const int t0 = r * kDC, nt = nlive - t0;
-    const long cu = u * a.nc_buf + (r - a.r_base);
-    const E* kp = row_of<E>(a.k, b, hk, t0) + kcol;
-    const E* qp = row_of<E>(a.q, b, hk, t0) + kcol;
-    const E* vp = row_of<E>(a.v, b, h, t0) + sc0 + vcol;
+    const long cu = (long)u * a.nc_buf + (r - a.r_base);
+    const Buf kb = buf_of(row_of<E>(a.k, b, hk, t0)), qb = buf_of(row_of<E>(a.q, b, hk, t0));
+    const Buf vb = buf_of(row_of<E>(a.v, b, h, t0) + sc0);
 #pragma unroll
     for (int x = 0; x < PK; ++x) {
       const int row = krow + x * (NTH / L::NP);
-      rk[x] = rq[x] = u32x4{0, 0, 0, 0};
-      if (kok && row < nt) {
-        rk[x] = *reinterpret_cast<const u32x4*>(kp + row * kst);
-        if constexpr (OUT) rq[x] = *reinterpret_cast<const u32x4*>(qp + row * qst);
-      }
+      const unsigned no = kok && row < nt ? 0 : kNowhere;
+      rk[x] = buf_ld(kb, (kat + (unsigned)(x * (NTH / L::NP) * kst) * ES) | no);
+      if constexpr (OUT) rq[x] = buf_ld(qb, (qat + (unsigned)(x * (NTH / L::NP) * qst) * ES) | no);
     }
 #pragma unroll
     for (int x = 0; x < PV; ++x) {
-      const int row = vrow + x * (NTH / LV::NP);
-      rv[x] = u32x4{0, 0, 0, 0};
-      if (vok && row < nt) rv[x] = *reinterpret_cast<const u32x4*>(vp + row * vst);
+      const unsigned no = vok && vrow + x * (NTH / LV::NP) < nt ? 0 : kNowhere;
+      rv[x] = buf_ld(vb, (vat + (unsigned)(x * (NTH / LV::NP) * vst) * ES) | no);
     }
-    const u32x4* f = reinterpret_cast<const u32x4*>(
-        a.frag + cu * (tri_bytes(BF, 3) + tri_bytes(BF, a.pterms)));
+    const Buf fb = buf_of(a.frag + cu * (tri_bytes(BF, 3) + tri_bytes(BF, a.pterms)));
 #pragma unroll
-    for (int x = 0; x < PF; ++x)
-      rf[x] = f[min(tid + x * NTH, NF - 1)];             // (the last piece by several)
-    if (tid < kGateChain / 4)
-      rg = *reinterpret_cast<const f32x4*>(a.gate + cu * kGateFloats + 4 * tid);
+    for (int x = 0; x < PF; ++x) rf[x] = buf_ld(fb, 16 * min(tid + x * NTH, NF - 1));   // (the last piece by several)
+    rg = buf_ld(buf_of(a.gate + cu * kGateFloats), 16 * min(tid, kGateChain / 4 - 1));
   };
-  if (r0 < rl) fetch(r0);
-
-  for (int r = r0; r < rl; ++r) {
-    const int t0 = r * kDC;
-    const long cu = u * a.nc_buf + (r - a.r_base);
-    __syncthreads();
+  auto stage = [&]() {
 #pragma unroll
     for (int x = 0; x < PK; ++x) {
       const int at = L::at(krow + x * (NTH / L::NP), tid % L::NP);
@@ -154,10 +146,20 @@ __device__ __forceinline__ void fwd_chain(const DeltaArgs& a, int nsl, long blk,
 #pragma unroll
     for (int x = 0; x < PF; ++x)
       reinterpret_cast<u32x4*>(ts)[min(tid + x * NTH, NF - 1)] = rf[x];
-    if (tid < kGateChain / 4) *reinterpret_cast<f32x4*>(gl + 4 * tid) = rg;
+    if (tid < kGateChain / 4) *reinterpret_cast<u32x4*>(gl + 4 * tid) = rg;
+  };
+  if (r0 < rl) {
+    fetch(r0);
+    stage();
+  }
+
+  for (int r = r0; r < rl; ++r) {
+    const int t0 = r * kDC;
+    const long cu = (long)u * a.nc_buf + (r - a.r_base);
     __syncthreads();
     if (r + 1 < rl) fetch(r + 1);
 
+    const Buf wb = buf_of(a.wst + cu * a.dvp * DK), ub_ = buf_of(a.ust + cu * a.dvp * kDC);
     // X, per 32 columns of the state
     typename O::S sb[KT];
     f32x4 xa[4], oa[4], ua[4];
@@ -167,8 +169,9 @@ __device__ __forceinline__ void fwd_chain(const DeltaArgs& a, int nsl, long blk,
     for (int kt = 0; kt < KT; ++kt) {
       sb[kt] = O::template split<3>(st[2 * kt], st[2 * kt + 1]);
       if constexpr (SAVE) {
-        if (col < a.dvp)
-          st_lane(a.wst + cu * a.dvp * DK + lane_at(tile, kt, KT, lane), st[2 * kt], st[2 * kt + 1]);
+        const unsigned at = sat + 4 * (unsigned)lane_at(tile, kt, KT, lane);
+        buf_st(wb, at, st[2 * kt]);
+        buf_st(wb, at + 1024, st[2 * kt + 1]);
       }
 #pragma unroll
       for (int m = 0; m < 4; m += 2)
@@ -212,8 +215,9 @@ __device__ __forceinline__ void fwd_chain(const DeltaArgs& a, int nsl, long blk,
         O::template ss2<3>(ua[2 * x], ld_frag<BF, 3>(ts, fidx(2 * x, y), lane), rb[y], ua[2 * x + 1],
                            ld_frag<BF, 3>(ts, fidx(2 * x + 1, y), lane), rb[y]);
       if constexpr (SAVE) {
-        if (col < a.dvp)
-          st_lane(a.ust + cu * a.dvp * kDC + lane_at(tile, x, 2, lane), ua[2 * x], ua[2 * x + 1]);
+        const unsigned at = sat + 4 * (unsigned)lane_at(tile, x, 2, lane);
+        buf_st(ub_, at, ua[2 * x]);
+        buf_st(ub_, at + 1024, ua[2 * x + 1]);
       }
       const f32x4 n0 = *reinterpret_cast<const f32x4*>(gl + kGEnd + 32 * x + 8 * g);
       const f32x4 n1 = *reinterpret_cast<const f32x4*>(gl + kGEnd + 32 * x + 8 * g + 4);
@@ -225,7 +229,7 @@ __device__ __forceinline__ void fwd_chain(const DeltaArgs& a, int nsl, long blk,
                            L::template frag_t<false>(ks, m + 1, x, g, c), ue[x]);
     }
     if constexpr (OUT) {
-    E* op = row_of_w<E>(a.out, b, h, t0) + sc0 + 16 * w + 4 * g;
+    const Buf ob = buf_of(row_of<E>(a.out, b, h, t0) + sc0);
 #pragma unroll
     for (int m = 0; m < 4; ++m) {
       if (m % 2 == 0) {
@@ -234,9 +238,13 @@ __device__ __forceinline__ void fwd_chain(const DeltaArgs& a, int nsl, long blk,
           O::template ss2<2>(oa[m], ub[x], ld_frag<BF, 2>(ps, fidx(m, x), lane), oa[m + 1], ub[x],
                              ld_frag<BF, 2>(ps, fidx(m + 1, x), lane));
       }
-      if (sc0 + 16 * w + 4 * g < a.dv && t0 + lab(m, c) < nlive)
-        IoT<BF>::st4(op + lab(m, c) * ost, oa[m]);
+      const unsigned no = sc0 + 16 * w + 4 * g < a.dv && t0 + lab(m, c) < nlive ? 0 : kNowhere;
+      buf_st_io<BF>(ob, (unsigned)(lab(m, c) * ost + 16 * w + 4 * g) * ES | no, oa[m]);
     }
+    }
+    if (r + 1 < rl) {
+      __syncthreads();                       // (the chunk in LDS is done with)
+      stage();
     }
   }
 
@@ -269,7 +277,7 @@ __device__ __forceinline__ void fwd_chain(const DeltaArgs& a, int nsl, long blk,
     for (int m = 0; m < MT; ++m) {
       const int kc = lab(m, 4 * g);
       if (col < a.dv && kc < a.dk)
-        *reinterpret_cast<f32x4*>(a.w_out + (u * a.dv + col) * a.dk + kc) = st[m];
+        *reinterpret_cast<f32x4*>(a.w_out + ((long)u * a.dv + col) * a.dk + kc) = st[m];
     }
   }
 }
