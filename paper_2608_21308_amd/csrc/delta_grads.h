@@ -21,7 +21,7 @@
 // waves up to DK = 64, so that two workgroups share a CU and one computes while
 // the other waits; eight, and one workgroup a CU, at 128.
 //
-// 16384 chunks of dk = dv = 64 (112 KB each) take 580 us, 3.2 TB/s: the waves wait
+// 16384 chunks of dk = dv = 64 (112 KB each) take 570 us, 3.2 TB/s: the waves wait
 // for 40 % of it, for the next block and for each other, and issue vector
 // instructions for half, a third of them to split fp32 values into terms (the
 // registers and the 77 KB of LDS leave two workgroups a CU).  8192 of 128: 790 us.
@@ -101,9 +101,9 @@ __device__ __forceinline__ void grads_chunk(const DeltaArgs& a, int c0, int nr, 
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, c = lane & 15;
   const int w = wave_id();
   const int rep = ONE ? 1 : a.H / a.HK;
-  const long bh = blk / nr;
-  const int r = c0 + (int)(blk % nr);
-  const int b = (int)(bh / a.HK), hk = (int)(bh % a.HK);
+  const int bh = __builtin_amdgcn_readfirstlane((int)(blk / nr));
+  const int r = __builtin_amdgcn_readfirstlane(c0 + (int)(blk % nr));
+  const int b = bh / a.HK, hk = bh % a.HK;
   const int t0 = r * kDC, nt = min(kDC, max(0, live_tokens(a, b) - t0));
   const int kst = (int)a.k.t, qst = (int)a.q.t, gst = (int)a.d_out.t, ost = (int)a.dv_.t;
 
@@ -128,37 +128,34 @@ __device__ __forceinline__ void grads_chunk(const DeltaArgs& a, int c0, int nr, 
   }
 
   // the next value block on its way: v0 of value head h (chunk unit cu)
-  f32x4 rw[PW][4], ru[PU][2];
-  u32x4 ro[PO];
+  u32x4 rw[PW][4], ru[PU][2], ro[PO];
   auto fetch = [&](int h, long cu, int v0) {
-    const float* w0g = a.wst + (cu * a.dvp + v0) * DK;
-    const float* dwg = a.dwst + (cu * a.dvp + v0) * DK;
-    const float* ug = a.ust + (cu * a.dvp + v0) * kDC;
-    const float* yg = a.yst + (cu * a.dvp + v0) * kDC;
+    const Buf w0b = buf_of(a.wst + (cu * a.dvp + v0) * DK), dwb = buf_of(a.dwst + (cu * a.dvp + v0) * DK);
+    const Buf ub = buf_of(a.ust + (cu * a.dvp + v0) * kDC), yb = buf_of(a.yst + (cu * a.dvp + v0) * kDC);
 #pragma unroll
     for (int x = 0; x < PW; ++x) {           // a wave takes 16 rows x 32 columns
       const int p = tid + x * NTH;
-      if (WP / 8 % NTH == 0 || p < WP / 8) {
-        const long at = lane_at(p / (64 * KT), (p >> 6) % KT, KT, lane);
-        rw[x][0] = *reinterpret_cast<const f32x4*>(w0g + at);
-        rw[x][1] = *reinterpret_cast<const f32x4*>(w0g + at + 256);
-        rw[x][2] = *reinterpret_cast<const f32x4*>(dwg + at);
-        rw[x][3] = *reinterpret_cast<const f32x4*>(dwg + at + 256);
-      }
+      const unsigned no = WP / 8 % NTH == 0 || p < WP / 8 ? 0 : kNowhere;
+      const unsigned at = 4 * (unsigned)lane_at(p / (64 * KT), (p >> 6) % KT, KT, lane) | no;
+      rw[x][0] = buf_ld(w0b, at);
+      rw[x][1] = buf_ld(w0b, at + 1024);
+      rw[x][2] = buf_ld(dwb, at);
+      rw[x][3] = buf_ld(dwb, at + 1024);
     }
 #pragma unroll
-    for (int x = 0; x < PU; ++x) {
+    for (int x = 0; x < PU; ++x) {           // (256 pieces of U, then of Y: a wave's are of one)
       const int p = tid + x * NTH;
-      const float* src = (p >> 8 ? yg : ug) + lane_at((p >> 7) & 1, (p >> 6) & 1, 2, lane);
-      ru[x][0] = *reinterpret_cast<const f32x4*>(src);
-      ru[x][1] = *reinterpret_cast<const f32x4*>(src + 256);
+      const unsigned at = 4 * (unsigned)lane_at((p >> 7) & 1, (p >> 6) & 1, 2, lane);
+      const bool y = 4 * x * NWV >= 16 || (NWV > 4 && w >= 4);
+      ru[x][0] = buf_ld(y ? yb : ub, at);
+      ru[x][1] = buf_ld(y ? yb : ub, at + 1024);
     }
-    const E* dop = row_of<E>(a.d_out, b, h, t0);
+    const Buf ob = buf_of(row_of<E>(a.d_out, b, h, t0) + v0);
 #pragma unroll
     for (int x = 0; x < PO; ++x) {
-      const int p = tid + x * NTH, row = p / LV::NP, col = v0 + (p % LV::NP) * LV::PE;
-      ro[x] = u32x4{0, 0, 0, 0};
-      if (row < nt && col < a.dv) ro[x] = *reinterpret_cast<const u32x4*>(dop + row * gst + col);
+      const int p = tid + x * NTH, row = p / LV::NP, col = (p % LV::NP) * LV::PE;
+      const unsigned no = row < nt && v0 + col < a.dv ? 0 : kNowhere;
+      ro[x] = buf_ld(ob, (unsigned)(row * gst + col) * (unsigned)sizeof(E) | no);
     }
   };
   {
@@ -204,26 +201,26 @@ __device__ __forceinline__ void grads_chunk(const DeltaArgs& a, int c0, int nr, 
     for (int n = 0; n < NB; ++n) du[n][0] = du[n][1] = yu[n][0] = yu[n][1] = zero4();
 #pragma unroll
     for (int m = 0; m < MR; ++m) ow[m] = yw[m] = uw[m] = zero4();
-    for (int v0 = 0; v0 < a.dvp; v0 += 32) {
+    auto stage = [&]() {
       E2TTT_LANE_IDS;                        // (addresses formed here, not kept in registers)
-      const int i = lab(rt, c);
-      if (v0) __syncthreads();
 #pragma unroll
       for (int x = 0; x < PW; ++x) {
         const int p = tid + x * NTH, row = 16 * (p / (64 * KT)) + c, p8 = 4 * ((p >> 6) % KT) + g;
         if (WP / 8 % NTH == 0 || p < WP / 8) {
-          put_terms<BF, DK>(w0s, WP, row, p8, rw[x][0], rw[x][1]);
-          put_terms<BF, DK>(dws, WP, row, p8, rw[x][2], rw[x][3]);
+          f32x4 v[4];
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            wdot = fmaf(rw[x][0][e], rw[x][2][e], fmaf(rw[x][1][e], rw[x][3][e], wdot));
+          for (int k = 0; k < 4; ++k) v[k] = __builtin_bit_cast(f32x4, rw[x][k]);
+          put_terms<BF, DK>(w0s, WP, row, p8, v[0], v[1]);
+          put_terms<BF, DK>(dws, WP, row, p8, v[2], v[3]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) wdot = fmaf(v[0][e], v[2][e], fmaf(v[1][e], v[3][e], wdot));
         }
       }
 #pragma unroll
       for (int x = 0; x < PU; ++x) {
         const int p = tid + x * NTH;
         put_terms<BF, kDC>(p >> 8 ? ys : us, UP, 16 * ((p >> 7) & 1) + c, 4 * ((p >> 6) & 1) + g,
-                           ru[x][0], ru[x][1]);
+                           __builtin_bit_cast(f32x4, ru[x][0]), __builtin_bit_cast(f32x4, ru[x][1]));
       }
 #pragma unroll
       for (int x = 0; x < PO; ++x) {
@@ -231,6 +228,11 @@ __device__ __forceinline__ void grads_chunk(const DeltaArgs& a, int c0, int nr, 
         if (kDC * LV::NP % NTH == 0 || p < kDC * LV::NP)
           *reinterpret_cast<u32x4*>(dos + LV::at(p / LV::NP, p % LV::NP)) = ro[x];
       }
+    };
+    stage();
+    for (int v0 = 0; v0 < a.dvp; v0 += 32) {
+      E2TTT_LANE_IDS;
+      const int i = lab(rt, c);
       __syncthreads();
       if (v0 + 32 < a.dvp)
         fetch(h, cu, v0 + 32);
@@ -249,12 +251,14 @@ __device__ __forceinline__ void grads_chunk(const DeltaArgs& a, int c0, int nr, 
       }
       const auto doi = LV::frag(dos, i, 0, g);
       const auto yi = terms_t<BF, kDC, false>(ys, UP, rt, g, c);
-      if (xb0 == 0 && i < nt && v0 + 8 * g < a.dv) {          // dV = eta Y, eight channels a lane
+      if (xb0 == 0) {                        // dV = eta Y, eight channels a lane
         f32x4 y0, y1;
         O::sum(yi, y0, y1);
-        E* p = row_of_w<E>(a.dv_, b, h, t0) + i * ost + v0 + 8 * g;
-        IoT<BF>::st4(p, y0 * gl[kGEta + i]);
-        IoT<BF>::st4(p + 4, y1 * gl[kGEta + i]);
+        const Buf vb = buf_of(row_of<E>(a.dv_, b, h, t0) + v0);
+        const unsigned no = i < nt && v0 + 8 * g < a.dv ? 0 : kNowhere;
+        const unsigned at = (unsigned)(i * ost + 8 * g) * (unsigned)sizeof(E) | no;
+        buf_st_io<BF>(vb, at, y0 * gl[kGEta + i]);
+        buf_st_io<BF>(vb, at + 4 * (unsigned)sizeof(E), y1 * gl[kGEta + i]);
       }
       auto pairs = [&](int n, int y, const auto& uj) {
         du[n][y] = O::template sx<3>(du[n][y], uj, doi);
@@ -276,6 +280,10 @@ __device__ __forceinline__ void grads_chunk(const DeltaArgs& a, int c0, int nr, 
           products(m, wf, df, um);
           if (m / 2 <= rt / 2 && (NB == 2 || m / 2 == xb0)) pairs(NB == 2 ? m / 2 : 0, m % 2, um);
         }
+      }
+      if (v0 + 32 < a.dvp) {
+        __syncthreads();                     // (the block in LDS is done with)
+        stage();
       }
     }
     __syncthreads();                         // the value blocks are done: buf holds A and N
