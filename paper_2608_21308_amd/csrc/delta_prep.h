@@ -59,18 +59,15 @@ __device__ __forceinline__ bool below(int r, int c, int h) {
   return ((r ^ c) & (15 & ~(h - 1))) == h && (r & h);
 }
 
+// Eight values (zeros at kNowhere).
 template <bool BF>
-__device__ __forceinline__ typename DOp<BF>::X ld_row(const typename DOp<BF>::E* p, bool ok) {
+__device__ __forceinline__ typename DOp<BF>::X ld_row(Buf p, unsigned at) {
   typename DOp<BF>::X x;
   if constexpr (BF) {
-    x.v = bf16x8{};
-    if (ok) x.v = *reinterpret_cast<const bf16x8*>(p);
+    x.v = __builtin_bit_cast(bf16x8, buf_ld(p, at));
   } else {
-    x.a = x.b = zero4();
-    if (ok) {
-      x.a = *reinterpret_cast<const f32x4*>(p);
-      x.b = *reinterpret_cast<const f32x4*>(p + 4);
-    }
+    x.a = __builtin_bit_cast(f32x4, buf_ld(p, at));
+    x.b = __builtin_bit_cast(f32x4, buf_ld(p, at + 16));
   }
   return x;
 }
@@ -86,11 +83,11 @@ __device__ __forceinline__ void prep_chunk(const DeltaArgs& a, int r0, int nr, l
   float* am = gl + kGateFloats;     // diag(eta) M, block by block replaced by the unit lower inverse
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, c = lane & 15;
   const int w = wave_id();
-  const long u = blk / nr;
-  const int r = r0 + (int)(blk % nr);
-  const int b = (int)(u / a.H), h = (int)(u % a.H), hk = h / (a.H / a.HK);
+  const int u = __builtin_amdgcn_readfirstlane((int)(blk / nr));
+  const int r = __builtin_amdgcn_readfirstlane(r0 + (int)(blk % nr));
+  const int b = u / a.H, h = u % a.H, hk = h / (a.H / a.HK);
   const int t0 = r * kDC, nt = min(kDC, max(0, live_tokens(a, b) - t0));
-  const long cu = u * a.nc_buf + (r - a.r_base);
+  const long cu = (long)u * a.nc_buf + (r - a.r_base);
   if (nt == 0) return;              // (no kernel reads anything of such a chunk)
 
   if (w == 0) {
@@ -119,16 +116,17 @@ __device__ __forceinline__ void prep_chunk(const DeltaArgs& a, int r0, int nr, l
 
   // rows of the products: i = lab(w, c) (columns of the MFMA tile), columns
   // j = lab(m, .) of tile m (its rows)
-  const E* kp = row_of<E>(a.k, b, hk, 0);
-  const E* qp = row_of<E>(a.q, b, hk, 0);
-  const int i = lab(w, c);
+  const Buf kp = buf_of(row_of<E>(a.k, b, hk, t0)), qp = buf_of(row_of<E>(a.q, b, hk, t0));
+  const int i = lab(w, c), kst = (int)a.k.t, qst = (int)a.q.t;
+  auto at = [&](int row, int st, int col) {   // byte offset of 8 elements of a live row
+    return (unsigned)(row * st + col) * (unsigned)sizeof(E) | (row < nt && col < a.dk ? 0 : kNowhere);
+  };
   typename O::X ki[DK / 32], qi[DK / 32];
 #pragma unroll
   for (int kt = 0; kt < DK / 32; ++kt) {
     const int col = 32 * kt + 8 * g;
-    const bool ok = i < nt && col < a.dk;
-    ki[kt] = ld_row<BF>(kp + (long)(t0 + i) * a.k.t + col, ok);
-    qi[kt] = ld_row<BF>(qp + (long)(t0 + i) * a.q.t + col, ok);
+    ki[kt] = ld_row<BF>(kp, at(i, kst, col));
+    qi[kt] = ld_row<BF>(qp, at(i, qst, col));
   }
   const int na = w / 2 + 1;         // 32-column blocks of this wave's rows
   f32x4 kk[4], qk[4];
@@ -140,7 +138,7 @@ __device__ __forceinline__ void prep_chunk(const DeltaArgs& a, int r0, int nr, l
 #pragma unroll
       for (int kt = 0; kt < DK / 32; ++kt) {
         const int col = 32 * kt + 8 * g;
-        const auto kj = ld_row<BF>(kp + (long)(t0 + j) * a.k.t + col, j < nt && col < a.dk);
+        const auto kj = ld_row<BF>(kp, at(j, kst, col));
         kk[m] = O::xx(kk[m], kj, ki[kt]);
         qk[m] = O::xx(qk[m], kj, qi[kt]);
       }
