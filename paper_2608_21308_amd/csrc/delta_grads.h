@@ -159,17 +159,14 @@ __device__ __forceinline__ void grads_chunk(const DeltaArgs& a, int c0, int nr, 
     }
   };
   {
-    const E* kp = row_of<E>(a.k, b, hk, t0);
-    const E* qp = row_of<E>(a.q, b, hk, t0);
+    const Buf kb = buf_of(row_of<E>(a.k, b, hk, t0)), qb = buf_of(row_of<E>(a.q, b, hk, t0));
     u32x4 rk[PK], rq[PK];
 #pragma unroll
     for (int x = 0; x < PK; ++x) {
       const int p = tid + x * NTH, row = p / L::NP, col = (p % L::NP) * L::PE;
-      rk[x] = rq[x] = u32x4{0, 0, 0, 0};
-      if (row < nt && col < a.dk) {
-        rk[x] = *reinterpret_cast<const u32x4*>(kp + row * kst + col);
-        rq[x] = *reinterpret_cast<const u32x4*>(qp + row * qst + col);
-      }
+      const unsigned no = row < nt && col < a.dk ? 0 : kNowhere;
+      rk[x] = buf_ld(kb, (unsigned)(row * kst + col) * (unsigned)sizeof(E) | no);
+      rq[x] = buf_ld(qb, (unsigned)(row * qst + col) * (unsigned)sizeof(E) | no);
     }
     fetch(hk * rep, ((long)b * a.H + hk * rep) * a.nc_buf + (r - a.r_base), 0);
 #pragma unroll
