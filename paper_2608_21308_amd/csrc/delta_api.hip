@@ -55,12 +55,12 @@ constexpr size_t kCacheBytes = (size_t)128 << 20, kStretchBytes = (size_t)512 <<
 // many times the units fit).  Segments cost a pass over dv + dk channels ahead of
 // the one over dv, so they pay where the units' own workgroups leave more than
 // two thirds of the 256 CUs idle (64 units, 32 chunks: a training step of 128 x 128
-// 588 us against 700, of 32 x 64 233 against 251) and not beyond (128 units of
-// 64 x 64, 64 chunks: 371 us against 315; a step of 128 of 32 x 32: 312 against
-// 289).  n of them take (nch / n) (t_state + t_chain) + n t_join, about 5 us and
-// 1 us: least at n = sqrt(5 nch).  They begin at 8 chunks with bf16 (32 units of
-// 64: 37 us either way, at 6 chunks 34 against 31), at 6 with the slower fp32
-// products (8 units of 64: 41 us against 49).
+// 575 us against 600, of 64 x 64 257 against 298, of 32 x 64 220 against 233) and
+// not beyond (128 units of 64 x 64, 64 chunks: 378 us against 295; a step of 128
+// of 32 x 32: 317 against 282).  n of them take (nch / n) (t_state + t_chain) + n
+// t_join, about 5 us and 1 us: least at n = sqrt(5 nch).  They begin at 8 chunks
+// with bf16 (32 units of 64: 36 us against 37, at 6 chunks 33 against 31), at 6
+// with the slower fp32 products (8 units of 64: 41 us against 51).
 long room(const e2ttt_delta_desc* d, long U) { return 2048 / (U * (delta_dvp(d->dv) / 16)); }
 long segments(const e2ttt_delta_desc* d, long U, long nch) {
   const int nw = delta_dkp(d->dk) > 64 ? 8 : 4;
@@ -72,13 +72,14 @@ long segments(const e2ttt_delta_desc* d, long U, long nch) {
 // Chunks of a part (bf16, dk in 33..64): where the chain's workgroups leave CUs
 // idle but are too many for segments, a launch takes a part of the chain beside
 // the preparation of the next part, in the backward beside the gradients of the
-// part before.  128 units of 64, 64 chunks: 296 us against 322, a training step
-// 845 against 890 (96 units: 692 against 783, of 256 chunks 2.56 ms against 3.12;
-// 192: 1163 us against 1159; 256: 1568 against 1461).  Launches cost some 10 us, so
-// a part has 16 chunks at least (8: 309 us) and there are at most eight.
+// part before.  128 units of 64, 64 chunks: 289 us against 311, a training step
+// 787 against 806 (96 units: 656 against 714, of 256 chunks 2.39 ms against 2.78;
+// 192: 1092 us against 1061).  Launches cost some 10 us, so a part has 16 chunks at
+// least (160 units, 64 chunks: 317 us, with parts of 8 334) and there are at most
+// eight.
 long part_of(const e2ttt_delta_desc* d, long U, long nch, long nseg) {
   const long groups = U * ((delta_dvp(d->dv) + 63) / 64);
-  if (d->io != E2TTT_DT_BF16 || delta_dkp(d->dk) != 64 || nseg > 1 || nch < 32 || groups > 192)
+  if (d->io != E2TTT_DT_BF16 || delta_dkp(d->dk) != 64 || nseg > 1 || nch < 32 || groups > 160)
     return nch;
   return std::max(16L, (nch + 7) / 8);
 }

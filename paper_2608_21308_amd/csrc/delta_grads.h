@@ -21,10 +21,10 @@
 // waves up to DK = 64, so that two workgroups share a CU and one computes while
 // the other waits; eight, and one workgroup a CU, at 128.
 //
-// 16384 chunks of dk = dv = 64 (112 KB each) take 570 us, 3.2 TB/s: the waves wait
+// 16384 chunks of dk = dv = 64 (112 KB each) take 550 us, 3.3 TB/s: the waves wait
 // for 40 % of it, for the next block and for each other, and issue vector
-// instructions for half, a third of them to split fp32 values into terms (the
-// registers and the 77 KB of LDS leave two workgroups a CU).  8192 of 128: 790 us.
+// instructions for half of it (registers and 77 KB of LDS leave two workgroups a
+// CU).  8192 of 128: 770 us.
 #pragma once
 
 #include "delta_common.h"
