@@ -497,3 +497,32 @@ def test_parts(c, lengths, layout):
                         ("eta", "d_eta", "f32"), ("log_gamma", "d_log_gamma", "f32"),
                         ("w_in", "d_w_in", "f32")):
             close(m, g[m][b:b + 1], rg[n], y)
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+def test_far_tokens(io):
+    """Tokens as far apart as they may be (2^23 elements, a chunk's offsets near 31 bits, a
+    sequence's beyond 32) give what contiguous ones give, to the bit."""
+    c, far = (1, 1, 1, 130, 64, 64), 1 << 23
+    x, d = make(*c, io, seed=71)
+    cfg = e2ttt.DeltaConfig(*c, e2ttt.DT_BF16 if io == "bf16" else e2ttt.DT_F32, 0.125)
+    t, td = to_dev(x, io), to_dev(d, io)
+    store = torch.empty(130 * far, dtype=t["q"].dtype, device="cuda")
+    room = iter(range(0, 4096, 64))
+
+    def spread(a=None):
+        o = store.as_strided((1, 1, 130, 64), (130 * far, 130 * far, far, 1), next(room))
+        return o if a is None else o.copy_(a)
+
+    gates = (t["eta"], t["log_gamma"])
+    out, w_out, ws = e2ttt.delta_forward(cfg, t["q"], t["k"], t["v"], *gates, t["w_in"], save_for_backward=True)
+    g = e2ttt.delta_backward(cfg, t["q"], t["k"], t["v"], *gates, ws, td["d_out"], td["d_w_out"])
+    q, k, v, do = [spread(a) for a in (t["q"], t["k"], t["v"], td["d_out"])]
+    far_out, far_w, ws = e2ttt.delta_forward(cfg, q, k, v, *gates, t["w_in"], out=spread(), save_for_backward=True)
+    grads = dict({n: torch.empty_like(a) for n, a in g.items()}, dq=spread(), dk=spread(), dv=spread())
+    e2ttt.delta_backward(cfg, q, k, v, *gates, ws, do, td["d_w_out"], grads=grads)
+    assert torch.equal(far_out, out) and torch.equal(far_w, w_out)
+    for n in g:
+        assert torch.equal(grads[n], g[n]), n
+    with pytest.raises(e2ttt.E2TTTError):
+        e2ttt.delta_forward(cfg, store.as_strided((1, 1, 130, 64), (0, 0, far + 8, 1)), k, v, *gates, t["w_in"])
