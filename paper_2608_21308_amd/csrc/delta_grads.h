@@ -199,7 +199,6 @@ __device__ __forceinline__ void grads_chunk(const DeltaArgs& a, int c0, int nr, 
 #pragma unroll
     for (int m = 0; m < MR; ++m) ow[m] = yw[m] = uw[m] = zero4();
     auto stage = [&]() {
-      E2TTT_LANE_IDS;                        // (addresses formed here, not kept in registers)
 #pragma unroll
       for (int x = 0; x < PW; ++x) {
         const int p = tid + x * NTH, row = 16 * (p / (64 * KT)) + c, p8 = 4 * ((p >> 6) % KT) + g;
@@ -228,7 +227,7 @@ __device__ __forceinline__ void grads_chunk(const DeltaArgs& a, int c0, int nr, 
     };
     stage();
     for (int v0 = 0; v0 < a.dvp; v0 += 32) {
-      E2TTT_LANE_IDS;
+      E2TTT_LANE_IDS;                        // (addresses formed here, not kept in registers)
       const int i = lab(rt, c);
       __syncthreads();
       if (v0 + 32 < a.dvp)
