@@ -365,9 +365,9 @@ e2ttt_status e2ttt_apply_ln(const e2ttt_desc* desc, const float* ln_weight, cons
  * B H up to 1.9 million units (more of dv <= 64) and 10^9 chunks of 64 tokens,
  * 7.8 million to train (else E2TTT_ERR_UNSUPPORTED).
  *
- * Precision: fp32 throughout (with bf16 tensors, fp32 values enter the matrix
- * products as sums of three bf16 numbers, which lose nothing, or of two, to
- * 2^-13 at the worst, where only a bf16 output follows).  Within a chunk of 64 tokens
+ * Precision: fp32 throughout, bf16 outputs rounded once (with bf16 tensors, fp32
+ * values enter the matrix products as sums of three bf16 numbers, which lose
+ * nothing).  Within a chunk of 64 tokens
  * (0..63, 64..127, ...) a token with a non-finite value may make the outputs
  * of its whole chunk non-finite, as it does those after it.
  */

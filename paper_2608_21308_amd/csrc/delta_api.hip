@@ -31,7 +31,6 @@ e2ttt_status check_desc(const e2ttt_delta_desc* d, bool save) {
 struct Plan {
   bool bf;
   long U, NC;
-  int pterms;
   long stretch;                   // chunks of a launch
   long nc_buf;                    // chunks whose gates and fragments are held (all, saving)
   long nseg, seglen;              // segments of a stretch
@@ -91,8 +90,7 @@ Plan plan(const e2ttt_delta_desc* d, bool save) {
   p.NC = ((long)d->T + kDC - 1) / kDC;
   const int dkp = delta_dkp(d->dk), dvp = delta_dvp(d->dv);
   const size_t gate = kGateFloats * sizeof(float);
-  p.pterms = save ? 3 : 2;
-  const size_t frag = tri_bytes(p.bf, 3) + tri_bytes(p.bf, p.pterms);
+  const size_t frag = 2 * tri_bytes(p.bf);
   p.w_bytes = 4L * dkp * dvp;
   p.u_bytes = 4L * kDC * dvp;
   const size_t each = (gate + frag) * (size_t)p.U;
@@ -167,7 +165,6 @@ void fill(DeltaArgs& a, const e2ttt_delta_desc* d, const Plan& p, char* ws) {
   a.scale = d->scale;
   a.gate = reinterpret_cast<float*>(ws + p.o_gate);
   a.frag = ws + p.o_frag;
-  a.pterms = p.pterms;
   a.segs = reinterpret_cast<float*>(ws + p.o_segs);
   a.segb = reinterpret_cast<float*>(ws + p.o_segb);
   a.segf = reinterpret_cast<float*>(ws + p.o_segf);
@@ -211,6 +208,7 @@ extern "C" e2ttt_status e2ttt_delta_forward(const e2ttt_delta_desc* desc,
   char* ws = static_cast<char*>(workspace);
   DeltaArgs a{};
   fill(a, desc, p, ws);
+  a.save = save;
   a.q = view(q, vw.q); a.k = view(k, vw.k); a.v = view(v, vw.v); a.out = view(out, vw.out);
   a.eta = view(eta, vw.eta); a.gam = view(log_gamma, vw.gam);
   a.lengths = lengths;

@@ -20,7 +20,7 @@ template <bool BF, int DK, int NW, bool STATE>
 struct BwdLds {
   static constexpr int e = (int)sizeof(typename DOp<BF>::E), ks = kDC * DK * e;
   static constexpr int qs = ks, vs = qs + (ks), ts = vs + kDC * 16 * NW * e;
-  static constexpr int gl = ts + 2 * tri_bytes(BF, 3), bytes = gl + kGateChain * 4;
+  static constexpr int gl = ts + 2 * tri_bytes(BF), bytes = gl + kGateChain * 4;
 };
 
 // STATE: only the adjoint at every segment's start, from zero at its end.
@@ -33,7 +33,7 @@ __device__ __forceinline__ void bwd_chain(const DeltaArgs& a, int nsl, long blk,
   constexpr unsigned ES = sizeof(E);
   constexpr int NTH = 64 * NW, KT = DK / 32, MT = DK / 16;
   constexpr int PK = kDC * L::NP / NTH, PV = kDC * LV::NP / NTH;
-  constexpr int NF = (tri_bytes(BF, 3) + tri_bytes(BF, 3)) / 16;   // pieces of T and P
+  constexpr int NF = 2 * tri_bytes(BF) / 16;   // pieces of T and P
   constexpr int PF = (NF + NTH - 1) / NTH;
   static_assert(kDC * L::NP % NTH == 0 && NTH % L::NP == 0 && NTH % LV::NP == 0,
                 "whole rounds of pieces");
@@ -44,7 +44,7 @@ __device__ __forceinline__ void bwd_chain(const DeltaArgs& a, int nsl, long blk,
   char* ts = lds + M::ts;                                // T, then P
   float* gl = reinterpret_cast<float*>(lds + M::gl);
 
-  const char* ps = ts + tri_bytes(BF, 3);
+  const char* ps = ts + tri_bytes(BF);
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, c = lane & 15;
   const int w = wave_id();
   const long U = (long)a.B * a.H;
@@ -102,7 +102,7 @@ __device__ __forceinline__ void bwd_chain(const DeltaArgs& a, int nsl, long blk,
       const unsigned no = vok && vrow + x * (NTH / LV::NP) < nt ? 0 : kNowhere;
       rv[x] = buf_ld(vb, (vat + (unsigned)(x * (NTH / LV::NP) * vst) * ES) | no);
     }
-    const Buf fb = buf_of(a.frag + cu * (tri_bytes(BF, 3) + tri_bytes(BF, a.pterms)));
+    const Buf fb = buf_of(a.frag + cu * 2 * tri_bytes(BF));
 #pragma unroll
     for (int x = 0; x < PF; ++x) rf[x] = buf_ld(fb, 16 * min(tid + x * NTH, NF - 1));   // (the last piece by several)
     rg = buf_ld(buf_of(a.gate + cu * kGateFloats), 16 * min(tid, kGateChain / 4 - 1));
@@ -136,7 +136,7 @@ __device__ __forceinline__ void bwd_chain(const DeltaArgs& a, int nsl, long blk,
     typename O::S sb[KT];
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt) {
-      sb[kt] = O::template split<3>(st[2 * kt], st[2 * kt + 1]);
+      sb[kt] = O::split(st[2 * kt], st[2 * kt + 1]);
       if constexpr (!STATE) {
         const unsigned at = sat + 4 * (unsigned)lane_at(tile, kt, KT, lane);
         buf_st(wb, at, st[2 * kt]);
@@ -149,8 +149,8 @@ __device__ __forceinline__ void bwd_chain(const DeltaArgs& a, int nsl, long blk,
       xa[m] = xa[m + 1] = zero4();
 #pragma unroll
       for (int kt = 0; kt < KT; ++kt)
-        O::template xs2<3>(xa[m], L::frag(ks, lab(m, c), kt, g), sb[kt], xa[m + 1],
-                           L::frag(ks, lab(m + 1, c), kt, g), sb[kt]);
+        O::xs2(xa[m], L::frag(ks, lab(m, c), kt, g), sb[kt], xa[m + 1],
+               L::frag(ks, lab(m + 1, c), kt, g), sb[kt]);
       xa[m] = xa[m] * *reinterpret_cast<const f32x4*>(gl + kGEnd + lab(m, 4 * g));
       xa[m + 1] = xa[m + 1] * *reinterpret_cast<const f32x4*>(gl + kGEnd + lab(m + 1, 4 * g));
     }
@@ -161,7 +161,7 @@ __device__ __forceinline__ void bwd_chain(const DeltaArgs& a, int nsl, long blk,
       dob[x] = LV::template frag_t<true>(vs, w, x, g, c);
       f32x4 d0, d1;
       O::values(dob[x], d0, d1);
-      gb[x] = O::template split<3>(
+      gb[x] = O::split(
           d0 * *reinterpret_cast<const f32x4*>(gl + kGsG + 32 * x + 8 * g),
           d1 * *reinterpret_cast<const f32x4*>(gl + kGsG + 32 * x + 8 * g + 4));
     }
@@ -169,11 +169,11 @@ __device__ __forceinline__ void bwd_chain(const DeltaArgs& a, int nsl, long blk,
     for (int m = 0; m < 4; m += 2)
 #pragma unroll
       for (int x = m / 2; x < 2; ++x)
-        O::template sx2<3>(xa[m], ld_frag_t<BF, 3>(ps, m, x, g, c), dob[x], xa[m + 1],
-                           ld_frag_t<BF, 3>(ps, m + 1, x, g, c), dob[x]);
+        O::sx2(xa[m], ld_frag_t<BF>(ps, m, x, g, c), dob[x], xa[m + 1],
+               ld_frag_t<BF>(ps, m + 1, x, g, c), dob[x]);
     typename O::S rb[2];
 #pragma unroll
-    for (int x = 0; x < 2; ++x) rb[x] = O::template split<3>(xa[2 * x], xa[2 * x + 1]);
+    for (int x = 0; x < 2; ++x) rb[x] = O::split(xa[2 * x], xa[2 * x + 1]);
     const float gC = gl[kGC];
 #pragma unroll
     for (int m = 0; m < MT; m += 2) {  // (needs nothing of Y: fills the waits of its products)
@@ -181,16 +181,16 @@ __device__ __forceinline__ void bwd_chain(const DeltaArgs& a, int nsl, long blk,
       st[m + 1] = st[m + 1] * gC;
 #pragma unroll
       for (int x = 0; x < 2; ++x)
-        O::template xs2<3>(st[m], L::template frag_t<false>(qs, m, x, g, c), gb[x], st[m + 1],
-                           L::template frag_t<false>(qs, m + 1, x, g, c), gb[x]);
+        O::xs2(st[m], L::template frag_t<false>(qs, m, x, g, c), gb[x], st[m + 1],
+               L::template frag_t<false>(qs, m + 1, x, g, c), gb[x]);
     }
 #pragma unroll
     for (int m = 0; m < 4; m += 2) {
       xa[m] = xa[m + 1] = zero4();
 #pragma unroll
       for (int x = m / 2; x < 2; ++x)
-        O::template ss2<3>(xa[m], ld_frag_t<BF, 3>(ts, m, x, g, c), rb[x], xa[m + 1],
-                           ld_frag_t<BF, 3>(ts, m + 1, x, g, c), rb[x]);
+        O::ss2(xa[m], ld_frag_t<BF>(ts, m, x, g, c), rb[x], xa[m + 1],
+               ld_frag_t<BF>(ts, m + 1, x, g, c), rb[x]);
     }
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
@@ -200,15 +200,15 @@ __device__ __forceinline__ void bwd_chain(const DeltaArgs& a, int nsl, long blk,
         buf_st(yb, at + 1024, xa[2 * x + 1]);
       }
       const float* gp = gl + kGEtaG + 32 * x + 8 * g;
-      rb[x] = O::template split<3>(xa[2 * x] * -*reinterpret_cast<const f32x4*>(gp),
-                                   xa[2 * x + 1] * -*reinterpret_cast<const f32x4*>(gp + 4));
+      rb[x] = O::split(xa[2 * x] * -*reinterpret_cast<const f32x4*>(gp),
+                       xa[2 * x + 1] * -*reinterpret_cast<const f32x4*>(gp + 4));
     }
 #pragma unroll
     for (int m = 0; m < MT; m += 2)
 #pragma unroll
       for (int x = 0; x < 2; ++x)
-        O::template xs2<3>(st[m], L::template frag_t<false>(ks, m, x, g, c), rb[x], st[m + 1],
-                           L::template frag_t<false>(ks, m + 1, x, g, c), rb[x]);
+        O::xs2(st[m], L::template frag_t<false>(ks, m, x, g, c), rb[x], st[m + 1],
+               L::template frag_t<false>(ks, m + 1, x, g, c), rb[x]);
     if (r > r0) {
       __syncthreads();                       // (the chunk in LDS is done with)
       stage();

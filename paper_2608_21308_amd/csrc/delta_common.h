@@ -55,8 +55,8 @@ struct DeltaArgs {
   float* w_out;               // nullable
   const float* d_w_out;       // nullable: zero
   float* d_w_in;              // nullable
-  char* frag;                 // [chunk unit] T in three terms, then P in pterms
-  int pterms;                 // two (not saving), or three
+  char* frag;                 // [chunk unit] T, then P, in terms
+  bool save;                  // a backward follows
   float* gate;                // [chunk unit][kGateFloats]
   float* wst;                 // [chunk unit][dvp x dkp] chunk-start states (saving), in lane order
   float* ust;                 // [chunk unit][dvp x 64] U^T (saving), in lane order
@@ -98,12 +98,11 @@ __host__ __device__ constexpr int fidx(int m, int a) { return m < 2 ? m : 2 * (m
 
 // Operands.  X: a value of the io type, exact.  S: an fp32 value; with bf16 io
 // the sum of NT = 3 bf16 terms, each the upper half of the word that the ones
-// before leave: 8 bits each, 24 in all, so that nothing is lost.  A product
-// takes the terms whose combined order is below N: with N = 3 it is an fp32
-// product (what is left out is of the order 2^-24), used for all that reaches
-// a state or a gate's gradient; with N = 2 its error is at most 2^-15 (2^-13 of
-// two S operands), far below the rounding of a bf16 output (2^-9), used for what
-// reaches such outputs only.  f32 io: fp32 MFMA.
+// before leave: 8 bits each, 24 in all, so that nothing is lost.  A product with
+// an X operand is then exact up to its fp32 sums.  One of two S operands takes the
+// six pairs of terms of combined order 0 to 2; with a term below 2^-7 of what it is
+// split from, what the other three leave out is below 2 (2^-7 2^-15) = 2^-21 of the
+// product, 2^-24 in the mean.  f32 io: fp32 MFMA.
 template <bool BF> struct DOp;
 
 template <> struct DOp<true> {
@@ -117,58 +116,51 @@ template <> struct DOp<true> {
   static __device__ __forceinline__ f32x4 xx(f32x4 acc, const X& a, const X& b) {
     return m1(acc, a.v, b.v);
   }
-  template <int N>
   static __device__ __forceinline__ f32x4 xs(f32x4 acc, const X& a, const S& b) {
 #pragma unroll
-    for (int i = N - 1; i >= 0; --i) acc = m1(acc, a.v, b.t[i]);
+    for (int i = NT - 1; i >= 0; --i) acc = m1(acc, a.v, b.t[i]);
     return acc;
   }
-  template <int N>
   static __device__ __forceinline__ f32x4 sx(f32x4 acc, const S& a, const X& b) {
 #pragma unroll
-    for (int i = N - 1; i >= 0; --i) acc = m1(acc, a.t[i], b.v);
+    for (int i = NT - 1; i >= 0; --i) acc = m1(acc, a.t[i], b.v);
     return acc;
   }
-  template <int N>
   static __device__ __forceinline__ f32x4 ss(f32x4 acc, const S& a, const S& b) {
 #pragma unroll
-    for (int n = N - 1; n >= 0; --n)
+    for (int n = NT - 1; n >= 0; --n)
 #pragma unroll
       for (int i = 0; i <= n; ++i) acc = m1(acc, a.t[i], b.t[n - i]);
     return acc;
   }
   // Two products at once, issued in turn: an MFMA waits for the one before it
   // on the same accumulator twice as long as for the matrix unit.
-  template <int N>
   static __device__ __forceinline__ void xs2(f32x4& c0, const X& a0, const S& b0, f32x4& c1,
                                              const X& a1, const S& b1) {
 #pragma unroll
-    for (int i = N - 1; i >= 0; --i) {
+    for (int i = NT - 1; i >= 0; --i) {
       c0 = m1(c0, a0.v, b0.t[i]);
       c1 = m1(c1, a1.v, b1.t[i]);
     }
   }
-  template <int N>
   static __device__ __forceinline__ void sx2(f32x4& c0, const S& a0, const X& b0, f32x4& c1,
                                              const S& a1, const X& b1) {
 #pragma unroll
-    for (int i = N - 1; i >= 0; --i) {
+    for (int i = NT - 1; i >= 0; --i) {
       c0 = m1(c0, a0.t[i], b0.v);
       c1 = m1(c1, a1.t[i], b1.v);
     }
   }
-  template <int N>
   static __device__ __forceinline__ void ss2(f32x4& c0, const S& a0, const S& b0, f32x4& c1,
                                              const S& a1, const S& b1) {
 #pragma unroll
-    for (int n = N - 1; n >= 0; --n)
+    for (int n = NT - 1; n >= 0; --n)
 #pragma unroll
       for (int i = 0; i <= n; ++i) {
         c0 = m1(c0, a0.t[i], b0.t[n - i]);
         c1 = m1(c1, a1.t[i], b1.t[n - i]);
       }
   }
-  template <int N>
   static __device__ __forceinline__ S split(f32x4 x, f32x4 y) {
     typedef __attribute__((ext_vector_type(4))) unsigned u4;
     S s;
@@ -179,14 +171,14 @@ template <> struct DOp<true> {
       v[4 + e] = y[e];
     }
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
+    for (int i = 0; i < NT; ++i) {
       u4 p;
 #pragma unroll
       for (int e = 0; e < 4; ++e)   // the upper halves of a pair of words
         p[e] = __builtin_amdgcn_perm(__float_as_uint(v[2 * e + 1]), __float_as_uint(v[2 * e]),
                                      0x07060302u);
       s.t[i] = __builtin_bit_cast(bf16x8, p);
-      if (i + 1 < N) {
+      if (i + 1 < NT) {
 #pragma unroll
         for (int e = 0; e < 8; ++e)
           v[e] -= __uint_as_float(__float_as_uint(v[e]) & 0xffff0000u);
@@ -226,13 +218,9 @@ template <> struct DOp<false> {
     for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(p.b[e], q.b[e], acc, 0, 0, 0);
     return acc;
   }
-  template <int N>
   static __device__ __forceinline__ f32x4 xs(f32x4 acc, const X& p, const X& q) { return xx(acc, p, q); }
-  template <int N>
   static __device__ __forceinline__ f32x4 sx(f32x4 acc, const X& p, const X& q) { return xx(acc, p, q); }
-  template <int N>
   static __device__ __forceinline__ f32x4 ss(f32x4 acc, const X& p, const X& q) { return xx(acc, p, q); }
-  template <int N>
   static __device__ __forceinline__ void ss2(f32x4& c0, const X& a0, const X& b0, f32x4& c1,
                                              const X& a1, const X& b1) {
 #pragma unroll
@@ -246,17 +234,14 @@ template <> struct DOp<false> {
       c1 = __builtin_amdgcn_mfma_f32_16x16x4f32(a1.b[e], b1.b[e], c1, 0, 0, 0);
     }
   }
-  template <int N>
   static __device__ __forceinline__ void xs2(f32x4& c0, const X& a0, const X& b0, f32x4& c1,
                                              const X& a1, const X& b1) {
-    ss2<N>(c0, a0, b0, c1, a1, b1);
+    ss2(c0, a0, b0, c1, a1, b1);
   }
-  template <int N>
   static __device__ __forceinline__ void sx2(f32x4& c0, const X& a0, const X& b0, f32x4& c1,
                                              const X& a1, const X& b1) {
-    ss2<N>(c0, a0, b0, c1, a1, b1);
+    ss2(c0, a0, b0, c1, a1, b1);
   }
-  template <int N>
   static __device__ __forceinline__ S split(f32x4 x, f32x4 y) { return S{x, y}; }
   static __device__ __forceinline__ void values(const X& p, f32x4& x, f32x4& y) {
     x = p.a;
@@ -264,12 +249,12 @@ template <> struct DOp<false> {
   }
 };
 
-// A lower triangular 64x64 matrix as the fragments of N terms, in global
+// A lower triangular 64x64 matrix as the fragments of its terms, in global
 // memory and in LDS: 16 bytes a lane and fragment (in the order of frag_slot), the
 // fragments of a term together (f32 io: the two halves of a fragment's fp32
 // values at lane * 16 and 1024 + lane * 16).
-__host__ __device__ constexpr int tri_bytes(bool bf, int n) {
-  return bf ? n * kDeltaFrags * 1024 : kDeltaFrags * 2048;
+__host__ __device__ constexpr int tri_bytes(bool bf) {
+  return bf ? DOp<true>::NT * kDeltaFrags * 1024 : kDeltaFrags * 2048;
 }
 // Lane l's 16 bytes of a term lie at slot l XOR 4 x, x = 0, 3, 1, 2 for lane
 // groups 0 .. 3: the sixteen lanes of a transposing read (four rows of four lane
@@ -278,24 +263,24 @@ __device__ __forceinline__ int frag_slot(int lane) {
   return lane ^ ((lane >> 3) & 4) ^ ((lane & 16) ? 12 : 0);
 }
 // One lane's part of fragment f.
-template <bool BF, int N>
+template <bool BF>
 __device__ __forceinline__ void put_frag(char* p, int f, int lane, f32x4 x, f32x4 y) {
   if constexpr (BF) {
-    const auto s = DOp<true>::split<N>(x, y);
+    const auto s = DOp<true>::split(x, y);
 #pragma unroll
-    for (int i = 0; i < N; ++i)
+    for (int i = 0; i < DOp<BF>::NT; ++i)
       *reinterpret_cast<bf16x8*>(p + ((i * kDeltaFrags + f) * 64 + frag_slot(lane)) * 16) = s.t[i];
   } else {
     *reinterpret_cast<f32x4*>(p + f * 2048 + lane * 16) = x;
     *reinterpret_cast<f32x4*>(p + f * 2048 + 1024 + lane * 16) = y;
   }
 }
-template <bool BF, int N>
+template <bool BF>
 __device__ __forceinline__ typename DOp<BF>::S ld_frag(const char* lds, int f, int lane) {
   typename DOp<BF>::S s;
   if constexpr (BF) {
 #pragma unroll
-    for (int i = 0; i < N; ++i)
+    for (int i = 0; i < DOp<BF>::NT; ++i)
       s.t[i] = *reinterpret_cast<const bf16x8*>(lds + ((i * kDeltaFrags + f) * 64 + frag_slot(lane)) * 16);
   } else {
     s.a = *reinterpret_cast<const f32x4*>(lds + f * 2048 + lane * 16);
@@ -338,14 +323,14 @@ __device__ __forceinline__ bf16x8 cat8(const bf16x4& a, const bf16x4& b) {
 // lab(m, c), contraction over i = 32 a + 8 g .. + 7, a >= m / 2.  Element
 // (i, j) sits in fragment (2 a + (i / 4) mod 2, m / 2), lane group
 // (j mod 32) / 8, lane 4 g + i mod 4, slot j mod 8.
-template <bool BF, int N>
+template <bool BF>
 __device__ __forceinline__ typename DOp<BF>::S ld_frag_t(const char* lds, int m, int a, int g,
                                                           int c) {
   typename DOp<BF>::S s;
   if constexpr (BF) {
     const int r = c >> 2, cq = c & 3;
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
+    for (int i = 0; i < DOp<BF>::NT; ++i) {
       bf16x4 h[2];
 #pragma unroll
       for (int x = 0; x < 2; ++x)
@@ -441,7 +426,7 @@ __device__ __forceinline__ void put_terms(typename DOp<BF>::E* t, int plane, int
                                           f32x4 x, f32x4 y) {
   using L = LTile<BF, D, true>;
   if constexpr (BF) {
-    const auto s = DOp<true>::split<DOp<true>::NT>(x, y);
+    const auto s = DOp<true>::split(x, y);
 #pragma unroll
     for (int i = 0; i < DOp<true>::NT; ++i)
       *reinterpret_cast<bf16x8*>(t + plane * i + L::at(row, p8)) = s.t[i];

@@ -38,7 +38,7 @@ template <bool BF, int DK, int NW, int MODE>
 struct FwdLds {
   static constexpr int e = (int)sizeof(typename DOp<BF>::E), ks = kDC * DK * e;
   static constexpr int qs = ks, vs = qs + (MODE != kState ? ks : 0), ts = vs + kDC * 16 * NW * e;
-  static constexpr int gl = ts + tri_bytes(BF, 3) + (MODE != kState ? tri_bytes(BF, 2) : 0), bytes = gl + kGateChain * 4;
+  static constexpr int gl = ts + (MODE != kState ? 2 : 1) * tri_bytes(BF), bytes = gl + kGateChain * 4;
 };
 
 template <bool BF, int DK, int NW, int MODE>
@@ -52,7 +52,7 @@ __device__ __forceinline__ void fwd_chain(const DeltaArgs& a, int nsl, long blk,
   constexpr int NTH = 64 * NW, KT = DK / 32, MT = DK / 16;
   constexpr int PK = kDC * L::NP / NTH;                 // a thread's pieces of K (Q) rows
   constexpr int PV = kDC * LV::NP / NTH;                // and of V rows
-  constexpr int NF = (tri_bytes(BF, 3) + (OUT ? tri_bytes(BF, 2) : 0)) / 16;   // pieces of T and P
+  constexpr int NF = (OUT ? 2 : 1) * tri_bytes(BF) / 16;   // pieces of T and P
   constexpr int PF = (NF + NTH - 1) / NTH;
   static_assert(kDC * L::NP % NTH == 0 && NTH % L::NP == 0 && NTH % LV::NP == 0,
                 "whole rounds of pieces");
@@ -63,7 +63,7 @@ __device__ __forceinline__ void fwd_chain(const DeltaArgs& a, int nsl, long blk,
   char* ts = lds + M::ts;                                // T, then P
   float* gl = reinterpret_cast<float*>(lds + M::gl);
 
-  const char* ps = ts + tri_bytes(BF, 3);
+  const char* ps = ts + tri_bytes(BF);
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, c = lane & 15;
   const int w = wave_id();
   // the slices of a unit go to one XCD (workgroups are dealt to the eight in turn)
@@ -75,7 +75,7 @@ __device__ __forceinline__ void fwd_chain(const DeltaArgs& a, int nsl, long blk,
   const int r0 = a.r0 + seg * a.seglen, r1 = min(a.r1, r0 + a.seglen);
   const int sl = (int)((blk / 8) % nsl);
   // (nothing starts behind the last segment; the backward wants its transition)
-  if (MODE == kState && seg == a.nseg - 1 && (a.pterms == 2 || (sl + 1) * NW <= a.dvp / 16)) return;
+  if (MODE == kState && seg == a.nseg - 1 && (!a.save || (sl + 1) * NW <= a.dvp / 16)) return;
   const int b = u / a.H, h = u % a.H, hk = h / (a.H / a.HK);
   const int nlive = live_tokens(a, b);
   const int rl = min(r1, (nlive + kDC - 1) / kDC);       // chunks up to the sequence's end (zeros behind)
@@ -128,7 +128,7 @@ __device__ __forceinline__ void fwd_chain(const DeltaArgs& a, int nsl, long blk,
       const unsigned no = vok && vrow + x * (NTH / LV::NP) < nt ? 0 : kNowhere;
       rv[x] = buf_ld(vb, (vat + (unsigned)(x * (NTH / LV::NP) * vst) * ES) | no);
     }
-    const Buf fb = buf_of(a.frag + cu * (tri_bytes(BF, 3) + tri_bytes(BF, a.pterms)));
+    const Buf fb = buf_of(a.frag + cu * 2 * tri_bytes(BF));
 #pragma unroll
     for (int x = 0; x < PF; ++x) rf[x] = buf_ld(fb, 16 * min(tid + x * NTH, NF - 1));   // (the last piece by several)
     rg = buf_ld(buf_of(a.gate + cu * kGateFloats), 16 * min(tid, kGateChain / 4 - 1));
@@ -167,7 +167,7 @@ __device__ __forceinline__ void fwd_chain(const DeltaArgs& a, int nsl, long blk,
     for (int m = 0; m < 4; ++m) xa[m] = oa[m] = ua[m] = zero4();
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt) {
-      sb[kt] = O::template split<3>(st[2 * kt], st[2 * kt + 1]);
+      sb[kt] = O::split(st[2 * kt], st[2 * kt + 1]);
       if constexpr (SAVE) {
         const unsigned at = sat + 4 * (unsigned)lane_at(tile, kt, KT, lane);
         buf_st(wb, at, st[2 * kt]);
@@ -175,8 +175,8 @@ __device__ __forceinline__ void fwd_chain(const DeltaArgs& a, int nsl, long blk,
       }
 #pragma unroll
       for (int m = 0; m < 4; m += 2)
-        O::template xs2<3>(xa[m], L::frag(ks, lab(m, c), kt, g), sb[kt], xa[m + 1],
-                           L::frag(ks, lab(m + 1, c), kt, g), sb[kt]);
+        O::xs2(xa[m], L::frag(ks, lab(m, c), kt, g), sb[kt], xa[m + 1],
+               L::frag(ks, lab(m + 1, c), kt, g), sb[kt]);
     }
     // R, and while it is formed the state's part of O
     typename O::S rb[2], ub[2], ue[2];
@@ -194,12 +194,12 @@ __device__ __forceinline__ void fwd_chain(const DeltaArgs& a, int nsl, long blk,
         xa[2 * x][e] = fmaf(-h0[e], xa[2 * x][e], e0[e] * v0[e]);
         xa[2 * x + 1][e] = fmaf(-h1[e], xa[2 * x + 1][e], e1[e] * v1[e]);
       }
-      rb[x] = O::template split<3>(xa[2 * x], xa[2 * x + 1]);
+      rb[x] = O::split(xa[2 * x], xa[2 * x + 1]);
       if constexpr (OUT) {
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt)
-          O::template sx2<2>(oa[2 * x], sb[kt], L::frag(qs, lab(2 * x, c), kt, g), oa[2 * x + 1],
-                             sb[kt], L::frag(qs, lab(2 * x + 1, c), kt, g));
+          O::sx2(oa[2 * x], sb[kt], L::frag(qs, lab(2 * x, c), kt, g), oa[2 * x + 1],
+                 sb[kt], L::frag(qs, lab(2 * x + 1, c), kt, g));
         oa[2 * x] = oa[2 * x] * gl[kGsG + lab(2 * x, c)];
         oa[2 * x + 1] = oa[2 * x + 1] * gl[kGsG + lab(2 * x + 1, c)];
       }
@@ -212,8 +212,8 @@ __device__ __forceinline__ void fwd_chain(const DeltaArgs& a, int nsl, long blk,
     for (int x = 0; x < 2; ++x) {
 #pragma unroll
       for (int y = 0; y <= x; ++y)
-        O::template ss2<3>(ua[2 * x], ld_frag<BF, 3>(ts, fidx(2 * x, y), lane), rb[y], ua[2 * x + 1],
-                           ld_frag<BF, 3>(ts, fidx(2 * x + 1, y), lane), rb[y]);
+        O::ss2(ua[2 * x], ld_frag<BF>(ts, fidx(2 * x, y), lane), rb[y], ua[2 * x + 1],
+               ld_frag<BF>(ts, fidx(2 * x + 1, y), lane), rb[y]);
       if constexpr (SAVE) {
         const unsigned at = sat + 4 * (unsigned)lane_at(tile, x, 2, lane);
         buf_st(ub_, at, ua[2 * x]);
@@ -221,12 +221,12 @@ __device__ __forceinline__ void fwd_chain(const DeltaArgs& a, int nsl, long blk,
       }
       const f32x4 n0 = *reinterpret_cast<const f32x4*>(gl + kGEnd + 32 * x + 8 * g);
       const f32x4 n1 = *reinterpret_cast<const f32x4*>(gl + kGEnd + 32 * x + 8 * g + 4);
-      ue[x] = O::template split<3>(ua[2 * x] * n0, ua[2 * x + 1] * n1);
-      if constexpr (OUT) ub[x] = O::template split<2>(ua[2 * x], ua[2 * x + 1]);
+      ue[x] = O::split(ua[2 * x] * n0, ua[2 * x + 1] * n1);
+      if constexpr (OUT) ub[x] = O::split(ua[2 * x], ua[2 * x + 1]);
 #pragma unroll
       for (int m = 0; m < MT; m += 2)
-        O::template xs2<3>(st[m], L::template frag_t<false>(ks, m, x, g, c), ue[x], st[m + 1],
-                           L::template frag_t<false>(ks, m + 1, x, g, c), ue[x]);
+        O::xs2(st[m], L::template frag_t<false>(ks, m, x, g, c), ue[x], st[m + 1],
+               L::template frag_t<false>(ks, m + 1, x, g, c), ue[x]);
     }
     if constexpr (OUT) {
     const Buf ob = buf_of(row_of<E>(a.out, b, h, t0) + sc0);
@@ -235,8 +235,8 @@ __device__ __forceinline__ void fwd_chain(const DeltaArgs& a, int nsl, long blk,
       if (m % 2 == 0) {
 #pragma unroll
         for (int x = 0; x <= m / 2; ++x)
-          O::template ss2<2>(oa[m], ub[x], ld_frag<BF, 2>(ps, fidx(m, x), lane), oa[m + 1], ub[x],
-                             ld_frag<BF, 2>(ps, fidx(m + 1, x), lane));
+          O::ss2(oa[m], ub[x], ld_frag<BF>(ps, fidx(m, x), lane), oa[m + 1], ub[x],
+                 ld_frag<BF>(ps, fidx(m + 1, x), lane));
       }
       const unsigned no = sc0 + 16 * w + 4 * g < a.dv && t0 + lab(m, c) < nlive ? 0 : kNowhere;
       buf_st_io<BF>(ob, (unsigned)(lab(m, c) * ost + 16 * w + 4 * g) * ES | no, oa[m]);

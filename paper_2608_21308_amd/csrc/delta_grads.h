@@ -54,7 +54,7 @@ struct GradsLds {
   static constexpr int kStage =
       (2 * DOp<BF>::NT * 32 * (DK + kDC) + kDC * 32) * (int)sizeof(E);
   static constexpr int qs = kDC * DK * (int)sizeof(E), buf = 2 * qs;
-  static constexpr int gl = buf + (kStage > 2 * tri_bytes(BF, 2) ? kStage : 2 * tri_bytes(BF, 2));
+  static constexpr int gl = buf + (kStage > 2 * tri_bytes(BF) ? kStage : 2 * tri_bytes(BF));
   static constexpr int srow = gl + kGateFloats * 4, srr = srow + 2 * (DK / 16) * kDC * 4;
   static constexpr int sx = srr + (DK / 16) * kDC * 4, scol = sx + 4 * kDC * 4;
   static constexpr int syu = scol + 4 * kDC * 4, bytes = syu + (kDC + NWV) * 4;
@@ -96,7 +96,7 @@ __device__ __forceinline__ void grads_chunk(const DeltaArgs& a, int c0, int nr, 
   E* ys = us + NT * UP;
   E* dos = ys + NT * UP;
   char* as = buf;
-  char* ns = buf + tri_bytes(BF, 2);
+  char* ns = buf + tri_bytes(BF);
 
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, c = lane & 15;
   const int w = wave_id();
@@ -235,9 +235,9 @@ __device__ __forceinline__ void grads_chunk(const DeltaArgs& a, int c0, int nr, 
       else if (!ONE && hv + 1 < rep)
         fetch(h + 1, cu + a.nc_buf, 0);
       auto products = [&](int m, const auto& wf, const auto& df, const auto& um) {
-        ow[m] = O::template xs<3>(ow[m], LV::frag(dos, lab(m0 + m, c), 0, g), wf);
-        yw[m] = O::template ss<3>(yw[m], terms_t<BF, kDC, false>(ys, UP, m0 + m, g, c), wf);
-        uw[m] = O::template ss<3>(uw[m], um, df);
+        ow[m] = O::xs(ow[m], LV::frag(dos, lab(m0 + m, c), 0, g), wf);
+        yw[m] = O::ss(yw[m], terms_t<BF, kDC, false>(ys, UP, m0 + m, g, c), wf);
+        uw[m] = O::ss(uw[m], um, df);
       };
       if constexpr (MR < 4) {
         const auto wf = terms_t<BF, DK, true>(w0s, WP, ct, g, c);
@@ -257,8 +257,8 @@ __device__ __forceinline__ void grads_chunk(const DeltaArgs& a, int c0, int nr, 
         buf_st_io<BF>(vb, at + 4 * (unsigned)sizeof(E), y1 * gl[kGEta + i]);
       }
       auto pairs = [&](int n, int y, const auto& uj) {
-        du[n][y] = O::template sx<3>(du[n][y], uj, doi);
-        yu[n][y] = O::template ss<3>(yu[n][y], uj, yi);
+        du[n][y] = O::sx(du[n][y], uj, doi);
+        yu[n][y] = O::ss(yu[n][y], uj, yi);
       };
       if constexpr (MR < 4) {
 #pragma unroll
@@ -331,8 +331,8 @@ __device__ __forceinline__ void grads_chunk(const DeltaArgs& a, int c0, int nr, 
         }
       }
       if (xb <= rt / 2) {
-        put_frag<BF, 2>(as, fidx(rt, xb), lane, pa[0], pa[1]);
-        put_frag<BF, 2>(ns, fidx(rt, xb), lane, pn[0], pn[1]);
+        put_frag<BF>(as, fidx(rt, xb), lane, pa[0], pa[1]);
+        put_frag<BF>(ns, fidx(rt, xb), lane, pn[0], pn[1]);
       }
       const float cs = sum16x8(pair[0], pair[1], c);     // of column 8 g + c / 2 of the block
       if (!(c & 1)) scol[rt][32 * xb + 8 * g + (c >> 1)] = cs;
@@ -388,12 +388,12 @@ __device__ __forceinline__ void grads_chunk(const DeltaArgs& a, int c0, int nr, 
       for (int mm = 0; mm < MR; ++mm) {
         const int m = m0 + mm;
         if (x <= m / 2) {
-          dq[mm] = O::template sx<2>(dq[mm], ld_frag<BF, 2>(as, fidx(m, x), lane), kf);
-          dk[mm] = O::template sx<2>(dk[mm], ld_frag<BF, 2>(ns, fidx(m, x), lane), kf);
+          dq[mm] = O::sx(dq[mm], ld_frag<BF>(as, fidx(m, x), lane), kf);
+          dk[mm] = O::sx(dk[mm], ld_frag<BF>(ns, fidx(m, x), lane), kf);
         }
         if (x >= m / 2) {
-          dk[mm] = O::template sx<2>(dk[mm], ld_frag_t<BF, 2>(as, m, x, g, c), qf);
-          dk[mm] = O::template sx<2>(dk[mm], ld_frag_t<BF, 2>(ns, m, x, g, c), kf);
+          dk[mm] = O::sx(dk[mm], ld_frag_t<BF>(as, m, x, g, c), qf);
+          dk[mm] = O::sx(dk[mm], ld_frag_t<BF>(ns, m, x, g, c), kf);
         }
       }
     }

@@ -47,7 +47,7 @@ __global__ void __launch_bounds__(4 * DK) delta_join_kernel(DeltaArgs a) {
   };
   auto one = [&](int i, f32x4 (&f)[KT][2], f32x4& bb) {
     const int p = first + step * i;
-    const O::S own = O::split<3>(st, zero4());
+    const O::S own = O::split(st, zero4());
 #pragma unroll
     for (int t = 0; t < 3; ++t)
       *reinterpret_cast<bf16x4*>(&ws[i & 1][t][c * LD + kc]) =
@@ -57,7 +57,7 @@ __global__ void __launch_bounds__(4 * DK) delta_join_kernel(DeltaArgs a) {
     st = bb;
     O::S fa[KT];
 #pragma unroll
-    for (int kt = 0; kt < KT; ++kt) fa[kt] = O::split<3>(f[kt][0], f[kt][1]);
+    for (int kt = 0; kt < KT; ++kt) fa[kt] = O::split(f[kt][0], f[kt][1]);
     if (i + 3 < a.nseg) fetch(p + 2 * step, f, bb);
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt) {
@@ -65,7 +65,7 @@ __global__ void __launch_bounds__(4 * DK) delta_join_kernel(DeltaArgs a) {
 #pragma unroll
       for (int t = 0; t < 3; ++t)
         sb.t[t] = *reinterpret_cast<const bf16x8*>(&ws[i & 1][t][c * LD + 32 * kt + 8 * g]);
-      st = O::ss<3>(st, fa[kt], sb);
+      st = O::ss(st, fa[kt], sb);
     }
     if ((long)(a.r0 + p * a.seglen) * kDC >= live) st = was;
     *reinterpret_cast<f32x4*>(a.segs + (u * a.nseg + p + step) * a.dvp * DK +

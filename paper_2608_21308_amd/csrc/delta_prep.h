@@ -145,7 +145,7 @@ __device__ __forceinline__ void prep_chunk(const DeltaArgs& a, int r0, int nr, l
   }
   __syncthreads();
 
-  char* frag = a.frag + cu * (tri_bytes(BF, 3) + tri_bytes(BF, a.pterms));
+  char* frag = a.frag + cu * 2 * tri_bytes(BF);
   const float bhi = gl[kGBh + i], bli = gl[kGBl + i], eta = gl[kGEta + i];
 #pragma unroll
   for (int x = 0; x < 2; ++x) {
@@ -166,10 +166,7 @@ __device__ __forceinline__ void prep_chunk(const DeltaArgs& a, int r0, int nr, l
         }
         *reinterpret_cast<f32x4*>(am + i * LDT + j0) = m4;
       }
-      if (a.pterms == 3)
-        put_frag<BF, 3>(frag + tri_bytes(BF, 3), fidx(w, x), lane, p[0], p[1]);
-      else
-        put_frag<BF, 2>(frag + tri_bytes(BF, 3), fidx(w, x), lane, p[0], p[1]);
+      put_frag<BF>(frag + tri_bytes(BF), fidx(w, x), lane, p[0], p[1]);
     }
   }
   if (w == 0) {
@@ -245,7 +242,7 @@ __device__ __forceinline__ void prep_chunk(const DeltaArgs& a, int r0, int nr, l
   for (int x = 0; x < 2; ++x) {
     if (x < na) {
       const float* p = am + i * LDT + 32 * x + 8 * g;
-      put_frag<BF, 3>(frag, fidx(w, x), lane, *reinterpret_cast<const f32x4*>(p),
+      put_frag<BF>(frag, fidx(w, x), lane, *reinterpret_cast<const f32x4*>(p),
                       *reinterpret_cast<const f32x4*>(p + 4));
     }
   }

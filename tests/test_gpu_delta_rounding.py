@@ -1,0 +1,56 @@
+"""The delta rule's bf16 outputs and gradients are fp32 results rounded once.
+
+They are compared with the 64-bit recurrence rounded to bf16.  An fp32 value
+that is off by e_i falls on the other side of a rounding border with
+probability |e_i| / u_i, where u_i <= 2^-7 |x_i| is the distance of neighbouring
+bf16 numbers, and is then u_i off.  The expected square of the difference is
+sum |e_i| u_i <= |e| |u| <= 2^-7 |e| |x|, which with the |e| <= 2^-18 |x| that is
+asked of fp32 results (test_gpu_delta.py) is (2^-12.5 |x|)^2; 2^-12 |x| is asked
+for, over tensors of 10^4 elements and more.  (Products of operands of two bf16
+parts, off by 2^-15, give 2^-11.)"""
+import pytest
+import torch
+
+from paper_2608_21308_amd import e2ttt
+from tests import deltaref
+from tests.test_gpu_delta import make, to_dev
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _lib():
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    e2ttt.load()
+
+
+def rounded_once(name, got, ref):
+    want = ref.bfloat16().double()
+    assert want.numel() >= 10000
+    err = ((got.double().cpu() - want).norm() / want.norm()).item()
+    print("%-4s %.2e" % (name, err), flush=True)
+    assert err <= 2.0 ** -12, (name, err)
+
+
+@pytest.mark.parametrize("c", [(2, 1, 2, 200, 64, 64),       # chunks in turn
+                               (1, 2, 2, 801, 32, 40),       # segments
+                               (1, 1, 2, 600, 128, 72),
+                               (4, 24, 24, 2049, 64, 8)])    # parts
+def test_rounded_once(c):
+    B, HK, H, T, dk, dv = c
+    x, d = make(*c, "bf16", seed=83)
+    cfg = e2ttt.DeltaConfig(*c, e2ttt.DT_BF16, 0.125)
+    t, td = to_dev(x, "bf16"), to_dev(d, "bf16")
+    names = ("q", "k", "v", "eta", "log_gamma")
+    print("delta", c, flush=True)
+    out, _, ws = e2ttt.delta_forward(cfg, *[t[n] for n in names], t["w_in"], save_for_backward=True)
+    plain, _, _ = e2ttt.delta_forward(cfg, *[t[n] for n in names], t["w_in"])
+    g = e2ttt.delta_backward(cfg, *[t[n] for n in names], ws, td["d_out"], td["d_w_out"])
+    torch.cuda.synchronize()
+    assert torch.equal(out, plain)
+    one = lambda a: a[:1]          # (the sequences do not meet)
+    ref, _, rg = deltaref.delta_grads({n: one(a) for n, a in x.items()}, 0.125, one(d["d_out"]),
+                                      one(d["d_w_out"]))
+    for name, got, want in (("out", out, ref), ("dq", g["dq"], rg["q"]), ("dk", g["dk"], rg["k"]),
+                            ("dv", g["dv"], rg["v"])):
+        rounded_once(name, one(got), want)
