@@ -226,7 +226,7 @@ extern "C" e2ttt_status e2ttt_delta_forward(const e2ttt_delta_desc* desc,
       a.w_out = a.r1 == p.NC ? w_out : carry;
       a.nseg = (a.r1 - a.r0 + a.seglen - 1) / a.seglen;  // (the last stretch may be shorter)
       if (a.nseg > 1 && (launch_delta_chain(a, p.bf, false, true, s) != hipSuccess ||
-                         launch_delta_join(a, false, s) != hipSuccess))
+                         launch_delta_join(a, p.bf, false, s) != hipSuccess))
         return E2TTT_ERR_HIP;
       const int next = (int)std::min(p.part, r1 - a.r1);
       if ((next ? launch_delta_chain_prep(a, save, a.r1, next, s)
@@ -279,7 +279,7 @@ extern "C" e2ttt_status e2ttt_delta_backward(
     a.d_w_in = a.r0 == 0 ? d_w_in : carry;
     a.nseg = (a.r1 - a.r0 + a.seglen - 1) / a.seglen;
     if (a.nseg > 1 && (launch_delta_chain_bwd(a, p.bf, true, s) != hipSuccess ||
-                       launch_delta_join(a, true, s) != hipSuccess))
+                       launch_delta_join(a, p.bf, true, s) != hipSuccess))
       return E2TTT_ERR_HIP;
     const int done = (int)std::min(part, p.NC - a.r1);
     if ((done ? launch_delta_chain_bwd_grads(a, a.r1, done, s)

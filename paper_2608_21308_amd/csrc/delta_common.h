@@ -497,7 +497,7 @@ hipError_t launch_delta_chain_bwd(const DeltaArgs& a, bool bf, bool state, hipSt
 hipError_t launch_delta_chain_prep(const DeltaArgs& a, bool save, int p0, int np, hipStream_t stream);
 hipError_t launch_delta_chain_bwd_grads(const DeltaArgs& a, int g0, int ng, hipStream_t stream);
 // The segments' start states from their parts, one after the other.
-hipError_t launch_delta_join(const DeltaArgs& a, bool bwd, hipStream_t stream);
+hipError_t launch_delta_join(const DeltaArgs& a, bool bf, bool bwd, hipStream_t stream);
 hipError_t launch_delta_grads(const DeltaArgs& a, bool bf, hipStream_t stream);
 // padded key dimension (32, 64 or 128) and value dimension (a multiple of 32)
 inline int delta_dkp(int dk) { return dk <= 32 ? 32 : dk <= 64 ? 64 : 128; }

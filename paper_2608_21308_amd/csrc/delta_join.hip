@@ -3,7 +3,7 @@
 // those that they end with,   dW_{p-1} = dW_p F_p^T + B_p   from d_w_out.
 //
 // One workgroup per unit and 16 rows of W (columns of W^T), a wave per 16 rows
-// of W^T, so that a step is dk / 32 products of fp32 accuracy a wave; the state
+// of W^T, so that a step is dk / 32 products of the state's precision a wave; the state
 // goes round through LDS, and the next two F are on their way meanwhile.  Bound
 // by that round: 1 us a segment at dk = 64, 2 us at 128 (backward 3).
 #include "delta_common.h"
@@ -11,11 +11,12 @@
 namespace e2ttt {
 namespace {
 
-template <int DK, bool BWD>
+template <bool BF, int DK, bool BWD>
 __global__ void __launch_bounds__(4 * DK) delta_join_kernel(DeltaArgs a) {
-  using O = DOp<true>;     // (fp32 products by bf16 terms, whatever the io type)
+  using O = DOp<BF>;
+  using E = typename O::E;
   constexpr int KT = DK / 32, LD = DK + 8;
-  __shared__ __align__(16) __bf16 ws[2][3][16 * LD];      // the state's rows, in three terms
+  __shared__ __align__(16) E ws[2][O::NT][16 * LD];       // the state's rows, in terms
   const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
   const int w = wave_id();
   const int nvt = a.dvp / 16;
@@ -47,24 +48,33 @@ __global__ void __launch_bounds__(4 * DK) delta_join_kernel(DeltaArgs a) {
   };
   auto one = [&](int i, f32x4 (&f)[KT][2], f32x4& bb) {
     const int p = first + step * i;
-    const O::S own = O::split(st, zero4());
+    if constexpr (BF) {
+      const auto own = O::split(st, zero4());
 #pragma unroll
-    for (int t = 0; t < 3; ++t)
-      *reinterpret_cast<bf16x4*>(&ws[i & 1][t][c * LD + kc]) =
-          __builtin_shufflevector(own.t[t], own.t[t], 0, 1, 2, 3);
+      for (int t = 0; t < O::NT; ++t)
+        *reinterpret_cast<bf16x4*>(&ws[i & 1][t][c * LD + kc]) =
+            __builtin_shufflevector(own.t[t], own.t[t], 0, 1, 2, 3);
+    } else {
+      *reinterpret_cast<f32x4*>(&ws[i & 1][0][c * LD + kc]) = st;
+    }
     __syncthreads();                                     // (the other buffer is read until the next)
     const f32x4 was = st;
     st = bb;
-    O::S fa[KT];
+    typename O::S fa[KT];
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt) fa[kt] = O::split(f[kt][0], f[kt][1]);
     if (i + 3 < a.nseg) fetch(p + 2 * step, f, bb);
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt) {
-      O::S sb;
+      typename O::S sb;
+      const E* row = &ws[i & 1][0][c * LD + 32 * kt + 8 * g];
+      if constexpr (BF) {
 #pragma unroll
-      for (int t = 0; t < 3; ++t)
-        sb.t[t] = *reinterpret_cast<const bf16x8*>(&ws[i & 1][t][c * LD + 32 * kt + 8 * g]);
+        for (int t = 0; t < O::NT; ++t) sb.t[t] = *reinterpret_cast<const bf16x8*>(row + t * 16 * LD);
+      } else {
+        sb.a = *reinterpret_cast<const f32x4*>(row);
+        sb.b = *reinterpret_cast<const f32x4*>(row + 4);
+      }
       st = O::ss(st, fa[kt], sb);
     }
     if ((long)(a.r0 + p * a.seglen) * kDC >= live) st = was;
@@ -83,21 +93,22 @@ __global__ void __launch_bounds__(4 * DK) delta_join_kernel(DeltaArgs a) {
   }
 }
 
-template <bool BWD>
+template <bool BF, bool BWD>
 hipError_t go(const DeltaArgs& a, hipStream_t s) {
   const dim3 grid((unsigned)(((long)a.B * a.H + 7) / 8 * 8 * (a.dvp / 16)));
   switch (delta_dkp(a.dk)) {
-    case 32: hipLaunchKernelGGL((delta_join_kernel<32, BWD>), grid, dim3(128), 0, s, a); break;
-    case 64: hipLaunchKernelGGL((delta_join_kernel<64, BWD>), grid, dim3(256), 0, s, a); break;
-    default: hipLaunchKernelGGL((delta_join_kernel<128, BWD>), grid, dim3(512), 0, s, a); break;
+    case 32: hipLaunchKernelGGL((delta_join_kernel<BF, 32, BWD>), grid, dim3(128), 0, s, a); break;
+    case 64: hipLaunchKernelGGL((delta_join_kernel<BF, 64, BWD>), grid, dim3(256), 0, s, a); break;
+    default: hipLaunchKernelGGL((delta_join_kernel<BF, 128, BWD>), grid, dim3(512), 0, s, a); break;
   }
   return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_delta_join(const DeltaArgs& a, bool bwd, hipStream_t stream) {
-  return bwd ? go<true>(a, stream) : go<false>(a, stream);
+hipError_t launch_delta_join(const DeltaArgs& a, bool bf, bool bwd, hipStream_t stream) {
+  if (bf) return bwd ? go<true, true>(a, stream) : go<true, false>(a, stream);
+  return bwd ? go<false, true>(a, stream) : go<false, false>(a, stream);
 }
 
 }  // namespace e2ttt
