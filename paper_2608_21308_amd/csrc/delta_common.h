@@ -97,12 +97,14 @@ __device__ __forceinline__ float exp_finite(float x) {
 __host__ __device__ constexpr int fidx(int m, int a) { return m < 2 ? m : 2 * (m - 1) + a; }
 
 // Operands.  X: a value of the io type, exact.  S: an fp32 value; with bf16 io
-// the sum of NT = 3 bf16 terms, each the upper half of the word that the ones
-// before leave: 8 bits each, 24 in all, so that nothing is lost.  A product with
-// an X operand is then exact up to its fp32 sums.  One of two S operands takes the
-// six pairs of terms of combined order 0 to 2; with a term below 2^-7 of what it is
-// split from, what the other three leave out is below 2 (2^-7 2^-15) = 2^-21 of the
-// product, 2^-24 in the mean.  f32 io: fp32 MFMA.
+// the sum of NT = 3 bf16 terms, each the rounding of what the ones before leave: 8
+// bits each, 24 in all, so that nothing is lost (of values whose rounding is finite,
+// to 3.39e38).  A product with an X operand is then exact up to its fp32 sums.  One of
+// two S operands takes the six pairs of terms of combined order 0 to 2; with a term at
+// most 2^-8 of the one before, what the other three leave out is at most 2 (2^-8
+// 2^-16) = 2^-23 of the product, of either sign.  (Terms cut off instead of rounded
+// save up to 2 % of the time, and lose up to 2^-21, always towards zero.)  f32 io: fp32
+// MFMA.
 template <bool BF> struct DOp;
 
 template <> struct DOp<true> {
@@ -162,26 +164,20 @@ template <> struct DOp<true> {
       }
   }
   static __device__ __forceinline__ S split(f32x4 x, f32x4 y) {
+    typedef __attribute__((ext_vector_type(8))) float f8;
     typedef __attribute__((ext_vector_type(4))) unsigned u4;
     S s;
-    float v[8];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      v[e] = x[e];
-      v[4 + e] = y[e];
-    }
+    f8 v = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
-      u4 p;
-#pragma unroll
-      for (int e = 0; e < 4; ++e)   // the upper halves of a pair of words
-        p[e] = __builtin_amdgcn_perm(__float_as_uint(v[2 * e + 1]), __float_as_uint(v[2 * e]),
-                                     0x07060302u);
-      s.t[i] = __builtin_bit_cast(bf16x8, p);
+      s.t[i] = __builtin_convertvector(v, bf16x8);
       if (i + 1 < NT) {
+        const u4 p = __builtin_bit_cast(u4, s.t[i]);   // (pairs: a term is the upper half of its float)
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-          v[e] -= __uint_as_float(__float_as_uint(v[e]) & 0xffff0000u);
+        for (int e = 0; e < 4; ++e) {
+          v[2 * e] -= __uint_as_float(p[e] << 16);
+          v[2 * e + 1] -= __uint_as_float(p[e] & 0xffff0000u);
+        }
       }
     }
     return s;

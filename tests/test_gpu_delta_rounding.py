@@ -56,18 +56,19 @@ def test_rounded_once(c):
         rounded_once(name, one(got), want)
 
 
-def test_f32_states_stay_f32_between_segments():
-    """A float32 call carries its state from segment to segment in float32.  With eta = 0 the
-    state decays by 1 - 2^-20 once in each of 16 segments; states just below 2 and that factor
-    have mantissas of ones, of which a product of bf16 terms leaves out 2^-23 every time
-    (2^-19 in all).  Asked for: the exponential an ulp (2^-24) off, 16 times, and the products'
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+def test_f32_states_stay_f32_between_segments(io):
+    """The state goes from segment to segment in float32.  With eta = 0 it decays by 1 - 2^-20
+    once in each of 16 segments; states just below 2 and that factor have mantissas of ones,
+    of which a product of cut off bf16 terms leaves out 2^-23 every time (2^-19 in all).  Asked for: the exponential an ulp (2^-24) off, 16 times, and the products'
     independent roundings, sqrt(16) 2^-24."""
     B, H, T, d = 1, 1, 4096, 64
     g = torch.Generator().manual_seed(3)
     rn = lambda *s: torch.randn(*s, generator=g).cuda()
     unit = lambda x: x / x.norm(dim=-1, keepdim=True)
-    cfg = e2ttt.DeltaConfig(B, H, H, T, d, d, e2ttt.DT_F32, 1.0)
-    q, k, v = unit(rn(B, H, T, d)), unit(rn(B, H, T, d)), rn(B, H, T, d)
+    cfg = e2ttt.DeltaConfig(B, H, H, T, d, d, e2ttt.DT_BF16 if io == "bf16" else e2ttt.DT_F32, 1.0)
+    dt = torch.bfloat16 if io == "bf16" else torch.float32
+    q, k, v = unit(rn(B, H, T, d)).to(dt), unit(rn(B, H, T, d)).to(dt), rn(B, H, T, d).to(dt)
     eta, lg = torch.zeros(B, H, T, device="cuda"), torch.zeros(B, H, T, device="cuda")
     lg[:, :, 100::256] = -2.0 ** -20
     ones = 2.0 - 2.0 ** -23 * torch.randint(1, 256, (B, H, d, d), generator=g).float().cuda()
