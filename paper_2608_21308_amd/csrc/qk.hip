@@ -72,11 +72,18 @@ __device__ __forceinline__ float row_sum(float v, int lanes) {
   return v;
 }
 
-// sigma(x) by the hardware's exponential and reciprocal (an ulp each; the
-// rounding of x log2 e costs |x| 2^-24 of e^-x, below 2^-24 of x sigma(x)'s
-// largest values).
+// sigma(x), to a few 2^-24 of its value however small (below 2^-126 it is zero), by
+// the hardware's exponential and reciprocal, an ulp each.  e^-x is 2^h (1 + d), h = -x
+// times the upper 16 bits of log2 e and d = -x times the rest of ln 2 log2 e: a bf16
+// x gives h without rounding, a float's rounding is put into d.  (e^-104 is zero; d > 0
+// where 2^h overflows.)
+template <bool BF>
 __device__ __forceinline__ float sigma(float x) {
-  return rcp_f(1.0f + __builtin_amdgcn_exp2f(-1.44269504f * x));
+  const float y = fmaxf(-x, -104.0f), h = y * 1.44268799f;
+  float d = y * 4.8885e-6f;
+  if constexpr (!BF) d = fmaf(fmaf(y, 1.44268799f, -h), 0.693147181f, d);
+  const float p = __builtin_amdgcn_exp2f(h);
+  return rcp_f(1.0f + fmaf(p, d, p));
 }
 
 // m times cosine and sine of 2 pi t, |t| <= 1/2: Taylor's series to x^9 around
@@ -208,7 +215,7 @@ __global__ void __launch_bounds__(256) qk_kernel(QkArgs a, unsigned flags) {
         for (int k = 0; k < 2; ++k)
 #pragma unroll
           for (int i = 0; i < V; ++i) {
-            const float sg = sigma(u[x][k][i]);
+            const float sg = sigma<BF>(u[x][k][i]);
             if (BWD) raw[x][k][i] = sg * fmaf(u[x][k][i], 1.0f - sg, 1.0f);   // the derivative
             u[x][k][i] *= sg;
           }
