@@ -86,16 +86,18 @@ __device__ __forceinline__ float sigma(float x) {
   return rcp_f(1.0f + fmaf(p, d, p));
 }
 
-// m times cosine and sine of 2 pi t, |t| <= 1/2: Taylor's series to x^9 around
-// the nearest quarter turn (|x| <= pi / 4, remainder below 2^-28).
-__device__ __forceinline__ void turn(float t, float m, float& co, float& si) {
-  const float q = rintf(4.0f * t);
-  const float x = fmaf(-0.25f, q, t) * 6.283185307f, x2 = x * x;
+// m times cosine and sine of 2 pi t, |t| <= 1/2: Taylor's series to x^10 around
+// the nearest quarter turn, which is taken off in 64 bits (|x| <= pi / 4; the
+// remainders, x^11 / 11! and x^12 / 12!, are below 2^-29).
+__device__ __forceinline__ void turn(double t, float m, float& co, float& si) {
+  const double q = rint(4.0 * t);
+  const float x = (float)(fma(-0.25, q, t) * 6.283185307179586), x2 = x * x;
   float s = fmaf(x2, 2.7557319e-6f, -1.9841270e-4f);
   s = fmaf(x2, s, 8.3333333e-3f);
   s = fmaf(x2, s, -1.6666667e-1f);
   s = m * fmaf(x * x2, s, x);
-  float c = fmaf(x2, 2.4801587e-5f, -1.3888889e-3f);
+  float c = fmaf(x2, -2.7557319e-7f, 2.4801587e-5f);
+  c = fmaf(x2, c, -1.3888889e-3f);
   c = fmaf(x2, c, 4.1666667e-2f);
   c = fmaf(x2, c, -0.5f);
   c = m * fmaf(x2, c, 1.0f);
@@ -151,7 +153,7 @@ __global__ void __launch_bounds__(256) qk_kernel(QkArgs a, unsigned flags) {
       for (int i = 0; i < V; ++i) {
         double turns = p * (double)a.inv_freq[it * V + i] * 0.15915494309189535;
         turns -= rint(turns);
-        turn((float)turns, a.m, co[x][i], si[x][i]);
+        turn(turns, a.m, co[x][i], si[x][i]);
       }
     } else {
       const int q = 2 * (it - np);

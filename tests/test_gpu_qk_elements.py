@@ -43,3 +43,26 @@ def test_silu_of_special_values():
     y, _ = e2ttt.qk_forward(cfg, x.view(1, 1, 1, 8).cuda(), None)
     want = x / (1.0 + torch.exp(-x))
     assert torch.equal(y.cpu().flatten().nan_to_num(7.0), want.nan_to_num(7.0))
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_sines_and_cosines(interleaved):
+    """Pairs (1, 0) turn into the cosine and the sine.  Each is off by the rounding of the
+    angle to its quarter turn (at most 2^-25 below pi / 4), of the last sum (2^-25) and of the
+    square and the terms below it (2^-25 together): 2^-23 is asked for."""
+    B, T, d = 4, 700, 128
+    flags = e2ttt.QK_INTERLEAVED if interleaved else 0
+    cfg = e2ttt.QKConfig(B, 1, 0, T, d, d, e2ttt.DT_F32, flags)
+    f, _ = e2ttt.rotary_frequencies(d, device="cpu")
+    pos = torch.randint(0, 200000, (B, T), generator=torch.Generator().manual_seed(2))
+    x = torch.zeros(B, 1, T, d)
+    first = slice(0, d, 2) if interleaved else slice(0, d // 2)
+    second = slice(1, d, 2) if interleaved else slice(d // 2, d)
+    x[..., first] = 1.0
+    y, _ = e2ttt.qk_forward(cfg, x.cuda(), None, f.cuda(), pos.cuda())
+    y = y.double().cpu()
+    angle = pos.double()[:, None, :, None] * f.double()
+    for name, got, ref in (("cos", y[..., first], torch.cos(angle)), ("sin", y[..., second], torch.sin(angle))):
+        err = (got - ref).abs().max().item()
+        print("%s %.2e" % (name, err), flush=True)
+        assert err <= 2.0 ** -23, name
