@@ -603,12 +603,19 @@ def _on_device(f):
 def _as_rows(g):
     """A gradient as the library takes it: rows contiguous, on 16 bytes and at
     most 2^23 elements apart."""
-    if g.is_contiguous() and g.data_ptr() % 16 == 0:
+    if g.data_ptr() % 16:          # (a contiguous view may start anywhere in its storage)
+        return g.clone(memory_format=torch.contiguous_format)
+    if g.is_contiguous():
         return g
-    if g.stride(-1) != 1 or g.stride(2) > 1 << 23 or g.data_ptr() % 16 or any(
+    if g.stride(-1) != 1 or g.stride(2) > 1 << 23 or any(
             s * g.element_size() % 16 for s, n in zip(g.stride()[:3], g.shape) if n > 1):
         return g.contiguous()
     return g
+
+
+def _as_state(g):
+    """The same of a state's gradient: contiguous, on 16 bytes."""
+    return g.clone(memory_format=torch.contiguous_format) if g.data_ptr() % 16 else g.contiguous()
 
 
 @dataclass(frozen=True)
@@ -803,7 +810,7 @@ def _delta_grads(ctx, d_out, d_w_out):
     q, k, v, eta, log_gamma, lengths, ws = ctx.saved_tensors
     d_out = torch.zeros_like(v) if d_out is None else _as_rows(d_out)
     if d_w_out is not None:
-        d_w_out = d_w_out.contiguous()
+        d_w_out = _as_state(d_w_out)
     _, io, _, s_v, _, s_w = cfg._call
     dev = q.get_device()
     if (ctx.flat and dev == _current_device() and _flat(d_out, s_v, io, dev) and

@@ -1,0 +1,73 @@
+"""The autograd wrappers of the delta rule and the query/key preparation with the
+upstream gradients that a graph may hand them."""
+import pytest
+import torch
+
+from paper_2608_21308_amd import e2ttt
+from tests.test_gpu_delta import make, to_dev
+
+pytestmark = pytest.mark.gpu
+
+NAMES = ("q", "k", "v", "eta", "log_gamma", "w_in")
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _lib():
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    e2ttt.load()
+
+
+def shifted(t, n):
+    """t as a contiguous tensor that starts n elements into its storage."""
+    s = torch.empty(t.numel() + n, dtype=t.dtype, device=t.device)
+    o = s[n:].view(t.shape)
+    assert o.is_contiguous()
+    return o.copy_(t)
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+@pytest.mark.parametrize("layout", ["bhtd", "bthd"])
+def test_gradients_at_any_offset(io, layout):
+    """Contiguous upstream gradients that do not start on 16 bytes, against aligned copies."""
+    B, HK, H, T, d = 2, 1, 2, 70, 64
+    x, up = make(B, HK, H, T, d, d, io, seed=91)
+    code = e2ttt.DT_BF16 if io == "bf16" else e2ttt.DT_F32
+    cfg = e2ttt.DeltaConfig(B, HK, H, T, d, d, code, 0.125)
+    t = {n: a.requires_grad_(True) for n, a in to_dev(x, io, layout).items()}
+    u = to_dev(up, io)
+    out, w_out = e2ttt.DeltaFunction.apply(cfg, *[t[n] for n in NAMES])
+    grads = lambda a, b: torch.autograd.grad([out, w_out], list(t.values()), [a, b], retain_graph=True)
+    ref = grads(u["d_out"], u["d_w_out"])
+    for n in (1, 3, 8):
+        off = shifted(u["d_out"], n), shifted(u["d_w_out"], n)
+        for got in (grads(*off), grads(off[0], u["d_w_out"]), grads(u["d_out"], off[1])):
+            assert all(torch.equal(a, b) for a, b in zip(got, ref)), n
+    qk = e2ttt.QKConfig(B, H, HK, T, d, d, code)
+    f, _ = e2ttt.rotary_frequencies(d)
+    q, k = [t[n].detach().requires_grad_(True) for n in ("v", "k")]
+    qo, ko = e2ttt.QKFunction.apply(qk, q, k, f)
+    grads = lambda a, b: torch.autograd.grad([qo, ko], [q, k], [a, b], retain_graph=True)
+    d_k = u["d_out"][:, :1].contiguous()
+    ref = grads(u["d_out"], d_k)
+    for n in (1, 3, 8):
+        for got in (grads(shifted(u["d_out"], n), shifted(d_k, n)), grads(u["d_out"], shifted(d_k, n))):
+            assert all(torch.equal(a, b) for a, b in zip(got, ref)), n
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+def test_gradients_through_a_concatenation(io):
+    """A loss over one tensor of several parts hands back views at odd offsets."""
+    c = (1, 1, 1, 70, 32, 32)
+    x, _ = make(*c, io, seed=92)
+    cfg = e2ttt.DeltaConfig(*c, e2ttt.DT_BF16 if io == "bf16" else e2ttt.DT_F32, 1.0)
+    t = {n: a.requires_grad_(True) for n, a in to_dev(x, io).items()}
+    aux = torch.ones(1, dtype=t["q"].dtype, device="cuda")
+    out, w_out = e2ttt.DeltaFunction.apply(cfg, *[t[n] for n in NAMES])
+    weight = torch.randn(1 + out.numel(), device="cuda").to(out.dtype)
+    state = torch.randn(1 + w_out.numel(), device="cuda")
+    loss = (torch.cat([aux, out.flatten()]) * weight).sum().float() + \
+        (torch.cat([aux.float(), w_out.flatten()]) * state).sum()
+    got = torch.autograd.grad(loss, list(t.values()), retain_graph=True)
+    ref = torch.autograd.grad([out, w_out], list(t.values()),
+                              [weight[1:].clone().view_as(out), state[1:].clone().view_as(w_out)])
+    assert all(torch.equal(a, b) for a, b in zip(got, ref))
