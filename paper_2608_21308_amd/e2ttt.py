@@ -780,7 +780,15 @@ def delta_step(cfg: DeltaConfig, q, k, v, eta, log_gamma, w, *, slots=None, out=
 
 class DeltaFunction(torch.autograd.Function):
     """Autograd wrapper of the gated delta rule: (out, w_out) of (cfg, q, k, v,
-    eta, log_gamma, w_in, lengths); the forward saves the workspace."""
+    eta, log_gamma, w_in, lengths); the forward saves the workspace where a
+    gradient may be asked for."""
+
+    @classmethod
+    def apply(cls, cfg, q, k, v, eta, log_gamma=None, w_in=None, lengths=None):
+        if torch.is_grad_enabled() and any(isinstance(t, torch.Tensor) and t.requires_grad
+                                           for t in (q, k, v, eta, log_gamma, w_in)):
+            return super().apply(cfg, q, k, v, eta, log_gamma, w_in, lengths)
+        return delta_forward(cfg, q, k, v, eta, log_gamma, w_in, lengths=lengths)[:2]
 
     @staticmethod
     def forward(ctx, cfg, q, k, v, eta, log_gamma=None, w_in=None, lengths=None):

@@ -71,3 +71,37 @@ def test_gradients_through_a_concatenation(io):
     ref = torch.autograd.grad([out, w_out], list(t.values()),
                               [weight[1:].clone().view_as(out), state[1:].clone().view_as(w_out)])
     assert all(torch.equal(a, b) for a, b in zip(got, ref))
+
+
+def test_nothing_saved_without_a_gradient():
+    """Where no gradient can be asked for, the wrapper's call keeps nothing for one."""
+    c = (1, 4, 4, 8192, 64, 64)
+    cfg = e2ttt.DeltaConfig(*c, e2ttt.DT_BF16, 0.125)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    rn = lambda *s: torch.randn(*s, device="cuda", generator=g)
+    unit = lambda a: (a / a.norm(dim=-1, keepdim=True)).bfloat16()
+    q, k, v = unit(rn(*c[:1], 4, 8192, 64)), unit(rn(*c[:1], 4, 8192, 64)), rn(1, 4, 8192, 64).bfloat16()
+    rest = torch.sigmoid(rn(1, 4, 8192)), -0.1 * torch.rand(1, 4, 8192, device="cuda", generator=g), \
+        rn(1, 4, 64, 64)
+
+    def peak(v):
+        torch.cuda.synchronize()
+        torch.cuda.reset_peak_memory_stats()
+        before = torch.cuda.memory_allocated()
+        got = e2ttt.DeltaFunction.apply(cfg, q, k, v, *rest)
+        return got, torch.cuda.max_memory_allocated() - before
+
+    need = e2ttt.delta_workspace_bytes(cfg, True)
+    leaf = v.clone().requires_grad_(True)
+    ref, used = peak(leaf)
+    assert used >= need and ref[0].requires_grad and ref[1].requires_grad
+    plain, used = peak(v)
+    assert used < need
+    with torch.no_grad():
+        quiet, also = peak(leaf)
+    assert also < need
+    for got in (plain, quiet):
+        assert not got[0].requires_grad and not got[1].requires_grad
+        assert torch.equal(got[0], ref[0]) and torch.equal(got[1], ref[1])
+    (dv,) = torch.autograd.grad(ref[0].float().sum(), leaf)
+    assert torch.isfinite(dv).all()
