@@ -351,8 +351,9 @@ e2ttt_status e2ttt_apply_ln(const e2ttt_desc* desc, const float* ln_weight, cons
  * with 0 <= eta <= 1 (eta |k|^2 <= 2): beyond that the rule itself diverges.
  *
  * Layouts: q, k [B][HK][T][dk] and v, out [B][H][T][dv] in desc.io; eta and
- * log_gamma [B][H][T] f32 (log_gamma NULL: gamma = 1; -inf clears the state); states [B][H][dv][dk] f32,
- * contiguous.  Token tensors and gates may have any non-negative strides
+ * log_gamma [B][H][T] f32; states [B][H][dv][dk] f32, contiguous.  log_gamma
+ * NULL: gamma = 1; -inf clears a finite state; growth (above 0) is taken while
+ * its sums over neighbouring tokens stay below 88, where exp leaves fp32.  Token tensors and gates may have any non-negative strides
  * (e2ttt_delta_strides, in elements; the last dimension is contiguous), for
  * example those of a projection's [B][T][H][d]; strides NULL means C order.
  * Rows of the io type start on 16 bytes, tokens are at most 2^23 elements

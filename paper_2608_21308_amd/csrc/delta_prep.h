@@ -93,9 +93,9 @@ __device__ __forceinline__ void prep_chunk(const DeltaArgs& a, int r0, int nr, l
     const bool ok = lane < nt;
     const float eta = ok ? *row_of<float>(a.eta, b, h, t0 + lane) : 0.0f;
     float gm = ok && a.gam.p ? *row_of<float>(a.gam, b, h, t0 + lane) : 0.0f;
-    // exp(-104) is below half the smallest fp32 number: as good as exp(-inf),
-    // and differences of sums stay finite (a NaN stays NaN)
-    gm = gm < -104.0f ? -104.0f : gm;
+    // -10^4 is as good as -inf (63 gates of at most e^88 each do not lift the sum back to
+    // what fp32 holds), and differences of sums stay finite (a NaN stays NaN)
+    gm = gm < -1e4f ? -1e4f : gm;
     double s = gm;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
