@@ -3,6 +3,7 @@ import pytest
 import torch
 
 from paper_2608_21308_amd import e2ttt
+from tests import deltaref
 from tests.test_gpu_delta import close, make, to_dev
 
 pytestmark = pytest.mark.gpu
@@ -43,3 +44,29 @@ def test_decays_to_nothing_and_back(io):
     close("d_log_gamma", g["d_log_gamma"][:, 0] * big, (left * dot).expand(1, 100), "f32")
     for a in (out[:, 1, 20:], w_out[:, 1], g["d_w_in"][:, 1], g["d_log_gamma"][:, 1]):
         assert (a == 0).all()
+
+
+def test_gates_of_the_framework():
+    """The gate parameterisation's eta and gamma drive the rule through log(gamma)."""
+    c = (2, 1, 2, 100, 32, 32)
+    x, d = make(*c, "f32", seed=97)
+    gen = torch.Generator().manual_seed(5)
+    logits = [torch.randn(2, 2, 100, generator=gen) for _ in range(3)]
+    params = dict(eta_base=0.9, alpha_base=0.5, tau=32.0)
+    cfg = e2ttt.DeltaConfig(*c, e2ttt.DT_F32, 0.25)
+    t, td = to_dev(x, "f32"), to_dev(d, "f32")
+    leaves = [a.cuda().requires_grad_(True) for a in (logits[0], logits[2])]
+    eta, _, gamma = e2ttt.GatesFunction.apply(e2ttt.GateParams(**params), leaves[0], logits[1].cuda(), leaves[1])
+    out, w_out = e2ttt.DeltaFunction.apply(cfg, t["q"], t["k"], t["v"], eta, gamma.log(), t["w_in"])
+    got = torch.autograd.grad([out, w_out], leaves, [td["d_out"], td["d_w_out"]])
+    ref = [logits[0].double().requires_grad_(True), logits[2].double().requires_grad_(True)]
+    r_eta = 0.9 * torch.sigmoid(ref[0])
+    r_gamma = 1 - r_eta * 0.5 * torch.sigmoid(ref[1])
+    ro, rw = deltaref.delta(x["q"], x["k"], x["v"], r_eta, r_gamma.log(), x["w_in"], 0.25)
+    want = torch.autograd.grad([ro, rw], ref, [d["d_out"], d["d_w_out"]])
+    # (gates to 2e-6 of their values and gradients to 1e-5, as their own tests ask)
+    for n, a, b, tol in (("out", out, ro, 1e-5), ("w_out", w_out, rw, 1e-5), ("d_l_eta", got[0], want[0], 4e-5),
+                         ("d_l_alpha", got[1], want[1], 4e-5)):
+        err = ((a.detach().double().cpu() - b.detach()).norm() / b.detach().norm()).item()
+        print("%-10s rel %.2e" % (n, err), flush=True)
+        assert err <= tol, (n, err)
