@@ -51,21 +51,30 @@ constexpr size_t kCacheBytes = (size_t)128 << 20, kStretchBytes = (size_t)512 <<
 
 // Segments that `nch` chunks of U units run as (1: none).  A wave holds 16 value
 // channels of a unit, and the card takes 2048 such waves at once (`room`: how
-// many times the units fit).  Segments cost a pass over dv + dk channels ahead of
-// the one over dv, so they pay where the units' own workgroups leave more than
-// two thirds of the 256 CUs idle (64 units, 32 chunks: a training step of 128 x 128
-// 575 us against 600, of 64 x 64 257 against 298, of 32 x 64 220 against 233) and
-// not beyond (128 units of 64 x 64, 64 chunks: 378 us against 295; a step of 128
-// of 32 x 32: 317 against 282).  n of them take (nch / n) (t_state + t_chain) + n
-// t_join, about 5 us and 1 us: least at n = sqrt(5 nch).  They begin at 8 chunks
-// with bf16 (32 units of 64: 36 us against 37, at 6 chunks 33 against 31), at 6
-// with the slower fp32 products (8 units of 64: 41 us against 51).
+// many times the units fit).  n segments take (nch / n) (t_state + t_chain) + n
+// t_join, about 5 us and 1 us: least at n = sqrt(5 nch).
+//
+// They cost a pass over dv + dk channels ahead of the one over dv, so they pay
+// where the units' own workgroups leave more than two thirds of the 256 CUs idle,
+// three quarters with heads of 128, whose pass takes them twice over (a training
+// step, with segments and without: 64 units of 64 x 64, 32 chunks, 275 us and 315; of
+// 128 x 128 620 and 625, 128 chunks 2.25 ms and 2.42; 80 of 128, 32 chunks, 746 us and
+// 687; 128 units of 64, 64 chunks, forward 407 and 352), and with bf16 where the
+// chain is long beside what the pass adds to each of its workgroups (48 units of 128:
+// 17 chunks 330 us and 300, 32 chunks 502 and 534; 80 of 64: 8 chunks 134 and 109, 17
+// 206 and 197, 32 331 and 348; 64 of 64, 17 chunks, 181 and 185; 80 of 32: 8 chunks 92
+// and 88, 17 135 and 153).  fp32 products are slower: four waves a workgroup at 128 too
+// (32 units, 17 chunks: 467 us and 508; 48: 650 and 575), and short chains pay (48 units
+// of 64, 8 chunks: 139 and 160; 80: 219 and 183).  Chains begin at 8 chunks with bf16 (32
+// units of 64: 39 us and 41, 6 chunks 35 and 34), at 6 with fp32 (8 units of 64: 41 and 51).
 long room(const e2ttt_delta_desc* d, long U) { return 2048 / (U * (delta_dvp(d->dv) / 16)); }
 long segments(const e2ttt_delta_desc* d, long U, long nch) {
-  const int nw = delta_dkp(d->dk) > 64 ? 8 : 4;
+  const bool bf = d->io == E2TTT_DT_BF16;
+  const int dkp = delta_dkp(d->dk), nw = bf && dkp > 64 ? 8 : 4;
   const long groups = U * ((delta_dvp(d->dv) / 16 + nw - 1) / nw);
   const long n = std::min(std::min(room(d, U), nch / 2), (long)sqrt(5.0 * nch));
-  return groups > 80 || n < 3 || nch < (d->io == E2TTT_DT_BF16 ? 8 : 6) ? 1 : n;
+  if (groups > (dkp > 64 ? 64 : 80) || groups > nch * (bf ? 256 / dkp : 8)) return 1;
+  return n < 3 || nch < (bf ? 8 : 6) ? 1 : n;
 }
 
 // Chunks of a part (bf16, dk in 33..64): where the chain's workgroups leave CUs

@@ -208,3 +208,18 @@ def test_launches_of_more_than_32_bits_of_threads(lib):
     assert lib.e2ttt_delta_scratch_bytes(ctypes.byref(ddesc(**big))) == 0
     assert calls(lib, ddesc(**big))[1] == 3
     assert qcalls(lib, qdesc(B=1 << 14, T=1 << 14, H=1, HK=0, rot=2)) == (3, 3)
+
+
+def test_segments_by_their_first_pass(lib):
+    """The pass that segments cost beside the chain is as wide as values and keys together:
+    short chains of many units run without them (no room is asked for the segments' states),
+    heads of 128 sooner than those of 64."""
+    def each(B, T, d):
+        return lib.e2ttt_delta_workspace_bytes(ctypes.byref(ddesc(B=B, HK=1, H=1, T=T, dk=d, dv=d)), 0) / B
+
+    plain = each(96, 1088, 128)
+    assert abs(each(80, 1088, 128) - plain) < 1024 and abs(each(48, 1088, 128) - plain) < 1024
+    assert each(32, 1088, 128) > plain + (1 << 18) and each(64, 8192, 128) > each(96, 8192, 128) + (1 << 18)
+    plain = each(96, 1088, 64)
+    assert abs(each(80, 1088, 64) - plain) < 1024 and each(64, 1088, 64) > plain + (1 << 16)
+    assert abs(each(80, 512, 64) - each(96, 512, 64)) < 1024 and each(80, 2048, 64) > each(96, 2048, 64) + (1 << 16)
