@@ -44,10 +44,10 @@ size_t up(size_t x) { return (x + 255) & ~(size_t)255; }
 
 // Gates and fragments of this many bytes are formed and used at a time.  What
 // one launch writes the next reads from the 256 MB last-level cache while it
-// is well below that (512 units of 64, 16 chunks: 222 us with 128 MB, 263 at
-// once); segments want long stretches instead, which they divide (16 units of
-// 128, 512 chunks: 795 us at once, 927 in four).
-constexpr size_t kCacheBytes = (size_t)128 << 20, kStretchBytes = (size_t)512 << 20;
+// is well below that (512 units of 64, 16 chunks: 267 us with 160 MB, 281 with 128,
+// 299 at once); segments want long stretches instead, which they divide (16 units
+// of 128, 512 chunks: 812 us at once, 902 in three).
+constexpr size_t kCacheBytes = (size_t)160 << 20, kStretchBytes = (size_t)512 << 20;
 
 // Segments that `nch` chunks of U units run as (1: none).  A wave holds 16 value
 // channels of a unit, and the card takes 2048 such waves at once (`room`: how
