@@ -448,8 +448,12 @@ e2ttt_status e2ttt_delta_step(const e2ttt_delta_desc* desc, const e2ttt_delta_st
  *                   rot_scale its factor on the turned elements, else 1)
  *   positions [B][T] int64   NULL: 0 .. T - 1; angles are formed in 64 bits
  * Outputs may be the inputs themselves (same strides).  Strides as for the
- * delta calls.  Supported: d <= 256, a multiple of 8, either io type, 10^9
- * rows, fewer where rot / 2 is odd (32 d threads' worth; E2TTT_ERR_UNSUPPORTED).
+ * delta calls.  Supported: d <= 256, a multiple of 8, either io type, up to 10^9
+ * rows, and B T ceil((H + HK) / 8) L < 2^32 - 255 (else E2TTT_ERR_UNSUPPORTED).  L,
+ * the lanes of a row, is d / (2 V) rounded up to a power of two, 64 at most; V, the
+ * elements of an access, is the largest of 8 (bf16), 4, 2 and 1 that divides rot / 2.
+ * (One head of bf16, d = rot = 128: 2^29 rows are too many.  An odd rot / 2 is
+ * taken an element at a time: half as long again as its neighbours.)
  */
 #define E2TTT_QK_SILU 0x1u
 #define E2TTT_QK_UNIT 0x2u

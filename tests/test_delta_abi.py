@@ -223,3 +223,22 @@ def test_segments_by_their_first_pass(lib):
     plain = each(96, 1088, 64)
     assert abs(each(80, 1088, 64) - plain) < 1024 and each(64, 1088, 64) > plain + (1 << 16)
     assert abs(each(80, 512, 64) - each(96, 512, 64)) < 1024 and each(80, 2048, 64) > each(96, 2048, 64) + (1 << 16)
+
+
+@pytest.mark.parametrize("kw,rows", [
+    (dict(H=1, HK=0, d=128, rot=128, io=1), 1 << 29), (dict(H=1, HK=0, d=64, rot=64, io=0), 1 << 29),
+    (dict(H=1, HK=0, d=256, rot=256, io=1), 1 << 28), (dict(H=2, HK=1, d=256, rot=6, io=1), 1 << 26),
+    (dict(H=1, HK=0, d=16, rot=2, io=1), 1 << 29)])
+def test_qk_lanes_of_a_launch(lib, kw, rows):
+    """The documented limit of rows times lanes, from both sides (a null pointer, looked at
+    behind the descriptor, ends the calls below it)."""
+    h = kw["rot"] // 2
+    v = next(v for v in ((8,) if kw["io"] else ()) + (4, 2, 1) if h % v == 0)
+    lanes = 1
+    while lanes < min(64, -(-kw["d"] // (2 * v))):
+        lanes *= 2
+    assert rows * lanes * -(-(kw["H"] + kw["HK"]) // 8) == 1 << 32
+    assert qcalls(lib, qdesc(B=1 << 10, T=rows >> 10, **kw)) == (3, 3)
+    below = ctypes.byref(qdesc(B=1, T=rows - 256 // lanes, **kw))
+    assert lib.e2ttt_qk_forward(below, None, *([None] * 6), None) == 1
+    assert lib.e2ttt_qk_backward(below, None, *([None] * 8), None) == 1
