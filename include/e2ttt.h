@@ -464,7 +464,7 @@ typedef struct {
   int32_t d, rot;       /* head dim, elements that turn              */
   int32_t io;           /* e2ttt_dtype                               */
   uint32_t flags;       /* E2TTT_QK_*                                */
-  float eps;            /* > 0 with E2TTT_QK_UNIT                    */
+  float eps;            /* at least 2^-126 with E2TTT_QK_UNIT        */
   float rot_scale;
 } e2ttt_qk_desc;
 

@@ -331,7 +331,9 @@ e2ttt_status check_desc(const e2ttt_qk_desc* d) {
   if (d->B <= 0 || d->H <= 0 || d->HK < 0 || d->T <= 0 || d->d <= 0 || d->rot < 0 ||
       d->rot > d->d || d->rot % 2)
     return E2TTT_ERR_BAD_SHAPE;
-  if (!isfinite(d->rot_scale) || ((d->flags & E2TTT_QK_UNIT) && !(isfinite(d->eps) && d->eps > 0.0f)))
+  // (the reciprocal root of a smaller number is infinite, and a row of zeros times it NaN)
+  if (!isfinite(d->rot_scale) ||
+      ((d->flags & E2TTT_QK_UNIT) && !(isfinite(d->eps) && d->eps >= 1.17549435e-38f)))
     return E2TTT_ERR_BAD_SHAPE;
   if ((d->io != E2TTT_DT_F32 && d->io != E2TTT_DT_BF16) || (d->flags & ~kFlags) || d->d % 8 ||
       d->d > 256 || (double)d->B * d->T * ((double)d->H + d->HK) > 1e9)

@@ -242,3 +242,11 @@ def test_qk_lanes_of_a_launch(lib, kw, rows):
     below = ctypes.byref(qdesc(B=1, T=rows - 256 // lanes, **kw))
     assert lib.e2ttt_qk_forward(below, None, *([None] * 6), None) == 1
     assert lib.e2ttt_qk_backward(below, None, *([None] * 8), None) == 1
+
+
+def test_qk_eps_is_a_normal_number(lib):
+    """A subnormal eps gave NaN for a row of zeros."""
+    assert qcalls(lib, qdesc(eps=1e-40)) == (2, 2) and qcalls(lib, qdesc(eps=-1.0)) == (2, 2)
+    r = ctypes.byref(qdesc(eps=2.0 ** -126))
+    assert lib.e2ttt_qk_forward(r, None, *([None] * 6), None) == 1
+    assert lib.e2ttt_qk_forward(ctypes.byref(qdesc(eps=1e-40, flags=1)), None, *([None] * 6), None) == 1

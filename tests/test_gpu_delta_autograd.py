@@ -105,3 +105,27 @@ def test_nothing_saved_without_a_gradient():
         assert torch.equal(got[0], ref[0]) and torch.equal(got[1], ref[1])
     (dv,) = torch.autograd.grad(ref[0].float().sum(), leaf)
     assert torch.isfinite(dv).all()
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+def test_broadcast_inputs(io):
+    """Inputs expanded over sequences, heads or tokens (strides of 0) give what their copies
+    give, gradients of the leaves among them."""
+    B, HK, H, T, d = 2, 1, 2, 90, 32
+    dt = torch.bfloat16 if io == "bf16" else torch.float32
+    cfg = e2ttt.DeltaConfig(B, HK, H, T, d, d, e2ttt.DT_BF16 if io == "bf16" else e2ttt.DT_F32, 1.0)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    rn = lambda *s: torch.randn(*s, device="cuda", generator=g)
+    unit = lambda x: x / x.norm(dim=-1, keepdim=True)
+    leaves = [a.requires_grad_(True) for a in (
+        unit(rn(1, 1, T, d)).to(dt), unit(rn(B, 1, 1, d)).to(dt), rn(B, 1, T, d).to(dt),
+        torch.sigmoid(rn(1, H, 1)), -torch.sigmoid(rn(B, 1, T)))]
+    shapes = [(B, HK, T, d)] * 2 + [(B, H, T, d)] + [(B, H, T)] * 2
+
+    def step(copy):
+        a = [t.expand(s) for t, s in zip(leaves, shapes)]
+        assert not any(t.is_contiguous() for t in a)
+        out, w = e2ttt.DeltaFunction.apply(cfg, *[t.contiguous() if copy else t for t in a])
+        return [out, w, *torch.autograd.grad((out.float() ** 2).sum() + w.sum(), leaves)]
+
+    assert all(torch.equal(a, b) for a, b in zip(step(False), step(True)))

@@ -66,3 +66,12 @@ def test_sines_and_cosines(interleaved):
         err = (got - ref).abs().max().item()
         print("%s %.2e" % (name, err), flush=True)
         assert err <= 2.0 ** -23, name
+
+
+def test_rows_of_zeros_at_the_smallest_eps():
+    cfg = e2ttt.QKConfig(1, 1, 0, 1, 8, 0, e2ttt.DT_F32, e2ttt.QK_SILU | e2ttt.QK_UNIT, eps=2.0 ** -126)
+    q = torch.zeros(1, 1, 1, 8, device="cuda")
+    assert (e2ttt.qk_forward(cfg, q, None)[0] == 0).all()
+    dx, _ = e2ttt.qk_backward(cfg, torch.ones_like(q), None, q)
+    # (half of 2^63: an ulp of the reciprocal root, of the reciprocal and two roundings)
+    assert ((dx / 2.0 ** 62 - 1).abs() <= 4 * 2.0 ** -23).all()
