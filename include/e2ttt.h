@@ -353,7 +353,9 @@ e2ttt_status e2ttt_apply_ln(const e2ttt_desc* desc, const float* ln_weight, cons
  * Layouts: q, k [B][HK][T][dk] and v, out [B][H][T][dv] in desc.io; eta and
  * log_gamma [B][H][T] f32; states [B][H][dv][dk] f32, contiguous.  log_gamma
  * NULL: gamma = 1; -inf clears a finite state; growth (above 0) is taken while
- * its sums over neighbouring tokens stay below 88, where exp leaves fp32.  Token tensors and gates may have any non-negative strides
+ * its sums over neighbouring tokens stay below 88, where exp leaves fp32.  (The
+ * chunk calls and e2ttt_gates_forward have gamma itself: its logarithm goes here.)
+ * Token tensors and gates may have any non-negative strides
  * (e2ttt_delta_strides, in elements; the last dimension is contiguous), for
  * example those of a projection's [B][T][H][d]; strides NULL means C order.
  * Rows of the io type start on 16 bytes, tokens are at most 2^23 elements
@@ -366,11 +368,12 @@ e2ttt_status e2ttt_apply_ln(const e2ttt_desc* desc, const float* ln_weight, cons
  * B H up to 1.9 million units (more of dv <= 64) and 10^9 chunks of 64 tokens,
  * 7.8 million to train (else E2TTT_ERR_UNSUPPORTED).
  *
- * Precision: fp32 throughout, bf16 outputs rounded once (with bf16 tensors, fp32
- * values enter the matrix products as sums of three bf16 numbers, which lose
- * nothing).  Within a chunk of 64 tokens
- * (0..63, 64..127, ...) a token with a non-finite value may make the outputs
- * of its whole chunk non-finite, as it does those after it.
+ * Precision: fp32 throughout, bf16 outputs rounded once.  (With bf16 tensors an
+ * fp32 value enters the matrix products as the sum of three bf16 numbers, which
+ * loses nothing; of a product of two such values at most 2^-23 is left out.)
+ * Within a chunk of 64 tokens (0..63, 64..127, ...) a token with a non-finite
+ * value may make the outputs of its whole chunk non-finite, as it does those
+ * after it.
  */
 typedef struct { int64_t b, h, t; } e2ttt_strides;
 

@@ -80,10 +80,10 @@ long segments(const e2ttt_delta_desc* d, long U, long nch) {
 // Chunks of a part (bf16, dk in 33..64): where the chain's workgroups leave CUs
 // idle but are too many for segments, a launch takes a part of the chain beside
 // the preparation of the next part, in the backward beside the gradients of the
-// part before.  128 units of 64, 64 chunks: 289 us against 311, a training step
-// 787 against 806 (96 units: 656 against 714, of 256 chunks 2.39 ms against 2.78;
-// 192: 1092 us against 1061).  Launches cost some 10 us, so a part has 16 chunks at
-// least (160 units, 64 chunks: 317 us, with parts of 8 334) and there are at most
+// part before.  128 units of 64, 64 chunks: 329 us against 358, a training step
+// 823 against 852 (96 units: 681 against 744, of 256 chunks 2.43 ms against 2.96;
+// 192: 1169 us against 1161).  Launches cost some 10 us, so a part has 16 chunks at
+// least (160 units, 64 chunks: 338 us, with parts of 8 399) and there are at most
 // eight.
 long part_of(const e2ttt_delta_desc* d, long U, long nch, long nseg) {
   const long groups = U * ((delta_dvp(d->dv) + 63) / 64);

@@ -9,7 +9,7 @@
 // sum over the value dimension (delta_grads.hip).  Long chains of few units run
 // as segments (delta_fwd.hip): a segment with the transition F takes the
 // adjoint at its end to dW F^T + B at its start.  256 units of 64, 64 chunks: 295
-// us, 5.2 TB/s of the 93 KB that a chunk moves; 128 units 250 us, 3.9 us a chunk.
+// us, 5.2 TB/s of the 93 KB that a chunk moves; 128 units 237 us, 3.7 us a chunk.
 #include "delta_grads.h"
 
 namespace e2ttt {
@@ -285,7 +285,7 @@ hipError_t launch_delta_chain_bwd(const DeltaArgs& a, bool bf, bool state, hipSt
   if (bf) {
     if (dkp == 32) return go<true, 32, 2>(a, state, s);
     if (dkp == 64) return go<true, 64, 4>(a, state, s);
-    // (as in the forward; a step of 256 units of 128, 16 chunks: 810 us, with four 822)
+    // (as in the forward; a step of 256 units of 128, 16 chunks, takes 870 us with either)
     if ((long)a.B * a.H * a.nseg * ((a.dvp / 16 + 7) / 8) <= 128) return go<true, 128, 4>(a, state, s);
     return go<true, 128, 8>(a, state, s);
   }

@@ -14,9 +14,9 @@
 // global loads are issued before the current one's products.
 //
 // With 256 units of 64 and more it is bound by HBM (saving: 101 KB a chunk, 64
-// chunks in 408 us, 4.1 TB/s; matrix units busy for 14 %, vector units for 18 %);
-// with fewer by one chunk's chain of dependent products and conversions, at dk =
-// 64 3.5 us saving and 3.0 us without, at 128 and two waves a SIMD 7.4 us.
+// chunks in 443 us, 3.8 TB/s; matrix units busy for 16 %, vector units for 18 %);
+// with fewer by one chunk's chain of dependent products and conversions, with 128
+// units of dk = 64 3.9 us saving and 3.7 us without, of 128 and two waves a SIMD 7.5.
 //
 // A chain is as long as its sequence, and few units leave most of the card
 // idle.  The chunks then run as segments: what a segment makes of a state is
@@ -336,9 +336,9 @@ hipError_t launch_delta_chain(const DeltaArgs& a, bool bf, bool save, bool state
   if (bf) {
     if (dkp == 32) return go<true, 32, 2>(a, save, state, s);
     if (dkp == 64) return go<true, 64, 4>(a, save, state, s);
-    // eight waves share a staged chunk (256 units of 128, 16 chunks: 184 us, with
-    // four 239); four where eight would leave half of the 256 CUs idle (128 units,
-    // 32 chunks: 241 us, with eight 249; saving, a step 870 and 914)
+    // eight waves share a staged chunk (256 units of 128, 16 chunks: 165 us, with
+    // four 224); four where eight would leave half of the 256 CUs idle (128 units,
+    // 32 chunks: 209 us, with eight 240; saving, a step 914 and 997)
     const long tiles = a.dvp / 16 + (state ? 8 : 0);
     if ((long)a.B * a.H * a.nseg * ((tiles + 7) / 8) <= 128) return go<true, 128, 4>(a, save, state, s);
     return go<true, 128, 8>(a, save, state, s);

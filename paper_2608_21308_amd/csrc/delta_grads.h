@@ -1,6 +1,6 @@
 // Gated delta rule, the gradients of a chunk that sum over the value
-// dimension, every chunk at once: one workgroup of eight waves per chunk of 64
-// tokens and key head, over the value heads that share it in turn.  With W_0,
+// dimension, every chunk at once: one workgroup per chunk of 64 tokens and key
+// head, over the value heads that share it in turn.  With W_0,
 // U from the forward and dW (chunk end), Y from the backward chain:
 //   A_ij = s D_ij (dO_i . U_j)   (j <= i),   N_ij = -eta_i D_ij (Y_i . U_j)  (j < i)
 //   dQ = s G dO W_0 + A K
@@ -21,10 +21,10 @@
 // waves up to DK = 64, so that two workgroups share a CU and one computes while
 // the other waits; eight, and one workgroup a CU, at 128.
 //
-// 16384 chunks of dk = dv = 64 (112 KB each) take 550 us, 3.3 TB/s: the waves wait
-// for 40 % of it, for the next block and for each other, and issue vector
-// instructions for half of it (registers and 77 KB of LDS leave two workgroups a
-// CU).  8192 of 128: 770 us.
+// 16384 chunks of dk = dv = 64 (112 KB each) take 559 us, 3.3 TB/s: a wave waits
+// for 30 % of it, for the next block and for the others, and the two of a SIMD issue
+// vector instructions for 60 % of it (registers and 77 KB of LDS leave two
+// workgroups a CU).  8192 of 128: 800 us.
 #pragma once
 
 #include "delta_common.h"

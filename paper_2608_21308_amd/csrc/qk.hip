@@ -11,11 +11,13 @@
 // gradient) and written once.  An item is the two pieces of V elements that hold V whole
 // pairs (p and p + rot / 2 of a half layout, neighbours otherwise), so a pair
 // never leaves its lane; V is the widest that divides rot / 2 (16 bytes for
-// the usual head).  The lanes of a row sum by shuffles.  A group of lanes
+// the usual head; an odd rot / 2 goes element by element, tail included: 8 x 4096
+// tokens of 16 + 16 heads of 128 take 204 and 303 us with rot = 34, 143 and 199 with
+// 32).  The lanes of a row sum by shuffles.  A group of lanes
 // keeps its angles' sines and cosines over several heads of a token.  Angles
 // are reduced in 64 bits: a far position times a frequency loses its fraction
-// of a turn in 32.  8 x 4096 tokens of 16 + 16 heads of 64: 54 us forward, 77
-// backward, 5.0 and 5.3 TB/s, the rate of a large copy.
+// of a turn in 32.  8 x 4096 tokens of 16 + 16 heads of 64: 55 us forward, 76
+// backward, 4.9 and 5.3 TB/s, the rate of a large copy.
 #include <math.h>
 
 #include "delta_common.h"
