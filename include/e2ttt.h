@@ -488,6 +488,61 @@ e2ttt_status e2ttt_qk_backward(const e2ttt_qk_desc* desc, const e2ttt_qk_strides
                                const int64_t* positions, const void* d_q_out,
                                const void* d_k_out, void* dq, void* dk, void* stream);
 
+/*
+ * Attention, the branch beside the state rules: per sequence, query head and
+ * query t, at position p = t + S - T (the last query is at the last key), over
+ * the keys j that it sees, p - left <= j <= p + right (a negative bound: none;
+ * right = 0 is causal, left = W - 1 a window of W tokens):
+ *   P_j = exp(scale q_t . k_j - lse_t),  o_t = sum_j P_j v_j,
+ *   lse_t = log sum_j exp(scale q_t . k_j)
+ * A query that sees no key has o = 0 and lse = -inf.  H query heads share HK key
+ * heads in groups: query head h reads the keys and values of key head h / (H / HK).
+ *   q, out [B][H][T][d], k, v [B][HK][S][d] io   strides as for the delta calls
+ *   lse [B][H][T] f32, contiguous                NULL in the forward: not wanted
+ *   lengths [B] int32 (device; NULL: all T)      of sequence b the first lengths[b]
+ *               (clamped to 0..T) queries and the first lengths[b] + S - T keys are
+ *               live; what lies behind is not read, its outputs and gradients are
+ *               written as zero and its lse as -inf
+ * scale is positive.  Outputs do not overlap inputs.  Supported: d <= 128, a multiple
+ * of 8, either io type, T and S up to 2^29, and B H ceil(T / 128), B HK ceil(S / 128)
+ * below 2^24 (else E2TTT_ERR_UNSUPPORTED).
+ *
+ * Precision: scores, softmax and sums in fp32.  With bf16 tensors P and dS are
+ * rounded to bf16 once as operands of the products that follow (half a step of
+ * 2^-8 each, of either sign), and outputs once.  A query's results depend on live
+ * values only; a non-finite live key or value may make those of queries within 64
+ * tokens of seeing it non-finite too.  Results do not change from run to run.
+ */
+typedef struct {
+  int32_t B;            /* sequences                            */
+  int32_t HK, H;        /* key heads, query heads (a multiple)  */
+  int32_t T, S;         /* queries, keys                        */
+  int32_t d;            /* head dim                             */
+  int32_t io;           /* e2ttt_dtype                          */
+  float scale;
+  int32_t left, right;  /* bounds of what a query sees          */
+} e2ttt_attn_desc;
+
+typedef struct {
+  e2ttt_strides q, k, v, out;
+  e2ttt_strides d_out, dq, dk, dv;
+} e2ttt_attn_strides;
+
+e2ttt_status e2ttt_attn_forward(const e2ttt_attn_desc* desc, const e2ttt_attn_strides* strides,
+                                const void* q, const void* k, const void* v,
+                                const int32_t* lengths, void* out, float* lse, void* stream);
+
+/* Backward of  sum <d_out, out> + <d_lse, lse>  (d_lse [B][H][T] NULL: zero; not
+ * read where lse is -inf) with the forward's inputs, out and lse.  The
+ * probabilities are computed again; dk and dv are summed over the query heads of
+ * a group.  scratch: e2ttt_attn_scratch_bytes bytes (0 for a bad descriptor). */
+size_t e2ttt_attn_scratch_bytes(const e2ttt_attn_desc* desc);
+e2ttt_status e2ttt_attn_backward(const e2ttt_attn_desc* desc, const e2ttt_attn_strides* strides,
+                                 const void* q, const void* k, const void* v,
+                                 const int32_t* lengths, const void* out, const float* lse,
+                                 const void* d_out, const float* d_lse, void* dq, void* dk,
+                                 void* dv, void* scratch, size_t scratch_bytes, void* stream);
+
 /* Static description of a status code. */
 const char* e2ttt_status_str(e2ttt_status status);
 

@@ -1,0 +1,268 @@
+// Attention, backward: the probabilities are formed again from the scores and lse,
+// once by queries for dq and once by keys for dk and dv, so that every sum stays in
+// its wave's registers and no order of atomics enters the results (seven products
+// where five would do with sums in memory):
+//   by queries: S^T = K Q^T, U^T = V do^T, dS^T = P^T o (U^T - D), dq^T += K^T dS^T
+//   by keys:    S = Q K^T, U = do V^T, dv^T += do^T P, dk^T += Q^T dS.
+// The first also leaves D = sum do o - d_lse and the exponents' part of lse for the
+// second.  P and dS are rounded
+// to the io type as operands (bf16: half a step each, of either sign); all sums and
+// the scores are fp32.
+#include <math.h>
+
+#include "attn_common.h"
+
+namespace e2ttt {
+namespace {
+
+// -lse log2 e, -inf for a query that sees nothing: its 2^(..) are then all zero.
+__device__ __forceinline__ float exponent_of(float lse) {
+  return lse == kNegInf ? kNegInf : -lse * kLog2e;
+}
+
+template <bool BF, int D, int BK>
+__global__ void __launch_bounds__(256, BF ? 2 : 1) attn_dq_kernel(AttnArgs a, int ntile) {
+  using O = MOp<BF>;
+  using E = typename O::E;
+  using X = typename O::X;
+  using A = ATile<BF, D>;
+  constexpr int KS = D / 16, NM = D / 32;
+  __shared__ __align__(16) E lk[2][BK * D];
+  __shared__ __align__(16) E lv[2][BK * D];
+  const int lane = threadIdx.x & 63, w = wave_id(), h = lane >> 5, c = lane & 31;
+  const long id = xcd_order(blockIdx.x, gridDim.x);
+  const int tile = ntile - 1 - (int)(id % ntile);
+  const long u = id / ntile;
+  const int b = (int)(u / a.H), hq = (int)(u % a.H), hk = hq / (a.H / a.HK);
+  const int off = a.S - a.T, live = live_of(a, b), end = live + off;
+  const int t0 = tile * 128, tw = t0 + 32 * w, t = tw + c;
+  const bool on = t < live;
+
+  X q[KS], g[KS];
+  const E* qrow = on ? row_of<E>(a.q, b, hq, t) : nullptr;
+  const E* grow = on ? row_of<E>(a.d_out, b, hq, t) : nullptr;
+  const E* orow = on ? row_of<E>(a.out, b, hq, t) : nullptr;
+  float dot = 0.0f;
+#pragma unroll
+  for (int s = 0; s < KS; ++s) {
+    q[s] = row_frag<BF>(qrow, 16 * s + 8 * h, a.d);
+    g[s] = row_frag<BF>(grow, 16 * s + 8 * h, a.d);
+    const X o = row_frag<BF>(orow, 16 * s + 8 * h, a.d);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      if constexpr (BF) dot = fmaf((float)g[s].v[j], (float)o.v[j], dot);
+      else dot = fmaf(j < 4 ? g[s].a[j & 3] : g[s].b[j & 3], j < 4 ? o.a[j & 3] : o.b[j & 3], dot);
+    }
+  }
+  dot = both_sum(dot);
+  const long at = ((long)b * a.H + hq) * a.T + t;
+  float ex = kNegInf;
+  if (on) {
+    ex = exponent_of(a.lse[at]);
+    if (a.d_lse && ex != kNegInf) dot -= a.d_lse[at];
+  }
+  if (t < a.T && h == 0) {
+    a.ex[at] = ex;
+    a.delta[at] = dot;
+  }
+
+  f32x16 o[NM];
+#pragma unroll
+  for (int m = 0; m < NM; ++m) o[m] = zero16();
+  const float cs = a.scale * kLog2e;
+  const int p0 = t0 + off, p1 = min(t0 + 128, live) + off;
+  const int lo = a.left < 0 ? 0 : max(0, p0 - a.left);
+  const int hi = t0 >= live ? lo : a.right < 0 ? end : min(end, p1 + a.right);
+  const int pw0 = tw + off, pw1 = min(tw + 32, live) + off, p = pw0 + c;
+  const int wlo = a.left < 0 ? 0 : max(0, pw0 - a.left);
+  const int whi = tw >= live ? wlo : a.right < 0 ? end : min(end, pw1 + a.right);
+
+  Stage<BF, D, BK, 4> sk, sv;
+  sk.init(a.k.t, a.d, w, lane);
+  sv.init(a.v.t, a.d, w, lane);
+  const E* kb = row_of<E>(a.k, b, hk, 0);
+  const E* vb = row_of<E>(a.v, b, hk, 0);
+  if (lo < hi) {
+    sk.load(lk[0], kb + lo * a.k.t, end - lo, w);
+    sv.load(lv[0], vb + lo * a.v.t, end - lo, w);
+  }
+  int cur = 0;
+  for (int j0 = lo; j0 < hi; j0 += BK, cur ^= 1) {
+    staged();
+    if (j0 + BK < hi) {
+      sk.load(lk[cur ^ 1], kb + (j0 + BK) * a.k.t, end - j0 - BK, w);
+      sv.load(lv[cur ^ 1], vb + (j0 + BK) * a.v.t, end - j0 - BK, w);
+    }
+    if (j0 + BK <= wlo || j0 >= whi) continue;
+    const bool cut = j0 + BK > end || (a.left >= 0 && j0 < pw1 - 1 - a.left) ||
+                     (a.right >= 0 && j0 + BK - 1 > pw0 + a.right);
+    const int k0 = a.left < 0 ? 0 : p - a.left;
+    const int k1 = a.right < 0 ? end : min(end, p + a.right + 1);
+#pragma unroll
+    for (int n = 0; n < BK / 32; ++n) {
+      f32x16 s = zero16(), v = zero16();
+#pragma unroll
+      for (int x = 0; x < KS; ++x) {
+        s = O::mm(s, A::rows(lk[cur], 32 * n + c, x, h), q[x]);
+        v = O::mm(v, A::rows(lv[cur], 32 * n + c, x, h), g[x]);
+      }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        float e = __builtin_amdgcn_exp2f(fmaf(s[i], cs, ex)) * (v[i] - dot);
+        if (cut) {
+          const int j = j0 + 32 * n + row_in(i, h);
+          if (j < k0 || j >= k1) e = 0.0f;
+        }
+        s[i] = e;
+      }
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const X f = O::of(s, x);
+#pragma unroll
+        for (int m = 0; m < NM; ++m)
+          o[m] = O::mm(o[m], A::rows_t(lk[cur], 32 * n + 16 * x, m, h, c), f);
+      }
+    }
+  }
+  if (t >= a.T) return;
+  E* drow = row_of_w<E>(a.dq, b, hq, t);
+  const float f = on ? a.scale : 0.0f;
+#pragma unroll
+  for (int m = 0; m < NM; ++m) st_tile<BF>(drow, o[m], f, m, h, a.d);
+}
+
+template <bool BF, int D, int BQ>
+__global__ void __launch_bounds__(256, BF && D <= 64 ? 2 : 1) attn_dkv_kernel(AttnArgs a, int ntile) {
+  using O = MOp<BF>;
+  using E = typename O::E;
+  using X = typename O::X;
+  using A = ATile<BF, D>;
+  constexpr int KS = D / 16, NM = D / 32;
+  __shared__ __align__(16) E lq[2][BQ * D];
+  __shared__ __align__(16) E lg[2][BQ * D];
+  __shared__ __align__(16) float lx[2][2][64];          // exponents and D of the queries
+  const int lane = threadIdx.x & 63, w = wave_id(), h = lane >> 5, c = lane & 31;
+  const long id = xcd_order(blockIdx.x, gridDim.x);
+  const int tile = (int)(id % ntile);
+  const long u = id / ntile;
+  const int b = (int)(u / a.HK), hk = (int)(u % a.HK), rep = a.H / a.HK;
+  const int off = a.S - a.T, live = live_of(a, b), end = live + off;
+  const int j0 = tile * 128, jw = j0 + 32 * w, j = jw + c;
+
+  X k[KS], v[KS];
+  const E* krow = j < end ? row_of<E>(a.k, b, hk, j) : nullptr;
+  const E* vrow = j < end ? row_of<E>(a.v, b, hk, j) : nullptr;
+#pragma unroll
+  for (int s = 0; s < KS; ++s) {
+    k[s] = row_frag<BF>(krow, 16 * s + 8 * h, a.d);
+    v[s] = row_frag<BF>(vrow, 16 * s + 8 * h, a.d);
+  }
+  f32x16 dk[NM], dv[NM];
+#pragma unroll
+  for (int m = 0; m < NM; ++m) {
+    dk[m] = zero16();
+    dv[m] = zero16();
+  }
+  const float cs = a.scale * kLog2e;
+  // queries that see a key of the workgroup, of this wave, of this lane: p >= j - right,
+  // p <= j + left
+  const int j1 = min(j0 + 128, end), jw1 = min(jw + 32, end);
+  const int lo = a.right < 0 ? 0 : max(0, j0 - a.right - off);
+  const int hi = j0 >= end ? lo : a.left < 0 ? live : min(live, j1 + a.left - off);
+  const int wlo = a.right < 0 ? 0 : max(0, jw - a.right - off);
+  const int whi = jw >= end ? wlo : a.left < 0 ? live : min(live, jw1 + a.left - off);
+  const int q0 = a.right < 0 ? 0 : j - a.right - off;
+  const int q1 = j >= end ? 0 : a.left < 0 ? live : min(live, j + a.left - off + 1);
+
+  Stage<BF, D, BQ, 4> sq, sg;
+  sq.init(a.q.t, a.d, w, lane);
+  sg.init(a.d_out.t, a.d, w, lane);
+  const int per = hi > lo ? (hi - lo + BQ - 1) / BQ : 0;
+  auto fetch = [&](int r, int t, int to) {
+    const int hq = hk * rep + r;
+    sq.load(lq[to], row_of<E>(a.q, b, hq, t), live - t, w);
+    sg.load(lg[to], row_of<E>(a.d_out, b, hq, t), live - t, w);
+    // (queries behind the live ones: q, do and D are zero, and so is what they add)
+    const long at = ((long)b * a.H + hq) * a.T + t;
+    if (w < 2) stage64(lx[to][w], (w ? a.delta : a.ex) + at, min(live - t, BQ), lane);
+  };
+  int r = 0, t0 = lo, cur = 0;
+  if (per) fetch(0, lo, 0);
+  for (long it = (long)per * rep; it > 0; --it, cur ^= 1) {
+    staged();
+    const int tt = t0;
+    t0 += BQ;
+    if (t0 >= hi) {
+      t0 = lo;
+      ++r;
+    }
+    if (it > 1) fetch(r, t0, cur ^ 1);
+    if (tt + BQ <= wlo || tt >= whi) continue;
+    const bool cut = jw + 32 > end || (a.right >= 0 && tt + off < jw + 31 - a.right) ||
+                     (a.left >= 0 && tt + BQ - 1 + off > jw + a.left);
+#pragma unroll
+    for (int n = 0; n < BQ / 32; ++n) {
+      f32x16 s = zero16(), x = zero16();
+#pragma unroll
+      for (int y = 0; y < KS; ++y) {
+        s = O::mm(s, A::rows(lq[cur], 32 * n + c, y, h), k[y]);
+        x = O::mm(x, A::rows(lg[cur], 32 * n + c, y, h), v[y]);
+      }
+#pragma unroll
+      for (int i4 = 0; i4 < 4; ++i4) {
+        const f32x4 ex = *reinterpret_cast<const f32x4*>(&lx[cur][0][32 * n + 8 * i4 + 4 * h]);
+        const f32x4 de = *reinterpret_cast<const f32x4*>(&lx[cur][1][32 * n + 8 * i4 + 4 * h]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int y = 4 * i4 + i;
+          float p = __builtin_amdgcn_exp2f(fmaf(s[y], cs, ex[i]));
+          float ds = p * (x[y] - de[i]);
+          if (cut) {
+            const int t = tt + 32 * n + row_in(y, h);
+            const bool seen = t >= q0 && t < q1;
+            p = seen ? p : 0.0f;
+            ds = seen ? ds : 0.0f;
+          }
+          s[y] = p;
+          x[y] = ds;
+        }
+      }
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+        const X pf = O::of(s, y), df = O::of(x, y);
+#pragma unroll
+        for (int m = 0; m < NM; ++m) {
+          dv[m] = O::mm(dv[m], A::rows_t(lg[cur], 32 * n + 16 * y, m, h, c), pf);
+          dk[m] = O::mm(dk[m], A::rows_t(lq[cur], 32 * n + 16 * y, m, h, c), df);
+        }
+      }
+    }
+  }
+  if (j >= a.S) return;
+  E* dkr = row_of_w<E>(a.dk, b, hk, j);
+  E* dvr = row_of_w<E>(a.dv, b, hk, j);
+#pragma unroll
+  for (int m = 0; m < NM; ++m) {
+    st_tile<BF>(dkr, dk[m], a.scale, m, h, a.d);
+    st_tile<BF>(dvr, dv[m], 1.0f, m, h, a.d);
+  }
+}
+
+template <bool BF, int D, int BK>
+hipError_t go(const AttnArgs& a, hipStream_t s) {
+  const int nq = (a.T + 127) / 128, nk = (a.S + 127) / 128;
+  hipLaunchKernelGGL((attn_dq_kernel<BF, D, BK>), dim3((unsigned)((long)a.B * a.H * nq)), dim3(256),
+                     0, s, a, nq);
+  hipLaunchKernelGGL((attn_dkv_kernel<BF, D, BK>), dim3((unsigned)((long)a.B * a.HK * nk)),
+                     dim3(256), 0, s, a, nk);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_attn_backward(const AttnArgs& a, bool bf, hipStream_t s) {
+  if (bf) return a.d <= 32 ? go<true, 32, 64>(a, s) : a.d <= 64 ? go<true, 64, 64>(a, s) : go<true, 128, 64>(a, s);
+  return a.d <= 32 ? go<false, 32, 64>(a, s) : a.d <= 64 ? go<false, 64, 64>(a, s) : go<false, 128, 32>(a, s);
+}
+
+}  // namespace e2ttt

@@ -1,0 +1,144 @@
+// Attention, forward: a wave holds 32 queries (as columns of the transposed scores)
+// and passes once over the keys that they see, with the running maximum m and sum
+// l of the softmax per query in a lane:
+//   S^T = K Q^T,  P^T = 2^(c (S^T - m)),  O^T <- O^T 2^(c (m_old - m)) + V^T P^T,
+// c = scale log2 e.  P is rounded to the io type for the second product (bf16: half
+// a step of 2^-8 each, of either sign, averaged over the keys; the sum l is of the
+// unrounded ones).
+#include <math.h>
+
+#include "attn_common.h"
+
+namespace e2ttt {
+namespace {
+
+template <bool BF, int D, int BK>
+__global__ void __launch_bounds__(256, BF ? 2 : 1) attn_fwd_kernel(AttnArgs a, int ntile) {
+  using O = MOp<BF>;
+  using E = typename O::E;
+  using X = typename O::X;
+  using A = ATile<BF, D>;
+  constexpr int NT = BK / 32, KS = D / 16, NM = D / 32;
+  __shared__ __align__(16) E lk[2][BK * D];
+  __shared__ __align__(16) E lv[2][BK * D];
+  const int lane = threadIdx.x & 63, w = wave_id(), h = lane >> 5, c = lane & 31;
+  const long id = xcd_order(blockIdx.x, gridDim.x);
+  const int tile = ntile - 1 - (int)(id % ntile);      // (long rows of a causal mask first)
+  const long u = id / ntile;
+  const int b = (int)(u / a.H), hq = (int)(u % a.H), hk = hq / (a.H / a.HK);
+  const int off = a.S - a.T, live = live_of(a, b), end = live + off;
+  const int t0 = tile * 128, tw = t0 + 32 * w, t = tw + c;
+
+  X q[KS];
+  const E* qrow = t < live ? row_of<E>(a.q, b, hq, t) : nullptr;
+#pragma unroll
+  for (int s = 0; s < KS; ++s) q[s] = row_frag<BF>(qrow, 16 * s + 8 * h, a.d);
+
+  f32x16 o[NM];
+#pragma unroll
+  for (int m = 0; m < NM; ++m) o[m] = zero16();
+  float top = kNegInf, sum = 0.0f;
+  const float cs = a.scale * kLog2e;
+
+  // keys that some query of the workgroup, of this wave sees
+  const int p0 = t0 + off, p1 = min(t0 + 128, live) + off;
+  const int lo = a.left < 0 ? 0 : max(0, p0 - a.left);
+  const int hi = t0 >= live ? lo : a.right < 0 ? end : min(end, p1 + a.right);
+  const int pw0 = tw + off, pw1 = min(tw + 32, live) + off, p = pw0 + c;
+  const int wlo = a.left < 0 ? 0 : max(0, pw0 - a.left);
+  const int whi = tw >= live ? wlo : a.right < 0 ? end : min(end, pw1 + a.right);
+
+  Stage<BF, D, BK, 4> sk, sv;
+  sk.init(a.k.t, a.d, w, lane);
+  sv.init(a.v.t, a.d, w, lane);
+  const E* kb = row_of<E>(a.k, b, hk, 0);
+  const E* vb = row_of<E>(a.v, b, hk, 0);
+  if (lo < hi) {
+    sk.load(lk[0], kb + lo * a.k.t, end - lo, w);
+    sv.load(lv[0], vb + lo * a.v.t, end - lo, w);
+  }
+  int cur = 0;
+  for (int j0 = lo; j0 < hi; j0 += BK, cur ^= 1) {
+    staged();
+    if (j0 + BK < hi) {
+      sk.load(lk[cur ^ 1], kb + (j0 + BK) * a.k.t, end - j0 - BK, w);
+      sv.load(lv[cur ^ 1], vb + (j0 + BK) * a.v.t, end - j0 - BK, w);
+    }
+    if (j0 + BK <= wlo || j0 >= whi) continue;
+    f32x16 s[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      s[n] = zero16();
+#pragma unroll
+      for (int x = 0; x < KS; ++x) s[n] = O::mm(s[n], A::rows(lk[cur], 32 * n + c, x, h), q[x]);
+    }
+    if (j0 + BK > end || (a.left >= 0 && j0 < pw1 - 1 - a.left) ||
+        (a.right >= 0 && j0 + BK - 1 > pw0 + a.right)) {
+      const int k0 = a.left < 0 ? 0 : p - a.left;
+      const int k1 = a.right < 0 ? end : min(end, p + a.right + 1);
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int j = j0 + 32 * n + row_in(i, h);
+          if (j < k0 || j >= k1) s[n][i] = kNegInf;
+        }
+    }
+    float most = s[0][0];
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) most = fmaxf(most, s[n][i]);
+    most = fmaxf(top, both_max(most));
+    const float ref = most == kNegInf ? 0.0f : most;     // (no key so far)
+    const float shrink = __builtin_amdgcn_exp2f((top - ref) * cs);
+    top = most;
+    sum *= shrink;
+#pragma unroll
+    for (int m = 0; m < NM; ++m)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[m][i] *= shrink;
+    const float off2 = -ref * cs;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        s[n][i] = __builtin_amdgcn_exp2f(fmaf(s[n][i], cs, off2));
+        sum += s[n][i];
+      }
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const X pf = O::of(s[n], x);
+#pragma unroll
+        for (int m = 0; m < NM; ++m)
+          o[m] = O::mm(o[m], A::rows_t(lv[cur], 32 * n + 16 * x, m, h, c), pf);
+      }
+    }
+  }
+  if (t >= a.T) return;
+  sum = both_sum(sum);
+  const float inv = t < live && sum > 0.0f ? 1.0f / sum : 0.0f;
+  E* orow = row_of_w<E>(a.out, b, hq, t);
+#pragma unroll
+  for (int m = 0; m < NM; ++m) st_tile<BF>(orow, o[m], inv, m, h, a.d);
+  if (a.lse && h == 0)
+    a.lse[((long)b * a.H + hq) * a.T + t] =
+        inv > 0.0f ? fmaf(top, a.scale, logf(sum)) : kNegInf;
+}
+
+template <bool BF, int D, int BK>
+hipError_t go(const AttnArgs& a, hipStream_t s) {
+  const int ntile = (a.T + 127) / 128;
+  hipLaunchKernelGGL((attn_fwd_kernel<BF, D, BK>), dim3((unsigned)((long)a.B * a.H * ntile)),
+                     dim3(256), 0, s, a, ntile);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_attn_forward(const AttnArgs& a, bool bf, hipStream_t s) {
+  if (bf) return a.d <= 32 ? go<true, 32, 64>(a, s) : a.d <= 64 ? go<true, 64, 64>(a, s) : go<true, 128, 64>(a, s);
+  return a.d <= 32 ? go<false, 32, 64>(a, s) : a.d <= 64 ? go<false, 64, 64>(a, s) : go<false, 128, 32>(a, s);
+}
+
+}  // namespace e2ttt

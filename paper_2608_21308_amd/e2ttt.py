@@ -40,7 +40,8 @@ EXPORTS = ("e2ttt_param_count", "e2ttt_workspace_bytes", "e2ttt_backward_scratch
            "e2ttt_chunk_forward_static", "e2ttt_chunk_forward_ln", "e2ttt_chunk_backward_ln",
            "e2ttt_apply_ln", "e2ttt_delta_workspace_bytes", "e2ttt_delta_scratch_bytes",
            "e2ttt_delta_forward", "e2ttt_delta_backward", "e2ttt_delta_step",
-           "e2ttt_qk_forward", "e2ttt_qk_backward", "e2ttt_status_str")
+           "e2ttt_qk_forward", "e2ttt_qk_backward", "e2ttt_attn_forward",
+           "e2ttt_attn_scratch_bytes", "e2ttt_attn_backward", "e2ttt_status_str")
 
 
 class E2TTTError(RuntimeError):
@@ -86,6 +87,15 @@ class QKDesc(ctypes.Structure):
 
 class QKStrides(ctypes.Structure):
     _fields_ = [(n, Strides) for n in ("q", "k", "q_out", "k_out", "d_q_out", "d_k_out", "dq", "dk")]
+
+
+class AttentionDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("B", "HK", "H", "T", "S", "d", "io")]
+    _fields_ += [("scale", ctypes.c_float), ("left", ctypes.c_int32), ("right", ctypes.c_int32)]
+
+
+class AttentionStrides(ctypes.Structure):
+    _fields_ = [(n, Strides) for n in ("q", "k", "v", "out", "d_out", "dq", "dk", "dv")]
 
 
 _lib = None
@@ -147,6 +157,13 @@ def load():
     lib.e2ttt_qk_forward.restype = i
     lib.e2ttt_qk_backward.argtypes = [qd, qs] + [vp] * 9
     lib.e2ttt_qk_backward.restype = i
+    ad, as_ = ctypes.POINTER(AttentionDesc), ctypes.POINTER(AttentionStrides)
+    lib.e2ttt_attn_forward.argtypes = [ad, as_] + [vp] * 7
+    lib.e2ttt_attn_forward.restype = i
+    lib.e2ttt_attn_scratch_bytes.argtypes = [ad]
+    lib.e2ttt_attn_scratch_bytes.restype = sz
+    lib.e2ttt_attn_backward.argtypes = [ad, as_] + [vp] * 12 + [sz, vp]
+    lib.e2ttt_attn_backward.restype = i
     lib.e2ttt_status_str.argtypes = [i]
     lib.e2ttt_status_str.restype = ctypes.c_char_p
     _lib = lib
@@ -994,3 +1011,118 @@ def _qk_grads(ctx, d_q, d_k):
     else:
         dq, dk = qk_backward(cfg, d_q, d_k, q, k, inv_freq, positions)
     return None, dq, dk, None, None
+
+
+# ------------------------------------------------------------------ attention
+@dataclass(frozen=True)
+class AttentionConfig:
+    """Attention of H query heads that share HK key heads: T queries, the last of
+    them at the last of S keys (0: T); a query at position p sees the keys
+    p - left .. p + right (negative: no bound)."""
+    B: int
+    HK: int
+    H: int
+    T: int
+    d: int
+    io: int = DT_BF16
+    S: int = 0
+    scale: float = 1.0
+    left: int = -1
+    right: int = 0
+
+    def desc(self) -> AttentionDesc:
+        return AttentionDesc(self.B, self.HK, self.H, self.T, self.S or self.T, self.d, self.io,
+                             self.scale, self.left, self.right)
+
+    @cached_property
+    def _call(self):
+        """The descriptor by reference, the io type and the tensors' shapes."""
+        return (ctypes.byref(self.desc()), torch.bfloat16 if self.io == DT_BF16 else torch.float32,
+                torch.Size((self.B, self.H, self.T, self.d)),
+                torch.Size((self.B, self.HK, self.S or self.T, self.d)),
+                torch.Size((self.B, self.H, self.T)))
+
+    def __getstate__(self):
+        return {n: v for n, v in self.__dict__.items() if n != "_call"}
+
+
+@_on_device
+def attention_forward(cfg: AttentionConfig, q, k, v, *, lengths=None, out=None, lse=None):
+    """Runs e2ttt_attn_forward on the current stream: attention of q [B, H, T, d]
+    over k, v [B, HK, S, d] (any strides with a contiguous last dimension) over
+    the first lengths [B] (int32) tokens of each sequence.  Returns (out, lse);
+    out has q's order in memory, lse [B, H, T] is float32."""
+    d, io, s_q, s_k, s_l = cfg._call
+    dev = q.get_device()
+    if out is None:
+        out = torch.empty_like(q)
+    if lse is None:
+        lse = torch.empty(s_l, dtype=torch.float32, device=q.device)
+    st = _layout(AttentionStrides, dev, ("q", q, s_q, io), ("k", k, s_k, io), ("v", v, s_k, io),
+                 ("out", out, s_q, io))
+    _plain("lse", lse, s_l, torch.float32, dev)
+    _plain("lengths", lengths, s_l[:1], torch.int32, dev)
+    st = (_lib or load()).e2ttt_attn_forward(d, st, q.data_ptr(), k.data_ptr(), v.data_ptr(),
+                                             _ptr(lengths), out.data_ptr(), lse.data_ptr(), _stream())
+    if st:
+        _check(st, "e2ttt_attn_forward")
+    return out, lse
+
+
+def attention_scratch_bytes(cfg: AttentionConfig) -> int:
+    return int((_lib or load()).e2ttt_attn_scratch_bytes(cfg._call[0]))
+
+
+@_on_device
+def attention_backward(cfg: AttentionConfig, q, k, v, out, lse, d_out, d_lse=None, *, lengths=None,
+                       grads=None, scratch=None):
+    """Runs e2ttt_attn_backward with the outputs of attention_forward; returns a
+    dict of gradients (dq, dk, dv)."""
+    d, io, s_q, s_k, s_l = cfg._call
+    dev = q.get_device()
+    g = grads if grads is not None else dict(dq=_like(q), dk=_like(k), dv=_like(v))
+    st = _layout(AttentionStrides, dev, ("q", q, s_q, io), ("k", k, s_k, io), ("v", v, s_k, io),
+                 ("out", out, s_q, io), ("d_out", d_out, s_q, io), ("dq", g["dq"], s_q, io),
+                 ("dk", g["dk"], s_k, io), ("dv", g["dv"], s_k, io))
+    _plain("lse", lse, s_l, torch.float32, dev)
+    _plain("d_lse", d_lse, s_l, torch.float32, dev)
+    _plain("lengths", lengths, s_l[:1], torch.int32, dev)
+    _buffer("scratch", scratch, dev)
+    if scratch is None:
+        scratch = torch.empty(attention_scratch_bytes(cfg), dtype=torch.uint8, device=q.device)
+    st = (_lib or load()).e2ttt_attn_backward(
+        d, st, q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(lengths), out.data_ptr(),
+        lse.data_ptr(), d_out.data_ptr(), _ptr(d_lse), g["dq"].data_ptr(), g["dk"].data_ptr(),
+        g["dv"].data_ptr(), scratch.data_ptr(), scratch.numel(), _stream())
+    _check(st, "e2ttt_attn_backward")
+    return g
+
+
+def _like(t):
+    """A new tensor of t's order in memory, or C order where t repeats elements."""
+    x = torch.empty_like(t)
+    return x if x.stride(-1) == 1 else torch.empty(t.shape, dtype=t.dtype, device=t.device)
+
+
+class AttentionFunction(torch.autograd.Function):
+    """Autograd wrapper of attention: (out, lse) of (cfg, q, k, v, lengths)."""
+
+    @staticmethod
+    def forward(ctx, cfg, q, k, v, lengths=None):
+        out, lse = attention_forward(cfg, q, k, v, lengths=lengths)
+        ctx.cfg = cfg
+        ctx.save_for_backward(q, k, v, lengths, out, lse)
+        ctx.set_materialize_grads(False)
+        return out, lse
+
+    @staticmethod
+    def backward(ctx, d_out, d_lse):
+        return _once(_attention_grads, ctx, d_out, d_lse)
+
+
+def _attention_grads(ctx, d_out, d_lse):
+    q, k, v, lengths, out, lse = ctx.saved_tensors
+    d_out = torch.zeros_like(out) if d_out is None else _as_rows(d_out)
+    g = attention_backward(ctx.cfg, q, k, v, out, lse, d_out,
+                           None if d_lse is None else d_lse.contiguous(), lengths=lengths)
+    return None, g["dq"], g["dk"], g["dv"], None

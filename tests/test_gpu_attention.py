@@ -1,0 +1,214 @@
+"""GPU parity of attention and its gradients with 64 bits (tests/attnref.py),
+element by element within the bounds derived there, and in the 2-norm: with bf16
+a result passes two roundings of rms at most 2^-8 / sqrt(3) each (its operand's,
+its own), so 2^-8 of the whole; a gradient of queries or keys a third one, of the
+out that D is formed from: 1.5 2^-8.  With float32 the errors behind the
+elements' bounds have either sign: 2^-18."""
+import math
+
+import pytest
+import torch
+
+from paper_2608_21308_amd import e2ttt
+from tests import attnref
+from tests.test_gpu_delta import dev
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _lib():
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    e2ttt.load()
+
+
+def rounded(x, io):
+    return x.to(torch.bfloat16 if io == "bf16" else torch.float32).double()
+
+
+def inputs(B, HK, H, T, S, d, io, seed, lengths=None, size=1.0):
+    """q, k, v, d_out in float64 at the io type's values; what is not live is NaN."""
+    g = torch.Generator().manual_seed(seed)
+    rn = lambda h, t: rounded(size * torch.randn(B, h, t, d, generator=g, dtype=torch.float64), io)
+    x = dict(q=rn(H, T), k=rn(HK, S), v=rn(HK, S))
+    d_out = rn(H, T)
+    if lengths is not None:
+        for b, n in enumerate(lengths.clamp(0, T).tolist()):
+            x["q"][b, :, n:] = math.nan
+            d_out[b, :, n:] = math.nan
+            for m in ("k", "v"):
+                x[m][b, :, max(0, n + S - T):] = math.nan
+    return x, d_out
+
+
+def within(name, got, ref, bound, norm):
+    got = got.detach().double().cpu()
+    assert got.shape == ref.shape and torch.equal(torch.isinf(got), torch.isinf(ref)), name
+    fin = torch.isfinite(ref)
+    err = (got - ref)[fin].abs()
+    rel = (err.norm() / ref[fin].norm().clamp(min=1e-30)).item()
+    worst = (err / bound[fin].clamp(min=1e-37)).max().item() if err.numel() else 0.0
+    print("%-4s rel %.2e, of the bound %.2f" % (name, rel, worst), flush=True)
+    assert not torch.isnan(got).any(), name
+    assert (err <= bound[fin] + 1e-37).all(), (name, worst)
+    # (a query that sees one key has P = 1 and dS = u - D = 0: what is left of such gradients
+    # is rounding alone, held to the elements' bounds)
+    if ref[fin].norm() > bound[fin].norm() and ref[fin].numel() >= 256:
+        assert rel <= norm, (name, rel)
+
+
+CASES = [  # B, HK, H, T, S, d, left, right
+    (1, 1, 1, 1, 1, 8, -1, 0), (2, 1, 3, 1, 200, 64, -1, 0), (1, 2, 2, 5, 3, 16, -1, 0),
+    (2, 2, 4, 33, 33, 64, 0, 0), (1, 1, 2, 129, 129, 128, 64, 0), (2, 1, 1, 100, 163, 40, 31, 0),
+    (1, 2, 6, 260, 260, 72, -1, -1), (1, 1, 1, 150, 70, 32, 20, -1), (2, 2, 2, 65, 300, 96, 100, 7),
+    (1, 1, 5, 257, 257, 24, 1 << 30, 1), (1, 3, 3, 192, 192, 128, -1, 0), (1, 1, 1, 300, 300, 64, 63, 0),
+    (3, 1, 2, 64, 64, 120, 2147483647, 2147483647), (1, 1, 1, 40, 400, 16, 5, 0)]
+
+
+@pytest.mark.parametrize("c", CASES)
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+@pytest.mark.parametrize("ragged", [False, True])
+def test_forward_backward(c, io, ragged):
+    B, HK, H, T, S, d, left, right = c
+    print("attention", c, io, ragged, flush=True)
+    lengths = torch.tensor([T - 1, 0, T + 5][:B] if T > 1 else [0, 1, -3][:B]) if ragged else None
+    layout = "bthd" if ragged else "bhtd"
+    x, d_out = inputs(B, HK, H, T, S, d, io, d + T, lengths)
+    d_lse = torch.randn(B, H, T, generator=torch.Generator().manual_seed(1)).double() if ragged else None
+    sc = d ** -0.5
+    out, lse, ref, a = attnref.gradients(x, sc, left, right, lengths, d_out, d_lse)
+    bd = attnref.bounds(a, out, lse, sc, HK, io == "bf16")
+    cfg = e2ttt.AttentionConfig(B, HK, H, T, d, e2ttt.DT_BF16 if io == "bf16" else e2ttt.DT_F32, S=S,
+                                scale=sc, left=left, right=right)
+    t = {n: dev(v, io, layout) for n, v in x.items()}
+    tl = None if lengths is None else lengths.to(torch.int32).cuda()
+    o, l = e2ttt.attention_forward(cfg, t["q"], t["k"], t["v"], lengths=tl)
+    n1, n2 = (2.0 ** -8, 1.5 * 2.0 ** -8) if io == "bf16" else (2.0 ** -18, 2.0 ** -18)
+    within("out", o, out, bd["out"], n1)
+    within("lse", l, lse, bd["lse"], 2.0 ** -18)
+    g = e2ttt.attention_backward(cfg, t["q"], t["k"], t["v"], o, l, dev(d_out, io, layout),
+                                 None if d_lse is None else d_lse.float().cuda(), lengths=tl)
+    for n, lim in (("q", n2), ("k", n2), ("v", n1)):
+        within("d" + n, g["d" + n], ref[n], 1.01 * bd[n] + bd["own"] * ref[n].abs(), lim)
+
+
+def make(B, HK, H, T, S, d, io="bf16", seed=0, **kw):
+    x, d_out = inputs(B, HK, H, T, S, d, io, seed, size=kw.pop("size", 1.0))
+    cfg = e2ttt.AttentionConfig(B, HK, H, T, d, e2ttt.DT_BF16 if io == "bf16" else e2ttt.DT_F32, S=S,
+                                scale=kw.pop("scale", d ** -0.5), **kw)
+    return cfg, {n: dev(v, io, "bhtd") for n, v in x.items()}, dev(d_out, io, "bhtd"), x, d_out
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+def test_logits_far_apart(io):
+    """Scores of some hundreds: all but a few probabilities vanish, the sum stays one."""
+    cfg, t, tg, x, d_out = make(1, 1, 2, 140, 140, 64, io, size=6.0, scale=1.0)
+    out, lse, ref, a = attnref.gradients(x, 1.0, -1, 0, None, d_out)
+    bd = attnref.bounds(a, out, lse, 1.0, 1, io == "bf16")
+    o, l = e2ttt.attention_forward(cfg, t["q"], t["k"], t["v"])
+    within("out", o, out, bd["out"], math.inf)
+    within("lse", l, lse, bd["lse"], 2.0 ** -18)
+    g = e2ttt.attention_backward(cfg, t["q"], t["k"], t["v"], o, l, tg)
+    for n in "qkv":
+        within("d" + n, g["d" + n], ref[n], 1.01 * bd[n] + bd["own"] * ref[n].abs(), math.inf)
+
+
+def test_keys_that_rise():
+    """The running maximum grows with every tile of keys."""
+    T, d = 400, 64
+    x, d_out = inputs(1, 1, 1, T, T, d, "bf16", 5)
+    x["k"] = rounded(x["q"].mean(2, keepdim=True) + torch.linspace(0, 30, T, dtype=torch.float64)[:, None] *
+                     torch.ones(d, dtype=torch.float64) / d, "bf16")
+    x["q"] = rounded(x["q"] * 0.1 + 1.0, "bf16")
+    out, lse, a = attnref.attention(x, 1.0, -1, -1, None)
+    cfg = e2ttt.AttentionConfig(1, 1, 1, T, d, scale=1.0, right=-1)
+    o, l = e2ttt.attention_forward(cfg, *(dev(x[n], "bf16", "bhtd") for n in "qkv"))
+    bd = attnref.bounds(a, out, lse, 1.0, 1, True)
+    within("out", o, out, bd["out"], 2.0 ** -8)
+    within("lse", l, lse, bd["lse"], 2.0 ** -18)
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+def test_autograd_of_shared_and_broadcast_inputs(io):
+    """AttentionFunction: leaves used twice, keys that repeat over the batch, an
+    upstream gradient without storage of its own, out alone and lse alone."""
+    B, HK, H, T, d = 2, 2, 4, 70, 64
+    x, _ = inputs(B, HK, H, T, T, d, io, 11)
+    x["k"], x["v"] = x["k"][:1], x["v"][:1]
+    cfg = e2ttt.AttentionConfig(B, HK, H, T, d, e2ttt.DT_BF16 if io == "bf16" else e2ttt.DT_F32,
+                                scale=0.125, left=40)
+    t = {n: dev(v, io, "bhtd").requires_grad_(True) for n, v in x.items()}
+    wide = {n: v.expand(B, -1, -1, -1) for n, v in x.items()}
+    for which in ("out", "lse"):
+        out, lse = e2ttt.AttentionFunction.apply(cfg, t["q"], t["k"].expand(B, -1, -1, -1),
+                                                 t["v"].expand(B, -1, -1, -1))
+        (out if which == "out" else lse).sum().backward()
+        one = torch.ones(B, H, T, d, dtype=torch.float64)
+        g0 = one if which == "out" else 0 * one
+        o, l, ref, a = attnref.gradients(wide, 0.125, 40, 0, None, g0,
+                                         None if which == "out" else one[..., 0])
+        bd = attnref.bounds(a, o, l, 0.125, HK, io == "bf16")
+        for n in "qkv":
+            r, lim = ref[n], 1.01 * bd[n] + bd["own"] * ref[n].abs()
+            if n != "q":        # (two gradients rounded, added and rounded)
+                lim = lim.sum(0, keepdim=True) + (bd["own"] * r.abs()).sum(0, keepdim=True) * 1.02
+                r = r.sum(0, keepdim=True)
+            within("d" + n, t[n].grad, r, lim, math.inf)
+            t[n].grad = None
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+def test_strided_views(io):
+    """q, k, v as slices of one projection [B, T, (H + 2 HK) d], gradients into such a tensor."""
+    B, HK, H, T, d = 2, 2, 4, 90, 64
+    dt = torch.bfloat16 if io == "bf16" else torch.float32
+    g = torch.Generator().manual_seed(2)
+    qkv = torch.randn(B, T, (H + 2 * HK) * d, generator=g).to(dt).cuda()
+    cut = lambda t: (t[..., :H * d].unflatten(-1, (H, d)).transpose(1, 2),
+                     t[..., H * d:(H + HK) * d].unflatten(-1, (HK, d)).transpose(1, 2),
+                     t[..., (H + HK) * d:].unflatten(-1, (HK, d)).transpose(1, 2))
+    cfg = e2ttt.AttentionConfig(B, HK, H, T, d, e2ttt.DT_BF16 if io == "bf16" else e2ttt.DT_F32,
+                                scale=0.125, left=33)
+    q, k, v = cut(qkv)
+    d_out = torch.randn(B, H, T, d, generator=g).to(dt).cuda()
+    o1, l1 = e2ttt.attention_forward(cfg, q, k, v)
+    o2, l2 = e2ttt.attention_forward(cfg, *(x.contiguous() for x in (q, k, v)))
+    assert torch.equal(o1, o2) and torch.equal(l1, l2)
+    into = torch.full_like(qkv, math.nan)
+    dq, dk, dv = cut(into)
+    e2ttt.attention_backward(cfg, q, k, v, o1, l1, d_out, grads=dict(dq=dq, dk=dk, dv=dv))
+    ref = e2ttt.attention_backward(cfg, q.contiguous(), k.contiguous(), v.contiguous(), o2, l2, d_out)
+    assert torch.equal(dq, ref["dq"]) and torch.equal(dk, ref["dk"]) and torch.equal(dv, ref["dv"])
+
+
+def test_graph_and_other_stream():
+    """Forward and backward captured once and replayed on new inputs, between eager calls
+    on another stream: as the eager results, bit for bit."""
+    cfg, t, tg, _, _ = make(2, 2, 4, 200, 200, 64, seed=1, left=70)
+    out, lse = torch.empty_like(t["q"]), torch.empty(2, 4, 200, device="cuda")
+    grads = {"d" + n: torch.empty_like(t[n]) for n in "qkv"}
+    scratch = torch.empty(e2ttt.attention_scratch_bytes(cfg), dtype=torch.uint8, device="cuda")
+
+    def both():
+        e2ttt.attention_forward(cfg, t["q"], t["k"], t["v"], out=out, lse=lse)
+        e2ttt.attention_backward(cfg, t["q"], t["k"], t["v"], out, lse, tg, grads=grads, scratch=scratch)
+
+    both()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        both()
+    other = torch.cuda.Stream()
+    for i in range(4):
+        _, t2, tg2, _, _ = make(2, 2, 4, 200, 200, 64, seed=20 + i, left=70)
+        for n in "qkv":
+            t[n].copy_(t2[n])
+        tg.copy_(tg2)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(other):
+            o, l = e2ttt.attention_forward(cfg, t2["q"], t2["k"], t2["v"])
+            ref = e2ttt.attention_backward(cfg, t2["q"], t2["k"], t2["v"], o, l, tg2)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, o) and torch.equal(lse, l)
+        assert all(torch.equal(grads[n], ref[n]) for n in ref)
