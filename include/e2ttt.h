@@ -543,6 +543,85 @@ e2ttt_status e2ttt_attn_backward(const e2ttt_attn_desc* desc, const e2ttt_attn_s
                                  const void* d_out, const float* d_lse, void* dq, void* dk,
                                  void* dv, void* scratch, size_t scratch_bytes, void* stream);
 
+/*
+ * A cache of keys and values in 4 bits, by pages of 64 tokens, and attention over
+ * it: what serves the branch above a few tokens at a time.
+ *
+ * An element is one of 0, 0.5, 1, 1.5, 2, 3, 4, 6, with a sign, times a power of
+ * two for every 32 elements of a row: with m the largest magnitude among them, the
+ * least 2^e with m <= 7 2^e (and e >= -125).  Values are rounded to the nearest, ties
+ * to the one whose last bit is zero; every element is off by at most 2^e.  A
+ * block with a non-finite element reads back as NaN (one above 1.75 2^127 may read
+ * back infinite).
+ *
+ *   cache   [n_pages][HK][68 d] bytes, 16-byte aligned (e2ttt_cache_page_bytes a page).
+ *           A page holds, per key head and with NB = d / 32 (token 16 a + r, or
+ *           16 a + 4 g + i, with i, a, g in 0..3, r in 0..15):
+ *             codes of K   [64 tokens][4 g][NB][4]   channels 32 blk + 8 g + 2 byte
+ *                          (low half) and + 1, as sign, exponent, mantissa bits
+ *             scales of K  [NB][16 r][4 a]           e + 127 (255: NaN)
+ *             codes of V   [NB][16 pairs][4 g][4 a][4 i]  channels 32 blk + 2 pair, + 1
+ *             scales of V  [NB][4 g][4 a][4 i]
+ *   table   [B][pages] int32 (device): position p of sequence b is in page
+ *           table[b][(p / 64) mod pages], so that a window goes round a ring of
+ *           pages.  An entry outside 0..n_pages-1 is no page: what would be written
+ *           there is dropped, it reads as zeros and attention leaves it out.
+ *   starts  [B] int32 (device; NULL: 0): the position of a sequence's first token
+ *           in this call.  Tokens whose position is negative are none.
+ *   lengths [B] int32 (device; NULL: all T): tokens t < lengths[b] (clamped to 0..T)
+ *           of the call are live, at positions starts[b] + t.
+ * With end = starts[b] + lengths[b], a sequence holds the pages (end - 1) / 64 -
+ * pages + 1 .. (end - 1) / 64, one for each entry: of a longer call only the tokens
+ * on these are written, and positions before them are not seen.  Pages that a call
+ * writes to belong to one sequence (what two write at once is left undefined).
+ * Token tensors are as in the attention calls, any strides.  Supported: d = 32, 64, 96
+ * or 128, either io type, T up to 2^29 and pages to 2^25, at most 2^32 / 256
+ * workgroups (B HK (T / 4) (d / 8) threads, B HK ceil(H / HK T / 16) workgroups and as
+ * many parts; else E2TTT_ERR_UNSUPPORTED).
+ */
+typedef struct {
+  int32_t B;            /* sequences                                         */
+  int32_t HK, H;        /* key heads, query heads (a multiple; attend alone) */
+  int32_t T;            /* tokens of the call                                */
+  int32_t d;            /* head dim                                          */
+  int32_t pages;        /* entries of a sequence in the table                */
+  int32_t io;           /* e2ttt_dtype of the token tensors                  */
+  float scale;          /* of the logits, positive (attend alone)            */
+  int32_t left;         /* keys seen before a query (negative: all)          */
+} e2ttt_cache_desc;
+
+typedef struct { e2ttt_strides q, k, v, out; } e2ttt_cache_strides;
+
+/* Bytes of a page of all key heads (0: not supported). */
+size_t e2ttt_cache_page_bytes(int32_t HK, int32_t d);
+
+/* The live tokens' k, v [B][HK][T][d] into the cache. */
+e2ttt_status e2ttt_cache_write(const e2ttt_cache_desc* desc, const e2ttt_cache_strides* strides,
+                               const void* k, const void* v, const int32_t* starts,
+                               const int32_t* lengths, const int32_t* table, void* cache,
+                               int32_t n_pages, void* stream);
+
+/* The cache's values of the tokens into k, v [B][HK][T][d], zeros where it holds
+ * none; a sequence holds what it does after lengths[b] tokens from starts[b] on
+ * (the stretch that is read is taken to be its last). */
+e2ttt_status e2ttt_cache_read(const e2ttt_cache_desc* desc, const e2ttt_cache_strides* strides,
+                              const int32_t* starts, const int32_t* lengths, const int32_t* table,
+                              const void* cache, int32_t n_pages, void* k, void* v, void* stream);
+
+/* Attention of the call's tokens q [B][H][T][d], which e2ttt_cache_write has put
+ * into the cache before: the query at position p sees the positions p - left .. p
+ * that the sequence holds.  out [B][H][T][d], lse [B][H][T] f32 (NULL: not wanted);
+ * zeros and -inf for what is not live and where nothing is seen.  Meant for few
+ * tokens: each 16 queries of a key head read its pages once.  fp32 throughout,
+ * outputs rounded once.  workspace: e2ttt_cache_workspace_bytes bytes, not to be
+ * shared by calls that may overlap. */
+size_t e2ttt_cache_workspace_bytes(const e2ttt_cache_desc* desc);
+e2ttt_status e2ttt_cache_attend(const e2ttt_cache_desc* desc, const e2ttt_cache_strides* strides,
+                                const void* q, const int32_t* starts, const int32_t* lengths,
+                                const int32_t* table, const void* cache, int32_t n_pages,
+                                void* out, float* lse, void* workspace, size_t workspace_bytes,
+                                void* stream);
+
 /* Static description of a status code. */
 const char* e2ttt_status_str(e2ttt_status status);
 

@@ -41,7 +41,9 @@ EXPORTS = ("e2ttt_param_count", "e2ttt_workspace_bytes", "e2ttt_backward_scratch
            "e2ttt_apply_ln", "e2ttt_delta_workspace_bytes", "e2ttt_delta_scratch_bytes",
            "e2ttt_delta_forward", "e2ttt_delta_backward", "e2ttt_delta_step",
            "e2ttt_qk_forward", "e2ttt_qk_backward", "e2ttt_attn_forward",
-           "e2ttt_attn_scratch_bytes", "e2ttt_attn_backward", "e2ttt_status_str")
+           "e2ttt_attn_scratch_bytes", "e2ttt_attn_backward", "e2ttt_cache_page_bytes",
+           "e2ttt_cache_write", "e2ttt_cache_read", "e2ttt_cache_workspace_bytes",
+           "e2ttt_cache_attend", "e2ttt_status_str")
 
 
 class E2TTTError(RuntimeError):
@@ -96,6 +98,15 @@ class AttentionDesc(ctypes.Structure):
 
 class AttentionStrides(ctypes.Structure):
     _fields_ = [(n, Strides) for n in ("q", "k", "v", "out", "d_out", "dq", "dk", "dv")]
+
+
+class CacheDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("B", "HK", "H", "T", "d", "pages", "io")]
+    _fields_ += [("scale", ctypes.c_float), ("left", ctypes.c_int32)]
+
+
+class CacheStrides(ctypes.Structure):
+    _fields_ = [(n, Strides) for n in ("q", "k", "v", "out")]
 
 
 _lib = None
@@ -164,6 +175,17 @@ def load():
     lib.e2ttt_attn_scratch_bytes.restype = sz
     lib.e2ttt_attn_backward.argtypes = [ad, as_] + [vp] * 12 + [sz, vp]
     lib.e2ttt_attn_backward.restype = i
+    cd, cs, i32 = ctypes.POINTER(CacheDesc), ctypes.POINTER(CacheStrides), ctypes.c_int32
+    lib.e2ttt_cache_page_bytes.argtypes = [i32, i32]
+    lib.e2ttt_cache_page_bytes.restype = sz
+    lib.e2ttt_cache_write.argtypes = [cd, cs] + [vp] * 6 + [i32, vp]
+    lib.e2ttt_cache_write.restype = i
+    lib.e2ttt_cache_read.argtypes = [cd, cs] + [vp] * 4 + [i32] + [vp] * 3
+    lib.e2ttt_cache_read.restype = i
+    lib.e2ttt_cache_workspace_bytes.argtypes = [cd]
+    lib.e2ttt_cache_workspace_bytes.restype = sz
+    lib.e2ttt_cache_attend.argtypes = [cd, cs] + [vp] * 5 + [i32] + [vp] * 3 + [sz, vp]
+    lib.e2ttt_cache_attend.restype = i
     lib.e2ttt_status_str.argtypes = [i]
     lib.e2ttt_status_str.restype = ctypes.c_char_p
     _lib = lib
@@ -1126,3 +1148,135 @@ def _attention_grads(ctx, d_out, d_lse):
     g = attention_backward(ctx.cfg, q, k, v, out, lse, d_out,
                            None if d_lse is None else d_lse.contiguous(), lengths=lengths)
     return None, g["dq"], g["dk"], g["dv"], None
+
+
+# ------------------------------------------------------------ cache in 4 bits
+@dataclass(frozen=True)
+class CacheConfig:
+    """Calls of T tokens on a cache of 4 bits: pages of 64 tokens, `pages` of them in
+    a sequence's row of the table; HK key heads, H query heads (attention alone)
+    whose tokens see themselves and `left` tokens before (negative: all)."""
+    B: int
+    HK: int
+    H: int
+    T: int
+    d: int
+    pages: int
+    io: int = DT_BF16
+    scale: float = 1.0
+    left: int = -1
+
+    def desc(self) -> CacheDesc:
+        return CacheDesc(self.B, self.HK, self.H, self.T, self.d, self.pages, self.io, self.scale,
+                         self.left)
+
+    @cached_property
+    def _call(self):
+        """The descriptor by reference, the io type and the tensors' shapes."""
+        return (ctypes.byref(self.desc()), torch.bfloat16 if self.io == DT_BF16 else torch.float32,
+                torch.Size((self.B, self.H, self.T, self.d)),
+                torch.Size((self.B, self.HK, self.T, self.d)), torch.Size((self.B, self.pages)),
+                torch.Size((self.B,)), torch.Size((self.HK, 68 * self.d)))
+
+    def __getstate__(self):
+        return {n: v for n, v in self.__dict__.items() if n != "_call"}
+
+
+def cache_page_bytes(HK: int, d: int) -> int:
+    return int((_lib or load()).e2ttt_cache_page_bytes(HK, d))
+
+
+def alloc_cache(cfg: CacheConfig, n_pages: int, device="cuda"):
+    """A pool of empty pages [n_pages, HK, 68 d] (uint8)."""
+    if not cache_page_bytes(cfg.HK, cfg.d):
+        raise E2TTTError(3, "e2ttt_cache_page_bytes")
+    return torch.zeros((n_pages, cfg.HK, 68 * cfg.d), dtype=torch.uint8, device=device)
+
+
+def cache_workspace_bytes(cfg: CacheConfig) -> int:
+    return int((_lib or load()).e2ttt_cache_workspace_bytes(cfg._call[0]))
+
+
+def alloc_cache_workspace(cfg: CacheConfig, device="cuda"):
+    n = cache_workspace_bytes(cfg)
+    if n == 0:
+        raise E2TTTError(3, "e2ttt_cache_workspace_bytes")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def _cache_common(cfg, dev, cache, table, starts, lengths):
+    """Checks what every cache call has; the number of pages."""
+    s_t, s_b, s_page = cfg._call[4:]
+    if not isinstance(cache, torch.Tensor) or cache.dim() != 3 or not 1 <= cache.shape[0] < 1 << 31:
+        raise ValueError("cache must be a tensor [n_pages, HK, 68 d] of bytes")
+    n = cache.shape[0]
+    _plain("cache", cache, (n, *s_page), torch.uint8, dev)
+    if table is None:
+        raise ValueError("table must be a tensor")
+    _plain("table", table, s_t, torch.int32, dev)
+    _plain("starts", starts, s_b, torch.int32, dev)
+    _plain("lengths", lengths, s_b, torch.int32, dev)
+    return n
+
+
+@_on_device
+def cache_write(cfg: CacheConfig, k, v, cache, table, starts=None, lengths=None):
+    """Runs e2ttt_cache_write on the current stream: the first lengths [B] (int32;
+    None: all T) tokens of k, v [B, HK, T, d] (any strides with a contiguous last
+    dimension) become positions starts [B] (int32; None: 0) + t of their
+    sequences, in the pages of cache that table [B, pages] (int32) names."""
+    d, io, _, s_k, _, _, _ = cfg._call
+    dev = k.get_device()
+    st = _layout(CacheStrides, dev, ("k", k, s_k, io), ("v", v, s_k, io))
+    n = _cache_common(cfg, dev, cache, table, starts, lengths)
+    st = (_lib or load()).e2ttt_cache_write(d, st, k.data_ptr(), v.data_ptr(), _ptr(starts),
+                                            _ptr(lengths), table.data_ptr(), cache.data_ptr(), n,
+                                            _stream())
+    if st:
+        _check(st, "e2ttt_cache_write")
+
+
+@_on_device
+def cache_read(cfg: CacheConfig, cache, table, starts=None, lengths=None, *, out=None):
+    """Runs e2ttt_cache_read on the current stream: the values of positions starts +
+    t, t < lengths, as (k, v) [B, HK, T, d]; zeros behind them and where the cache
+    holds none.  `out`: optional (k, v) tensors to write into, of any strides."""
+    d, io, _, s_k, _, _, _ = cfg._call
+    dev = cache.get_device()
+    n = _cache_common(cfg, dev, cache, table, starts, lengths)
+    if out is None:
+        k, v = (torch.empty(s_k, dtype=io, device=cache.device) for _ in "kv")
+        st = None
+    else:
+        k, v = out
+        st = _layout(CacheStrides, dev, ("k", k, s_k, io), ("v", v, s_k, io))
+    st = (_lib or load()).e2ttt_cache_read(d, st, _ptr(starts), _ptr(lengths), table.data_ptr(),
+                                           cache.data_ptr(), n, k.data_ptr(), v.data_ptr(), _stream())
+    if st:
+        _check(st, "e2ttt_cache_read")
+    return k, v
+
+
+@_on_device
+def cache_attention(cfg: CacheConfig, q, cache, table, starts=None, lengths=None, *, out=None,
+                    lse=None, workspace=None):
+    """Runs e2ttt_cache_attend on the current stream: attention of the arriving
+    tokens' q [B, H, T, d] at positions starts + t over what the cache holds up to
+    them, themselves included (cache_write comes first).  Returns (out, lse); lse
+    [B, H, T] is written only if given, else None."""
+    d, io, s_q, _, _, _, _ = cfg._call
+    dev = q.get_device()
+    if out is None:
+        out = torch.empty_like(q)
+    st = _layout(CacheStrides, dev, ("q", q, s_q, io), ("out", out, s_q, io))
+    n = _cache_common(cfg, dev, cache, table, starts, lengths)
+    _plain("lse", lse, s_q[:3], torch.float32, dev)
+    _buffer("workspace", workspace, dev)
+    if workspace is None:
+        workspace = alloc_cache_workspace(cfg, q.device)
+    st = (_lib or load()).e2ttt_cache_attend(
+        d, st, q.data_ptr(), _ptr(starts), _ptr(lengths), table.data_ptr(), cache.data_ptr(), n,
+        out.data_ptr(), _ptr(lse), workspace.data_ptr(), workspace.numel(), _stream())
+    if st:
+        _check(st, "e2ttt_cache_attend")
+    return out, lse
