@@ -27,8 +27,7 @@ __global__ void __launch_bounds__(256, BF ? 2 : 1) attn_dq_kernel(AttnArgs a, in
   using X = typename O::X;
   using A = ATile<BF, D>;
   constexpr int KS = D / 16, NM = D / 32;
-  __shared__ __align__(16) E lk[2][BK * D];
-  __shared__ __align__(16) E lv[2][BK * D];
+  __shared__ __align__(16) E lk0[BK * D], lk1[BK * D], lv0[BK * D], lv1[BK * D];
   const int lane = threadIdx.x & 63, w = wave_id(), h = lane >> 5, c = lane & 31;
   const long id = xcd_order(blockIdx.x, gridDim.x);
   const int tile = ntile - 1 - (int)(id % ntile);
@@ -83,17 +82,16 @@ __global__ void __launch_bounds__(256, BF ? 2 : 1) attn_dq_kernel(AttnArgs a, in
   const E* kb = row_of<E>(a.k, b, hk, 0);
   const E* vb = row_of<E>(a.v, b, hk, 0);
   if (lo < hi) {
-    sk.load(lk[0], kb + lo * a.k.t, end - lo, w);
-    sv.load(lv[0], vb + lo * a.v.t, end - lo, w);
+    sk.load(lk0, kb + lo * a.k.t, end - lo, w);
+    sv.load(lv0, vb + lo * a.v.t, end - lo, w);
   }
-  int cur = 0;
-  for (int j0 = lo; j0 < hi; j0 += BK, cur ^= 1) {
+  auto step = [&](int j0, const E* lk, const E* lv, E* nk, E* nv) __attribute__((always_inline)) {
     staged();
     if (j0 + BK < hi) {
-      sk.load(lk[cur ^ 1], kb + (j0 + BK) * a.k.t, end - j0 - BK, w);
-      sv.load(lv[cur ^ 1], vb + (j0 + BK) * a.v.t, end - j0 - BK, w);
+      sk.load(nk, kb + (j0 + BK) * a.k.t, end - j0 - BK, w);
+      sv.load(nv, vb + (j0 + BK) * a.v.t, end - j0 - BK, w);
     }
-    if (j0 + BK <= wlo || j0 >= whi) continue;
+    if (j0 + BK <= wlo || j0 >= whi) return;
     const bool cut = j0 + BK > end || (a.left >= 0 && j0 < pw1 - 1 - a.left) ||
                      (a.right >= 0 && j0 + BK - 1 > pw0 + a.right);
     const int k0 = a.left < 0 ? 0 : p - a.left;
@@ -103,8 +101,8 @@ __global__ void __launch_bounds__(256, BF ? 2 : 1) attn_dq_kernel(AttnArgs a, in
       f32x16 s = zero16(), v = zero16();
 #pragma unroll
       for (int x = 0; x < KS; ++x) {
-        s = O::mm(s, A::rows(lk[cur], 32 * n + c, x, h), q[x]);
-        v = O::mm(v, A::rows(lv[cur], 32 * n + c, x, h), g[x]);
+        s = O::mm(s, A::rows(lk, 32 * n + c, x, h), q[x]);
+        v = O::mm(v, A::rows(lv, 32 * n + c, x, h), g[x]);
       }
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
@@ -120,9 +118,13 @@ __global__ void __launch_bounds__(256, BF ? 2 : 1) attn_dq_kernel(AttnArgs a, in
         const X f = O::of(s, x);
 #pragma unroll
         for (int m = 0; m < NM; ++m)
-          o[m] = O::mm(o[m], A::rows_t(lk[cur], 32 * n + 16 * x, m, h, c), f);
+          o[m] = O::mm(o[m], A::rows_t(lk, 32 * n + 16 * x, m, h, c), f);
       }
     }
+  };
+  for (int j0 = lo; j0 < hi; j0 += 2 * BK) {
+    step(j0, lk0, lv0, lk1, lv1);
+    if (j0 + BK < hi) step(j0 + BK, lk1, lv1, lk0, lv0);
   }
   if (t >= a.T) return;
   E* drow = row_of_w<E>(a.dq, b, hq, t);
@@ -138,9 +140,8 @@ __global__ void __launch_bounds__(256, BF && D <= 64 ? 2 : 1) attn_dkv_kernel(At
   using X = typename O::X;
   using A = ATile<BF, D>;
   constexpr int KS = D / 16, NM = D / 32;
-  __shared__ __align__(16) E lq[2][BQ * D];
-  __shared__ __align__(16) E lg[2][BQ * D];
-  __shared__ __align__(16) float lx[2][2][64];          // exponents and D of the queries
+  __shared__ __align__(16) E lq0[BQ * D], lq1[BQ * D], lg0[BQ * D], lg1[BQ * D];
+  __shared__ __align__(16) float lx0[2][64], lx1[2][64];   // exponents and D of the queries
   const int lane = threadIdx.x & 63, w = wave_id(), h = lane >> 5, c = lane & 31;
   const long id = xcd_order(blockIdx.x, gridDim.x);
   const int tile = (int)(id % ntile);
@@ -178,17 +179,19 @@ __global__ void __launch_bounds__(256, BF && D <= 64 ? 2 : 1) attn_dkv_kernel(At
   sq.init(a.q.t, a.d, w, lane);
   sg.init(a.d_out.t, a.d, w, lane);
   const int per = hi > lo ? (hi - lo + BQ - 1) / BQ : 0;
-  auto fetch = [&](int r, int t, int to) {
+  auto fetch = [&](int r, int t, E* nq, E* ng, float (*nx)[64]) __attribute__((always_inline)) {
     const int hq = hk * rep + r;
-    sq.load(lq[to], row_of<E>(a.q, b, hq, t), live - t, w);
-    sg.load(lg[to], row_of<E>(a.d_out, b, hq, t), live - t, w);
+    sq.load(nq, row_of<E>(a.q, b, hq, t), live - t, w);
+    sg.load(ng, row_of<E>(a.d_out, b, hq, t), live - t, w);
     // (queries behind the live ones: q, do and D are zero, and so is what they add)
     const long at = ((long)b * a.H + hq) * a.T + t;
-    if (w < 2) stage64(lx[to][w], (w ? a.delta : a.ex) + at, min(live - t, BQ), lane);
+    if (w < 2) stage64(nx[w], (w ? a.delta : a.ex) + at, min(live - t, BQ), lane);
   };
-  int r = 0, t0 = lo, cur = 0;
-  if (per) fetch(0, lo, 0);
-  for (long it = (long)per * rep; it > 0; --it, cur ^= 1) {
+  int r = 0, t0 = lo;
+  long left = (long)per * rep;
+  if (per) fetch(0, lo, lq0, lg0, lx0);
+  auto step = [&](const E* lq, const E* lg, const float (*lx)[64], E* nq, E* ng,
+                  float (*nx)[64]) __attribute__((always_inline)) {
     staged();
     const int tt = t0;
     t0 += BQ;
@@ -196,8 +199,8 @@ __global__ void __launch_bounds__(256, BF && D <= 64 ? 2 : 1) attn_dkv_kernel(At
       t0 = lo;
       ++r;
     }
-    if (it > 1) fetch(r, t0, cur ^ 1);
-    if (tt + BQ <= wlo || tt >= whi) continue;
+    if (--left > 0) fetch(r, t0, nq, ng, nx);
+    if (tt + BQ <= wlo || tt >= whi) return;
     const bool cut = jw + 32 > end || (a.right >= 0 && tt + off < jw + 31 - a.right) ||
                      (a.left >= 0 && tt + BQ - 1 + off > jw + a.left);
 #pragma unroll
@@ -205,13 +208,13 @@ __global__ void __launch_bounds__(256, BF && D <= 64 ? 2 : 1) attn_dkv_kernel(At
       f32x16 s = zero16(), x = zero16();
 #pragma unroll
       for (int y = 0; y < KS; ++y) {
-        s = O::mm(s, A::rows(lq[cur], 32 * n + c, y, h), k[y]);
-        x = O::mm(x, A::rows(lg[cur], 32 * n + c, y, h), v[y]);
+        s = O::mm(s, A::rows(lq, 32 * n + c, y, h), k[y]);
+        x = O::mm(x, A::rows(lg, 32 * n + c, y, h), v[y]);
       }
 #pragma unroll
       for (int i4 = 0; i4 < 4; ++i4) {
-        const f32x4 ex = *reinterpret_cast<const f32x4*>(&lx[cur][0][32 * n + 8 * i4 + 4 * h]);
-        const f32x4 de = *reinterpret_cast<const f32x4*>(&lx[cur][1][32 * n + 8 * i4 + 4 * h]);
+        const f32x4 ex = *reinterpret_cast<const f32x4*>(&lx[0][32 * n + 8 * i4 + 4 * h]);
+        const f32x4 de = *reinterpret_cast<const f32x4*>(&lx[1][32 * n + 8 * i4 + 4 * h]);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int y = 4 * i4 + i;
@@ -232,11 +235,15 @@ __global__ void __launch_bounds__(256, BF && D <= 64 ? 2 : 1) attn_dkv_kernel(At
         const X pf = O::of(s, y), df = O::of(x, y);
 #pragma unroll
         for (int m = 0; m < NM; ++m) {
-          dv[m] = O::mm(dv[m], A::rows_t(lg[cur], 32 * n + 16 * y, m, h, c), pf);
-          dk[m] = O::mm(dk[m], A::rows_t(lq[cur], 32 * n + 16 * y, m, h, c), df);
+          dv[m] = O::mm(dv[m], A::rows_t(lg, 32 * n + 16 * y, m, h, c), pf);
+          dk[m] = O::mm(dk[m], A::rows_t(lq, 32 * n + 16 * y, m, h, c), df);
         }
       }
     }
+  };
+  while (left > 0) {
+    step(lq0, lg0, lx0, lq1, lg1, lx1);
+    if (left > 0) step(lq1, lg1, lx1, lq0, lg0, lx0);
   }
   if (j >= a.S) return;
   E* dkr = row_of_w<E>(a.dk, b, hk, j);

@@ -19,8 +19,8 @@ __global__ void __launch_bounds__(256, BF ? 2 : 1) attn_fwd_kernel(AttnArgs a, i
   using X = typename O::X;
   using A = ATile<BF, D>;
   constexpr int NT = BK / 32, KS = D / 16, NM = D / 32;
-  __shared__ __align__(16) E lk[2][BK * D];
-  __shared__ __align__(16) E lv[2][BK * D];
+  // (apart by name: a read of one is then known not to wait for loads into another)
+  __shared__ __align__(16) E lk0[BK * D], lk1[BK * D], lv0[BK * D], lv1[BK * D];
   const int lane = threadIdx.x & 63, w = wave_id(), h = lane >> 5, c = lane & 31;
   const long id = xcd_order(blockIdx.x, gridDim.x);
   const int tile = ntile - 1 - (int)(id % ntile);      // (long rows of a causal mask first)
@@ -37,8 +37,10 @@ __global__ void __launch_bounds__(256, BF ? 2 : 1) attn_fwd_kernel(AttnArgs a, i
   f32x16 o[NM];
 #pragma unroll
   for (int m = 0; m < NM; ++m) o[m] = zero16();
-  float top = kNegInf, sum = 0.0f;
-  const float cs = a.scale * kLog2e;
+  // ref stands in for the maximum: it follows once a score passes it by 8 powers of
+  // two, so that O is rarely scaled again
+  float top = kNegInf, ref = 0.0f, sum = 0.0f;
+  const float cs = a.scale * kLog2e, slack = 8.0f / cs;
 
   // keys that some query of the workgroup, of this wave sees
   const int p0 = t0 + off, p1 = min(t0 + 128, live) + off;
@@ -54,23 +56,22 @@ __global__ void __launch_bounds__(256, BF ? 2 : 1) attn_fwd_kernel(AttnArgs a, i
   const E* kb = row_of<E>(a.k, b, hk, 0);
   const E* vb = row_of<E>(a.v, b, hk, 0);
   if (lo < hi) {
-    sk.load(lk[0], kb + lo * a.k.t, end - lo, w);
-    sv.load(lv[0], vb + lo * a.v.t, end - lo, w);
+    sk.load(lk0, kb + lo * a.k.t, end - lo, w);
+    sv.load(lv0, vb + lo * a.v.t, end - lo, w);
   }
-  int cur = 0;
-  for (int j0 = lo; j0 < hi; j0 += BK, cur ^= 1) {
+  auto step = [&](int j0, const E* lk, const E* lv, E* nk, E* nv) __attribute__((always_inline)) {
     staged();
     if (j0 + BK < hi) {
-      sk.load(lk[cur ^ 1], kb + (j0 + BK) * a.k.t, end - j0 - BK, w);
-      sv.load(lv[cur ^ 1], vb + (j0 + BK) * a.v.t, end - j0 - BK, w);
+      sk.load(nk, kb + (j0 + BK) * a.k.t, end - j0 - BK, w);
+      sv.load(nv, vb + (j0 + BK) * a.v.t, end - j0 - BK, w);
     }
-    if (j0 + BK <= wlo || j0 >= whi) continue;
+    if (j0 + BK <= wlo || j0 >= whi) return;
     f32x16 s[NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
       s[n] = zero16();
 #pragma unroll
-      for (int x = 0; x < KS; ++x) s[n] = O::mm(s[n], A::rows(lk[cur], 32 * n + c, x, h), q[x]);
+      for (int x = 0; x < KS; ++x) s[n] = O::mm(s[n], A::rows(lk, 32 * n + c, x, h), q[x]);
     }
     if (j0 + BK > end || (a.left >= 0 && j0 < pw1 - 1 - a.left) ||
         (a.right >= 0 && j0 + BK - 1 > pw0 + a.right)) {
@@ -89,15 +90,18 @@ __global__ void __launch_bounds__(256, BF ? 2 : 1) attn_fwd_kernel(AttnArgs a, i
     for (int n = 0; n < NT; ++n)
 #pragma unroll
       for (int i = 0; i < 16; ++i) most = fmaxf(most, s[n][i]);
-    most = fmaxf(top, both_max(most));
-    const float ref = most == kNegInf ? 0.0f : most;     // (no key so far)
-    const float shrink = __builtin_amdgcn_exp2f((top - ref) * cs);
-    top = most;
-    sum *= shrink;
+    most = both_max(most);
+    if (__any(most > top + slack)) {
+      const float was = top == kNegInf ? kNegInf : ref;       // (no key before: nothing to keep)
+      top = fmaxf(top, most);
+      ref = top == kNegInf ? 0.0f : top;
+      const float shrink = __builtin_amdgcn_exp2f((was - ref) * cs);
+      sum *= shrink;
 #pragma unroll
-    for (int m = 0; m < NM; ++m)
+      for (int m = 0; m < NM; ++m)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) o[m][i] *= shrink;
+        for (int i = 0; i < 16; ++i) o[m][i] *= shrink;
+    }
     const float off2 = -ref * cs;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
@@ -111,9 +115,13 @@ __global__ void __launch_bounds__(256, BF ? 2 : 1) attn_fwd_kernel(AttnArgs a, i
         const X pf = O::of(s[n], x);
 #pragma unroll
         for (int m = 0; m < NM; ++m)
-          o[m] = O::mm(o[m], A::rows_t(lv[cur], 32 * n + 16 * x, m, h, c), pf);
+          o[m] = O::mm(o[m], A::rows_t(lv, 32 * n + 16 * x, m, h, c), pf);
       }
     }
+  };
+  for (int j0 = lo; j0 < hi; j0 += 2 * BK) {
+    step(j0, lk0, lv0, lk1, lv1);
+    if (j0 + BK < hi) step(j0 + BK, lk1, lv1, lk0, lv0);
   }
   if (t >= a.T) return;
   sum = both_sum(sum);
@@ -123,7 +131,7 @@ __global__ void __launch_bounds__(256, BF ? 2 : 1) attn_fwd_kernel(AttnArgs a, i
   for (int m = 0; m < NM; ++m) st_tile<BF>(orow, o[m], inv, m, h, a.d);
   if (a.lse && h == 0)
     a.lse[((long)b * a.H + hq) * a.T + t] =
-        inv > 0.0f ? fmaf(top, a.scale, logf(sum)) : kNegInf;
+        inv > 0.0f ? fmaf(ref, a.scale, logf(sum)) : kNegInf;
 }
 
 template <bool BF, int D, int BK>
