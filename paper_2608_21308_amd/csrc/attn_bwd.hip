@@ -26,15 +26,14 @@ __global__ void __launch_bounds__(256, BF ? 2 : 1) attn_dq_kernel(AttnArgs a, in
   using E = typename O::E;
   using X = typename O::X;
   using A = ATile<BF, D>;
-  constexpr int KS = D / 16, NM = D / 32;
+  constexpr int NT = BK / 32, KS = D / 16, NM = D / 32;
   __shared__ __align__(16) E lk0[BK * D], lk1[BK * D], lv0[BK * D], lv1[BK * D];
   const int lane = threadIdx.x & 63, w = wave_id(), h = lane >> 5, c = lane & 31;
-  const long id = xcd_order(blockIdx.x, gridDim.x);
-  const int tile = ntile - 1 - (int)(id % ntile);
-  const long u = id / ntile;
-  const int b = (int)(u / a.H), hq = (int)(u % a.H), hk = hq / (a.H / a.HK);
+  const int id = xcd_order(blockIdx.x, gridDim.x), u = id / ntile;
+  const int part = ntile - 1 - id % ntile;
+  const int b = u / a.H, hq = u % a.H, hk = hq / (a.H / a.HK);
   const int off = a.S - a.T, live = live_of(a, b), end = live + off;
-  const int t0 = tile * 128, tw = t0 + 32 * w, t = tw + c;
+  const int t0 = part * 128, tw = t0 + 32 * w, t = tw + c;
   const bool on = t < live;
 
   X q[KS], g[KS];
@@ -62,12 +61,14 @@ __global__ void __launch_bounds__(256, BF ? 2 : 1) attn_dq_kernel(AttnArgs a, in
   }
   if (t < a.T && h == 0) {
     a.ex[at] = ex;
-    a.delta[at] = dot;
+    a.delta[at] = -dot;
   }
 
-  f32x16 o[NM];
+  f32x16 o[NM], none;         // (-D where the products with do begin)
 #pragma unroll
   for (int m = 0; m < NM; ++m) o[m] = zero16();
+#pragma unroll
+  for (int i = 0; i < 16; ++i) none[i] = -dot;
   const float cs = a.scale * kLog2e;
   const int p0 = t0 + off, p1 = min(t0 + 128, live) + off;
   const int lo = a.left < 0 ? 0 : max(0, p0 - a.left);
@@ -92,30 +93,36 @@ __global__ void __launch_bounds__(256, BF ? 2 : 1) attn_dq_kernel(AttnArgs a, in
       sv.load(nv, vb + (j0 + BK) * a.v.t, end - j0 - BK, w);
     }
     if (j0 + BK <= wlo || j0 >= whi) return;
-    const bool cut = j0 + BK > end || (a.left >= 0 && j0 < pw1 - 1 - a.left) ||
-                     (a.right >= 0 && j0 + BK - 1 > pw0 + a.right);
-    const int k0 = a.left < 0 ? 0 : p - a.left;
-    const int k1 = a.right < 0 ? end : min(end, p + a.right + 1);
+    f32x16 s[NT];
 #pragma unroll
-    for (int n = 0; n < BK / 32; ++n) {
-      f32x16 s = zero16(), v = zero16();
+    for (int n = 0; n < NT; ++n) {
+      s[n] = zero16();
 #pragma unroll
-      for (int x = 0; x < KS; ++x) {
-        s = O::mm(s, A::rows(lk, 32 * n + c, x, h), q[x]);
-        v = O::mm(v, A::rows(lv, 32 * n + c, x, h), g[x]);
-      }
+      for (int x = 0; x < KS; ++x) s[n] = O::mm(s[n], A::rows(lk, 32 * n + c, x, h), q[x]);
+    }
+    if (j0 + BK > end || (a.left >= 0 && j0 < pw1 - 1 - a.left) ||
+        (a.right >= 0 && j0 + BK - 1 > pw0 + a.right)) {
+      const int k0 = a.left < 0 ? 0 : p - a.left;
+      const int k1 = a.right < 0 ? end : min(end, p + a.right + 1);
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        float e = __builtin_amdgcn_exp2f(fmaf(s[i], cs, ex)) * (v[i] - dot);
-        if (cut) {
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
           const int j = j0 + 32 * n + row_in(i, h);
-          if (j < k0 || j >= k1) e = 0.0f;
+          if (j < k0 || j >= k1) s[n][i] = kNegInf;
         }
-        s[i] = e;
-      }
+    }
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      f32x16 v = none;
+#pragma unroll
+      for (int x = 0; x < KS; ++x) v = O::mm(v, A::rows(lv, 32 * n + c, x, h), g[x]);
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        s[n][i] = __builtin_amdgcn_exp2f(fmaf(s[n][i], cs, ex)) * v[i];
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
-        const X f = O::of(s, x);
+        const X f = O::of(s[n], x);
 #pragma unroll
         for (int m = 0; m < NM; ++m)
           o[m] = O::mm(o[m], A::rows_t(lk, 32 * n + 16 * x, m, h, c), f);
@@ -139,16 +146,14 @@ __global__ void __launch_bounds__(256, BF && D <= 64 ? 2 : 1) attn_dkv_kernel(At
   using E = typename O::E;
   using X = typename O::X;
   using A = ATile<BF, D>;
-  constexpr int KS = D / 16, NM = D / 32;
+  constexpr int NT = BQ / 32, KS = D / 16, NM = D / 32;
   __shared__ __align__(16) E lq0[BQ * D], lq1[BQ * D], lg0[BQ * D], lg1[BQ * D];
-  __shared__ __align__(16) float lx0[2][64], lx1[2][64];   // exponents and D of the queries
+  __shared__ __align__(16) float lx0[2][64], lx1[2][64];   // exponents and -D of the queries
   const int lane = threadIdx.x & 63, w = wave_id(), h = lane >> 5, c = lane & 31;
-  const long id = xcd_order(blockIdx.x, gridDim.x);
-  const int tile = (int)(id % ntile);
-  const long u = id / ntile;
-  const int b = (int)(u / a.HK), hk = (int)(u % a.HK), rep = a.H / a.HK;
+  const int id = xcd_order(blockIdx.x, gridDim.x), u = id / ntile;
+  const int b = u / a.HK, hk = u % a.HK, rep = a.H / a.HK;
   const int off = a.S - a.T, live = live_of(a, b), end = live + off;
-  const int j0 = tile * 128, jw = j0 + 32 * w, j = jw + c;
+  const int j0 = id % ntile * 128, jw = j0 + 32 * w, j = jw + c;
 
   X k[KS], v[KS];
   const E* krow = j < end ? row_of<E>(a.k, b, hk, j) : nullptr;
@@ -201,38 +206,47 @@ __global__ void __launch_bounds__(256, BF && D <= 64 ? 2 : 1) attn_dkv_kernel(At
     }
     if (--left > 0) fetch(r, t0, nq, ng, nx);
     if (tt + BQ <= wlo || tt >= whi) return;
-    const bool cut = jw + 32 > end || (a.right >= 0 && tt + off < jw + 31 - a.right) ||
-                     (a.left >= 0 && tt + BQ - 1 + off > jw + a.left);
+    f32x16 s[NT];
 #pragma unroll
-    for (int n = 0; n < BQ / 32; ++n) {
-      f32x16 s = zero16(), x = zero16();
+    for (int n = 0; n < NT; ++n) {
+      s[n] = zero16();
 #pragma unroll
-      for (int y = 0; y < KS; ++y) {
-        s = O::mm(s, A::rows(lq, 32 * n + c, y, h), k[y]);
-        x = O::mm(x, A::rows(lg, 32 * n + c, y, h), v[y]);
-      }
+      for (int y = 0; y < KS; ++y) s[n] = O::mm(s[n], A::rows(lq, 32 * n + c, y, h), k[y]);
+    }
+    if (jw + 32 > end || (a.right >= 0 && tt + off < jw + 31 - a.right) ||
+        (a.left >= 0 && tt + BQ - 1 + off > jw + a.left)) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int y = 0; y < 16; ++y) {
+          const int t = tt + 32 * n + row_in(y, h);
+          if (t < q0 || t >= q1) s[n][y] = kNegInf;
+        }
+    }
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      f32x16 x;
 #pragma unroll
       for (int i4 = 0; i4 < 4; ++i4) {
-        const f32x4 ex = *reinterpret_cast<const f32x4*>(&lx[0][32 * n + 8 * i4 + 4 * h]);
-        const f32x4 de = *reinterpret_cast<const f32x4*>(&lx[1][32 * n + 8 * i4 + 4 * h]);
+        const f32x4 d4 = *reinterpret_cast<const f32x4*>(&lx[1][32 * n + 8 * i4 + 4 * h]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[4 * i4 + i] = d4[i];
+      }
+#pragma unroll
+      for (int y = 0; y < KS; ++y) x = O::mm(x, A::rows(lg, 32 * n + c, y, h), v[y]);
+#pragma unroll
+      for (int i4 = 0; i4 < 4; ++i4) {
+        const f32x4 e4 = *reinterpret_cast<const f32x4*>(&lx[0][32 * n + 8 * i4 + 4 * h]);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int y = 4 * i4 + i;
-          float p = __builtin_amdgcn_exp2f(fmaf(s[y], cs, ex[i]));
-          float ds = p * (x[y] - de[i]);
-          if (cut) {
-            const int t = tt + 32 * n + row_in(y, h);
-            const bool seen = t >= q0 && t < q1;
-            p = seen ? p : 0.0f;
-            ds = seen ? ds : 0.0f;
-          }
-          s[y] = p;
-          x[y] = ds;
+          s[n][y] = __builtin_amdgcn_exp2f(fmaf(s[n][y], cs, e4[i]));
+          x[y] *= s[n][y];
         }
       }
 #pragma unroll
       for (int y = 0; y < 2; ++y) {
-        const X pf = O::of(s, y), df = O::of(x, y);
+        const X pf = O::of(s[n], y), df = O::of(x, y);
 #pragma unroll
         for (int m = 0; m < NM; ++m) {
           dv[m] = O::mm(dv[m], A::rows_t(lg, 32 * n + 16 * y, m, h, c), pf);

@@ -28,7 +28,7 @@ struct AttnArgs {
   float* lse;                 // [B][H][T], nullable in the forward
   const float* d_lse;         // nullable
   float* ex;                  // backward, [B][H][T]: -lse log2 e (-inf for queries that see nothing)
-  float* delta;               // backward, [B][H][T]: D
+  float* delta;               // backward, [B][H][T]: -D
   const int* lengths;         // nullable
   int B, HK, H, T, S, d;
   int left, right;            // at most 2^30 - 1; negative: no bound
@@ -212,9 +212,9 @@ __device__ __forceinline__ void st_tile(typename MOp<BF>::E* row, const f32x16& 
 
 // Workgroups are dealt to the 8 XCDs in turn: those of an XCD get a stretch of the
 // work, so that what shares keys and values shares an L2.
-__device__ __forceinline__ long xcd_order(long id, long n) {
-  const long x = id & 7, y = id >> 3, per = n >> 3, more = n & 7;
-  return x * per + (x < more ? x : more) + y;
+__device__ __forceinline__ int xcd_order(int id, int n) {
+  const int x = id & 7, y = id >> 3, per = n >> 3, more = n & 7;
+  return x * per + min(x, more) + y;
 }
 
 // Queries of sequence b that the call takes.

@@ -22,10 +22,9 @@ __global__ void __launch_bounds__(256, BF ? 2 : 1) attn_fwd_kernel(AttnArgs a, i
   // (apart by name: a read of one is then known not to wait for loads into another)
   __shared__ __align__(16) E lk0[BK * D], lk1[BK * D], lv0[BK * D], lv1[BK * D];
   const int lane = threadIdx.x & 63, w = wave_id(), h = lane >> 5, c = lane & 31;
-  const long id = xcd_order(blockIdx.x, gridDim.x);
-  const int tile = ntile - 1 - (int)(id % ntile);      // (long rows of a causal mask first)
-  const long u = id / ntile;
-  const int b = (int)(u / a.H), hq = (int)(u % a.H), hk = hq / (a.H / a.HK);
+  const int id = xcd_order(blockIdx.x, gridDim.x), u = id / ntile;
+  const int tile = ntile - 1 - id % ntile;             // (long rows of a causal mask first)
+  const int b = u / a.H, hq = u % a.H, hk = hq / (a.H / a.HK);
   const int off = a.S - a.T, live = live_of(a, b), end = live + off;
   const int t0 = tile * 128, tw = t0 + 32 * w, t = tw + c;
 
