@@ -124,13 +124,14 @@ __global__ void __launch_bounds__(256, BF ? 2 : 1) attn_fwd_kernel(AttnArgs a, i
   }
   if (t >= a.T) return;
   sum = both_sum(sum);
-  const float inv = t < live && sum > 0.0f ? 1.0f / sum : 0.0f;
+  const bool some = t < live && sum != 0.0f;
+  const float inv = some ? 1.0f / sum : 0.0f;
   E* orow = row_of_w<E>(a.out, b, hq, t);
 #pragma unroll
   for (int m = 0; m < NM; ++m) st_tile<BF>(orow, o[m], inv, m, h, a.d);
   if (a.lse && h == 0)
     a.lse[((long)b * a.H + hq) * a.T + t] =
-        inv > 0.0f ? fmaf(ref, a.scale, logf(sum)) : kNegInf;
+        some ? fmaf(ref, a.scale, logf(sum)) : kNegInf;
 }
 
 template <bool BF, int D, int BK>

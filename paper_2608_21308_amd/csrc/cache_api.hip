@@ -80,8 +80,8 @@ extern "C" e2ttt_status e2ttt_cache_write(const e2ttt_cache_desc* desc,
   if (!k || !v) return E2TTT_ERR_NULL_ARG;
   if ((st = common(starts, lengths, table, cache, n_pages, &a)) != E2TTT_OK) return st;
   const RowSpec rows{desc->B, desc->T, desc->d, desc->io};
-  if (!rows.read(strides ? &strides->k : nullptr, k, desc->HK, &a.k) ||
-      !rows.read(strides ? &strides->v : nullptr, v, desc->HK, &a.v))
+  if (!rows.read(strides ? &strides->k : nullptr, k, desc->HK, &a.x) ||
+      !rows.read(strides ? &strides->v : nullptr, v, desc->HK, &a.y))
     return E2TTT_ERR_BAD_SHAPE;
   return launch_cache_write(a, desc->io == E2TTT_DT_BF16, static_cast<hipStream_t>(stream)) == hipSuccess
              ? E2TTT_OK : E2TTT_ERR_HIP;
@@ -98,8 +98,8 @@ extern "C" e2ttt_status e2ttt_cache_read(const e2ttt_cache_desc* desc,
   if (!k || !v) return E2TTT_ERR_NULL_ARG;
   if ((st = common(starts, lengths, table, cache, n_pages, &a)) != E2TTT_OK) return st;
   const RowSpec rows{desc->B, desc->T, desc->d, desc->io};
-  if (!rows.write(strides ? &strides->k : nullptr, k, desc->HK, &a.k) ||
-      !rows.write(strides ? &strides->v : nullptr, v, desc->HK, &a.v))
+  if (!rows.write(strides ? &strides->k : nullptr, k, desc->HK, &a.x) ||
+      !rows.write(strides ? &strides->v : nullptr, v, desc->HK, &a.y))
     return E2TTT_ERR_BAD_SHAPE;
   return launch_cache_read(a, desc->io == E2TTT_DT_BF16, static_cast<hipStream_t>(stream)) == hipSuccess
              ? E2TTT_OK : E2TTT_ERR_HIP;
@@ -117,8 +117,8 @@ extern "C" e2ttt_status e2ttt_cache_attend(const e2ttt_cache_desc* desc,
   if (!q || !out || !workspace) return E2TTT_ERR_NULL_ARG;
   if ((st = common(starts, lengths, table, cache, n_pages, &a)) != E2TTT_OK) return st;
   const RowSpec rows{desc->B, desc->T, desc->d, desc->io};
-  if (!rows.read(strides ? &strides->q : nullptr, q, desc->H, &a.q) ||
-      !rows.write(strides ? &strides->out : nullptr, out, desc->H, &a.out) || misaligned(workspace))
+  if (!rows.read(strides ? &strides->q : nullptr, q, desc->H, &a.x) ||
+      !rows.write(strides ? &strides->out : nullptr, out, desc->H, &a.y) || misaligned(workspace))
     return E2TTT_ERR_BAD_SHAPE;
   if (workspace_bytes < std::max<size_t>(part_bytes(a), 256)) return E2TTT_ERR_WORKSPACE_TOO_SMALL;
   a.lse = lse;

@@ -12,13 +12,14 @@
 // a second kernel.
 #include <math.h>
 
+#include <algorithm>
+
 #include "cache_common.h"
 
 namespace e2ttt {
 namespace {
 
 constexpr float kLog2e = 1.44269504088896f;
-constexpr int kWaves = 4;
 
 // What one wave's lane takes of a page.
 template <int NB>
@@ -28,32 +29,38 @@ struct Raw {
   u32x4 v[NB], vs[NB];
   bool on;
 };
+// (Without branches, so that the loads of one page are waited for without those of the
+// next: of no page the lane asks for nothing.)
 template <int NB>
-__device__ __forceinline__ void fetch(Raw<NB>& x, const unsigned char* page, int g, int r) {
-  x.on = page != nullptr;
-  if (!page) return;
+__device__ __forceinline__ void fetch(Raw<NB>& x, const CacheArgs& a, const unsigned char* page,
+                                      int g, int r) {
   constexpr int D = 32 * NB;
+  x.on = page != nullptr;
+  const Buf b = buf_of(x.on ? page : a.cache);
+  const unsigned none = x.on ? 0u : kNowhere;
+  const unsigned kc = none + r * 16 * NB + g * 4 * NB, ks = none + 32 * D + r * 4;
+  const unsigned vc = none + 34 * D + r * 64 + g * 16, vs = none + 66 * D + g * 16;
 #pragma unroll
-  for (int a = 0; a < 4; ++a) {
-    const unsigned char* p = page + (16 * a + r) * 16 * NB + g * 4 * NB;
+  for (int t = 0; t < 4; ++t) {
+    const unsigned at = kc + 16 * t * 16 * NB;
     if constexpr (NB == 4) {
-      const u32x4 w = *reinterpret_cast<const u32x4*>(p);
+      const u32x4 w = buf_ld(b, at);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) x.k[a][i] = w[i];
+      for (int i = 0; i < 4; ++i) x.k[t][i] = w[i];
     } else if constexpr (NB == 2) {
-      const uint2 w = *reinterpret_cast<const uint2*>(p);
-      x.k[a][0] = w.x;
-      x.k[a][1] = w.y;
+      const auto w = __builtin_amdgcn_raw_buffer_load_b64(b, (int)at, 0, 0);
+      x.k[t][0] = w[0];
+      x.k[t][1] = w[1];
     } else {
 #pragma unroll
-      for (int i = 0; i < NB; ++i) x.k[a][i] = *reinterpret_cast<const unsigned*>(p + 4 * i);
+      for (int i = 0; i < NB; ++i) x.k[t][i] = __builtin_amdgcn_raw_buffer_load_b32(b, (int)(at + 4 * i), 0, 0);
     }
   }
 #pragma unroll
   for (int i = 0; i < NB; ++i) {
-    x.ks[i] = *reinterpret_cast<const unsigned*>(page + 32 * D + i * 64 + r * 4);
-    x.v[i] = *reinterpret_cast<const u32x4*>(page + 34 * D + (i * 16 + r) * 64 + g * 16);
-    x.vs[i] = *reinterpret_cast<const u32x4*>(page + 66 * D + i * 64 + g * 16);
+    x.ks[i] = __builtin_amdgcn_raw_buffer_load_b32(b, (int)(ks + i * 64), 0, 0);
+    x.v[i] = buf_ld(b, vc + i * 1024);
+    x.vs[i] = buf_ld(b, vs + i * 64);
   }
 }
 
@@ -85,21 +92,19 @@ __device__ __forceinline__ float groups_sum(float x) {
   return __uint_as_float(u[0]) + __uint_as_float(u[1]);
 }
 
-// Partial results of a stretch: per sequence, key head and tile of 16 columns, [16]
-// maxima (of the scores), [16] sums, then [d][16] outputs.
+// Partial results of a stretch, per sequence, key head and tile of 16 columns: [16]
+// maxima (of the scores), [16] sums, then the outputs of [16] columns, d each.
 __host__ __device__ inline long part_floats(int d) { return 32 + 16L * d; }
 
-template <bool BF, int NB>
-__global__ void __launch_bounds__(64 * kWaves, 2) cache_attend_kernel(CacheArgs a, int ntile) {
+template <bool BF, int NB, int NW>
+__global__ void __launch_bounds__(64 * NW, 2) cache_attend_kernel(CacheArgs a, int ntile) {
   using E = typename DOp<BF>::E;
   constexpr int NQ = BF ? 1 : 3, NP = BF ? 2 : 3, D = 32 * NB;
-  __shared__ __align__(16) float lo_[kWaves][D * 16];
-  __shared__ float lm[kWaves][16], ll[kWaves][16];
+  __shared__ __align__(16) float lo_[NW][D * 16];
+  __shared__ float lm[NW][16], ll[NW][16];
   const int lane = threadIdx.x & 63, w = wave_id(), g = lane >> 4, r = lane & 15;
-  const int split = (int)(blockIdx.x % a.nsplit);
-  const long u = blockIdx.x / a.nsplit;
-  const int tile = (int)(u % ntile);
-  const int hk = (int)(u / ntile % a.HK), b = (int)(u / ntile / a.HK);
+  const int id = blockIdx.x, split = id % a.nsplit, u = id / a.nsplit;
+  const int tile = u % ntile, hk = u / ntile % a.HK, b = u / ntile / a.HK;
   const int rep = a.H / a.HK, col = 16 * tile + r;
   const int qt = col / rep, hq = hk * rep + col % rep;      // token, head of the lane's column
   const Held h = held_of(a, b);
@@ -111,11 +116,11 @@ __global__ void __launch_bounds__(64 * kWaves, 2) cache_attend_kernel(CacheArgs 
   for (int i = 0; i < NB; ++i) {
     if constexpr (BF) {
       q[i][0] = bf16x8{};
-      if (on) q[i][0] = *reinterpret_cast<const bf16x8*>(row_of<E>(a.q, b, hq, qt) + 32 * i + 8 * g);
+      if (on) q[i][0] = *reinterpret_cast<const bf16x8*>(row_of<E>(a.x, b, hq, qt) + 32 * i + 8 * g);
     } else {
       f32x4 x = zero4(), y = zero4();
       if (on) {
-        const E* p = row_of<E>(a.q, b, hq, qt) + 32 * i + 8 * g;
+        const E* p = row_of<E>(a.x, b, hq, qt) + 32 * i + 8 * g;
         x = *reinterpret_cast<const f32x4*>(p);
         y = *reinterpret_cast<const f32x4*>(p + 4);
       }
@@ -129,35 +134,40 @@ __global__ void __launch_bounds__(64 * kWaves, 2) cache_attend_kernel(CacheArgs 
   const long see0 = on ? max(h.first, a.left < 0 ? 0L : p - a.left) : 0, see1 = on ? p + 1 : 0;
   const long any0 = max(h.first, a.left < 0 ? 0L : max(0L, h.start - a.left));
   const long any1 = live > 0 ? h.end : any0;
-  const long pg0 = any0 / kPage, np = any1 > any0 ? (any1 + kPage - 1) / kPage - pg0 : 0;
-  const long s0 = pg0 + np * split / a.nsplit, s1 = pg0 + np * (split + 1) / a.nsplit;
+  const int pg0 = (int)(any0 / kPage), np = any1 > any0 ? (int)((any1 + kPage - 1) / kPage) - pg0 : 0;
+  const int s0 = pg0 + (int)((long)np * split / a.nsplit), s1 = pg0 + (int)((long)np * (split + 1) / a.nsplit);
 
   f32x4 o[NB][2];
 #pragma unroll
   for (int i = 0; i < NB; ++i) o[i][0] = o[i][1] = zero4();
-  float top = -INFINITY, sum = 0.0f;
-  const float cs = a.scale * kLog2e;
+  // (ref stands in for the maximum: it follows once a score passes it by 8 powers of two)
+  float top = -INFINITY, ref = 0.0f, sum = 0.0f;
+  const float cs = a.scale * kLog2e, slack = 8.0f / cs;
 
-  Raw<NB> cur, next;
-  long pg = s0 + w;
-  next.on = false;
-  if (pg < s1) fetch<NB>(next, page_of(a, b, hk, pg), g, r);
-  for (; pg < s1; pg += kWaves) {
-    cur = next;
-    if (pg + kWaves < s1) fetch<NB>(next, page_of(a, b, hk, pg + kWaves), g, r);
-    if (!cur.on) continue;
+  // the wave's pages w, w + NW, ..: their bytes one turn ahead, their places two
+  int entry = s0 + w < s1 ? (s0 + w) % a.P : 0;
+  auto place = [&](int pg) __attribute__((always_inline)) {
+    const unsigned char* x = pg < s1 ? page_at(a, b, hk, entry) : nullptr;
+    entry += NW;
+    while (entry >= a.P) entry -= a.P;
+    return x;
+  };
+  auto turn = [&](Raw<NB>& cur, int pg) __attribute__((always_inline)) {
+    if (!cur.on) return;
     f32x4 s[4];
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
       s[x] = zero4();
 #pragma unroll
       for (int i = 0; i < NB; ++i) {
-        const bf16x8 k = eight_of(cur.k[x][i], pow_of(cur.ks[i] >> (8 * x) & 255u));
+        const float f = x == 0 ? scale_of<0>(cur.ks[i]) : x == 1 ? scale_of<1>(cur.ks[i]) :
+                        x == 2 ? scale_of<2>(cur.ks[i]) : scale_of<3>(cur.ks[i]);
+        const bf16x8 k = eight_of(cur.k[x][i], f);
 #pragma unroll
         for (int n = NQ - 1; n >= 0; --n) s[x] = mm(s[x], k, q[i][n]);
       }
     }
-    const long j0 = pg * kPage;
+    const long j0 = (long)pg * kPage;
     const bool cut = j0 < any0 || j0 + kPage > h.start + 1 || (a.left >= 0 && j0 < h.end - 1 - a.left);
     if (cut) {
       const int k0 = (int)max(see0 - j0, -1L), k1 = (int)min(see1 - j0, 64L);
@@ -179,18 +189,21 @@ __global__ void __launch_bounds__(64 * kWaves, 2) cache_attend_kernel(CacheArgs 
     for (int x = 0; x < 4; ++x)
 #pragma unroll
       for (int i = 0; i < 4; ++i) most = fmaxf(most, s[x][i]);
-    most = fmaxf(top, groups_max(most));
-    const float ref = most == -INFINITY ? 0.0f : most;
-    const float shrink = __builtin_amdgcn_exp2f((top - ref) * cs);
-    top = most;
-    sum *= shrink;
+    most = groups_max(most);
+    if (__any(most > top + slack)) {
+      const float was = top == -INFINITY ? -INFINITY : ref;     // (no key before: nothing to keep)
+      top = fmaxf(top, most);
+      ref = top == -INFINITY ? 0.0f : top;
+      const float shrink = __builtin_amdgcn_exp2f((was - ref) * cs);
+      sum *= shrink;
 #pragma unroll
-    for (int i = 0; i < NB; ++i)
+      for (int i = 0; i < NB; ++i)
 #pragma unroll
-      for (int y = 0; y < 4; ++y) {
-        o[i][0][y] *= shrink;
-        o[i][1][y] *= shrink;
-      }
+        for (int y = 0; y < 4; ++y) {
+          o[i][0][y] *= shrink;
+          o[i][1][y] *= shrink;
+        }
+    }
     const float off = -ref * cs;
 #pragma unroll
     for (int x = 0; x < 4; ++x)
@@ -208,8 +221,8 @@ __global__ void __launch_bounds__(64 * kWaves, 2) cache_attend_kernel(CacheArgs 
 #pragma unroll
         for (int y = 0; y < 2; ++y) {
           const unsigned c = cur.v[i][2 * x + y], sc = cur.vs[i][2 * x + y];
-          const unsigned t0 = pair_of<0>(c, pow_of(sc & 255u)), t1 = pair_of<1>(c, pow_of(sc >> 8 & 255u));
-          const unsigned t2 = pair_of<2>(c, pow_of(sc >> 16 & 255u)), t3 = pair_of<3>(c, pow_of(sc >> 24));
+          const unsigned t0 = pair_of<0>(c, scale_of<0>(sc)), t1 = pair_of<1>(c, scale_of<1>(sc));
+          const unsigned t2 = pair_of<2>(c, scale_of<2>(sc)), t3 = pair_of<3>(c, scale_of<3>(sc));
           even[2 * y] = __builtin_amdgcn_perm(t1, t0, 0x05040100u);
           even[2 * y + 1] = __builtin_amdgcn_perm(t3, t2, 0x05040100u);
           odd[2 * y] = __builtin_amdgcn_perm(t1, t0, 0x07060302u);
@@ -222,6 +235,19 @@ __global__ void __launch_bounds__(64 * kWaves, 2) cache_attend_kernel(CacheArgs 
         }
       }
     }
+  };
+  Raw<NB> x, y;
+  int pg = s0 + w;
+  const unsigned char* next = place(pg);
+  fetch<NB>(x, a, next, g, r);
+  next = place(pg + NW);
+  for (; pg < s1; pg += 2 * NW) {
+    fetch<NB>(y, a, next, g, r);
+    next = place(pg + 2 * NW);
+    turn(x, pg);
+    fetch<NB>(x, a, next, g, r);
+    next = place(pg + 3 * NW);
+    turn(y, pg + NW);
   }
 
   if (!on) {                  // (a column of no live query has gone along with the others)
@@ -233,7 +259,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) cache_attend_kernel(CacheArgs 
   // the waves' parts together: lane (g, r) has channels 32 i + 8 g + 2 y + n of column r
   sum = groups_sum(sum);
   if (g == 0) {
-    lm[w][r] = top;
+    lm[w][r] = sum == 0.0f ? -INFINITY : ref;
     ll[w][r] = sum;
   }
 #pragma unroll
@@ -243,13 +269,13 @@ __global__ void __launch_bounds__(64 * kWaves, 2) cache_attend_kernel(CacheArgs 
 #pragma unroll
       for (int y = 0; y < 4; ++y) lo_[w][(32 * i + 8 * g + 2 * y + n) * 16 + r] = o[i][n][y];
   __syncthreads();
-  float f[kWaves], all = -INFINITY, total = 0.0f;
+  float f[NW], all = -INFINITY, total = 0.0f;
 #pragma unroll
-  for (int x = 0; x < kWaves; ++x) all = fmaxf(all, lm[x][r]);
-  const float ref = all == -INFINITY ? 0.0f : all;
+  for (int x = 0; x < NW; ++x) all = fmaxf(all, lm[x][r]);
+  const float base = all == -INFINITY ? 0.0f : all;
 #pragma unroll
-  for (int x = 0; x < kWaves; ++x) {
-    f[x] = __builtin_amdgcn_exp2f((lm[x][r] - ref) * cs);
+  for (int x = 0; x < NW; ++x) {
+    f[x] = __builtin_amdgcn_exp2f((lm[x][r] - base) * cs);
     total += ll[x][r] * f[x];
   }
   if (a.nsplit > 1) {
@@ -258,59 +284,88 @@ __global__ void __launch_bounds__(64 * kWaves, 2) cache_attend_kernel(CacheArgs 
       part[r] = all;
       part[16 + r] = total;
     }
-    for (int y = threadIdx.x; y < D * 16; y += 64 * kWaves) {     // (column y % 16 = r)
-      float x = 0.0f;
+    for (int ch = 4 * (threadIdx.x >> 4); ch < D; ch += 16 * NW) {
+      f32x4 x = zero4();
 #pragma unroll
-      for (int n = 0; n < kWaves; ++n) x += lo_[n][y] * f[n];
-      part[32 + y] = x;
+      for (int n = 0; n < NW; ++n)
+#pragma unroll
+        for (int y = 0; y < 4; ++y) x[y] = fmaf(lo_[n][(ch + y) * 16 + r], f[n], x[y]);
+      *reinterpret_cast<f32x4*>(part + 32 + r * D + ch) = x;
     }
     return;
   }
   if (qt >= a.T) return;
-  const float inv = total > 0.0f ? 1.0f / total : 0.0f;
-  E* orow = row_of_w<E>(a.out, b, hq, qt);
-  for (int ch = 4 * (threadIdx.x >> 4); ch < D; ch += 4 * 4 * kWaves) {
+  const float inv = total == 0.0f ? 0.0f : 1.0f / total;
+  E* orow = row_of_w<E>(a.y, b, hq, qt);
+  for (int ch = 4 * (threadIdx.x >> 4); ch < D; ch += 16 * NW) {
     f32x4 x = zero4();
 #pragma unroll
-    for (int n = 0; n < kWaves; ++n)
+    for (int n = 0; n < NW; ++n)
 #pragma unroll
       for (int y = 0; y < 4; ++y) x[y] = fmaf(lo_[n][(ch + y) * 16 + r], f[n] * inv, x[y]);
     IoT<BF>::st4(orow + ch, x);
   }
   if (a.lse && threadIdx.x < 16)
-    a.lse[((long)b * a.H + hq) * a.T + qt] = inv > 0.0f ? fmaf(all, a.scale, logf(total)) : -INFINITY;
+    a.lse[((long)b * a.H + hq) * a.T + qt] = total == 0.0f ? -INFINITY : fmaf(all, a.scale, logf(total));
 }
 
-// The stretches' parts joined: a workgroup per sequence, key head and tile of columns.
+// The stretches' parts joined: a workgroup per sequence, key head, tile of columns and
+// 16 channels (16 columns x 4 quads of channels x 4 shares of the stretches).
+constexpr int kMostSplits = 256;
 template <bool BF>
 __global__ void __launch_bounds__(256) cache_join_kernel(CacheArgs a, int ntile) {
   using E = typename DOp<BF>::E;
-  const long u = blockIdx.x;
-  const int tile = (int)(u % ntile), hk = (int)(u / ntile % a.HK), b = (int)(u / ntile / a.HK);
-  const int r = threadIdx.x & 15, rep = a.H / a.HK, col = 16 * tile + r;
+  __shared__ float wt[kMostSplits * 16];
+  __shared__ float red[16][16];
+  __shared__ f32x4 acc[4][64];
+  const int nc = a.d / 16, u = blockIdx.x / nc, c0 = (int)(blockIdx.x % nc) * 16;
+  const int tile = u % ntile, hk = u / ntile % a.HK, b = u / ntile / a.HK;
+  const int r = threadIdx.x & 15, y = threadIdx.x >> 4, rep = a.H / a.HK, col = 16 * tile + r;
   const int qt = col / rep, hq = hk * rep + col % rep;
-  if (qt >= a.T) return;
   const long each = part_floats(a.d);
-  const float* part = a.part + u * a.nsplit * each;
+  const float* part = a.part + (long)u * a.nsplit * each;
   const float cs = a.scale * kLog2e;
-  float all = -INFINITY, total = 0.0f;
-  for (int s = 0; s < a.nsplit; ++s) all = fmaxf(all, part[s * each + r]);
-  const float ref = all == -INFINITY ? 0.0f : all;
-  for (int s = 0; s < a.nsplit; ++s)
-    total += part[s * each + 16 + r] * __builtin_amdgcn_exp2f((part[s * each + r] - ref) * cs);
-  const float inv = total > 0.0f ? 1.0f / total : 0.0f;
-  E* orow = row_of_w<E>(a.out, b, hq, qt);
-  for (int ch = 4 * (threadIdx.x >> 4); ch < a.d; ch += 64) {
-    f32x4 x = zero4();
-    for (int s = 0; s < a.nsplit; ++s) {
-      const float f = __builtin_amdgcn_exp2f((part[s * each + r] - ref) * cs) * inv;
+  float m = -INFINITY, total = 0.0f;
+  for (int s = y; s < a.nsplit; s += 16) m = fmaxf(m, part[s * each + r]);
+  red[y][r] = m;
+  __syncthreads();
 #pragma unroll
-      for (int y = 0; y < 4; ++y) x[y] = fmaf(part[s * each + 32 + (ch + y) * 16 + r], f, x[y]);
-    }
-    IoT<BF>::st4(orow + ch, x);
+  for (int i = 0; i < 16; ++i) m = fmaxf(m, red[i][r]);
+  const float ref = m == -INFINITY ? 0.0f : m;
+  __syncthreads();
+  for (int s = y; s < a.nsplit; s += 16) {
+    const float f = __builtin_amdgcn_exp2f((part[s * each + r] - ref) * cs);
+    wt[s * 16 + r] = f;
+    total += part[s * each + 16 + r] * f;
   }
-  if (a.lse && threadIdx.x < 16)
-    a.lse[((long)b * a.H + hq) * a.T + qt] = inv > 0.0f ? fmaf(all, a.scale, logf(total)) : -INFINITY;
+  red[y][r] = total;
+  __syncthreads();
+  total = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) total += red[i][r];
+  const float inv = total == 0.0f ? 0.0f : 1.0f / total;
+  f32x4 x = zero4();
+  const float* from = part + 32 + r * a.d + c0 + 4 * (y & 3);
+#pragma unroll 4
+  for (int s = y >> 2; s < a.nsplit; s += 4) {
+    const f32x4 o = *reinterpret_cast<const f32x4*>(from + s * each);
+    const float f = wt[s * 16 + r];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = fmaf(o[i], f, x[i]);
+  }
+  acc[y >> 2][(y & 3) * 16 + r] = x;
+  __syncthreads();
+  if (threadIdx.x >= 64 || qt >= a.T) return;
+  f32x4 o = zero4();
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int n = 0; n < 4; ++n) o[n] += acc[i][threadIdx.x][n];
+#pragma unroll
+  for (int n = 0; n < 4; ++n) o[n] *= inv;
+  IoT<BF>::st4(row_of_w<E>(a.y, b, hq, qt) + c0 + 4 * y, o);
+  if (a.lse && c0 == 0 && y == 0)
+    a.lse[((long)b * a.H + hq) * a.T + qt] = total == 0.0f ? -INFINITY : fmaf(m, a.scale, logf(total));
 }
 
 int tiles_of(const CacheArgs& a) { return (int)(((long)a.H / a.HK * a.T + 15) / 16); }
@@ -319,10 +374,10 @@ template <bool BF, int NB>
 hipError_t go(const CacheArgs& a, hipStream_t s) {
   const int nt = tiles_of(a);
   const long units = (long)a.B * a.HK * nt;
-  hipLaunchKernelGGL((cache_attend_kernel<BF, NB>), dim3((unsigned)(units * a.nsplit)),
-                     dim3(64 * kWaves), 0, s, a, nt);
+  hipLaunchKernelGGL((cache_attend_kernel<BF, NB, 8>), dim3((unsigned)(units * a.nsplit)),
+                     dim3(512), 0, s, a, nt);
   if (a.nsplit > 1)
-    hipLaunchKernelGGL((cache_join_kernel<BF>), dim3((unsigned)units), dim3(256), 0, s, a, nt);
+    hipLaunchKernelGGL((cache_join_kernel<BF>), dim3((unsigned)(units * (a.d / 16))), dim3(256), 0, s, a, nt);
   return hipGetLastError();
 }
 template <bool BF>
@@ -337,13 +392,17 @@ hipError_t pick(const CacheArgs& a, hipStream_t s) {
 
 }  // namespace
 
+// A workgroup's eight waves take a page each at a time, some 1.2 us; a split adds the
+// join, 4 us. (128 units of 64, 34 pages: 12.8 us whole, 15.3 in two, 17.5 in three.)  So
+// the pages are split from 64 on, into stretches of 16 at least, while the stretches of
+// all units find a CU each (16 units of 128, 1030 pages: 34.6 us in 16, 38.6 in 32, 47.7
+// in 8).
 int cache_splits(const CacheArgs& a) {
   const long units = (long)a.B * a.HK * tiles_of(a);
   long pages = a.P;
-  if (a.left >= 0) pages = pages < ((long)a.left + a.T) / kPage + 2 ? pages : ((long)a.left + a.T) / kPage + 2;
-  const long want = (768 + units - 1) / units, most = (pages + 7) / 8;
-  const long n = want < most ? want : most;
-  return n < 1 ? 1 : (int)n;
+  if (a.left >= 0) pages = std::min(pages, ((long)a.left + a.T) / kPage + 2);
+  if (pages < 64) return 1;
+  return (int)std::max(1L, std::min({256 / units, (pages + 15) / 16, (long)kMostSplits}));
 }
 size_t cache_part_floats(const CacheArgs& a) {
   const int n = cache_splits(a);

@@ -28,7 +28,7 @@ constexpr int kMinExp = 2;           // least scale byte: every value but zero i
 constexpr int kNanExp = 255;         // of a block with a non-finite element: reads as NaN
 
 struct CacheArgs {
-  View q, k, v, out;        // [B][H or HK][T][d]
+  View x, y;                // k, v; q, out for attention: [B][HK or H][T][d]
   float* lse;               // [B][H][T], nullable
   const int* starts;        // [B]: position of a sequence's first token of this call
   const int* lengths;       // nullable
@@ -54,16 +54,18 @@ __device__ __forceinline__ Held held_of(const CacheArgs& a, int b) {
   x.first = x.end <= 0 ? 0 : max(0L, ((x.end - 1) / kPage - a.P + 1) * kPage);
   return x;
 }
-// The page of position p >= 0 (null: none).
-__device__ __forceinline__ unsigned char* page_of(const CacheArgs& a, int b, int hk, long pg) {
-  const int id = a.table[(long)b * a.P + (int)(pg % a.P)];
+// The page that entry e of a sequence's row of the table names (null: none).
+__device__ __forceinline__ unsigned char* page_at(const CacheArgs& a, int b, int hk, int e) {
+  const int id = a.table[(long)b * a.P + e];
   if (id < 0 || id >= a.n_pages) return nullptr;
   return a.cache + ((long)id * a.HK + hk) * (68L * a.d);
 }
 
-// A scale byte as a float.
-__device__ __forceinline__ float pow_of(unsigned byte) {
-  return __uint_as_float(byte == kNanExp ? 0x7fc00000u : byte << 23);
+// Byte i of a word of scales, as the factor of the hardware's conversions: of that
+// float they take the exponent's bits alone (255: NaN).
+template <int I>
+__device__ __forceinline__ float scale_of(unsigned w) {
+  return __uint_as_float(I == 3 ? w >> 1 : w << (23 - 8 * I));
 }
 
 hipError_t launch_cache_write(const CacheArgs& a, bool bf, hipStream_t stream);

@@ -91,7 +91,7 @@ __global__ void __launch_bounds__(256) cache_write_kernel(CacheArgs a, int ngrou
   const Held h = held_of(a, o.b);
   const long p0 = ((h.start >> 2) + o.grp) * 4;
   if (p0 + 4 <= 0 || p0 + 4 <= h.first || p0 >= h.end) return;
-  unsigned char* page = p0 >= 0 ? page_of(a, o.b, o.hk, p0 / kPage) : nullptr;
+  unsigned char* page = p0 >= 0 ? page_at(a, o.b, o.hk, (int)(p0 / kPage % a.P)) : nullptr;
   if (!page) return;
   const int j0 = (int)(p0 % kPage), ta = j0 >> 4, tg = (j0 >> 2) & 3;
   const int ch = 32 * o.blk + 8 * o.g;
@@ -105,8 +105,8 @@ __global__ void __launch_bounds__(256) cache_write_kernel(CacheArgs a, int ngrou
     float x[8] = {}, y[8] = {};
     if (on[i]) {
       const int t = (int)(p - h.start);
-      ld8<BF>(x, row_of<E>(a.k, o.b, o.hk, t) + ch);
-      ld8<BF>(y, row_of<E>(a.v, o.b, o.hk, t) + ch);
+      ld8<BF>(x, row_of<E>(a.x, o.b, o.hk, t) + ch);
+      ld8<BF>(y, row_of<E>(a.y, o.b, o.hk, t) + ch);
     }
     kc[i] = encode(x, ke[i]);
     vc[i] = encode(y, ve[i]);
@@ -160,7 +160,7 @@ __global__ void __launch_bounds__(256) cache_read_kernel(CacheArgs a, int ngroup
   const Held h = held_of(a, o.b);
   const long p0 = ((h.start >> 2) + o.grp) * 4;
   const unsigned char* page = p0 >= 0 && p0 + 4 > h.first && p0 < h.end
-                                  ? page_of(a, o.b, o.hk, p0 / kPage) : nullptr;
+                                  ? page_at(a, o.b, o.hk, (int)(p0 / kPage % a.P)) : nullptr;
   const int j0 = (int)((p0 >= 0 ? p0 : 0) % kPage), ta = j0 >> 4, tg = (j0 >> 2) & 3;
   const int ch = 32 * o.blk + 8 * o.g;
   unsigned kc[4] = {}, vw[4] = {}, ke[4] = {}, ve = 0;
@@ -183,12 +183,12 @@ __global__ void __launch_bounds__(256) cache_read_kernel(CacheArgs a, int ngroup
       unsigned c = 0;
 #pragma unroll
       for (int j = 0; j < 4; ++j) c |= (vw[j] >> (8 * i) & 255u) << (8 * j);
-      decode(x, kc[i], pow_of(ke[i]));
-      decode(y, c, pow_of(ve >> (8 * i) & 255u));
+      decode(x, kc[i], scale_of<0>(ke[i]));
+      decode(y, c, scale_of<0>(ve >> (8 * i)));
     }
     const int t = (int)(p - h.start);
-    st8<BF>(row_of_w<E>(a.k, o.b, o.hk, t) + ch, x);
-    st8<BF>(row_of_w<E>(a.v, o.b, o.hk, t) + ch, y);
+    st8<BF>(row_of_w<E>(a.x, o.b, o.hk, t) + ch, x);
+    st8<BF>(row_of_w<E>(a.y, o.b, o.hk, t) + ch, y);
   }
 }
 
@@ -200,14 +200,14 @@ unsigned blocks_of(const CacheArgs& a) {
 }  // namespace
 
 hipError_t launch_cache_write(const CacheArgs& a, bool bf, hipStream_t s) {
-  const bool tf = a.k.t < a.k.h;
+  const bool tf = a.x.t < a.x.h;
   if (bf) hipLaunchKernelGGL(cache_write_kernel<true>, dim3(blocks_of(a)), dim3(256), 0, s, a, groups_of(a), tf);
   else hipLaunchKernelGGL(cache_write_kernel<false>, dim3(blocks_of(a)), dim3(256), 0, s, a, groups_of(a), tf);
   return hipGetLastError();
 }
 
 hipError_t launch_cache_read(const CacheArgs& a, bool bf, hipStream_t s) {
-  const bool tf = a.k.t < a.k.h;
+  const bool tf = a.x.t < a.x.h;
   if (bf) hipLaunchKernelGGL(cache_read_kernel<true>, dim3(blocks_of(a)), dim3(256), 0, s, a, groups_of(a), tf);
   else hipLaunchKernelGGL(cache_read_kernel<false>, dim3(blocks_of(a)), dim3(256), 0, s, a, groups_of(a), tf);
   return hipGetLastError();
