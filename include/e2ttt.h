@@ -528,9 +528,13 @@ typedef struct {
   e2ttt_strides d_out, dq, dk, dv;
 } e2ttt_attn_strides;
 
+/* workspace: e2ttt_attn_workspace_bytes bytes (where that is 0, NULL will do; it is
+ * 0 for a bad descriptor too), not to be shared by calls that may overlap. */
+size_t e2ttt_attn_workspace_bytes(const e2ttt_attn_desc* desc);
 e2ttt_status e2ttt_attn_forward(const e2ttt_attn_desc* desc, const e2ttt_attn_strides* strides,
                                 const void* q, const void* k, const void* v,
-                                const int32_t* lengths, void* out, float* lse, void* stream);
+                                const int32_t* lengths, void* out, float* lse, void* workspace,
+                                size_t workspace_bytes, void* stream);
 
 /* Backward of  sum <d_out, out> + <d_lse, lse>  (d_lse [B][H][T] NULL: zero; not
  * read where lse is -inf) with the forward's inputs, out and lse.  The

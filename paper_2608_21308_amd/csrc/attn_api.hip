@@ -28,8 +28,30 @@ e2ttt_status check_desc(const e2ttt_attn_desc* d) {
   return E2TTT_OK;
 }
 
-size_t rows_bytes(const e2ttt_attn_desc* d) {
-  return ((size_t)d->B * d->H * d->T * 4 + 255) & ~(size_t)255;
+size_t up(size_t x) { return (x + 255) & ~(size_t)255; }
+size_t rows_bytes(const e2ttt_attn_desc* d) { return up((size_t)d->B * d->H * d->T * 4); }
+
+// How the workgroups of both directions are split, and the bytes that this takes.
+struct Plan {
+  int nsplit, nsplit_kv;
+  size_t ml, forward, backward;
+};
+// Of n, those within reach of 128 neighbouring tokens.
+long within(const e2ttt_attn_desc* d, long n) {
+  return d->left < 0 || d->right < 0 ? n : std::min(n, (long)d->left + d->right + 128);
+}
+Plan plan(const e2ttt_attn_desc* d) {
+  Plan p{};
+  const long B = d->B, H = d->H, HK = d->HK, T = d->T, S = d->S;
+  const long tile = attn_tile(d->io == E2TTT_DT_BF16, d->d);
+  p.nsplit = attn_splits(B * H * ((T + 127) / 128), within(d, S) / tile);
+  p.nsplit_kv = attn_splits(B * HK * ((S + 127) / 128), H / HK * ((within(d, T) + tile - 1) / tile));
+  const size_t q = p.nsplit > 1 ? up((size_t)p.nsplit * B * H * T * d->d * 4) : 0;
+  const size_t kv = p.nsplit_kv > 1 ? up((size_t)p.nsplit_kv * B * HK * S * d->d * 8) : 0;
+  p.ml = q;
+  p.forward = q ? q + up((size_t)p.nsplit * B * H * T * 8) : 0;
+  p.backward = 2 * rows_bytes(d) + std::max(q, kv);
+  return p;
 }
 
 AttnArgs args_of(const e2ttt_attn_desc* d, const int32_t* lengths) {
@@ -48,25 +70,35 @@ AttnArgs args_of(const e2ttt_attn_desc* d, const int32_t* lengths) {
 using namespace e2ttt;
 
 extern "C" size_t e2ttt_attn_scratch_bytes(const e2ttt_attn_desc* desc) {
-  return check_desc(desc) == E2TTT_OK ? 2 * rows_bytes(desc) : 0;
+  return check_desc(desc) == E2TTT_OK ? plan(desc).backward : 0;
+}
+
+extern "C" size_t e2ttt_attn_workspace_bytes(const e2ttt_attn_desc* desc) {
+  return check_desc(desc) == E2TTT_OK ? plan(desc).forward : 0;
 }
 
 extern "C" e2ttt_status e2ttt_attn_forward(const e2ttt_attn_desc* desc,
                                            const e2ttt_attn_strides* strides, const void* q,
                                            const void* k, const void* v, const int32_t* lengths,
-                                           void* out, float* lse, void* stream) {
+                                           void* out, float* lse, void* workspace,
+                                           size_t workspace_bytes, void* stream) {
   e2ttt_status st = check_desc(desc);
   if (st != E2TTT_OK) return st;
-  if (!q || !k || !v || !out) return E2TTT_ERR_NULL_ARG;
+  const Plan p = plan(desc);
+  if (!q || !k || !v || !out || (p.forward && !workspace)) return E2TTT_ERR_NULL_ARG;
   AttnArgs a = args_of(desc, lengths);
   const RowSpec qs{desc->B, desc->T, desc->d, desc->io}, ks{desc->B, desc->S, desc->d, desc->io};
   const e2ttt_attn_strides* s = strides;
   if (!qs.read(s ? &s->q : nullptr, q, desc->H, &a.q) ||
       !ks.read(s ? &s->k : nullptr, k, desc->HK, &a.k) ||
       !ks.read(s ? &s->v : nullptr, v, desc->HK, &a.v) ||
-      !qs.write(s ? &s->out : nullptr, out, desc->H, &a.out))
+      !qs.write(s ? &s->out : nullptr, out, desc->H, &a.out) || misaligned(workspace))
     return E2TTT_ERR_BAD_SHAPE;
+  if (workspace_bytes < p.forward) return E2TTT_ERR_WORKSPACE_TOO_SMALL;
   a.lse = lse;
+  a.nsplit = p.nsplit;
+  a.part = static_cast<float*>(workspace);
+  a.part_ml = reinterpret_cast<float2*>(static_cast<char*>(workspace) + p.ml);
   return launch_attn_forward(a, desc->io == E2TTT_DT_BF16, static_cast<hipStream_t>(stream)) == hipSuccess
              ? E2TTT_OK : E2TTT_ERR_HIP;
 }
@@ -93,11 +125,15 @@ extern "C" e2ttt_status e2ttt_attn_backward(const e2ttt_attn_desc* desc,
       !ks.write(s ? &s->dk : nullptr, dk, desc->HK, &a.dk) ||
       !ks.write(s ? &s->dv : nullptr, dv, desc->HK, &a.dv) || misaligned(scratch))
     return E2TTT_ERR_BAD_SHAPE;
-  if (scratch_bytes < 2 * rows_bytes(desc)) return E2TTT_ERR_WORKSPACE_TOO_SMALL;
+  const Plan p = plan(desc);
+  if (scratch_bytes < p.backward) return E2TTT_ERR_WORKSPACE_TOO_SMALL;
   a.lse = const_cast<float*>(lse);
   a.d_lse = d_lse;
   a.ex = static_cast<float*>(scratch);
   a.delta = reinterpret_cast<float*>(static_cast<char*>(scratch) + rows_bytes(desc));
+  a.nsplit = p.nsplit;
+  a.nsplit_kv = p.nsplit_kv;
+  a.part = reinterpret_cast<float*>(static_cast<char*>(scratch) + 2 * rows_bytes(desc));
   return launch_attn_backward(a, desc->io == E2TTT_DT_BF16, static_cast<hipStream_t>(stream)) == hipSuccess
              ? E2TTT_OK : E2TTT_ERR_HIP;
 }

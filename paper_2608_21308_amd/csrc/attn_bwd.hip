@@ -29,11 +29,11 @@ __global__ void __launch_bounds__(256, BF ? 2 : 1) attn_dq_kernel(AttnArgs a, in
   constexpr int NT = BK / 32, KS = D / 16, NM = D / 32;
   __shared__ __align__(16) E lk0[BK * D], lk1[BK * D], lv0[BK * D], lv1[BK * D];
   const int lane = threadIdx.x & 63, w = wave_id(), h = lane >> 5, c = lane & 31;
-  const int id = xcd_order(blockIdx.x, gridDim.x), u = id / ntile;
-  const int part = ntile - 1 - id % ntile;
+  const int id = xcd_order(blockIdx.x, gridDim.x), y = id / ntile;
+  const int tile = ntile - 1 - id % ntile, split = y % a.nsplit, u = y / a.nsplit;
   const int b = u / a.H, hq = u % a.H, hk = hq / (a.H / a.HK);
   const int off = a.S - a.T, live = live_of(a, b), end = live + off;
-  const int t0 = part * 128, tw = t0 + 32 * w, t = tw + c;
+  const int t0 = tile * 128, tw = t0 + 32 * w, t = tw + c;
   const bool on = t < live;
 
   X q[KS], g[KS];
@@ -53,13 +53,13 @@ __global__ void __launch_bounds__(256, BF ? 2 : 1) attn_dq_kernel(AttnArgs a, in
     }
   }
   dot = both_sum(dot);
-  const long at = ((long)b * a.H + hq) * a.T + t;
+  const long at = (long)u * a.T + t;
   float ex = kNegInf;
   if (on) {
     ex = exponent_of(a.lse[at]);
     if (a.d_lse && ex != kNegInf) dot -= a.d_lse[at];
   }
-  if (t < a.T && h == 0) {
+  if (t < a.T && h == 0 && split == 0) {
     a.ex[at] = ex;
     a.delta[at] = -dot;
   }
@@ -71,8 +71,9 @@ __global__ void __launch_bounds__(256, BF ? 2 : 1) attn_dq_kernel(AttnArgs a, in
   for (int i = 0; i < 16; ++i) none[i] = -dot;
   const float cs = a.scale * kLog2e;
   const int p0 = t0 + off, p1 = min(t0 + 128, live) + off;
-  const int lo = a.left < 0 ? 0 : max(0, p0 - a.left);
-  const int hi = t0 >= live ? lo : a.right < 0 ? end : min(end, p1 + a.right);
+  int lo = a.left < 0 ? 0 : max(0, p0 - a.left);
+  int hi = t0 >= live ? lo : a.right < 0 ? end : min(end, p1 + a.right);
+  if (a.nsplit > 1) stretch_of(lo, hi, BK, split, a.nsplit);
   const int pw0 = tw + off, pw1 = min(tw + 32, live) + off, p = pw0 + c;
   const int wlo = a.left < 0 ? 0 : max(0, pw0 - a.left);
   const int whi = tw >= live ? wlo : a.right < 0 ? end : min(end, pw1 + a.right);
@@ -134,6 +135,12 @@ __global__ void __launch_bounds__(256, BF ? 2 : 1) attn_dq_kernel(AttnArgs a, in
     if (j0 + BK < hi) step(j0 + BK, lk1, lv1, lk0, lv0);
   }
   if (t >= a.T) return;
+  if (a.nsplit > 1) {
+    float* row = a.part + ((long)split * a.B * a.H * a.T + at) * a.d;
+#pragma unroll
+    for (int m = 0; m < NM; ++m) st_part(row, o[m], m, h, a.d);
+    return;
+  }
   E* drow = row_of_w<E>(a.dq, b, hq, t);
   const float f = on ? a.scale : 0.0f;
 #pragma unroll
@@ -150,7 +157,8 @@ __global__ void __launch_bounds__(256, BF && D <= 64 ? 2 : 1) attn_dkv_kernel(At
   __shared__ __align__(16) E lq0[BQ * D], lq1[BQ * D], lg0[BQ * D], lg1[BQ * D];
   __shared__ __align__(16) float lx0[2][64], lx1[2][64];   // exponents and -D of the queries
   const int lane = threadIdx.x & 63, w = wave_id(), h = lane >> 5, c = lane & 31;
-  const int id = xcd_order(blockIdx.x, gridDim.x), u = id / ntile;
+  const int id = xcd_order(blockIdx.x, gridDim.x), y = id / ntile;
+  const int split = y % a.nsplit_kv, u = y / a.nsplit_kv;
   const int b = u / a.HK, hk = u % a.HK, rep = a.H / a.HK;
   const int off = a.S - a.T, live = live_of(a, b), end = live + off;
   const int j0 = id % ntile * 128, jw = j0 + 32 * w, j = jw + c;
@@ -192,9 +200,11 @@ __global__ void __launch_bounds__(256, BF && D <= 64 ? 2 : 1) attn_dkv_kernel(At
     const long at = ((long)b * a.H + hq) * a.T + t;
     if (w < 2) stage64(nx[w], (w ? a.delta : a.ex) + at, min(live - t, BQ), lane);
   };
-  int r = 0, t0 = lo;
-  long left = (long)per * rep;
-  if (per) fetch(0, lo, lq0, lg0, lx0);
+  // the stretch of (head, tile of queries) that this workgroup takes
+  const long n0 = (long)per * rep * split / a.nsplit_kv, n1 = (long)per * rep * (split + 1) / a.nsplit_kv;
+  int r = per ? (int)(n0 / per) : 0, t0 = per ? lo + (int)(n0 % per) * BQ : lo;
+  long left = n1 - n0;
+  if (left > 0) fetch(r, t0, lq0, lg0, lx0);
   auto step = [&](const E* lq, const E* lg, const float (*lx)[64], E* nq, E* ng,
                   float (*nx)[64]) __attribute__((always_inline)) {
     staged();
@@ -260,6 +270,15 @@ __global__ void __launch_bounds__(256, BF && D <= 64 ? 2 : 1) attn_dkv_kernel(At
     if (left > 0) step(lq1, lg1, lx1, lq0, lg0, lx0);
   }
   if (j >= a.S) return;
+  if (a.nsplit_kv > 1) {
+    const long rows = (long)a.B * a.HK * a.S, row = split * rows + (long)u * a.S + j;
+#pragma unroll
+    for (int m = 0; m < NM; ++m) {
+      st_part(a.part + row * a.d, dk[m], m, h, a.d);
+      st_part(a.part + (a.nsplit_kv * rows + row) * a.d, dv[m], m, h, a.d);
+    }
+    return;
+  }
   E* dkr = row_of_w<E>(a.dk, b, hk, j);
   E* dvr = row_of_w<E>(a.dv, b, hk, j);
 #pragma unroll
@@ -269,21 +288,54 @@ __global__ void __launch_bounds__(256, BF && D <= 64 ? 2 : 1) attn_dkv_kernel(At
   }
 }
 
-template <bool BF, int D, int BK>
+// The stretches of a row [B][H][T] joined: a thread per four channels.
+template <bool BF>
+__global__ void __launch_bounds__(256) attn_sum_kernel(View out, const float* part, int n, int B, int H,
+                                                       int T, int d, float scale) {
+  const int nq = d / 4;
+  const long id = (long)blockIdx.x * 256 + threadIdx.x, rows = (long)B * H * T;
+  if (id >= rows * nq) return;
+  const long row = id / nq;
+  const int ch = (int)(id % nq) * 4, t = (int)(row % T), u = (int)(row / T);
+  f32x4 x = zero4();
+#pragma unroll 4
+  for (int s = 0; s < n; ++s) {
+    const f32x4 o = *reinterpret_cast<const f32x4*>(part + (s * rows + row) * d + ch);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] += o[i];
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x[i] *= scale;
+  IoT<BF>::st4(row_of_w<typename MOp<BF>::E>(out, u / H, u % H, t) + ch, x);
+}
+template <bool BF>
+void join(const View& out, const float* part, int n, int B, int H, int T, int d, float scale, hipStream_t s) {
+  hipLaunchKernelGGL((attn_sum_kernel<BF>), dim3((unsigned)(((long)B * H * T * (d / 4) + 255) / 256)),
+                     dim3(256), 0, s, out, part, n, B, H, T, d, scale);
+}
+
+template <bool BF, int D>
 hipError_t go(const AttnArgs& a, hipStream_t s) {
+  constexpr int BK = attn_tile(BF, D);
   const int nq = (a.T + 127) / 128, nk = (a.S + 127) / 128;
-  hipLaunchKernelGGL((attn_dq_kernel<BF, D, BK>), dim3((unsigned)((long)a.B * a.H * nq)), dim3(256),
-                     0, s, a, nq);
-  hipLaunchKernelGGL((attn_dkv_kernel<BF, D, BK>), dim3((unsigned)((long)a.B * a.HK * nk)),
-                     dim3(256), 0, s, a, nk);
+  hipLaunchKernelGGL((attn_dq_kernel<BF, D, BK>), dim3((unsigned)((long)a.B * a.H * nq * a.nsplit)),
+                     dim3(256), 0, s, a, nq);
+  if (a.nsplit > 1) join<BF>(a.dq, a.part, a.nsplit, a.B, a.H, a.T, a.d, a.scale, s);
+  hipLaunchKernelGGL((attn_dkv_kernel<BF, D, BK>),
+                     dim3((unsigned)((long)a.B * a.HK * nk * a.nsplit_kv)), dim3(256), 0, s, a, nk);
+  if (a.nsplit_kv > 1) {
+    const long all = (long)a.nsplit_kv * a.B * a.HK * a.S * a.d;
+    join<BF>(a.dk, a.part, a.nsplit_kv, a.B, a.HK, a.S, a.d, a.scale, s);
+    join<BF>(a.dv, a.part + all, a.nsplit_kv, a.B, a.HK, a.S, a.d, 1.0f, s);
+  }
   return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_attn_backward(const AttnArgs& a, bool bf, hipStream_t s) {
-  if (bf) return a.d <= 32 ? go<true, 32, 64>(a, s) : a.d <= 64 ? go<true, 64, 64>(a, s) : go<true, 128, 64>(a, s);
-  return a.d <= 32 ? go<false, 32, 64>(a, s) : a.d <= 64 ? go<false, 64, 64>(a, s) : go<false, 128, 32>(a, s);
+  if (bf) return a.d <= 32 ? go<true, 32>(a, s) : a.d <= 64 ? go<true, 64>(a, s) : go<true, 128>(a, s);
+  return a.d <= 32 ? go<false, 32>(a, s) : a.d <= 64 ? go<false, 64>(a, s) : go<false, 128>(a, s);
 }
 
 }  // namespace e2ttt

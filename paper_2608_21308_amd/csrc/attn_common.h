@@ -33,6 +33,12 @@ struct AttnArgs {
   int B, HK, H, T, S, d;
   int left, right;            // at most 2^30 - 1; negative: no bound
   float scale;
+  // A tile of queries (keys) as several workgroups, each over a stretch of the keys
+  // (queries): their sums [stretch][row][d] and, in the forward, [stretch][row] {reference,
+  // sum} are joined by another kernel.
+  int nsplit, nsplit_kv;
+  float* part;
+  float2* part_ml;
 };
 
 constexpr float kLog2e = 1.44269504088896f;
@@ -221,6 +227,28 @@ __device__ __forceinline__ int xcd_order(int id, int n) {
 __device__ __forceinline__ int live_of(const AttnArgs& a, int b) {
   return a.lengths ? max(0, min(a.T, a.lengths[b])) : a.T;
 }
+
+// The sums of a lane's row, before they are joined.
+__device__ __forceinline__ void st_part(float* row, const f32x16& o, int m, int h, int d) {
+#pragma unroll
+  for (int a = 0; a < 4; ++a) {
+    const int ch = 32 * m + 8 * a + 4 * h;
+    if (ch < d)
+      *reinterpret_cast<f32x4*>(row + ch) = f32x4{o[4 * a], o[4 * a + 1], o[4 * a + 2], o[4 * a + 3]};
+  }
+}
+// Stretch `split` of `n` of the range lo .. hi - 1, in whole tiles of `tile`.
+__device__ __forceinline__ void stretch_of(int& lo, int& hi, int tile, int split, int n) {
+  const int nt = hi > lo ? (hi - lo + tile - 1) / tile : 0;
+  const int l = lo;
+  lo = l + (int)((long)nt * split / n) * tile;
+  hi = min(hi, l + (int)((long)nt * (split + 1) / n) * tile);
+}
+
+// Rows of keys (queries) of a tile of the inner loops.
+constexpr int attn_tile(bool bf, int d) { return !bf && d > 64 ? 32 : 64; }
+// Stretches that `groups` workgroups of `tiles` tiles each are split into.
+int attn_splits(long groups, long tiles);
 
 hipError_t launch_attn_forward(const AttnArgs& a, bool bf, hipStream_t stream);
 hipError_t launch_attn_backward(const AttnArgs& a, bool bf, hipStream_t stream);

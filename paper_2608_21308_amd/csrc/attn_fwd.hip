@@ -7,6 +7,8 @@
 // unrounded ones).
 #include <math.h>
 
+#include <algorithm>
+
 #include "attn_common.h"
 
 namespace e2ttt {
@@ -22,8 +24,9 @@ __global__ void __launch_bounds__(256, BF ? 2 : 1) attn_fwd_kernel(AttnArgs a, i
   // (apart by name: a read of one is then known not to wait for loads into another)
   __shared__ __align__(16) E lk0[BK * D], lk1[BK * D], lv0[BK * D], lv1[BK * D];
   const int lane = threadIdx.x & 63, w = wave_id(), h = lane >> 5, c = lane & 31;
-  const int id = xcd_order(blockIdx.x, gridDim.x), u = id / ntile;
+  const int id = xcd_order(blockIdx.x, gridDim.x), x = id / ntile;
   const int tile = ntile - 1 - id % ntile;             // (long rows of a causal mask first)
+  const int split = x % a.nsplit, u = x / a.nsplit;
   const int b = u / a.H, hq = u % a.H, hk = hq / (a.H / a.HK);
   const int off = a.S - a.T, live = live_of(a, b), end = live + off;
   const int t0 = tile * 128, tw = t0 + 32 * w, t = tw + c;
@@ -43,8 +46,9 @@ __global__ void __launch_bounds__(256, BF ? 2 : 1) attn_fwd_kernel(AttnArgs a, i
 
   // keys that some query of the workgroup, of this wave sees
   const int p0 = t0 + off, p1 = min(t0 + 128, live) + off;
-  const int lo = a.left < 0 ? 0 : max(0, p0 - a.left);
-  const int hi = t0 >= live ? lo : a.right < 0 ? end : min(end, p1 + a.right);
+  int lo = a.left < 0 ? 0 : max(0, p0 - a.left);
+  int hi = t0 >= live ? lo : a.right < 0 ? end : min(end, p1 + a.right);
+  if (a.nsplit > 1) stretch_of(lo, hi, BK, split, a.nsplit);
   const int pw0 = tw + off, pw1 = min(tw + 32, live) + off, p = pw0 + c;
   const int wlo = a.left < 0 ? 0 : max(0, pw0 - a.left);
   const int whi = tw >= live ? wlo : a.right < 0 ? end : min(end, pw1 + a.right);
@@ -124,29 +128,79 @@ __global__ void __launch_bounds__(256, BF ? 2 : 1) attn_fwd_kernel(AttnArgs a, i
   }
   if (t >= a.T) return;
   sum = both_sum(sum);
+  const long at = (long)u * a.T + t;
+  if (a.nsplit > 1) {
+    const long row = (long)split * a.B * a.H * a.T + at;
+#pragma unroll
+    for (int m = 0; m < NM; ++m) st_part(a.part + row * a.d, o[m], m, h, a.d);
+    if (h == 0) a.part_ml[row] = make_float2(sum == 0.0f ? kNegInf : ref, sum);
+    return;
+  }
   const bool some = t < live && sum != 0.0f;
   const float inv = some ? 1.0f / sum : 0.0f;
   E* orow = row_of_w<E>(a.out, b, hq, t);
 #pragma unroll
   for (int m = 0; m < NM; ++m) st_tile<BF>(orow, o[m], inv, m, h, a.d);
   if (a.lse && h == 0)
-    a.lse[((long)b * a.H + hq) * a.T + t] =
-        some ? fmaf(ref, a.scale, logf(sum)) : kNegInf;
+    a.lse[at] = some ? fmaf(ref, a.scale, logf(sum)) : kNegInf;
 }
 
-template <bool BF, int D, int BK>
+// The stretches of a query joined: a thread per four channels.
+template <bool BF>
+__global__ void __launch_bounds__(256) attn_join_kernel(AttnArgs a) {
+  using E = typename MOp<BF>::E;
+  const int nq = a.d / 4;
+  const long id = (long)blockIdx.x * 256 + threadIdx.x, rows = (long)a.B * a.H * a.T;
+  if (id >= rows * nq) return;
+  const long row = id / nq;
+  const int ch = (int)(id % nq) * 4, t = (int)(row % a.T), u = (int)(row / a.T), b = u / a.H;
+  const float cs = a.scale * kLog2e;
+  float most = kNegInf, sum = 0.0f;
+  for (int s = 0; s < a.nsplit; ++s) most = fmaxf(most, a.part_ml[s * rows + row].x);
+  const float ref = most == kNegInf ? 0.0f : most;
+  f32x4 x = zero4();
+#pragma unroll 4
+  for (int s = 0; s < a.nsplit; ++s) {
+    const float2 ml = a.part_ml[s * rows + row];
+    const float f = __builtin_amdgcn_exp2f((ml.x - ref) * cs);
+    const f32x4 o = *reinterpret_cast<const f32x4*>(a.part + (s * rows + row) * a.d + ch);
+    sum = fmaf(ml.y, f, sum);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = fmaf(o[i], f, x[i]);
+  }
+  const bool some = t < live_of(a, b) && sum != 0.0f;
+  const float inv = some ? 1.0f / sum : 0.0f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x[i] *= inv;
+  IoT<BF>::st4(row_of_w<E>(a.out, b, u % a.H, t) + ch, x);
+  if (a.lse && ch == 0) a.lse[row] = some ? fmaf(ref, a.scale, logf(sum)) : kNegInf;
+}
+
+template <bool BF, int D>
 hipError_t go(const AttnArgs& a, hipStream_t s) {
   const int ntile = (a.T + 127) / 128;
-  hipLaunchKernelGGL((attn_fwd_kernel<BF, D, BK>), dim3((unsigned)((long)a.B * a.H * ntile)),
-                     dim3(256), 0, s, a, ntile);
+  hipLaunchKernelGGL((attn_fwd_kernel<BF, D, attn_tile(BF, D)>),
+                     dim3((unsigned)((long)a.B * a.H * ntile * a.nsplit)), dim3(256), 0, s, a, ntile);
+  if (a.nsplit > 1)
+    hipLaunchKernelGGL((attn_join_kernel<BF>),
+                       dim3((unsigned)(((long)a.B * a.H * a.T * (a.d / 4) + 255) / 256)), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
 }  // namespace
 
+// A workgroup alone on its CU takes a tile of keys in 1 to 2 us, a split costs the
+// join, 5 us. Forward, in two halves of the card's 512 places and more, and whole: 64
+// groups of 72 tiles (head dim 128) 41 us and 82, of 128 tiles (64) 31 and 116, of 32
+// tiles in 4 and in 8 (128) 25.5 and 29.6, whole 41; 8 groups of 15 tiles in 3 14.2 and
+// 18.8; but 16 groups of 9 tiles in 2 17.6 and 15.4, 192 groups of 24 tiles 37 and 33.
+int attn_splits(long groups, long tiles) {
+  return groups > 160 ? 1 : (int)std::max(1L, std::min(512 / groups, tiles / 6));
+}
+
 hipError_t launch_attn_forward(const AttnArgs& a, bool bf, hipStream_t s) {
-  if (bf) return a.d <= 32 ? go<true, 32, 64>(a, s) : a.d <= 64 ? go<true, 64, 64>(a, s) : go<true, 128, 64>(a, s);
-  return a.d <= 32 ? go<false, 32, 64>(a, s) : a.d <= 64 ? go<false, 64, 64>(a, s) : go<false, 128, 32>(a, s);
+  if (bf) return a.d <= 32 ? go<true, 32>(a, s) : a.d <= 64 ? go<true, 64>(a, s) : go<true, 128>(a, s);
+  return a.d <= 32 ? go<false, 32>(a, s) : a.d <= 64 ? go<false, 64>(a, s) : go<false, 128>(a, s);
 }
 
 }  // namespace e2ttt

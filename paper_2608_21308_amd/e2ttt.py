@@ -40,8 +40,8 @@ EXPORTS = ("e2ttt_param_count", "e2ttt_workspace_bytes", "e2ttt_backward_scratch
            "e2ttt_chunk_forward_static", "e2ttt_chunk_forward_ln", "e2ttt_chunk_backward_ln",
            "e2ttt_apply_ln", "e2ttt_delta_workspace_bytes", "e2ttt_delta_scratch_bytes",
            "e2ttt_delta_forward", "e2ttt_delta_backward", "e2ttt_delta_step",
-           "e2ttt_qk_forward", "e2ttt_qk_backward", "e2ttt_attn_forward",
-           "e2ttt_attn_scratch_bytes", "e2ttt_attn_backward", "e2ttt_cache_page_bytes",
+           "e2ttt_qk_forward", "e2ttt_qk_backward", "e2ttt_attn_workspace_bytes",
+           "e2ttt_attn_forward", "e2ttt_attn_scratch_bytes", "e2ttt_attn_backward", "e2ttt_cache_page_bytes",
            "e2ttt_cache_write", "e2ttt_cache_read", "e2ttt_cache_workspace_bytes",
            "e2ttt_cache_attend", "e2ttt_status_str")
 
@@ -169,7 +169,9 @@ def load():
     lib.e2ttt_qk_backward.argtypes = [qd, qs] + [vp] * 9
     lib.e2ttt_qk_backward.restype = i
     ad, as_ = ctypes.POINTER(AttentionDesc), ctypes.POINTER(AttentionStrides)
-    lib.e2ttt_attn_forward.argtypes = [ad, as_] + [vp] * 7
+    lib.e2ttt_attn_workspace_bytes.argtypes = [ad]
+    lib.e2ttt_attn_workspace_bytes.restype = sz
+    lib.e2ttt_attn_forward.argtypes = [ad, as_] + [vp] * 7 + [sz, vp]
     lib.e2ttt_attn_forward.restype = i
     lib.e2ttt_attn_scratch_bytes.argtypes = [ad]
     lib.e2ttt_attn_scratch_bytes.restype = sz
@@ -1068,8 +1070,13 @@ class AttentionConfig:
         return {n: v for n, v in self.__dict__.items() if n != "_call"}
 
 
+def attention_workspace_bytes(cfg: AttentionConfig) -> int:
+    return int((_lib or load()).e2ttt_attn_workspace_bytes(cfg._call[0]))
+
+
 @_on_device
-def attention_forward(cfg: AttentionConfig, q, k, v, *, lengths=None, out=None, lse=None):
+def attention_forward(cfg: AttentionConfig, q, k, v, *, lengths=None, out=None, lse=None,
+                      workspace=None):
     """Runs e2ttt_attn_forward on the current stream: attention of q [B, H, T, d]
     over k, v [B, HK, S, d] (any strides with a contiguous last dimension) over
     the first lengths [B] (int32) tokens of each sequence.  Returns (out, lse);
@@ -1084,8 +1091,13 @@ def attention_forward(cfg: AttentionConfig, q, k, v, *, lengths=None, out=None, 
                  ("out", out, s_q, io))
     _plain("lse", lse, s_l, torch.float32, dev)
     _plain("lengths", lengths, s_l[:1], torch.int32, dev)
-    st = (_lib or load()).e2ttt_attn_forward(d, st, q.data_ptr(), k.data_ptr(), v.data_ptr(),
-                                             _ptr(lengths), out.data_ptr(), lse.data_ptr(), _stream())
+    _buffer("workspace", workspace, dev)
+    if workspace is None:
+        n = attention_workspace_bytes(cfg)
+        workspace = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
+    st = (_lib or load()).e2ttt_attn_forward(
+        d, st, q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(lengths), out.data_ptr(),
+        lse.data_ptr(), _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream())
     if st:
         _check(st, "e2ttt_attn_forward")
     return out, lse

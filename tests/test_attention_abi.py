@@ -27,7 +27,7 @@ def adesc(**kw):
 def calls(lib, d, s=None):
     r = ctypes.byref(d)
     s = None if s is None else ctypes.byref(s)
-    return (lib.e2ttt_attn_forward(r, s, *([FAKE] * 7)),
+    return (lib.e2ttt_attn_forward(r, s, *([FAKE] * 7), 1 << 50, None),
             lib.e2ttt_attn_backward(r, s, *([FAKE] * 12), 1 << 50, None))
 
 
@@ -41,17 +41,25 @@ def test_bad_descriptors(lib, kw, status):
     d = adesc(**kw)
     assert calls(lib, d) == (status,) * 2
     assert lib.e2ttt_attn_scratch_bytes(ctypes.byref(d)) == 0
+    assert lib.e2ttt_attn_workspace_bytes(ctypes.byref(d)) == 0
 
 
 def test_null_alignment_and_sizes(lib):
     d = adesc()
     r = ctypes.byref(d)
-    # forward: q k v lengths out lse stream
+    # forward: q k v lengths out lse workspace
     for i in (0, 1, 2, 4):
         for x, status in ((None, 1), (ctypes.c_void_p(4104), 2)):
-            a = [FAKE] * 6
+            a = [FAKE] * 7
             a[i] = x
-            assert lib.e2ttt_attn_forward(r, None, *a, None) == status, i
+            assert lib.e2ttt_attn_forward(r, None, *a, 1 << 50, None) == status, i
+    long = adesc(B=1, HK=1, H=1, T=64, S=8192)         # (its keys are split)
+    n = lib.e2ttt_attn_workspace_bytes(ctypes.byref(long))
+    assert n >= 2 * 64 * 66 * 4
+    a = [FAKE] * 7
+    assert lib.e2ttt_attn_forward(ctypes.byref(long), None, *a, n - 1, None) == 4
+    assert lib.e2ttt_attn_forward(ctypes.byref(long), None, *a[:6], None, n, None) == 1
+    assert lib.e2ttt_attn_forward(ctypes.byref(long), None, *a[:6], ctypes.c_void_p(4104), n, None) == 2
     # backward: q k v lengths out lse d_out d_lse dq dk dv scratch
     n = lib.e2ttt_attn_scratch_bytes(r)
     assert n >= 8 * 2 * 4 * 100

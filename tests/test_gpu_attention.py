@@ -62,7 +62,10 @@ CASES = [  # B, HK, H, T, S, d, left, right
     (2, 2, 4, 33, 33, 64, 0, 0), (1, 1, 2, 129, 129, 128, 64, 0), (2, 1, 1, 100, 163, 40, 31, 0),
     (1, 2, 6, 260, 260, 72, -1, -1), (1, 1, 1, 150, 70, 32, 20, -1), (2, 2, 2, 65, 300, 96, 100, 7),
     (1, 1, 5, 257, 257, 24, 1 << 30, 1), (1, 3, 3, 192, 192, 128, -1, 0), (1, 1, 1, 300, 300, 64, 63, 0),
-    (3, 1, 2, 64, 64, 120, 2147483647, 2147483647), (1, 1, 1, 40, 400, 16, 5, 0)]
+    (3, 1, 2, 64, 64, 120, 2147483647, 2147483647), (1, 1, 1, 40, 400, 16, 5, 0),
+    # (few tiles of queries, or of keys, that see many: split into stretches and joined)
+    (1, 1, 1, 130, 700, 64, -1, 0), (1, 1, 2, 64, 2000, 128, -1, -1), (1, 2, 8, 300, 300, 64, -1, 0),
+    (2, 1, 4, 70, 900, 32, 600, 0), (1, 1, 1, 1, 1500, 72, -1, 0), (1, 1, 1, 900, 33, 40, -1, -1)]
 
 
 @pytest.mark.parametrize("c", CASES)
