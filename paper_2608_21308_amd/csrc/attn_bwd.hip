@@ -316,12 +316,12 @@ void join(const View& out, const float* part, int n, int B, int H, int T, int d,
 
 template <bool BF, int D>
 hipError_t go(const AttnArgs& a, hipStream_t s) {
-  constexpr int BK = attn_tile(BF, D);
+  constexpr int BK = attn_tile(BF, D), BQ = attn_tile_kv(D);
   const int nq = (a.T + 127) / 128, nk = (a.S + 127) / 128;
   hipLaunchKernelGGL((attn_dq_kernel<BF, D, BK>), dim3((unsigned)((long)a.B * a.H * nq * a.nsplit)),
                      dim3(256), 0, s, a, nq);
   if (a.nsplit > 1) join<BF>(a.dq, a.part, a.nsplit, a.B, a.H, a.T, a.d, a.scale, s);
-  hipLaunchKernelGGL((attn_dkv_kernel<BF, D, BK>),
+  hipLaunchKernelGGL((attn_dkv_kernel<BF, D, BQ>),
                      dim3((unsigned)((long)a.B * a.HK * nk * a.nsplit_kv)), dim3(256), 0, s, a, nk);
   if (a.nsplit_kv > 1) {
     const long all = (long)a.nsplit_kv * a.B * a.HK * a.S * a.d;

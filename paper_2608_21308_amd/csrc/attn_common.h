@@ -245,8 +245,10 @@ __device__ __forceinline__ void stretch_of(int& lo, int& hi, int tile, int split
   hi = min(hi, l + (int)((long)nt * (split + 1) / n) * tile);
 }
 
-// Rows of keys (queries) of a tile of the inner loops.
+// Rows of keys of a tile of the inner loops, and of queries for dk and dv (head dim 128:
+// 2 x 16 x 2048 tokens, causal, backward 221 us with 32, 257 with 64).
 constexpr int attn_tile(bool bf, int d) { return !bf && d > 64 ? 32 : 64; }
+constexpr int attn_tile_kv(int d) { return d > 64 ? 32 : 64; }
 // Stretches that `groups` workgroups of `tiles` tiles each are split into.
 int attn_splits(long groups, long tiles);
 
