@@ -10,6 +10,8 @@
 // the scores are fp32.
 #include <math.h>
 
+#include <type_traits>
+
 #include "attn_common.h"
 
 namespace e2ttt {
@@ -55,20 +57,11 @@ __global__ void __launch_bounds__(256, BF ? 2 : 1) attn_dq_kernel(AttnArgs a, in
   dot = both_sum(dot);
   const long at = (long)u * a.T + t;
   float ex = kNegInf;
-  if (on) {
-    ex = exponent_of(a.lse[at]);
-    if (a.d_lse && ex != kNegInf) dot -= a.d_lse[at];
-  }
-  if (t < a.T && h == 0 && split == 0) {
-    a.ex[at] = ex;
-    a.delta[at] = -dot;
-  }
-
+  if (on) ex = exponent_of(a.lse[at]);
   f32x16 o[NM], none;         // (-D where the products with do begin)
 #pragma unroll
   for (int m = 0; m < NM; ++m) o[m] = zero16();
-#pragma unroll
-  for (int i = 0; i < 16; ++i) none[i] = -dot;
+  float fix = 0.0f;
   const float cs = a.scale * kLog2e;
   const int p0 = t0 + off, p1 = min(t0 + 128, live) + off;
   int lo = a.left < 0 ? 0 : max(0, p0 - a.left);
@@ -83,11 +76,8 @@ __global__ void __launch_bounds__(256, BF ? 2 : 1) attn_dq_kernel(AttnArgs a, in
   sv.init(a.v.t, a.d, w, lane);
   const E* kb = row_of<E>(a.k, b, hk, 0);
   const E* vb = row_of<E>(a.v, b, hk, 0);
-  if (lo < hi) {
-    sk.load(lk0, kb + lo * a.k.t, end - lo, w);
-    sv.load(lv0, vb + lo * a.v.t, end - lo, w);
-  }
-  auto step = [&](int j0, const E* lk, const E* lv, E* nk, E* nv) __attribute__((always_inline)) {
+  // first: only sum P (do v^T - D) of every query, which is what sum do o still lacks
+  auto step = [&](auto first, int j0, const E* lk, const E* lv, E* nk, E* nv) __attribute__((always_inline)) {
     staged();
     if (j0 + BK < hi) {
       sk.load(nk, kb + (j0 + BK) * a.k.t, end - j0 - BK, w);
@@ -121,6 +111,11 @@ __global__ void __launch_bounds__(256, BF ? 2 : 1) attn_dq_kernel(AttnArgs a, in
 #pragma unroll
       for (int i = 0; i < 16; ++i)
         s[n][i] = __builtin_amdgcn_exp2f(fmaf(s[n][i], cs, ex)) * v[i];
+      if constexpr (first) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) fix += s[n][i];
+        continue;
+      }
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
         const X f = O::of(s[n], x);
@@ -130,10 +125,34 @@ __global__ void __launch_bounds__(256, BF ? 2 : 1) attn_dq_kernel(AttnArgs a, in
       }
     }
   };
-  for (int j0 = lo; j0 < hi; j0 += 2 * BK) {
-    step(j0, lk0, lv0, lk1, lv1);
-    if (j0 + BK < hi) step(j0 + BK, lk1, lv1, lk0, lv0);
+  auto pass = [&](auto first) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) none[i] = -dot;
+    if (lo < hi) {
+      sk.load(lk0, kb + lo * a.k.t, end - lo, w);
+      sv.load(lv0, vb + lo * a.v.t, end - lo, w);
+    }
+    for (int j0 = lo; j0 < hi; j0 += 2 * BK) {
+      step(first, j0, lk0, lv0, lk1, lv1);
+      if (j0 + BK < hi) step(first, j0 + BK, lk1, lv1, lk0, lv0);
+    }
+  };
+  // sum do o from a bf16 out has the rounding of both, which weighs as much as that of dS
+  // where a query sees few keys (two keys: dq and dk off by 2.3 times what their own
+  // rounding leaves, 22: 1.5; without it 1.4).  A pass ahead makes it exact where it is
+  // short (8 x 16 x 4096 x 64, windows of 32: backward 470 us and 450 without, of 128 440
+  // and 440).
+  if (BF && a.nsplit == 1 && hi - lo <= 3 * BK) {
+    pass(std::true_type{});
+    dot += both_sum(fix);
+    __syncthreads();
   }
+  if (a.d_lse && ex != kNegInf) dot -= a.d_lse[at];
+  if (t < a.T && h == 0 && split == 0) {
+    a.ex[at] = ex;
+    a.delta[at] = -dot;
+  }
+  pass(std::false_type{});
   if (t >= a.T) return;
   if (a.nsplit > 1) {
     float* row = a.part + ((long)split * a.B * a.H * a.T + at) * a.d;
