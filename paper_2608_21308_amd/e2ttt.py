@@ -1066,12 +1066,23 @@ class AttentionConfig:
                 torch.Size((self.B, self.HK, self.S or self.T, self.d)),
                 torch.Size((self.B, self.H, self.T)))
 
+    @cached_property
+    def _bytes(self):
+        """Those of the workspace and of the scratch."""
+        lib = _lib or load()
+        return (int(lib.e2ttt_attn_workspace_bytes(self._call[0])),
+                int(lib.e2ttt_attn_scratch_bytes(self._call[0])))
+
     def __getstate__(self):
-        return {n: v for n, v in self.__dict__.items() if n != "_call"}
+        return {n: v for n, v in self.__dict__.items() if n not in ("_call", "_bytes")}
 
 
 def attention_workspace_bytes(cfg: AttentionConfig) -> int:
-    return int((_lib or load()).e2ttt_attn_workspace_bytes(cfg._call[0]))
+    return cfg._bytes[0]
+
+
+def attention_scratch_bytes(cfg: AttentionConfig) -> int:
+    return cfg._bytes[1]
 
 
 @_on_device
@@ -1086,14 +1097,14 @@ def attention_forward(cfg: AttentionConfig, q, k, v, *, lengths=None, out=None, 
     if out is None:
         out = torch.empty_like(q)
     if lse is None:
-        lse = torch.empty(s_l, dtype=torch.float32, device=q.device)
+        lse = q.new_empty(s_l, dtype=torch.float32)
     st = _layout(AttentionStrides, dev, ("q", q, s_q, io), ("k", k, s_k, io), ("v", v, s_k, io),
                  ("out", out, s_q, io))
     _plain("lse", lse, s_l, torch.float32, dev)
     _plain("lengths", lengths, s_l[:1], torch.int32, dev)
     _buffer("workspace", workspace, dev)
     if workspace is None:
-        n = attention_workspace_bytes(cfg)
+        n = cfg._bytes[0]
         workspace = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
     st = (_lib or load()).e2ttt_attn_forward(
         d, st, q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(lengths), out.data_ptr(),
@@ -1103,8 +1114,17 @@ def attention_forward(cfg: AttentionConfig, q, k, v, *, lengths=None, out=None, 
     return out, lse
 
 
-def attention_scratch_bytes(cfg: AttentionConfig) -> int:
-    return int((_lib or load()).e2ttt_attn_scratch_bytes(cfg._call[0]))
+def _run_attention_backward(cfg, st, q, k, v, out, lse, d_out, d_lse, lengths, g, scratch):
+    """The library's call on checked tensors (st: their strides argument)."""
+    if scratch is None:
+        scratch = torch.empty(cfg._bytes[1], dtype=torch.uint8, device=q.device)
+    st = (_lib or load()).e2ttt_attn_backward(
+        cfg._call[0], st, q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(lengths), out.data_ptr(),
+        lse.data_ptr(), d_out.data_ptr(), _ptr(d_lse), g["dq"].data_ptr(), g["dk"].data_ptr(),
+        g["dv"].data_ptr(), scratch.data_ptr(), scratch.numel(), _stream())
+    if st:
+        _check(st, "e2ttt_attn_backward")
+    return g
 
 
 @_on_device
@@ -1122,14 +1142,7 @@ def attention_backward(cfg: AttentionConfig, q, k, v, out, lse, d_out, d_lse=Non
     _plain("d_lse", d_lse, s_l, torch.float32, dev)
     _plain("lengths", lengths, s_l[:1], torch.int32, dev)
     _buffer("scratch", scratch, dev)
-    if scratch is None:
-        scratch = torch.empty(attention_scratch_bytes(cfg), dtype=torch.uint8, device=q.device)
-    st = (_lib or load()).e2ttt_attn_backward(
-        d, st, q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(lengths), out.data_ptr(),
-        lse.data_ptr(), d_out.data_ptr(), _ptr(d_lse), g["dq"].data_ptr(), g["dk"].data_ptr(),
-        g["dv"].data_ptr(), scratch.data_ptr(), scratch.numel(), _stream())
-    _check(st, "e2ttt_attn_backward")
-    return g
+    return _run_attention_backward(cfg, st, q, k, v, out, lse, d_out, d_lse, lengths, g, scratch)
 
 
 def _like(t):
@@ -1145,6 +1158,7 @@ class AttentionFunction(torch.autograd.Function):
     def forward(ctx, cfg, q, k, v, lengths=None):
         out, lse = attention_forward(cfg, q, k, v, lengths=lengths)
         ctx.cfg = cfg
+        ctx.flat = q.is_contiguous() and k.is_contiguous() and v.is_contiguous()
         ctx.save_for_backward(q, k, v, lengths, out, lse)
         ctx.set_materialize_grads(False)
         return out, lse
@@ -1155,10 +1169,20 @@ class AttentionFunction(torch.autograd.Function):
 
 
 def _attention_grads(ctx, d_out, d_lse):
+    cfg = ctx.cfg
     q, k, v, lengths, out, lse = ctx.saved_tensors
     d_out = torch.zeros_like(out) if d_out is None else _as_rows(d_out)
-    g = attention_backward(ctx.cfg, q, k, v, out, lse, d_out,
-                           None if d_lse is None else d_lse.contiguous(), lengths=lengths)
+    if d_lse is not None:
+        d_lse = d_lse.contiguous()
+    _, io, s_q, _, _ = cfg._call
+    dev = q.get_device()
+    if ctx.flat and dev == _current_device() and _flat(d_out, s_q, io, dev):
+        # (the rest was checked by the forward; d_lse is of lse's type and shape)
+        g = _run_attention_backward(cfg, None, q, k, v, out, lse, d_out, d_lse, lengths,
+                                    dict(dq=torch.empty_like(q), dk=torch.empty_like(k),
+                                         dv=torch.empty_like(v)), None)
+    else:
+        g = attention_backward(cfg, q, k, v, out, lse, d_out, d_lse, lengths=lengths)
     return None, g["dq"], g["dk"], g["dv"], None
 
 
