@@ -31,7 +31,7 @@ __global__ void __launch_bounds__(256, BF ? 2 : 1) attn_dq_kernel(AttnArgs a, in
   constexpr int NT = BK / 32, KS = D / 16, NM = D / 32;
   __shared__ __align__(16) E lk0[BK * D], lk1[BK * D], lv0[BK * D], lv1[BK * D];
   const int lane = threadIdx.x & 63, w = wave_id(), h = lane >> 5, c = lane & 31;
-  const int id = xcd_order(blockIdx.x, gridDim.x), y = id / ntile;
+  const int id = xcd_order(blockIdx.x, gridDim.x, a.B * a.HK), y = id / ntile;
   const int tile = ntile - 1 - id % ntile, split = y % a.nsplit, u = y / a.nsplit;
   const int b = u / a.H, hq = u % a.H, hk = hq / (a.H / a.HK);
   const int off = a.S - a.T, live = live_of(a, b), end = live + off;
@@ -142,7 +142,7 @@ __global__ void __launch_bounds__(256, BF ? 2 : 1) attn_dq_kernel(AttnArgs a, in
   // rounding leaves, 22: 1.5; without it 1.4).  A pass ahead makes it exact where it is
   // short (8 x 16 x 4096 x 64, windows of 32: backward 470 us and 450 without, of 128 440
   // and 440).
-  if (BF && a.nsplit == 1 && hi - lo <= 3 * BK) {
+  if (BF && a.nsplit == 1 && hi - lo <= 192) {
     pass(std::true_type{});
     dot += both_sum(fix);
     __syncthreads();
@@ -176,7 +176,7 @@ __global__ void __launch_bounds__(256, BF && D <= 64 ? 2 : 1) attn_dkv_kernel(At
   __shared__ __align__(16) E lq0[BQ * D], lq1[BQ * D], lg0[BQ * D], lg1[BQ * D];
   __shared__ __align__(16) float lx0[2][64], lx1[2][64];   // exponents and -D of the queries
   const int lane = threadIdx.x & 63, w = wave_id(), h = lane >> 5, c = lane & 31;
-  const int id = xcd_order(blockIdx.x, gridDim.x), y = id / ntile;
+  const int id = xcd_order(blockIdx.x, gridDim.x, a.B * a.HK), y = id / ntile;
   const int split = y % a.nsplit_kv, u = y / a.nsplit_kv;
   const int b = u / a.HK, hk = u % a.HK, rep = a.H / a.HK;
   const int off = a.S - a.T, live = live_of(a, b), end = live + off;
@@ -335,12 +335,12 @@ void join(const View& out, const float* part, int n, int B, int H, int T, int d,
 
 template <bool BF, int D>
 hipError_t go(const AttnArgs& a, hipStream_t s) {
-  constexpr int BK = attn_tile(BF, D), BQ = attn_tile_kv(D);
+  constexpr int BK = attn_tile_bwd(D);
   const int nq = (a.T + 127) / 128, nk = (a.S + 127) / 128;
   hipLaunchKernelGGL((attn_dq_kernel<BF, D, BK>), dim3((unsigned)((long)a.B * a.H * nq * a.nsplit)),
                      dim3(256), 0, s, a, nq);
   if (a.nsplit > 1) join<BF>(a.dq, a.part, a.nsplit, a.B, a.H, a.T, a.d, a.scale, s);
-  hipLaunchKernelGGL((attn_dkv_kernel<BF, D, BQ>),
+  hipLaunchKernelGGL((attn_dkv_kernel<BF, D, BK>),
                      dim3((unsigned)((long)a.B * a.HK * nk * a.nsplit_kv)), dim3(256), 0, s, a, nk);
   if (a.nsplit_kv > 1) {
     const long all = (long)a.nsplit_kv * a.B * a.HK * a.S * a.d;

@@ -216,11 +216,14 @@ __device__ __forceinline__ void st_tile(typename MOp<BF>::E* row, const f32x16& 
   }
 }
 
-// Workgroups are dealt to the 8 XCDs in turn: those of an XCD get a stretch of the
-// work, so that what shares keys and values shares an L2.
-__device__ __forceinline__ int xcd_order(int id, int n) {
-  const int x = id & 7, y = id >> 3, per = n >> 3, more = n & 7;
-  return x * per + min(x, more) + y;
+// Workgroups are dealt to the 8 XCDs in turn: those of a key head, which share its keys
+// and values, go to one of them and its L2, the key heads in turn (12 sequences of 250
+// to 3000 tokens, 8 query and 2 key heads of 128: 180 us, backward 600; with an eighth of
+// the workgroups in a row to each XCD 235 and 1017).  What 8 does not divide stays as it is
+// dealt.
+__device__ __forceinline__ int xcd_order(int id, int n, int heads) {
+  const int per = n / heads, full = heads / 8 * 8 * per, y = id >> 3;
+  return id < full ? ((id & 7) + 8 * (y / per)) * per + y % per : id;
 }
 
 // Queries of sequence b that the call takes.
@@ -245,10 +248,12 @@ __device__ __forceinline__ void stretch_of(int& lo, int& hi, int tile, int split
   hi = min(hi, l + (int)((long)nt * (split + 1) / n) * tile);
 }
 
-// Rows of keys of a tile of the inner loops, and of queries for dk and dv (head dim 128:
-// 2 x 16 x 2048 tokens, causal, backward 221 us with 32, 257 with 64).
+// Rows of a tile of the inner loops: of keys in the forward and for dq, of queries for dk
+// and dv.  (Head dim 128, 2 x 16 x 2048 tokens, causal: backward 221 us with 32 rows for dk
+// and dv, 257 with 64; 4 x 32 x 4096, window 1024: 1135 us with 32 for dq, 1170 with 64;
+// the forward 361 with 32, 343 with 64.)
 constexpr int attn_tile(bool bf, int d) { return !bf && d > 64 ? 32 : 64; }
-constexpr int attn_tile_kv(int d) { return d > 64 ? 32 : 64; }
+constexpr int attn_tile_bwd(int d) { return d > 64 ? 32 : 64; }
 // Stretches that `groups` workgroups of `tiles` tiles each are split into.
 int attn_splits(long groups, long tiles);
 

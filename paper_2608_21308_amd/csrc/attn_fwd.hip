@@ -24,7 +24,7 @@ __global__ void __launch_bounds__(256, BF ? 2 : 1) attn_fwd_kernel(AttnArgs a, i
   // (apart by name: a read of one is then known not to wait for loads into another)
   __shared__ __align__(16) E lk0[BK * D], lk1[BK * D], lv0[BK * D], lv1[BK * D];
   const int lane = threadIdx.x & 63, w = wave_id(), h = lane >> 5, c = lane & 31;
-  const int id = xcd_order(blockIdx.x, gridDim.x), x = id / ntile;
+  const int id = xcd_order(blockIdx.x, gridDim.x, a.B * a.HK), x = id / ntile;
   const int tile = ntile - 1 - id % ntile;             // (long rows of a causal mask first)
   const int split = x % a.nsplit, u = x / a.nsplit;
   const int b = u / a.H, hq = u % a.H, hk = hq / (a.H / a.HK);
