@@ -56,7 +56,7 @@ Plan plan(const e2ttt_attn_desc* d) {
 
 AttnArgs args_of(const e2ttt_attn_desc* d, const int32_t* lengths) {
   AttnArgs a{};
-  a.B = d->B; a.HK = d->HK; a.H = d->H; a.T = d->T; a.S = d->S; a.d = d->d;
+  a.B = d->B; a.HK = d->HK; a.H = d->H; a.rep = d->H / d->HK; a.T = d->T; a.S = d->S; a.d = d->d;
   a.left = std::min(d->left, (1 << 30) - 1);
   a.right = std::min(d->right, (1 << 30) - 1);
   a.scale = d->scale;

@@ -31,9 +31,9 @@ __global__ void __launch_bounds__(256, BF ? 2 : 1) attn_dq_kernel(AttnArgs a, in
   constexpr int NT = BK / 32, KS = D / 16, NM = D / 32;
   __shared__ __align__(16) E lk0[BK * D], lk1[BK * D], lv0[BK * D], lv1[BK * D];
   const int lane = threadIdx.x & 63, w = wave_id(), h = lane >> 5, c = lane & 31;
-  const int id = xcd_order(blockIdx.x, gridDim.x, a.B * a.HK), y = id / ntile;
-  const int tile = ntile - 1 - id % ntile, split = y % a.nsplit, u = y / a.nsplit;
-  const int b = u / a.H, hq = u % a.H, hk = hq / (a.H / a.HK);
+  const Place wk = place_of(a.work, blockIdx.x);
+  const int tile = ntile - 1 - wk.tile;
+  const int b = wk.b, hk = wk.hk, hq = hk * a.rep + wk.head, split = wk.split, u = b * a.H + hq;
   const int off = a.S - a.T, live = live_of(a, b), end = live + off;
   const int t0 = tile * 128, tw = t0 + 32 * w, t = tw + c;
   const bool on = t < live;
@@ -167,7 +167,7 @@ __global__ void __launch_bounds__(256, BF ? 2 : 1) attn_dq_kernel(AttnArgs a, in
 }
 
 template <bool BF, int D, int BQ>
-__global__ void __launch_bounds__(256, BF && D <= 64 ? 2 : 1) attn_dkv_kernel(AttnArgs a, int ntile) {
+__global__ void __launch_bounds__(256, BF && D <= 64 ? 2 : 1) attn_dkv_kernel(AttnArgs a) {
   using O = MOp<BF>;
   using E = typename O::E;
   using X = typename O::X;
@@ -176,11 +176,10 @@ __global__ void __launch_bounds__(256, BF && D <= 64 ? 2 : 1) attn_dkv_kernel(At
   __shared__ __align__(16) E lq0[BQ * D], lq1[BQ * D], lg0[BQ * D], lg1[BQ * D];
   __shared__ __align__(16) float lx0[2][64], lx1[2][64];   // exponents and -D of the queries
   const int lane = threadIdx.x & 63, w = wave_id(), h = lane >> 5, c = lane & 31;
-  const int id = xcd_order(blockIdx.x, gridDim.x, a.B * a.HK), y = id / ntile;
-  const int split = y % a.nsplit_kv, u = y / a.nsplit_kv;
-  const int b = u / a.HK, hk = u % a.HK, rep = a.H / a.HK;
+  const Place wk = place_of(a.work, blockIdx.x);
+  const int b = wk.b, hk = wk.hk, rep = a.rep, split = wk.split, u = b * a.HK + hk;
   const int off = a.S - a.T, live = live_of(a, b), end = live + off;
-  const int j0 = id % ntile * 128, jw = j0 + 32 * w, j = jw + c;
+  const int j0 = wk.tile * 128, jw = j0 + 32 * w, j = jw + c;
 
   X k[KS], v[KS];
   const E* krow = j < end ? row_of<E>(a.k, b, hk, j) : nullptr;
@@ -334,14 +333,16 @@ void join(const View& out, const float* part, int n, int B, int H, int T, int d,
 }
 
 template <bool BF, int D>
-hipError_t go(const AttnArgs& a, hipStream_t s) {
+hipError_t go(AttnArgs a, hipStream_t s) {
   constexpr int BK = attn_tile_bwd(D);
   const int nq = (a.T + 127) / 128, nk = (a.S + 127) / 128;
+  a.work = work_of(a.B, a.HK, a.rep, nq, a.nsplit);
   hipLaunchKernelGGL((attn_dq_kernel<BF, D, BK>), dim3((unsigned)((long)a.B * a.H * nq * a.nsplit)),
                      dim3(256), 0, s, a, nq);
   if (a.nsplit > 1) join<BF>(a.dq, a.part, a.nsplit, a.B, a.H, a.T, a.d, a.scale, s);
+  a.work = work_of(a.B, a.HK, 1, nk, a.nsplit_kv);
   hipLaunchKernelGGL((attn_dkv_kernel<BF, D, BK>),
-                     dim3((unsigned)((long)a.B * a.HK * nk * a.nsplit_kv)), dim3(256), 0, s, a, nk);
+                     dim3((unsigned)((long)a.B * a.HK * nk * a.nsplit_kv)), dim3(256), 0, s, a);
   if (a.nsplit_kv > 1) {
     const long all = (long)a.nsplit_kv * a.B * a.HK * a.S * a.d;
     join<BF>(a.dk, a.part, a.nsplit_kv, a.B, a.HK, a.S, a.d, a.scale, s);

@@ -22,6 +22,49 @@ namespace e2ttt {
 
 typedef __attribute__((ext_vector_type(16))) float f32x16;
 
+// Division by a fixed number in five scalar instructions (Granlund and Montgomery 1994):
+// with l = ceil(log2 d) and m = floor(2^32 (2^l - d) / d) + 1, n / d is (t + (n - t) / 2) /
+// 2^(l - 1), t the upper half of m n, for every n (d = 1: l - 1 counts as 0 and t is 0).
+struct Div {
+  unsigned d, m, s1, s2;
+  __device__ __forceinline__ unsigned of(unsigned n) const {
+    const unsigned t = __umulhi(m, n);
+    return (t + ((n - t) >> s1)) >> s2;
+  }
+};
+inline Div div_by(unsigned d) {
+  unsigned l = 0;
+  while (l < 32 && (1ull << l) < d) ++l;
+  const unsigned m = (unsigned)((((1ull << l) - d) << 32) / d + 1);
+  return Div{d, m, l > 1 ? 1 : l, l > 0 ? l - 1 : 0};
+}
+
+// What a workgroup works on.  Workgroups are dealt to the 8 XCDs in turn: those of a key
+// head, which share its keys and values, go to one of them and its L2, the key heads in
+// turn (12 sequences of 250 to 3000 tokens, 8 query and 2 key heads of 128: 180 us, backward
+// 600; with an eighth of the workgroups in a row to each XCD 235 and 1017).  What 8 does not
+// divide stays as it is dealt.
+struct Work {
+  Div per, tiles, splits, HK;    // workgroups of a key head; their factors
+  unsigned full;                 // workgroups of the key heads that 8 divides
+};
+inline Work work_of(int B, int HK, int heads, int tiles, int splits) {
+  const unsigned per = (unsigned)heads * tiles * splits;
+  return Work{div_by(per), div_by((unsigned)tiles), div_by((unsigned)splits), div_by((unsigned)HK),
+              (unsigned)((long)B * HK / 8 * 8 * per)};
+}
+struct Place {
+  int b, hk, head, split, tile;  // head: of the query heads of a key head
+};
+__device__ __forceinline__ Place place_of(const Work& w, unsigned id) {
+  const bool dealt = id < w.full;
+  const unsigned y = dealt ? id >> 3 : id, q = w.per.of(y), r = y - q * w.per.d;
+  const unsigned u = dealt ? (id & 7) + 8 * q : q, b = w.HK.of(u);
+  const unsigned z = w.tiles.of(r), head = w.splits.of(z);
+  return Place{(int)b, (int)(u - b * w.HK.d), (int)head, (int)(z - head * w.splits.d),
+               (int)(r - z * w.tiles.d)};
+}
+
 struct AttnArgs {
   View q, k, v, out;          // [B][H or HK][T or S][d]
   View d_out, dq, dk, dv;
@@ -30,13 +73,14 @@ struct AttnArgs {
   float* ex;                  // backward, [B][H][T]: -lse log2 e (-inf for queries that see nothing)
   float* delta;               // backward, [B][H][T]: -D
   const int* lengths;         // nullable
-  int B, HK, H, T, S, d;
+  int B, HK, H, rep, T, S, d;   // rep: query heads of a key head
   int left, right;            // at most 2^30 - 1; negative: no bound
   float scale;
   // A tile of queries (keys) as several workgroups, each over a stretch of the keys
   // (queries): their sums [stretch][row][d] and, in the forward, [stretch][row] {reference,
   // sum} are joined by another kernel.
   int nsplit, nsplit_kv;
+  Work work;                  // of a launch
   float* part;
   float2* part_ml;
 };
@@ -214,16 +258,6 @@ __device__ __forceinline__ void st_tile(typename MOp<BF>::E* row, const f32x16& 
       IoT<BF>::st4(row + ch, x);
     }
   }
-}
-
-// Workgroups are dealt to the 8 XCDs in turn: those of a key head, which share its keys
-// and values, go to one of them and its L2, the key heads in turn (12 sequences of 250
-// to 3000 tokens, 8 query and 2 key heads of 128: 180 us, backward 600; with an eighth of
-// the workgroups in a row to each XCD 235 and 1017).  What 8 does not divide stays as it is
-// dealt.
-__device__ __forceinline__ int xcd_order(int id, int n, int heads) {
-  const int per = n / heads, full = heads / 8 * 8 * per, y = id >> 3;
-  return id < full ? ((id & 7) + 8 * (y / per)) * per + y % per : id;
 }
 
 // Queries of sequence b that the call takes.

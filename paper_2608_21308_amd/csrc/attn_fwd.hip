@@ -24,10 +24,9 @@ __global__ void __launch_bounds__(256, BF ? 2 : 1) attn_fwd_kernel(AttnArgs a, i
   // (apart by name: a read of one is then known not to wait for loads into another)
   __shared__ __align__(16) E lk0[BK * D], lk1[BK * D], lv0[BK * D], lv1[BK * D];
   const int lane = threadIdx.x & 63, w = wave_id(), h = lane >> 5, c = lane & 31;
-  const int id = xcd_order(blockIdx.x, gridDim.x, a.B * a.HK), x = id / ntile;
-  const int tile = ntile - 1 - id % ntile;             // (long rows of a causal mask first)
-  const int split = x % a.nsplit, u = x / a.nsplit;
-  const int b = u / a.H, hq = u % a.H, hk = hq / (a.H / a.HK);
+  const Place wk = place_of(a.work, blockIdx.x);
+  const int tile = ntile - 1 - wk.tile;               // (long rows of a causal mask first)
+  const int b = wk.b, hk = wk.hk, hq = hk * a.rep + wk.head, split = wk.split, u = b * a.H + hq;
   const int off = a.S - a.T, live = live_of(a, b), end = live + off;
   const int t0 = tile * 128, tw = t0 + 32 * w, t = tw + c;
 
@@ -177,8 +176,9 @@ __global__ void __launch_bounds__(256) attn_join_kernel(AttnArgs a) {
 }
 
 template <bool BF, int D>
-hipError_t go(const AttnArgs& a, hipStream_t s) {
+hipError_t go(AttnArgs a, hipStream_t s) {
   const int ntile = (a.T + 127) / 128;
+  a.work = work_of(a.B, a.HK, a.rep, ntile, a.nsplit);
   hipLaunchKernelGGL((attn_fwd_kernel<BF, D, attn_tile(BF, D)>),
                      dim3((unsigned)((long)a.B * a.H * ntile * a.nsplit)), dim3(256), 0, s, a, ntile);
   if (a.nsplit > 1)
