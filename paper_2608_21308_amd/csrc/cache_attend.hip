@@ -103,10 +103,10 @@ __global__ void __launch_bounds__(64 * NW, 2) cache_attend_kernel(CacheArgs a, i
   __shared__ __align__(16) float lo_[NW][D * 16];
   __shared__ float lm[NW][16], ll[NW][16];
   const int lane = threadIdx.x & 63, w = wave_id(), g = lane >> 4, r = lane & 15;
-  const int id = blockIdx.x, split = id % a.nsplit, u = id / a.nsplit;
-  const int tile = u % ntile, hk = u / ntile % a.HK, b = u / ntile / a.HK;
-  const int rep = a.H / a.HK, col = 16 * tile + r;
-  const int qt = col / rep, hq = hk * rep + col % rep;      // token, head of the lane's column
+  const int u = a.by_split.of(blockIdx.x), split = blockIdx.x - u * a.nsplit;
+  const int y = a.by_tile.of(u), tile = u - y * ntile, b = a.by_HK.of(y), hk = y - b * a.HK;
+  const int rep = a.by_rep.d, col = 16 * tile + r;
+  const int qt = a.by_rep.of(col), hq = hk * rep + col - qt * rep;   // token, head of the lane's column
   const Held h = held_of(a, b);
   const int live = (int)(h.end - h.start);
   const bool on = qt < live && h.start + qt >= 0;
@@ -135,7 +135,8 @@ __global__ void __launch_bounds__(64 * NW, 2) cache_attend_kernel(CacheArgs a, i
   const long any0 = max(h.first, a.left < 0 ? 0L : max(0L, h.start - a.left));
   const long any1 = live > 0 ? h.end : any0;
   const int pg0 = (int)(any0 / kPage), np = any1 > any0 ? (int)((any1 + kPage - 1) / kPage) - pg0 : 0;
-  const int s0 = pg0 + (int)((long)np * split / a.nsplit), s1 = pg0 + (int)((long)np * (split + 1) / a.nsplit);
+  const int each = a.by_split.of(np + a.nsplit - 1);
+  const int s0 = pg0 + min(np, each * split), s1 = pg0 + min(np, each * (split + 1));
 
   f32x4 o[NB][2];
 #pragma unroll
@@ -145,7 +146,7 @@ __global__ void __launch_bounds__(64 * NW, 2) cache_attend_kernel(CacheArgs a, i
   const float cs = a.scale * kLog2e, slack = 8.0f / cs;
 
   // the wave's pages w, w + NW, ..: their bytes one turn ahead, their places two
-  int entry = s0 + w < s1 ? (s0 + w) % a.P : 0;
+  int entry = s0 + w - (int)a.by_P.of(s0 + w) * a.P;
   auto place = [&](int pg) __attribute__((always_inline)) {
     const unsigned char* x = pg < s1 ? page_at(a, b, hk, entry) : nullptr;
     entry += NW;
@@ -170,19 +171,22 @@ __global__ void __launch_bounds__(64 * NW, 2) cache_attend_kernel(CacheArgs a, i
     const long j0 = (long)pg * kPage;
     const bool cut = j0 < any0 || j0 + kPage > h.start + 1 || (a.left >= 0 && j0 < h.end - 1 - a.left);
     if (cut) {
-      const int k0 = (int)max(see0 - j0, -1L), k1 = (int)min(see1 - j0, 64L);
-      const int n0 = (int)max(any0 - j0, -1L), n1 = (int)min(any1 - j0, 64L);
+      // (tokens of the lane counted from 4 g on)
+      const int k0 = (int)max(see0 - j0, -1L) - 4 * g, k1 = (int)min(see1 - j0, 64L) - 4 * g;
+      const int n0 = (int)max(any0 - j0, -1L) - 4 * g, n1 = (int)min(any1 - j0, 64L) - 4 * g;
 #pragma unroll
-      for (int x = 0; x < 4; ++x)
+      for (int x = 0; x < 4; ++x) {
+        unsigned held = 0;         // (rows that hold nothing: finite values for zeros to meet)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const int j = 16 * x + 4 * g + i;
-          if (j < k0 || j >= k1) s[x][i] = -INFINITY;
-          if (j < n0 || j >= n1) {      // (rows that hold nothing: finite values for zeros to meet)
-#pragma unroll
-            for (int m = 0; m < NB; ++m) cur.vs[m][x] &= ~(255u << (8 * i));
-          }
+          const int j = 16 * x + i;
+          s[x][i] = j >= k0 && j < k1 ? s[x][i] : -INFINITY;
+          held |= j >= n0 && j < n1 ? 255u << (8 * i) : 0u;
         }
+#pragma unroll
+        for (int m = 0; m < NB; ++m) cur.vs[m][x] &= held;
+        sched_fence();
+      }
     }
     float most = s[0][0];
 #pragma unroll
@@ -236,18 +240,18 @@ __global__ void __launch_bounds__(64 * NW, 2) cache_attend_kernel(CacheArgs a, i
       }
     }
   };
-  Raw<NB> x, y;
+  Raw<NB> x, z;
   int pg = s0 + w;
   const unsigned char* next = place(pg);
   fetch<NB>(x, a, next, g, r);
   next = place(pg + NW);
   for (; pg < s1; pg += 2 * NW) {
-    fetch<NB>(y, a, next, g, r);
+    fetch<NB>(z, a, next, g, r);
     next = place(pg + 2 * NW);
     turn(x, pg);
     fetch<NB>(x, a, next, g, r);
     next = place(pg + 3 * NW);
-    turn(y, pg + NW);
+    turn(z, pg + NW);
   }
 
   if (!on) {                  // (a column of no live query has gone along with the others)
@@ -371,9 +375,14 @@ __global__ void __launch_bounds__(256) cache_join_kernel(CacheArgs a, int ntile)
 int tiles_of(const CacheArgs& a) { return (int)(((long)a.H / a.HK * a.T + 15) / 16); }
 
 template <bool BF, int NB>
-hipError_t go(const CacheArgs& a, hipStream_t s) {
+hipError_t go(CacheArgs a, hipStream_t s) {
   const int nt = tiles_of(a);
   const long units = (long)a.B * a.HK * nt;
+  a.by_split = div_by(a.nsplit);
+  a.by_tile = div_by(nt);
+  a.by_HK = div_by(a.HK);
+  a.by_rep = div_by(a.H / a.HK);
+  a.by_P = div_by(a.P);
   hipLaunchKernelGGL((cache_attend_kernel<BF, NB, 8>), dim3((unsigned)(units * a.nsplit)),
                      dim3(512), 0, s, a, nt);
   if (a.nsplit > 1)

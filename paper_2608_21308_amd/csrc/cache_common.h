@@ -20,6 +20,7 @@
 #pragma once
 
 #include "delta_common.h"
+#include "div.h"
 
 namespace e2ttt {
 
@@ -39,6 +40,7 @@ struct CacheArgs {
   int B, HK, H, T, d, P;
   int left;                 // at most 2^30 - 1; negative: no bound
   int nsplit;
+  Div by_split, by_tile, by_HK, by_rep, by_P;   // attention: of the workgroup's number, of columns, pages
   float scale;
 };
 
