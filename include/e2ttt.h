@@ -503,14 +503,14 @@ e2ttt_status e2ttt_qk_backward(const e2ttt_qk_desc* desc, const e2ttt_qk_strides
  *               (clamped to 0..T) queries and the first lengths[b] + S - T keys are
  *               live; what lies behind is not read, its outputs and gradients are
  *               written as zero and its lse as -inf
- * scale is positive.  Outputs do not overlap inputs.  Supported: d <= 128, a multiple
+ * scale is at least 2^-126.  Outputs do not overlap inputs.  Supported: d <= 128, a multiple
  * of 8, either io type, T and S up to 2^29, and B H ceil(T / 128), B HK ceil(S / 128)
  * below 2^24 (else E2TTT_ERR_UNSUPPORTED).
  *
  * Precision: scores, softmax and sums in fp32.  With bf16 tensors P and dS are
  * rounded to bf16 once as operands of the products that follow (half a step of
  * 2^-8 each, of either sign), and outputs once.  A query's results depend on live
- * values only; a non-finite live key or value may make those of queries within 64
+ * values only; a non-finite live key or value may make those of queries within 128
  * tokens of seeing it non-finite too.  Results do not change from run to run.
  */
 typedef struct {
@@ -590,7 +590,7 @@ typedef struct {
   int32_t d;            /* head dim                                          */
   int32_t pages;        /* entries of a sequence in the table                */
   int32_t io;           /* e2ttt_dtype of the token tensors                  */
-  float scale;          /* of the logits, positive (attend alone)            */
+  float scale;          /* of the logits, at least 2^-126 (attend alone)     */
   int32_t left;         /* keys seen before a query (negative: all)          */
 } e2ttt_cache_desc;
 

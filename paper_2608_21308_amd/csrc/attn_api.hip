@@ -16,7 +16,7 @@ constexpr long kMostTiles = 0xffffff;
 e2ttt_status check_desc(const e2ttt_attn_desc* d) {
   if (!d) return E2TTT_ERR_NULL_ARG;
   if (d->B <= 0 || d->HK <= 0 || d->H <= 0 || d->T <= 0 || d->S <= 0 || d->d <= 0 ||
-      d->H % d->HK != 0 || !(d->scale > 0.0f) || !isfinite(d->scale * kLog2e))
+      d->H % d->HK != 0 || !(d->scale >= 1.17549435e-38f) || !isfinite(d->scale * kLog2e))
     return E2TTT_ERR_BAD_SHAPE;
   if ((d->io != E2TTT_DT_F32 && d->io != E2TTT_DT_BF16) || d->d % 8 || d->d > 128 ||
       d->T > (1 << 29) || d->S > (1 << 29))

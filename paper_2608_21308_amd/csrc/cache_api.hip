@@ -24,7 +24,7 @@ CacheArgs args_of(const e2ttt_cache_desc* d) {
 e2ttt_status check_desc(const e2ttt_cache_desc* d, bool attend) {
   if (!d) return E2TTT_ERR_NULL_ARG;
   if (d->B <= 0 || d->HK <= 0 || d->T <= 0 || d->d <= 0 || d->pages <= 0) return E2TTT_ERR_BAD_SHAPE;
-  if (attend && (d->H <= 0 || d->H % d->HK != 0 || !(d->scale > 0.0f) ||
+  if (attend && (d->H <= 0 || d->H % d->HK != 0 || !(d->scale >= 1.17549435e-38f) ||
                  !isfinite(d->scale * 1.44269504f)))
     return E2TTT_ERR_BAD_SHAPE;
   if ((d->io != E2TTT_DT_F32 && d->io != E2TTT_DT_BF16) || d->d % 32 || d->d > 128 ||

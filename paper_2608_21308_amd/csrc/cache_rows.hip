@@ -8,26 +8,30 @@ namespace e2ttt {
 namespace {
 
 // Thread -> (sequence, key head, group of four tokens, block, eighth of 32 channels).
+struct Deal {
+  Div blocks, groups, heads;
+  unsigned n;                         // sequences x key heads x groups
+  bool tokens_first;
+};
 struct Where {
   int b, hk, grp, blk, g;
 };
-__device__ __forceinline__ bool where_of(const CacheArgs& a, int ngroup, bool tokens_first, Where& o) {
-  const int nb = a.d / 32;
-  const long id = (long)blockIdx.x * 256 + threadIdx.x;
-  o.g = (int)(id & 3);
-  const long x = id >> 2;
-  o.blk = (int)(x % nb);
-  const long y = x / nb;
-  const long n = (long)a.B * a.HK * ngroup;
-  if (y >= n) return false;
-  if (tokens_first) {                 // neighbouring rows of a head
-    o.grp = (int)(y % ngroup);
-    o.hk = (int)(y / ngroup % a.HK);
+__device__ __forceinline__ bool where_of(const Deal& d, Where& o) {
+  const unsigned id = blockIdx.x * 256u + threadIdx.x, x = id >> 2, y = d.blocks.of(x);
+  o.g = id & 3;
+  o.blk = x - y * d.blocks.d;
+  if (y >= d.n) return false;
+  if (d.tokens_first) {               // neighbouring rows of a head
+    const unsigned z = d.groups.of(y), b = d.heads.of(z);
+    o.grp = y - z * d.groups.d;
+    o.hk = z - b * d.heads.d;
+    o.b = b;
   } else {                            // neighbouring heads of a token
-    o.hk = (int)(y % a.HK);
-    o.grp = (int)(y / a.HK % ngroup);
+    const unsigned z = d.heads.of(y), b = d.groups.of(z);
+    o.hk = y - z * d.heads.d;
+    o.grp = z - b * d.groups.d;
+    o.b = b;
   }
-  o.b = (int)(y / ((long)ngroup * a.HK));
   return true;
 }
 
@@ -83,10 +87,10 @@ __device__ __forceinline__ unsigned encode(const float (&x)[8], unsigned& exp) {
 }
 
 template <bool BF>
-__global__ void __launch_bounds__(256) cache_write_kernel(CacheArgs a, int ngroup, bool tokens_first) {
+__global__ void __launch_bounds__(256) cache_write_kernel(CacheArgs a, Deal deal) {
   using E = typename DOp<BF>::E;
   Where o;
-  if (!where_of(a, ngroup, tokens_first, o)) return;      // (whole quads leave together)
+  if (!where_of(deal, o)) return;      // (whole quads leave together)
   const int nb = a.d / 32;
   const Held h = held_of(a, o.b);
   const long p0 = ((h.start >> 2) + o.grp) * 4;
@@ -152,10 +156,10 @@ __device__ __forceinline__ void decode(float (&x)[8], unsigned c, float s) {
 }
 
 template <bool BF>
-__global__ void __launch_bounds__(256) cache_read_kernel(CacheArgs a, int ngroup, bool tokens_first) {
+__global__ void __launch_bounds__(256) cache_read_kernel(CacheArgs a, Deal deal) {
   using E = typename DOp<BF>::E;
   Where o;
-  if (!where_of(a, ngroup, tokens_first, o)) return;
+  if (!where_of(deal, o)) return;
   const int nb = a.d / 32;
   const Held h = held_of(a, o.b);
   const long p0 = ((h.start >> 2) + o.grp) * 4;
@@ -192,24 +196,28 @@ __global__ void __launch_bounds__(256) cache_read_kernel(CacheArgs a, int ngroup
   }
 }
 
-int groups_of(const CacheArgs& a) { return (a.T + 2) / 4 + 1; }
-unsigned blocks_of(const CacheArgs& a) {
-  return (unsigned)(((long)a.B * a.HK * groups_of(a) * (a.d / 8) + 255) / 256);
+Deal deal_of(const CacheArgs& a) {
+  const int groups = (a.T + 2) / 4 + 1;
+  return Deal{div_by(a.d / 32), div_by(groups), div_by(a.HK), (unsigned)((long)a.B * a.HK * groups),
+              a.x.t < a.x.h};
+}
+dim3 grid_of(const CacheArgs& a, const Deal& d) {
+  return dim3((unsigned)(((long)d.n * (a.d / 8) + 255) / 256));
 }
 
 }  // namespace
 
 hipError_t launch_cache_write(const CacheArgs& a, bool bf, hipStream_t s) {
-  const bool tf = a.x.t < a.x.h;
-  if (bf) hipLaunchKernelGGL(cache_write_kernel<true>, dim3(blocks_of(a)), dim3(256), 0, s, a, groups_of(a), tf);
-  else hipLaunchKernelGGL(cache_write_kernel<false>, dim3(blocks_of(a)), dim3(256), 0, s, a, groups_of(a), tf);
+  const Deal d = deal_of(a);
+  if (bf) hipLaunchKernelGGL(cache_write_kernel<true>, grid_of(a, d), dim3(256), 0, s, a, d);
+  else hipLaunchKernelGGL(cache_write_kernel<false>, grid_of(a, d), dim3(256), 0, s, a, d);
   return hipGetLastError();
 }
 
 hipError_t launch_cache_read(const CacheArgs& a, bool bf, hipStream_t s) {
-  const bool tf = a.x.t < a.x.h;
-  if (bf) hipLaunchKernelGGL(cache_read_kernel<true>, dim3(blocks_of(a)), dim3(256), 0, s, a, groups_of(a), tf);
-  else hipLaunchKernelGGL(cache_read_kernel<false>, dim3(blocks_of(a)), dim3(256), 0, s, a, groups_of(a), tf);
+  const Deal d = deal_of(a);
+  if (bf) hipLaunchKernelGGL(cache_read_kernel<true>, grid_of(a, d), dim3(256), 0, s, a, d);
+  else hipLaunchKernelGGL(cache_read_kernel<false>, grid_of(a, d), dim3(256), 0, s, a, d);
   return hipGetLastError();
 }
 

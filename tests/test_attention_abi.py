@@ -34,7 +34,7 @@ def calls(lib, d, s=None):
 @pytest.mark.parametrize("kw,status", [
     (dict(B=0), 2), (dict(HK=0), 2), (dict(H=3), 2), (dict(H=-4), 2), (dict(T=0), 2), (dict(S=0), 2),
     (dict(d=0), 2), (dict(scale=0.0), 2), (dict(scale=-1.0), 2), (dict(scale=math.inf), 2),
-    (dict(scale=math.nan), 2), (dict(scale=3e38), 2), (dict(io=2), 3), (dict(d=12), 3), (dict(d=136), 3),
+    (dict(scale=math.nan), 2), (dict(scale=3e38), 2), (dict(scale=1e-39), 2), (dict(io=2), 3), (dict(d=12), 3), (dict(d=136), 3),
     (dict(T=(1 << 29) + 1), 3), (dict(S=(1 << 29) + 1), 3), (dict(B=1 << 20, T=2048), 3),
     (dict(B=1 << 20, T=1, S=2048), 3)])
 def test_bad_descriptors(lib, kw, status):

@@ -65,7 +65,9 @@ CASES = [  # B, HK, H, T, S, d, left, right
     (3, 1, 2, 64, 64, 120, 2147483647, 2147483647), (1, 1, 1, 40, 400, 16, 5, 0),
     # (few tiles of queries, or of keys, that see many: split into stretches and joined)
     (1, 1, 1, 130, 700, 64, -1, 0), (1, 1, 2, 64, 2000, 128, -1, -1), (1, 2, 8, 300, 300, 64, -1, 0),
-    (2, 1, 4, 70, 900, 32, 600, 0), (1, 1, 1, 1, 1500, 72, -1, 0), (1, 1, 1, 900, 33, 40, -1, -1)]
+    (2, 1, 4, 70, 900, 32, 600, 0), (1, 1, 1, 1, 1500, 72, -1, 0), (1, 1, 1, 900, 33, 40, -1, -1),
+    # (key heads that 8 does not divide)
+    (5, 2, 4, 140, 150, 64, 90, 0), (3, 3, 3, 260, 260, 128, -1, 0), (4, 4, 8, 40, 40, 32, 10, 3)]
 
 
 @pytest.mark.parametrize("c", CASES)
@@ -74,7 +76,7 @@ CASES = [  # B, HK, H, T, S, d, left, right
 def test_forward_backward(c, io, ragged):
     B, HK, H, T, S, d, left, right = c
     print("attention", c, io, ragged, flush=True)
-    lengths = torch.tensor([T - 1, 0, T + 5][:B] if T > 1 else [0, 1, -3][:B]) if ragged else None
+    lengths = torch.tensor(([T - 1, 0, T + 5, T // 2, T] if T > 1 else [0, 1, -3])[:B]) if ragged else None
     layout = "bthd" if ragged else "bhtd"
     x, d_out = inputs(B, HK, H, T, S, d, io, d + T, lengths)
     d_lse = torch.randn(B, H, T, generator=torch.Generator().manual_seed(1)).double() if ragged else None
@@ -215,3 +217,66 @@ def test_graph_and_other_stream():
         torch.cuda.synchronize()
         assert torch.equal(out, o) and torch.equal(lse, l)
         assert all(torch.equal(grads[n], ref[n]) for n in ref)
+
+
+def test_lse_not_wanted_and_workspace_given():
+    """The C entry without lse, and a split call on a workspace of the caller's."""
+    import ctypes
+    cfg, t, _, _, _ = make(1, 1, 2, 100, 1500, 64, seed=2)
+    n = e2ttt.attention_workspace_bytes(cfg)
+    assert n > 0
+    ws = torch.full((n,), 255, dtype=torch.uint8, device="cuda")
+    o, l = e2ttt.attention_forward(cfg, t["q"], t["k"], t["v"], workspace=ws)
+    o2 = torch.full_like(o, math.nan)
+    p = lambda x: x.data_ptr()
+    st = e2ttt.load().e2ttt_attn_forward(ctypes.byref(cfg.desc()), None, p(t["q"]), p(t["k"]), p(t["v"]),
+                                         None, p(o2), None, p(ws), n, torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    assert st == 0 and torch.equal(o, o2)
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+def test_smallest_and_largest_scale(io):
+    """Scores that all vanish (a mean of the values) and the largest scale there is."""
+    cfg, t, _, x, _ = make(1, 1, 1, 70, 70, 32, io, scale=2.0 ** -126)
+    o, l = e2ttt.attention_forward(cfg, t["q"], t["k"], t["v"])
+    n = torch.arange(1, 71, dtype=torch.float64)
+    ref = x["v"].cumsum(2) / n[:, None]
+    u = 2.0 ** -7 if io == "bf16" else 2.0 ** -17      # (a sum of 70 terms, its rounding, the out's)
+    assert ((o.double().cpu() - ref).abs() <= u * x["v"].abs().cumsum(2) / n[:, None] + 1e-30).all()
+    assert (l.double().cpu() - n.log()).abs().max() <= 2.0 ** -20
+    k = dict(t, q=torch.zeros_like(t["q"]))
+    cfg = e2ttt.AttentionConfig(1, 1, 1, 70, 32, cfg.io, scale=2.0 ** 127)
+    o2, _ = e2ttt.attention_forward(cfg, k["q"], k["k"], k["v"])
+    assert torch.equal(o2, o)
+
+
+def test_split_calls_as_graphs_on_two_streams():
+    """Two captured split calls with workspaces of their own, replayed at once."""
+    runs = []
+    for seed in (1, 2):
+        cfg, t, tg, _, _ = make(1, 1, 4, 130, 1300, 64, seed=seed)
+        o, l = e2ttt.attention_forward(cfg, t["q"], t["k"], t["v"])
+        ref = e2ttt.attention_backward(cfg, t["q"], t["k"], t["v"], o, l, tg)
+        ws = torch.empty(e2ttt.attention_workspace_bytes(cfg), dtype=torch.uint8, device="cuda")
+        sc = torch.empty(e2ttt.attention_scratch_bytes(cfg), dtype=torch.uint8, device="cuda")
+        assert ws.numel() and sc.numel() > 8 * 4 * 130 * 2
+        o2, l2, g2 = torch.empty_like(o), torch.empty_like(l), {n: torch.empty_like(x) for n, x in ref.items()}
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            e2ttt.attention_forward(cfg, t["q"], t["k"], t["v"], out=o2, lse=l2, workspace=ws)
+            e2ttt.attention_backward(cfg, t["q"], t["k"], t["v"], o2, l2, tg, grads=g2, scratch=sc)
+        runs.append((graph, torch.cuda.Stream(), o, l, ref, o2, l2, g2, ws, sc, t, tg))
+    for _ in range(4):
+        for r in runs:
+            for x in (r[5], r[6], *r[7].values()):
+                x.zero_()
+        torch.cuda.synchronize()
+        for r in runs:
+            with torch.cuda.stream(r[1]):
+                r[0].replay()
+        torch.cuda.synchronize()
+        for _, _, o, l, ref, o2, l2, g2, *_ in runs:
+            assert torch.equal(o, o2) and torch.equal(l, l2)
+            assert all(torch.equal(ref[n], g2[n]) for n in ref)
