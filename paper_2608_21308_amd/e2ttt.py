@@ -1246,24 +1246,32 @@ def _cache_common(cfg, dev, cache, table, starts, lengths):
     if not isinstance(cache, torch.Tensor) or cache.dim() != 3 or not 1 <= cache.shape[0] < 1 << 31:
         raise ValueError("cache must be a tensor [n_pages, HK, 68 d] of bytes")
     n = cache.shape[0]
-    _plain("cache", cache, (n, *s_page), torch.uint8, dev)
+    if not _flat(cache, (n, *s_page), torch.uint8, dev):
+        _plain("cache", cache, (n, *s_page), torch.uint8, dev)
     if table is None:
         raise ValueError("table must be a tensor")
-    _plain("table", table, s_t, torch.int32, dev)
-    _plain("starts", starts, s_b, torch.int32, dev)
-    _plain("lengths", lengths, s_b, torch.int32, dev)
+    if not _flat(table, s_t, torch.int32, dev):
+        _plain("table", table, s_t, torch.int32, dev)
+    if starts is not None and not _flat(starts, s_b, torch.int32, dev):
+        _plain("starts", starts, s_b, torch.int32, dev)
+    if lengths is not None:
+        _plain("lengths", lengths, s_b, torch.int32, dev)
     return n
 
 
-@_on_device
 def cache_write(cfg: CacheConfig, k, v, cache, table, starts=None, lengths=None):
     """Runs e2ttt_cache_write on the current stream: the first lengths [B] (int32;
     None: all T) tokens of k, v [B, HK, T, d] (any strides with a contiguous last
     dimension) become positions starts [B] (int32; None: 0) + t of their
     sequences, in the pages of cache that table [B, pages] (int32) names."""
+    dev = _device_of(k)
+    if dev != _current_device():
+        with torch.cuda.device(dev):
+            return cache_write(cfg, k, v, cache, table, starts, lengths)
     d, io, _, s_k, _, _, _ = cfg._call
-    dev = k.get_device()
-    st = _layout(CacheStrides, dev, ("k", k, s_k, io), ("v", v, s_k, io))
+    st = None        # (_layout's answer, for a call of a few microseconds)
+    if not (_flat(k, s_k, io, dev) and _flat(v, s_k, io, dev)):
+        st = _layout(CacheStrides, dev, ("k", k, s_k, io), ("v", v, s_k, io))
     n = _cache_common(cfg, dev, cache, table, starts, lengths)
     st = (_lib or load()).e2ttt_cache_write(d, st, k.data_ptr(), v.data_ptr(), _ptr(starts),
                                             _ptr(lengths), table.data_ptr(), cache.data_ptr(), n,
@@ -1272,17 +1280,19 @@ def cache_write(cfg: CacheConfig, k, v, cache, table, starts=None, lengths=None)
         _check(st, "e2ttt_cache_write")
 
 
-@_on_device
 def cache_read(cfg: CacheConfig, cache, table, starts=None, lengths=None, *, out=None):
     """Runs e2ttt_cache_read on the current stream: the values of positions starts +
     t, t < lengths, as (k, v) [B, HK, T, d]; zeros behind them and where the cache
     holds none.  `out`: optional (k, v) tensors to write into, of any strides."""
+    dev = _device_of(cache)
+    if dev != _current_device():
+        with torch.cuda.device(dev):
+            return cache_read(cfg, cache, table, starts, lengths, out=out)
     d, io, _, s_k, _, _, _ = cfg._call
-    dev = cache.get_device()
     n = _cache_common(cfg, dev, cache, table, starts, lengths)
     if out is None:
-        k, v = (torch.empty(s_k, dtype=io, device=cache.device) for _ in "kv")
-        st = None
+        k = torch.empty(s_k, dtype=io, device=cache.device)
+        v, st = torch.empty_like(k), None
     else:
         k, v = out
         st = _layout(CacheStrides, dev, ("k", k, s_k, io), ("v", v, s_k, io))
@@ -1293,22 +1303,29 @@ def cache_read(cfg: CacheConfig, cache, table, starts=None, lengths=None, *, out
     return k, v
 
 
-@_on_device
 def cache_attention(cfg: CacheConfig, q, cache, table, starts=None, lengths=None, *, out=None,
                     lse=None, workspace=None):
     """Runs e2ttt_cache_attend on the current stream: attention of the arriving
     tokens' q [B, H, T, d] at positions starts + t over what the cache holds up to
     them, themselves included (cache_write comes first).  Returns (out, lse); lse
     [B, H, T] is written only if given, else None."""
+    dev = _device_of(q)
+    if dev != _current_device():
+        with torch.cuda.device(dev):
+            return cache_attention(cfg, q, cache, table, starts, lengths, out=out, lse=lse,
+                                   workspace=workspace)
     d, io, s_q, _, _, _, _ = cfg._call
-    dev = q.get_device()
     if out is None:
         out = torch.empty_like(q)
-    st = _layout(CacheStrides, dev, ("q", q, s_q, io), ("out", out, s_q, io))
+    st = None        # (_layout's answer, for a call of a few microseconds)
+    if not (_flat(q, s_q, io, dev) and _flat(out, s_q, io, dev)):
+        st = _layout(CacheStrides, dev, ("q", q, s_q, io), ("out", out, s_q, io))
     n = _cache_common(cfg, dev, cache, table, starts, lengths)
-    _plain("lse", lse, s_q[:3], torch.float32, dev)
-    _buffer("workspace", workspace, dev)
-    if workspace is None:
+    if lse is not None:
+        _plain("lse", lse, s_q[:3], torch.float32, dev)
+    if workspace is not None:
+        _buffer("workspace", workspace, dev)
+    else:
         workspace = alloc_cache_workspace(cfg, q.device)
     st = (_lib or load()).e2ttt_cache_attend(
         d, st, q.data_ptr(), _ptr(starts), _ptr(lengths), table.data_ptr(), cache.data_ptr(), n,
