@@ -27,22 +27,28 @@ typedef __attribute__((ext_vector_type(16))) float f32x16;
 // head, which share its keys and values, go to one of them and its L2, the key heads in
 // turn (12 sequences of 250 to 3000 tokens, 8 query and 2 key heads of 128: 180 us, backward
 // 600; with an eighth of the workgroups in a row to each XCD 235 and 1017).  What 8 does not
-// divide stays as it is dealt.
+// divide stays as it is dealt.  Where rows are of unequal length (causal, say) the 32 CUs of
+// an XCD get long and short ones in turn, by `fold` (forward: 2 x 8 x 4096 x 128 111 us
+// without and 89 with it, 16 x 8192 x 64 198 and 173; dq: 324 and 312, 489 and 496; not for
+// dk and dv, whose workgroups have a CU to themselves or nearly: 324 and 383).
 struct Work {
   Div per, tiles, splits, HK;    // workgroups of a key head; their factors
   unsigned full;                 // workgroups of the key heads that 8 divides
+  bool fold;                     // every second 32 of an XCD's workgroups in reverse
 };
-inline Work work_of(int B, int HK, int heads, int tiles, int splits) {
+inline Work work_of(int B, int HK, int heads, int tiles, int splits, bool fold) {
   const unsigned per = (unsigned)heads * tiles * splits;
   return Work{div_by(per), div_by((unsigned)tiles), div_by((unsigned)splits), div_by((unsigned)HK),
-              (unsigned)((long)B * HK / 8 * 8 * per)};
+              (unsigned)((long)B * HK / 8 * 8 * per), fold};
 }
 struct Place {
   int b, hk, head, split, tile;  // head: of the query heads of a key head
 };
 __device__ __forceinline__ Place place_of(const Work& w, unsigned id) {
   const bool dealt = id < w.full;
-  const unsigned y = dealt ? id >> 3 : id, q = w.per.of(y), r = y - q * w.per.d;
+  unsigned y = dealt ? id >> 3 : id;
+  if (dealt && w.fold && (y & 32) && (y | 31) < w.full / 8) y ^= 31;
+  const unsigned q = w.per.of(y), r = y - q * w.per.d;
   const unsigned u = dealt ? (id & 7) + 8 * q : q, b = w.HK.of(u);
   const unsigned z = w.tiles.of(r), head = w.splits.of(z);
   return Place{(int)b, (int)(u - b * w.HK.d), (int)head, (int)(z - head * w.splits.d),

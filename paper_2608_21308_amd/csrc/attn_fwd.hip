@@ -178,7 +178,7 @@ __global__ void __launch_bounds__(256) attn_join_kernel(AttnArgs a) {
 template <bool BF, int D>
 hipError_t go(AttnArgs a, hipStream_t s) {
   const int ntile = (a.T + 127) / 128;
-  a.work = work_of(a.B, a.HK, a.rep, ntile, a.nsplit);
+  a.work = work_of(a.B, a.HK, a.rep, ntile, a.nsplit, (a.left < 0) != (a.right < 0));
   hipLaunchKernelGGL((attn_fwd_kernel<BF, D, attn_tile(BF, D)>),
                      dim3((unsigned)((long)a.B * a.H * ntile * a.nsplit)), dim3(256), 0, s, a, ntile);
   if (a.nsplit > 1)
