@@ -106,8 +106,12 @@ __global__ void __launch_bounds__(256, BF ? 2 : 1) attn_dq_kernel(AttnArgs a, in
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
       f32x16 v = none;
+      X fr[KS];
 #pragma unroll
-      for (int x = 0; x < KS; ++x) v = O::mm(v, A::rows(lv, 32 * n + c, x, h), g[x]);
+      for (int x = 0; x < KS; ++x) fr[x] = A::rows(lv, 32 * n + c, x, h);
+      sched_fence();
+#pragma unroll
+      for (int x = 0; x < KS; ++x) v = O::mm(v, fr[x], g[x]);
 #pragma unroll
       for (int i = 0; i < 16; ++i)
         s[n][i] = __builtin_amdgcn_exp2f(fmaf(s[n][i], cs, ex)) * v[i];
@@ -238,8 +242,12 @@ __global__ void __launch_bounds__(256, BF && D <= 64 ? 2 : 1) attn_dkv_kernel(At
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
       s[n] = zero16();
+      X fr[KS];
 #pragma unroll
-      for (int y = 0; y < KS; ++y) s[n] = O::mm(s[n], A::rows(lq, 32 * n + c, y, h), k[y]);
+      for (int y = 0; y < KS; ++y) fr[y] = A::rows(lq, 32 * n + c, y, h);
+      sched_fence();
+#pragma unroll
+      for (int y = 0; y < KS; ++y) s[n] = O::mm(s[n], fr[y], k[y]);
     }
     if (jw + 32 > end || (a.right >= 0 && tt + off < jw + 31 - a.right) ||
         (a.left >= 0 && tt + BQ - 1 + off > jw + a.left)) {
@@ -260,8 +268,12 @@ __global__ void __launch_bounds__(256, BF && D <= 64 ? 2 : 1) attn_dkv_kernel(At
 #pragma unroll
         for (int i = 0; i < 4; ++i) x[4 * i4 + i] = d4[i];
       }
+      X fr[KS];
 #pragma unroll
-      for (int y = 0; y < KS; ++y) x = O::mm(x, A::rows(lg, 32 * n + c, y, h), v[y]);
+      for (int y = 0; y < KS; ++y) fr[y] = A::rows(lg, 32 * n + c, y, h);
+      sched_fence();
+#pragma unroll
+      for (int y = 0; y < KS; ++y) x = O::mm(x, fr[y], v[y]);
 #pragma unroll
       for (int i4 = 0; i4 < 4; ++i4) {
         const f32x4 e4 = *reinterpret_cast<const f32x4*>(&lx[0][32 * n + 8 * i4 + 4 * h]);
