@@ -95,13 +95,7 @@ __global__ void __launch_bounds__(256, BF ? 2 : 1) attn_dq_kernel(AttnArgs a, in
         (a.right >= 0 && j0 + BK - 1 > pw0 + a.right)) {
       const int k0 = a.left < 0 ? 0 : p - a.left;
       const int k1 = a.right < 0 ? end : min(end, p + a.right + 1);
-#pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int j = j0 + 32 * n + row_in(i, h);
-          if (j < k0 || j >= k1) s[n][i] = kNegInf;
-        }
+      cut_rows(s, k0 - j0, k1 - j0, h);
     }
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
@@ -250,15 +244,8 @@ __global__ void __launch_bounds__(256, BF && D <= 64 ? 2 : 1) attn_dkv_kernel(At
       for (int y = 0; y < KS; ++y) s[n] = O::mm(s[n], fr[y], k[y]);
     }
     if (jw + 32 > end || (a.right >= 0 && tt + off < jw + 31 - a.right) ||
-        (a.left >= 0 && tt + BQ - 1 + off > jw + a.left)) {
-#pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int y = 0; y < 16; ++y) {
-          const int t = tt + 32 * n + row_in(y, h);
-          if (t < q0 || t >= q1) s[n][y] = kNegInf;
-        }
-    }
+        (a.left >= 0 && tt + BQ - 1 + off > jw + a.left))
+      cut_rows(s, q0 - tt, q1 - tt, h);
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
       f32x16 x;

@@ -120,8 +120,20 @@ __device__ __forceinline__ f32x16 zero16() {
   for (int i = 0; i < 16; ++i) x[i] = 0.0f;
   return x;
 }
-// The row of register i of an accumulator.
-__device__ __forceinline__ int row_in(int i, int h) { return 8 * (i >> 2) + 4 * h + (i & 3); }
+// Scores of rows before `from` and from `to` on (counted from the first accumulator's) do
+// not count.
+template <int NT>
+__device__ __forceinline__ void cut_rows(f32x16 (&s)[NT], int from, int to, int h) {
+  from -= 4 * h;                   // (row 8 (i / 4) + 4 h + i mod 4 of register i)
+  to -= 4 * h;
+#pragma unroll
+  for (int n = 0; n < NT; ++n)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int r = 32 * n + 8 * (i >> 2) + (i & 3);
+      s[n][i] = r >= from && r < to ? s[n][i] : kNegInf;
+    }
+}
 
 // Across the two halves of a wave.
 __device__ __forceinline__ void halves(float x, float& lo, float& hi) {

@@ -88,13 +88,7 @@ __global__ void __launch_bounds__(256, BF ? 2 : 1) attn_fwd_kernel(AttnArgs a, i
         (a.right >= 0 && j0 + BK - 1 > pw0 + a.right)) {
       const int k0 = a.left < 0 ? 0 : p - a.left;
       const int k1 = a.right < 0 ? end : min(end, p + a.right + 1);
-#pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int j = j0 + 32 * n + row_in(i, h);
-          if (j < k0 || j >= k1) s[n][i] = kNegInf;
-        }
+      cut_rows(s, k0 - j0, k1 - j0, h);
     }
     float most = s[0][0];
 #pragma unroll
