@@ -43,9 +43,12 @@ long within(const e2ttt_attn_desc* d, long n) {
 Plan plan(const e2ttt_attn_desc* d) {
   Plan p{};
   const long B = d->B, H = d->H, HK = d->HK, T = d->T, S = d->S;
-  const long tile = attn_tile(d->io == E2TTT_DT_BF16, d->d), tile_kv = attn_tile_bwd(d->d);
-  p.nsplit = attn_splits(B * H * ((T + 127) / 128), within(d, S) / tile);
-  p.nsplit_kv = attn_splits(B * HK * ((S + 127) / 128), H / HK * ((within(d, T) + tile_kv - 1) / tile_kv));
+  const bool bf = d->io == E2TTT_DT_BF16, small = bf && d->d <= 64;
+  const long tile = attn_tile(bf, d->d), tile_kv = attn_tile_bwd(d->d);
+  const long g = B * H * ((T + 127) / 128);
+  p.nsplit = attn_splits(g, within(d, S) / tile, small || (bf && 256 / g * g < 208) ? 512 : 256);
+  p.nsplit_kv = attn_splits(B * HK * ((S + 127) / 128), H / HK * ((within(d, T) + tile_kv - 1) / tile_kv),
+                            small ? 512 : 256);
   const size_t q = p.nsplit > 1 ? up((size_t)p.nsplit * B * H * T * d->d * 4) : 0;
   const size_t kv = p.nsplit_kv > 1 ? up((size_t)p.nsplit_kv * B * HK * S * d->d * 8) : 0;
   p.ml = q;

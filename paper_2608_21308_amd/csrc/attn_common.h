@@ -290,8 +290,9 @@ __device__ __forceinline__ void stretch_of(int& lo, int& hi, int tile, int split
 // the forward 361 with 32, 343 with 64.)
 constexpr int attn_tile(bool bf, int d) { return !bf && d > 64 ? 32 : 64; }
 constexpr int attn_tile_bwd(int d) { return d > 64 ? 32 : 64; }
-// Stretches that `groups` workgroups of `tiles` tiles each are split into.
-int attn_splits(long groups, long tiles);
+// Stretches that `groups` workgroups of `tiles` tiles each are split into, for at most
+// `places` workgroups.
+int attn_splits(long groups, long tiles, long places);
 
 hipError_t launch_attn_forward(const AttnArgs& a, bool bf, hipStream_t stream);
 hipError_t launch_attn_backward(const AttnArgs& a, bool bf, hipStream_t stream);

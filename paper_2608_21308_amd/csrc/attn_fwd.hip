@@ -202,12 +202,17 @@ hipError_t go(AttnArgs a, hipStream_t s) {
 }  // namespace
 
 // A workgroup alone on its CU takes a tile of keys in 1 to 2 us, a split costs the
-// join, 5 us. Forward, in two halves of the card's 512 places and more, and whole: 64
-// groups of 72 tiles (head dim 128) 41 us and 82, of 128 tiles (64) 31 and 116, of 32
-// tiles in 4 and in 8 (128) 25.5 and 29.6, whole 41; 8 groups of 15 tiles in 3 14.2 and
-// 18.8; but 16 groups of 9 tiles in 2 17.6 and 15.4, 192 groups of 24 tiles 37 and 33.
-int attn_splits(long groups, long tiles) {
-  return groups > 160 ? 1 : (int)std::max(1L, std::min(512 / groups, tiles / 6));
+// join, 5 us and more with the head dim.  `places` 512 (two workgroups on a CU) and 256,
+// us, forward / backward.  Head dim 64: 64 groups of 128 tiles 32.7 / 79 and 38.1 / 89;
+// 16 groups of 140 tiles 30.6 / 64 and 29.4 / 68.  Head dim 128: 64 groups of 32 tiles
+// 28.1 / 82 and 22.8 / 63, of 72 tiles 40.1 / 120 and 38.8 / 112, 80 of 32 29.2 / 87 and
+// 25.2 / 72, 128 of 32 33.9 / 102 and 30.9 / 89; where 256 leaves a fifth of the CUs
+// empty, the forward turns: 96 groups of 64 tiles 39.3 / 124 and 44.9 / 123, 144 of 32
+// 35.9 / 111 and 37.9 / 110.  float32, 64 groups of 32 tiles 77 / 242 and 51 / 156.
+// Not split: 8 groups of 15 tiles 18.8 (in 3: 14.2), 192 groups of 24 tiles 33 (in 2:
+// 37), 16 groups of 9 tiles 15.4 (in 2: 17.6).
+int attn_splits(long groups, long tiles, long places) {
+  return groups > 160 ? 1 : (int)std::max(1L, std::min(places / groups, tiles / 6));
 }
 
 hipError_t launch_attn_forward(const AttnArgs& a, bool bf, hipStream_t s) {
