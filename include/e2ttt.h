@@ -511,7 +511,8 @@ e2ttt_status e2ttt_qk_backward(const e2ttt_qk_desc* desc, const e2ttt_qk_strides
  * rounded to bf16 once as operands of the products that follow (half a step of
  * 2^-8 each, of either sign), and outputs once.  A query's results depend on live
  * values only; a non-finite live key or value may make those of queries within 128
- * tokens of seeing it non-finite too.  Results do not change from run to run.
+ * tokens of seeing it non-finite too, where they see some key at all.  Results do not
+ * change from run to run.
  */
 typedef struct {
   int32_t B;            /* sequences                            */
@@ -579,9 +580,9 @@ e2ttt_status e2ttt_attn_backward(const e2ttt_attn_desc* desc, const e2ttt_attn_s
  * on these are written, and positions before them are not seen.  Pages that a call
  * writes to belong to one sequence (what two write at once is left undefined).
  * Token tensors are as in the attention calls, any strides.  Supported: d = 32, 64, 96
- * or 128, either io type, T up to 2^29 and pages to 2^25, at most 2^32 / 256
- * workgroups (B HK (T / 4) (d / 8) threads, B HK ceil(H / HK T / 16) workgroups and as
- * many parts; else E2TTT_ERR_UNSUPPORTED).
+ * or 128, either io type, T up to 2^29 and pages to 2^25, and launches below 2^32 threads
+ * (B HK ((T + 2) / 4 + 1) (d / 8) to write or read; to attend 512 for each of B HK
+ * ceil(H / HK T / 16) workgroups and their parts; else E2TTT_ERR_UNSUPPORTED).
  */
 typedef struct {
   int32_t B;            /* sequences                                         */
@@ -617,7 +618,8 @@ e2ttt_status e2ttt_cache_read(const e2ttt_cache_desc* desc, const e2ttt_cache_st
  * that the sequence holds.  out [B][H][T][d], lse [B][H][T] f32 (NULL: not wanted);
  * zeros and -inf for what is not live and where nothing is seen.  Meant for few
  * tokens: each 16 queries of a key head read its pages once.  fp32 throughout,
- * outputs rounded once.  workspace: e2ttt_cache_workspace_bytes bytes, not to be
+ * outputs rounded once.  A NaN that the sequence holds may reach every live query of
+ * the call whose 16 read its page.  workspace: e2ttt_cache_workspace_bytes bytes, not to be
  * shared by calls that may overlap. */
 size_t e2ttt_cache_workspace_bytes(const e2ttt_cache_desc* desc);
 e2ttt_status e2ttt_cache_attend(const e2ttt_cache_desc* desc, const e2ttt_cache_strides* strides,

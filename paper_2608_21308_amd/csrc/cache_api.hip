@@ -10,8 +10,9 @@
 namespace e2ttt {
 namespace {
 
-// (a launch numbers its threads in 32 bits, 256 to a workgroup)
-constexpr double kMostGroups = 0xffffff;
+// A launch numbers its threads in 32 bits: 256 to a workgroup that writes or reads, 512 to
+// one that attends.
+constexpr double kMostRowGroups = 0xffffff, kMostGroups = 0x7fffff;
 
 CacheArgs args_of(const e2ttt_cache_desc* d) {
   CacheArgs a{};
@@ -31,7 +32,7 @@ e2ttt_status check_desc(const e2ttt_cache_desc* d, bool attend) {
       d->T > (1 << 29) || d->pages > (1 << 25))
     return E2TTT_ERR_UNSUPPORTED;
   const double rows = (double)d->B * d->HK;
-  if (rows * ((d->T + 2) / 4 + 1) * (d->d / 8) > 256 * kMostGroups) return E2TTT_ERR_UNSUPPORTED;
+  if (rows * ((d->T + 2) / 4 + 1) * (d->d / 8) > 256 * kMostRowGroups) return E2TTT_ERR_UNSUPPORTED;
   if (attend) {
     const double tiles = ((double)(d->H / d->HK) * d->T + 15) / 16;
     if (rows * tiles > kMostGroups || tiles * 16 > (1 << 30) ||

@@ -85,6 +85,12 @@ def test_null_alignment_and_sizes(lib):
     assert calls(lib, d, n=0) == (2,) * 3 and calls(lib, d, n=-4) == (2,) * 3
 
 
+def test_the_largest_launch(lib):
+    """2^32 threads are too many for a launch; a workgroup that attends has 512."""
+    at = lambda B: e2ttt.cache_workspace_bytes(e2ttt.CacheConfig(B, 1, 1, 1, 32, 1))
+    assert at((1 << 23) - 1) > 0 and at(1 << 23) == 0
+
+
 def test_sizes(lib):
     assert e2ttt.cache_page_bytes(3, 96) == 3 * 68 * 96
     assert e2ttt.cache_page_bytes(0, 64) == e2ttt.cache_page_bytes(2, 40) == e2ttt.cache_page_bytes(2, 256) == 0
