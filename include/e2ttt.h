@@ -511,8 +511,9 @@ e2ttt_status e2ttt_qk_backward(const e2ttt_qk_desc* desc, const e2ttt_qk_strides
  * rounded to bf16 once as operands of the products that follow (half a step of
  * 2^-8 each, of either sign), and outputs once.  A query's results depend on live
  * values only; a non-finite live key or value may make those of queries within 128
- * tokens of seeing it non-finite too, where they see some key at all.  Results do not
- * change from run to run.
+ * tokens of seeing it non-finite too, where they see some key at all, and a
+ * non-finite query, its gradient or lse those of live keys.  Results do not change from
+ * run to run.
  */
 typedef struct {
   int32_t B;            /* sequences                            */

@@ -152,6 +152,10 @@ __global__ void __launch_bounds__(256, BF ? 2 : 1) attn_dq_kernel(AttnArgs a, in
   }
   pass(std::false_type{});
   if (t >= a.T) return;
+  if (ex == kNegInf) {            // (zero also where zeros have met an infinity)
+#pragma unroll
+    for (int m = 0; m < NM; ++m) o[m] = zero16();
+  }
   if (a.nsplit > 1) {
     float* row = a.part + ((long)split * a.B * a.H * a.T + at) * a.d;
 #pragma unroll
@@ -159,9 +163,8 @@ __global__ void __launch_bounds__(256, BF ? 2 : 1) attn_dq_kernel(AttnArgs a, in
     return;
   }
   E* drow = row_of_w<E>(a.dq, b, hq, t);
-  const float f = on ? a.scale : 0.0f;
 #pragma unroll
-  for (int m = 0; m < NM; ++m) st_tile<BF>(drow, o[m], f, m, h, a.d);
+  for (int m = 0; m < NM; ++m) st_tile<BF>(drow, o[m], a.scale, m, h, a.d);
 }
 
 template <bool BF, int D, int BQ>
@@ -287,6 +290,13 @@ __global__ void __launch_bounds__(256, BF && D <= 64 ? 2 : 1) attn_dkv_kernel(At
     if (left > 0) step(lq1, lg1, lx1, lq0, lg0, lx0);
   }
   if (j >= a.S) return;
+  if (j >= end) {
+#pragma unroll
+    for (int m = 0; m < NM; ++m) {
+      dk[m] = zero16();
+      dv[m] = zero16();
+    }
+  }
   if (a.nsplit_kv > 1) {
     const long rows = (long)a.B * a.HK * a.S, row = split * rows + (long)u * a.S + j;
 #pragma unroll

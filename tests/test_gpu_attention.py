@@ -280,3 +280,29 @@ def test_split_calls_as_graphs_on_two_streams():
         for _, _, o, l, ref, o2, l2, g2, *_ in runs:
             assert torch.equal(o, o2) and torch.equal(l, l2)
             assert all(torch.equal(ref[n], g2[n]) for n in ref)
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+@pytest.mark.parametrize("B,H,T,S,d,n,left", [
+    (1, 2, 40, 40, 64, 5, -1), (2, 2, 150, 150, 128, 40, 20),   # live rows, then dead ones in their tile
+    (1, 1, 40, 10, 32, 40, -1),                                 # queries ahead of the first key
+    (1, 1, 16, 4096, 64, 7, -1), (1, 1, 40, 4096, 128, 9, -1)])  # split
+def test_zeros_beside_infinities(B, H, T, S, d, n, left, io):
+    """What is not live, and what sees nothing, is zero also where live values of its
+    tile are infinite."""
+    cfg, x, g, _, _ = make(B, 1, H, T, S, d, io, left=left)
+    q, k, v = x["q"], x["k"], x["v"]
+    lengths = torch.full((B,), n, dtype=torch.int32, device="cuda")
+    end = n + S - T
+    first = max(0, T - S)             # of the queries with a key
+    k[:, :, end - 2] = math.inf
+    v[:, :, end - 1] = math.inf
+    out, lse = e2ttt.attention_forward(cfg, q, k, v, lengths=lengths)
+    dead = torch.ones(T, dtype=torch.bool, device=q.device)
+    dead[first:n] = False
+    assert (out[:, :, dead] == 0).all() and (lse[:, :, dead] == -math.inf).all()
+    assert not torch.isfinite(out[:, :, n - 1]).any()
+    g[:, :, n - 1] = math.inf
+    r = e2ttt.attention_backward(cfg, q, k, v, out, lse, g, lengths=lengths)
+    assert (r["dq"][:, :, dead] == 0).all()
+    assert (r["dk"][:, :, end:] == 0).all() and (r["dv"][:, :, end:] == 0).all()
