@@ -254,14 +254,12 @@ __global__ void __launch_bounds__(64 * NW, 2) cache_attend_kernel(CacheArgs a, i
     turn(z, pg + NW);
   }
 
-  if (!on) {                  // (a column of no live query has gone along with the others)
-    top = -INFINITY;
-    sum = 0.0f;
+  sum = groups_sum(on ? sum : 0.0f);
+  if (sum == 0.0f) {          // (a column that sees nothing has gone along with the others)
 #pragma unroll
     for (int i = 0; i < NB; ++i) o[i][0] = o[i][1] = zero4();
   }
   // the waves' parts together: lane (g, r) has channels 32 i + 8 g + 2 y + n of column r
-  sum = groups_sum(sum);
   if (g == 0) {
     lm[w][r] = sum == 0.0f ? -INFINITY : ref;
     ll[w][r] = sum;

@@ -201,6 +201,22 @@ def test_pages_that_are_none():
     within("lse", l, lse, bl, 2.0 ** -18)
 
 
+def test_zeros_beside_nan():
+    """A token whose page is none and that sees no other is zero also where the call's
+    other token reads a NaN."""
+    for io in ("bf16", "f32"):
+        cfg = e2ttt.CacheConfig(1, 1, 2, 2, 64, 2, IO(io), left=0)
+        k, v = (dev(x, io) for x in rows(1, 1, 2, 64, io, 5))
+        v[0, 0, 0, 3] = math.nan
+        cache, table, starts = e2ttt.alloc_cache(cfg, 2), i32([[1, -1]]), i32([63])
+        e2ttt.cache_write(cfg, k, v, cache, table, starts)
+        lse = torch.zeros(1, 2, 2, device="cuda")
+        q = dev(rows(1, 2, 2, 64, io, 6)[0], io)
+        out, _ = e2ttt.cache_attention(cfg, q, cache, table, starts, lse=lse)
+        assert torch.isnan(out[0, :, 0, :32]).all() and torch.isfinite(lse[0, :, 0]).all()
+        assert (out[0, :, 1] == 0).all() and (lse[0, :, 1] == -math.inf).all()
+
+
 def test_shared_pages_are_read_by_both():
     """Two sequences whose tables name the same pages (a prompt in common)."""
     cfg, cache, table, k, v, q = small()
