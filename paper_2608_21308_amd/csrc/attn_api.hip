@@ -46,9 +46,11 @@ Plan plan(const e2ttt_attn_desc* d) {
   const bool bf = d->io == E2TTT_DT_BF16, small = bf && d->d <= 64;
   const long tile = attn_tile(bf, d->d), tile_kv = attn_tile_bwd(d->d);
   const long g = B * H * ((T + 127) / 128);
-  p.nsplit = attn_splits(g, within(d, S) / tile, small || (bf && 256 / g * g < 208) ? 512 : 256);
+  const bool uneven = (d->left < 0) != (d->right < 0) && 2 * T > S;
+  const auto halve = [&](long rows) { return uneven && rows * (bf ? 1 : 4) >= 2560; };
+  p.nsplit = attn_splits(g, within(d, S) / tile, small || (bf && 256 / g * g < 208) ? 512 : 256, halve(S));
   p.nsplit_kv = attn_splits(B * HK * ((S + 127) / 128), H / HK * ((within(d, T) + tile_kv - 1) / tile_kv),
-                            small ? 512 : 256);
+                            small ? 512 : 256, halve(H / HK * T));
   const size_t q = p.nsplit > 1 ? up((size_t)p.nsplit * B * H * T * d->d * 4) : 0;
   const size_t kv = p.nsplit_kv > 1 ? up((size_t)p.nsplit_kv * B * HK * S * d->d * 8) : 0;
   p.ml = q;

@@ -345,11 +345,12 @@ template <bool BF, int D>
 hipError_t go(AttnArgs a, hipStream_t s) {
   constexpr int BK = attn_tile_bwd(D);
   const int nq = (a.T + 127) / 128, nk = (a.S + 127) / 128;
-  a.work = work_of(a.B, a.HK, a.rep, nq, a.nsplit, (a.left < 0) != (a.right < 0));
+  const bool uneven = (a.left < 0) != (a.right < 0);
+  a.work = work_of(a.B, a.HK, a.rep, nq, a.nsplit, uneven ? 64 : 0, uneven && (BF || D <= 32));
   hipLaunchKernelGGL((attn_dq_kernel<BF, D, BK>), dim3((unsigned)((long)a.B * a.H * nq * a.nsplit)),
                      dim3(256), 0, s, a, nq);
   if (a.nsplit > 1) join<BF>(a.dq, a.part, a.nsplit, a.B, a.H, a.T, a.d, a.scale, s);
-  a.work = work_of(a.B, a.HK, 1, nk, a.nsplit_kv, false);
+  a.work = work_of(a.B, a.HK, 1, nk, a.nsplit_kv, uneven ? BF && D <= 64 ? 64 : 32 : 0, false);
   hipLaunchKernelGGL((attn_dkv_kernel<BF, D, BK>),
                      dim3((unsigned)((long)a.B * a.HK * nk * a.nsplit_kv)), dim3(256), 0, s, a);
   if (a.nsplit_kv > 1) {

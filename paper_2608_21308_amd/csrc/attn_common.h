@@ -27,32 +27,48 @@ typedef __attribute__((ext_vector_type(16))) float f32x16;
 // head, which share its keys and values, go to one of them and its L2, the key heads in
 // turn (12 sequences of 250 to 3000 tokens, 8 query and 2 key heads of 128: 180 us, backward
 // 600; with an eighth of the workgroups in a row to each XCD 235 and 1017).  What 8 does not
-// divide stays as it is dealt.  Where rows are of unequal length (causal, say) the 32 CUs of
-// an XCD get long and short ones in turn, by `fold` (forward: 2 x 8 x 4096 x 128 111 us
-// without and 89 with it, 16 x 8192 x 64 198 and 173; dq: 324 and 312, 489 and 496; not for
-// dk and dv, whose workgroups have a CU to themselves or nearly: 324 and 383).
+// divide stays as it is dealt.
+//   Where rows are of unequal length (causal, say) a head deals its long ones first, and the
+// next head's long ones would begin late: heads that fill an XCD's places together are
+// dealt in turn, row by row (dk and dv, 2 x 16 x 2048 x 128: 162 us one head after the
+// other, 121 by two, 142 by four; of 64: 59, 57 and 52; 8 x 16 x 2048 x 64: 193 and 179 by
+// four; forward and dq, 32 heads of 4096 x 128: 175 + 254 and 154 + 216 by two).  Where two
+// workgroups share a CU (position y with y + 32) long and short ones meet by `fold` (forward
+// 2 x 8 x 4096 x 128 111 us without and 89 with it, 16 x 8192 x 64 202 and 177; dq 216 and
+// 222; where they do not, float32 4 x 8 x 2048 x 64: 157 + 233 and 197 + 294).
 struct Work {
-  Div per, tiles, splits, HK;    // workgroups of a key head; their factors
+  Div row, tiles, heads, HK;     // workgroups of a head; tiles of them; heads of a key head
+  Div bunch, block;              // heads that are dealt in turn; the workgroups of these
   unsigned full;                 // workgroups of the key heads that 8 divides
   bool fold;                     // every second 32 of an XCD's workgroups in reverse
 };
-inline Work work_of(int B, int HK, int heads, int tiles, int splits, bool fold) {
-  const unsigned per = (unsigned)heads * tiles * splits;
-  return Work{div_by(per), div_by((unsigned)tiles), div_by((unsigned)splits), div_by((unsigned)HK),
-              (unsigned)((long)B * HK / 8 * 8 * per), fold};
+// uneven: the places of an XCD that are filled at once where rows are of unequal length, else 0
+inline Work work_of(int B, int HK, int heads, int tiles, int splits, int uneven, bool fold) {
+  const unsigned row = (unsigned)tiles * splits, each = (unsigned)((long)B * HK / 8 * heads);
+  unsigned n = 1;
+  while (n < each && ((long)n * row < uneven || each % n)) ++n;
+  return Work{div_by(row), div_by((unsigned)tiles), div_by((unsigned)heads), div_by((unsigned)HK),
+              div_by(n), div_by(n * row), each * 8 * row, fold};
 }
 struct Place {
   int b, hk, head, split, tile;  // head: of the query heads of a key head
 };
 __device__ __forceinline__ Place place_of(const Work& w, unsigned id) {
   const bool dealt = id < w.full;
-  unsigned y = dealt ? id >> 3 : id;
-  if (dealt && w.fold && (y & 32) && (y | 31) < w.full / 8) y ^= 31;
-  const unsigned q = w.per.of(y), r = y - q * w.per.d;
-  const unsigned u = dealt ? (id & 7) + 8 * q : q, b = w.HK.of(u);
-  const unsigned z = w.tiles.of(r), head = w.splits.of(z);
-  return Place{(int)b, (int)(u - b * w.HK.d), (int)head, (int)(z - head * w.splits.d),
-               (int)(r - z * w.tiles.d)};
+  unsigned y = dealt ? id >> 3 : id, hh, r;
+  if (dealt) {
+    if (w.fold && (y & 32) && (y | 31) < w.full / 8) y ^= 31;
+    const unsigned i = w.block.of(y), j = y - i * w.block.d;
+    r = w.bunch.of(j);
+    hh = i * w.bunch.d + j - r * w.bunch.d;
+  } else {
+    hh = w.row.of(y);
+    r = y - hh * w.row.d;
+  }
+  const unsigned q = w.heads.of(hh), u = dealt ? (id & 7) + 8 * q : q, b = w.HK.of(u);
+  const unsigned split = w.tiles.of(r);
+  return Place{(int)b, (int)(u - b * w.HK.d), (int)(hh - q * w.heads.d), (int)split,
+               (int)(r - split * w.tiles.d)};
 }
 
 struct AttnArgs {
@@ -291,8 +307,8 @@ __device__ __forceinline__ void stretch_of(int& lo, int& hi, int tile, int split
 constexpr int attn_tile(bool bf, int d) { return !bf && d > 64 ? 32 : 64; }
 constexpr int attn_tile_bwd(int d) { return d > 64 ? 32 : 64; }
 // Stretches that `groups` workgroups of `tiles` tiles each are split into, for at most
-// `places` workgroups.
-int attn_splits(long groups, long tiles, long places);
+// `places` workgroups (halve: in two where a few more leave CUs to the longest rows).
+int attn_splits(long groups, long tiles, long places, bool halve);
 
 hipError_t launch_attn_forward(const AttnArgs& a, bool bf, hipStream_t stream);
 hipError_t launch_attn_backward(const AttnArgs& a, bool bf, hipStream_t stream);

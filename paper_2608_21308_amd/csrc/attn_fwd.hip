@@ -195,7 +195,9 @@ __global__ void __launch_bounds__(256) attn_join_kernel(AttnArgs a) {
 template <bool BF, int D>
 hipError_t go(AttnArgs a, hipStream_t s) {
   const int ntile = (a.T + 127) / 128;
-  a.work = work_of(a.B, a.HK, a.rep, ntile, a.nsplit, (a.left < 0) != (a.right < 0));
+  const bool uneven = (a.left < 0) != (a.right < 0);
+  a.work = work_of(a.B, a.HK, a.rep, ntile, a.nsplit, uneven ? 64 : 0,
+                   uneven && (BF || D <= 32));
   hipLaunchKernelGGL((attn_fwd_kernel<BF, D, attn_tile(BF, D)>),
                      dim3((unsigned)((long)a.B * a.H * ntile * a.nsplit)), dim3(256), 0, s, a, ntile);
   if (a.nsplit > 1)
@@ -216,8 +218,14 @@ hipError_t go(AttnArgs a, hipStream_t s) {
 // 35.9 / 111 and 37.9 / 110.  float32, 64 groups of 32 tiles 77 / 242 and 51 / 156.
 // Not split: 8 groups of 15 tiles 18.8 (in 3: 14.2), 192 groups of 24 tiles 33 (in 2:
 // 37), 16 groups of 9 tiles 15.4 (in 2: 17.6).
-int attn_splits(long groups, long tiles, long places) {
-  return groups > 160 ? 1 : (int)std::max(1L, std::min(places / groups, tiles / 6));
+// Up to 256 groups have a CU each and the longest row sets the end, `halve`, whole and
+// in two: 8 heads of 4096 rows 59.7 / 140 and 45 / 115 (64), 76 / 229 and 63 / 189 (128),
+// dk and dv of 32 query and 8 key heads (128) 493 and 403; but 16 of 2048 32.3 / 77 and 31 / 76
+// (64), 39 / 124 and 41 / 136 (128).  float32, 64: 8 of 4096 275 / 959 and 169 / 579, 32
+// of 1024 74 / 252 and 57 / 220.
+int attn_splits(long groups, long tiles, long places, bool halve) {
+  if (groups > 160) return halve && groups <= 256 ? 2 : 1;
+  return (int)std::max(1L, std::min(places / groups, tiles / 6));
 }
 
 hipError_t launch_attn_forward(const AttnArgs& a, bool bf, hipStream_t s) {

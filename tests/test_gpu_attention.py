@@ -77,6 +77,12 @@ def test_forward_backward(c, io, ragged):
     B, HK, H, T, S, d, left, right = c
     print("attention", c, io, ragged, flush=True)
     lengths = torch.tensor(([T - 1, 0, T + 5, T // 2, T] if T > 1 else [0, 1, -3])[:B]) if ragged else None
+    check(B, HK, H, T, S, d, left, right, io, lengths)
+
+
+def check(B, HK, H, T, S, d, left, right, io, lengths):
+    """Forward and backward (ragged: other strides, and with a gradient of lse)."""
+    ragged = lengths is not None
     layout = "bthd" if ragged else "bhtd"
     x, d_out = inputs(B, HK, H, T, S, d, io, d + T, lengths)
     d_lse = torch.randn(B, H, T, generator=torch.Generator().manual_seed(1)).double() if ragged else None
@@ -306,3 +312,16 @@ def test_zeros_beside_infinities(B, H, T, S, d, n, left, io):
     r = e2ttt.attention_backward(cfg, q, k, v, out, lse, g, lengths=lengths)
     assert (r["dq"][:, :, dead] == 0).all()
     assert (r["dk"][:, :, end:] == 0).all() and (r["dv"][:, :, end:] == 0).all()
+
+
+@pytest.mark.parametrize("io,B,HK,H,T,S,d,left,right,ragged", [
+    ("bf16", 1, 9, 9, 2570, 2570, 64, -1, 0, True),      # in two, both directions
+    ("f32", 1, 32, 32, 700, 700, 16, -1, 0, False),
+    ("bf16", 9, 1, 3, 900, 900, 64, -1, 3, True),        # heads dealt in threes; one of nine behind
+    ("bf16", 8, 1, 2, 700, 700, 32, 2, -1, False),       # long rows the other way round
+    ("bf16", 16, 1, 1, 300, 290, 128, -1, 0, True),      # in pairs
+    ("f32", 4, 2, 6, 600, 600, 72, -1, 0, True)])
+def test_rows_of_unequal_length(io, B, HK, H, T, S, d, left, right, ragged):
+    """Each workgroup's place in its launch, and the stretches that are joined."""
+    lengths = torch.randint(T // 3, T + 1, (B,), generator=torch.Generator().manual_seed(T)) if ragged else None
+    check(B, HK, H, T, S, d, left, right, io, lengths)
