@@ -16,6 +16,8 @@
 // operand takes the same indices from LDS (rows_t).  Scores never leave the lane.
 #pragma once
 
+#include <algorithm>
+
 #include "delta_common.h"
 #include "div.h"
 
@@ -38,17 +40,17 @@ typedef __attribute__((ext_vector_type(16))) float f32x16;
 // 222; where they do not, float32 4 x 8 x 2048 x 64: 157 + 233 and 197 + 294).
 struct Work {
   Div row, tiles, heads, HK;     // workgroups of a head; tiles of them; heads of a key head
-  Div bunch, block;              // heads that are dealt in turn; the workgroups of these
+  Div bunch, block, rest;        // heads that are dealt in turn; their workgroups; the last heads
+  unsigned bunches;              // whole ones of an XCD
   unsigned full;                 // workgroups of the key heads that 8 divides
   bool fold;                     // every second 32 of an XCD's workgroups in reverse
 };
 // uneven: the places of an XCD that are filled at once where rows are of unequal length, else 0
-inline Work work_of(int B, int HK, int heads, int tiles, int splits, int uneven, bool fold) {
+inline Work work_of(int B, int HK, int heads, int tiles, int splits, unsigned uneven, bool fold) {
   const unsigned row = (unsigned)tiles * splits, each = (unsigned)((long)B * HK / 8 * heads);
-  unsigned n = 1;
-  while (n < each && ((long)n * row < uneven || each % n)) ++n;
+  const unsigned n = std::max(1u, std::min(each, (uneven + row - 1) / row));
   return Work{div_by(row), div_by((unsigned)tiles), div_by((unsigned)heads), div_by((unsigned)HK),
-              div_by(n), div_by(n * row), each * 8 * row, fold};
+              div_by(n), div_by(n * row), div_by(std::max(1u, each % n)), each / n, each * 8 * row, fold};
 }
 struct Place {
   int b, hk, head, split, tile;  // head: of the query heads of a key head
@@ -59,8 +61,9 @@ __device__ __forceinline__ Place place_of(const Work& w, unsigned id) {
   if (dealt) {
     if (w.fold && (y & 32) && (y | 31) < w.full / 8) y ^= 31;
     const unsigned i = w.block.of(y), j = y - i * w.block.d;
-    r = w.bunch.of(j);
-    hh = i * w.bunch.d + j - r * w.bunch.d;
+    const Div& n = i < w.bunches ? w.bunch : w.rest;
+    r = n.of(j);
+    hh = i * w.bunch.d + j - r * n.d;
   } else {
     hh = w.row.of(y);
     r = y - hh * w.row.d;

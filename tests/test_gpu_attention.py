@@ -320,6 +320,7 @@ def test_zeros_beside_infinities(B, H, T, S, d, n, left, io):
     ("bf16", 9, 1, 3, 900, 900, 64, -1, 3, True),        # heads dealt in threes; one of nine behind
     ("bf16", 8, 1, 2, 700, 700, 32, 2, -1, False),       # long rows the other way round
     ("bf16", 16, 1, 1, 300, 290, 128, -1, 0, True),      # in pairs
+    ("bf16", 15, 8, 8, 600, 600, 128, -1, 0, True),      # thirteen and two; twice seven and one
     ("f32", 4, 2, 6, 600, 600, 72, -1, 0, True)])
 def test_rows_of_unequal_length(io, B, HK, H, T, S, d, left, right, ragged):
     """Each workgroup's place in its launch, and the stretches that are joined."""
