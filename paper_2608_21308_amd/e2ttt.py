@@ -1152,7 +1152,10 @@ def _like(t):
 
 
 class AttentionFunction(torch.autograd.Function):
-    """Autograd wrapper of attention: (out, lse) of (cfg, q, k, v, lengths)."""
+    """Autograd wrapper of attention: (out, lse) of (cfg, q, k, v, lengths).  A step to be
+    captured into a graph calls attention_forward and attention_backward: torch ties a
+    capture of its own backward to the stream of any eager step of the same leaves that
+    is still alive, and ends the process."""
 
     @staticmethod
     def forward(ctx, cfg, q, k, v, lengths=None):
