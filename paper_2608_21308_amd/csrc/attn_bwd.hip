@@ -66,7 +66,6 @@ __global__ void __launch_bounds__(256, BF ? 2 : 1) attn_dq_kernel(AttnArgs a, in
   const int p0 = t0 + off, p1 = min(t0 + 128, live) + off;
   int lo = a.left < 0 ? 0 : max(0, p0 - a.left);
   int hi = t0 >= live ? lo : a.right < 0 ? end : min(end, p1 + a.right);
-  if (a.nsplit > 1) stretch_of(lo, hi, BK, split, a.nsplit);
   const int pw0 = tw + off, pw1 = min(tw + 32, live) + off, p = pw0 + c;
   const int wlo = a.left < 0 ? 0 : max(0, pw0 - a.left);
   const int whi = tw >= live ? wlo : a.right < 0 ? end : min(end, pw1 + a.right);
@@ -139,8 +138,8 @@ __global__ void __launch_bounds__(256, BF ? 2 : 1) attn_dq_kernel(AttnArgs a, in
   // where a query sees few keys (two keys: dq and dk off by 2.3 times what their own
   // rounding leaves, 22: 1.5; without it 1.4).  A pass ahead makes it exact where it is
   // short (8 x 16 x 4096 x 64, windows of 32: backward 470 us and 450 without, of 128 440
-  // and 440).
-  if (BF && a.nsplit == 1 && hi - lo <= 192) {
+  // and 440).  Each stretch takes the whole range, so that they agree on D.
+  if (BF && hi - lo <= 192) {
     pass(std::true_type{});
     dot += both_sum(fix);
     __syncthreads();
@@ -150,6 +149,7 @@ __global__ void __launch_bounds__(256, BF ? 2 : 1) attn_dq_kernel(AttnArgs a, in
     a.ex[at] = ex;
     a.delta[at] = -dot;
   }
+  if (a.nsplit > 1) stretch_of(lo, hi, BK, split, a.nsplit);
   pass(std::false_type{});
   if (t >= a.T) return;
   if (ex == kNegInf) {            // (zero also where zeros have met an infinity)

@@ -4,6 +4,7 @@ a result passes two roundings of rms at most 2^-8 / sqrt(3) each (its operand's,
 its own), so 2^-8 of the whole; a gradient of queries or keys a third one, of the
 out that D is formed from: 1.5 2^-8.  With float32 the errors behind the
 elements' bounds have either sign: 2^-18."""
+import dataclasses
 import math
 
 import pytest
@@ -326,3 +327,19 @@ def test_rows_of_unequal_length(io, B, HK, H, T, S, d, left, right, ragged):
     """Each workgroup's place in its launch, and the stretches that are joined."""
     lengths = torch.randint(T // 3, T + 1, (B,), generator=torch.Generator().manual_seed(T)) if ragged else None
     check(B, HK, H, T, S, d, left, right, io, lengths)
+
+
+def test_first_rows_of_split_calls():
+    """Rows that see few keys take the same D, and so the same dS, whether their call is
+    split (189 tiles) or not (378): sums in another order alone, some 2^-20, which turn
+    a rounding of 2^-8 in 2^-11 of all elements, 2^-13 in the 2-norm.  D from a bf16 out
+    alone would leave about 2^-8."""
+    cfg, x, g, _, _ = make(2, 9, 9, 2570, 2570, 64, seed=3)
+    one = dataclasses.replace(cfg, B=1)
+    got = []
+    for c, n in ((cfg, 2), (one, 1)):
+        q, k, v = (x[m][:n] for m in "qkv")
+        out, lse = e2ttt.attention_forward(c, q, k, v)
+        got.append(e2ttt.attention_backward(c, q, k, v, out, lse, g[:n])["dq"][0, :, :128].float())
+    a, b = got
+    assert (a - b).norm() <= 2.0 ** -12 * a.norm()
