@@ -286,6 +286,14 @@ __device__ __forceinline__ int live_of(const AttnArgs& a, int b) {
   return a.lengths ? max(0, min(a.T, a.lengths[b])) : a.T;
 }
 
+// Whether a live query at position p sees a key of a sequence that ends at `end`.
+__device__ __forceinline__ bool sees_some(const AttnArgs& a, int p, int end) {
+  return (a.left < 0 ? 0 : max(0, p - a.left)) < (a.right < 0 ? end : min(end, p + a.right + 1));
+}
+// The sum of a query that sees keys: it is positive and finite (the largest of its terms
+// is at least one) unless a score has left the range of fp32, which is no sum of zero.
+__device__ __forceinline__ float sum_of(float x) { return x > 0.0f && x < INFINITY ? x : NAN; }
+
 // The sums of a lane's row, before they are joined.
 __device__ __forceinline__ void st_part(float* row, const f32x16& o, int m, int h, int d) {
 #pragma unroll

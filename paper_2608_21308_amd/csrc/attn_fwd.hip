@@ -140,8 +140,8 @@ __global__ void __launch_bounds__(256, BF ? 2 : 1) attn_fwd_kernel(AttnArgs a, i
   if (t >= a.T) return;
   sum = both_sum(sum);
   const long at = (long)u * a.T + t;
-  const bool some = t < live && sum != 0.0f;
-  if (!some) {                    // (zero also where zeros have met an infinity)
+  const bool on = t < live;
+  if (!on || sum == 0.0f) {       // (zero also where zeros have met an infinity)
     sum = 0.0f;
 #pragma unroll
     for (int m = 0; m < NM; ++m) o[m] = zero16();
@@ -150,9 +150,11 @@ __global__ void __launch_bounds__(256, BF ? 2 : 1) attn_fwd_kernel(AttnArgs a, i
     const long row = (long)split * a.B * a.H * a.T + at;
 #pragma unroll
     for (int m = 0; m < NM; ++m) st_part(a.part + row * a.d, o[m], m, h, a.d);
-    if (h == 0) a.part_ml[row] = make_float2(some ? ref : kNegInf, sum);
+    if (h == 0) a.part_ml[row] = make_float2(on && (sum != 0.0f || top != kNegInf) ? ref : kNegInf, sum);
     return;
   }
+  const bool some = on && sees_some(a, p, end);
+  sum = sum_of(sum);
   const float inv = some ? 1.0f / sum : 0.0f;
   E* orow = row_of_w<E>(a.out, b, hq, t);
 #pragma unroll
@@ -184,7 +186,9 @@ __global__ void __launch_bounds__(256) attn_join_kernel(AttnArgs a) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) x[i] = fmaf(o[i], f, x[i]);
   }
-  const bool some = sum != 0.0f;
+  const int live = live_of(a, b), off = a.S - a.T;
+  const bool some = t < live && sees_some(a, t + off, live + off);
+  sum = sum_of(sum);
   const float inv = some ? 1.0f / sum : 0.0f;
 #pragma unroll
   for (int i = 0; i < 4; ++i) x[i] *= inv;

@@ -343,3 +343,52 @@ def test_first_rows_of_split_calls():
         got.append(e2ttt.attention_backward(c, q, k, v, out, lse, g[:n])["dq"][0, :, :128].float())
     a, b = got
     assert (a - b).norm() <= 2.0 ** -12 * a.norm()
+
+
+RANGE = [  # T, S, d (the last two are split)
+    (70, 70, 32), (40, 30, 64), (130, 130, 128), (16, 4096, 64), (20, 4000, 128)]
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+@pytest.mark.parametrize("c", RANGE)
+@pytest.mark.parametrize("how", ["up", "down", "raw"])
+def test_scores_out_of_range(c, how, io):
+    """Finite queries and keys whose scores pass the range of fp32, as q . k or times the
+    scale: NaN, in the gradients of the queries too, and not the zeros of a query that
+    sees no key; those keep theirs."""
+    T, S, d = c
+    cfg, t, tg, _, _ = make(2, 1, 2, T, S, d, io, scale=2.0 ** 127 if how != "raw" else 1.0)
+    q, k = t["q"].fill_(1.0 if how != "raw" else 1e25), t["k"].fill_(1.0)
+    if how != "up":
+        k.fill_(-1.0 if how == "down" else -1e25)
+    lengths = torch.tensor([T, T - 3], dtype=torch.int32, device="cuda")
+    out, lse = e2ttt.attention_forward(cfg, q, k, t["v"], lengths=lengths)
+    sees = torch.zeros(2, T, dtype=torch.bool, device="cuda")
+    sees[0, max(0, T - S):] = sees[1, max(0, T - S):T - 3] = True
+    sees = sees[:, None].expand(2, 2, T)
+    assert torch.isnan(out[sees]).all() and torch.isnan(lse[sees]).all()
+    assert (out[~sees] == 0).all() and (lse[~sees] == -math.inf).all()
+    g = e2ttt.attention_backward(cfg, q, k, t["v"], out, lse, tg, lengths=lengths)
+    assert torch.isnan(g["dq"][sees]).all() and (g["dq"][~sees] == 0).all()
+    end = T - 3 + S - T
+    assert (g["dk"][1, :, end:] == 0).all() and (g["dv"][1, :, end:] == 0).all()
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+@pytest.mark.parametrize("S", [200, 4096])
+def test_keys_whose_scores_vanish_below_the_range(S, io):
+    """A whole stretch of keys with q . k below fp32's range weighs nothing beside
+    the other keys: as the same call without them."""
+    d, T, n = 64, 16, S // 2
+    cfg, t, _, x, _ = make(1, 1, 2, T, S, d, io, right=-1, scale=1.0)
+    q = torch.full_like(t["q"], 1e25)
+    q[..., 1:] = 0.0
+    k = torch.zeros_like(t["k"])
+    k[:, :, :n, 0] = -1e25
+    out, lse = e2ttt.attention_forward(cfg, q, k, t["v"])
+    ref = x["v"][:, :, n:].mean(2, keepdim=True).expand(1, 2, T, d)
+    # (sums of S terms, their rounding to the type and, bf16, one of the weights, here exact)
+    u = attnref.UBF if io == "bf16" else 0.0
+    lim = attnref.U32 * (S + 8) * x["v"][:, :, n:].abs().mean(2, keepdim=True) + u * ref.abs()
+    assert ((out.double().cpu() - ref).abs() <= 1.01 * lim).all()
+    assert (lse.double().cpu() - math.log(S - n)).abs().max() <= 2.0 ** -20
