@@ -17,9 +17,11 @@
 namespace e2ttt {
 namespace {
 
-// -lse log2 e, -inf for a query that sees nothing: its 2^(..) are then all zero.
+// -lse log2 e, -inf for a query that sees nothing: its 2^(..) are then all zero.  (Another
+// lse whose product passes fp32's range does not look like that.)
 __device__ __forceinline__ float exponent_of(float lse) {
-  return lse == kNegInf ? kNegInf : -lse * kLog2e;
+  const float x = -lse * kLog2e;
+  return lse == kNegInf ? kNegInf : x == kNegInf ? NAN : x;
 }
 
 template <bool BF, int D, int BK>

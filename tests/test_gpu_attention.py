@@ -392,3 +392,12 @@ def test_keys_whose_scores_vanish_below_the_range(S, io):
     lim = attnref.U32 * (S + 8) * x["v"][:, :, n:].abs().mean(2, keepdim=True) + u * ref.abs()
     assert ((out.double().cpu() - ref).abs() <= 1.01 * lim).all()
     assert (lse.double().cpu() - math.log(S - n)).abs().max() <= 2.0 ** -20
+
+
+def test_an_lse_that_leaves_the_range():
+    """An lse that fp32 holds but not times log2 e: no gradient of zero."""
+    cfg, t, tg, _, _ = make(1, 1, 1, 40, 40, 32)
+    out, lse = e2ttt.attention_forward(cfg, t["q"], t["k"], t["v"])
+    lse[0, 0, 7] = 3e38
+    g = e2ttt.attention_backward(cfg, t["q"], t["k"], t["v"], out, lse, tg)
+    assert torch.isnan(g["dq"][0, 0, 7]).all() and torch.isfinite(g["dq"][0, 0, :7]).all()
