@@ -622,7 +622,8 @@ e2ttt_status e2ttt_cache_read(const e2ttt_cache_desc* desc, const e2ttt_cache_st
  * zeros and -inf for what is not live and where nothing is seen.  Meant for few
  * tokens: each 16 queries of a key head read its pages once.  fp32 throughout,
  * outputs rounded once.  A NaN that the sequence holds may reach every live query of
- * the call whose 16 read its page, if it sees a key.  workspace:
+ * the call whose 16 read its page, if it sees a key; scores beyond the range of fp32 are
+ * as in e2ttt_attn_forward.  workspace:
  * e2ttt_cache_workspace_bytes bytes, not to be shared by calls that may overlap. */
 size_t e2ttt_cache_workspace_bytes(const e2ttt_cache_desc* desc);
 e2ttt_status e2ttt_cache_attend(const e2ttt_cache_desc* desc, const e2ttt_cache_strides* strides,

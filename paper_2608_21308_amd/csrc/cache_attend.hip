@@ -92,6 +92,13 @@ __device__ __forceinline__ float groups_sum(float x) {
   return __uint_as_float(u[0]) + __uint_as_float(u[1]);
 }
 
+// The maximum of a column that sees keys, all of them with scores of -inf (below fp32's
+// range): with a sum of zero, and not the -inf of a column that sees none.
+constexpr float kNoScore = -3.402823466e38f;
+// The sum of a column that sees keys: positive and finite (the largest of its terms is at
+// least one) unless a score has left the range of fp32.
+__device__ __forceinline__ float sum_of(float x) { return x > 0.0f && x < INFINITY ? x : NAN; }
+
 // Partial results of a stretch, per sequence, key head and tile of 16 columns: [16]
 // maxima (of the scores), [16] sums, then the outputs of [16] columns, d each.
 __host__ __device__ inline long part_floats(int d) { return 32 + 16L * d; }
@@ -143,6 +150,7 @@ __global__ void __launch_bounds__(64 * NW, 2) cache_attend_kernel(CacheArgs a, i
   for (int i = 0; i < NB; ++i) o[i][0] = o[i][1] = zero4();
   // (ref stands in for the maximum: it follows once a score passes it by 8 powers of two)
   float top = -INFINITY, ref = 0.0f, sum = 0.0f;
+  bool seen = false;              // whether the column sees a key of the wave's pages
   const float cs = a.scale * kLog2e, slack = 8.0f / cs;
 
   // the wave's pages w, w + NW, ..: their bytes one turn ahead, their places two
@@ -169,6 +177,7 @@ __global__ void __launch_bounds__(64 * NW, 2) cache_attend_kernel(CacheArgs a, i
       }
     }
     const long j0 = (long)pg * kPage;
+    seen = seen || max(see0, j0) < min(see1, j0 + kPage);
     const bool cut = j0 < any0 || j0 + kPage > h.start + 1 || (a.left >= 0 && j0 < h.end - 1 - a.left);
     if (cut) {
       // (tokens of the lane counted from 4 g on)
@@ -261,7 +270,7 @@ __global__ void __launch_bounds__(64 * NW, 2) cache_attend_kernel(CacheArgs a, i
   }
   // the waves' parts together: lane (g, r) has channels 32 i + 8 g + 2 y + n of column r
   if (g == 0) {
-    lm[w][r] = sum == 0.0f ? -INFINITY : ref;
+    lm[w][r] = on && (sum != 0.0f || top != -INFINITY) ? ref : seen ? kNoScore : -INFINITY;
     ll[w][r] = sum;
   }
 #pragma unroll
@@ -297,7 +306,9 @@ __global__ void __launch_bounds__(64 * NW, 2) cache_attend_kernel(CacheArgs a, i
     return;
   }
   if (qt >= a.T) return;
-  const float inv = total == 0.0f ? 0.0f : 1.0f / total;
+  const bool some = all != -INFINITY;
+  total = sum_of(total);
+  const float inv = some ? 1.0f / total : 0.0f;
   E* orow = row_of_w<E>(a.y, b, hq, qt);
   for (int ch = 4 * (threadIdx.x >> 4); ch < D; ch += 16 * NW) {
     f32x4 x = zero4();
@@ -308,7 +319,7 @@ __global__ void __launch_bounds__(64 * NW, 2) cache_attend_kernel(CacheArgs a, i
     IoT<BF>::st4(orow + ch, x);
   }
   if (a.lse && threadIdx.x < 16)
-    a.lse[((long)b * a.H + hq) * a.T + qt] = total == 0.0f ? -INFINITY : fmaf(all, a.scale, logf(total));
+    a.lse[((long)b * a.H + hq) * a.T + qt] = some ? fmaf(all, a.scale, logf(total)) : -INFINITY;
 }
 
 // The stretches' parts joined: a workgroup per sequence, key head, tile of columns and
@@ -345,7 +356,9 @@ __global__ void __launch_bounds__(256) cache_join_kernel(CacheArgs a, int ntile)
   total = 0.0f;
 #pragma unroll
   for (int i = 0; i < 16; ++i) total += red[i][r];
-  const float inv = total == 0.0f ? 0.0f : 1.0f / total;
+  const bool some = m != -INFINITY;
+  total = sum_of(total);
+  const float inv = some ? 1.0f / total : 0.0f;
   f32x4 x = zero4();
   const float* from = part + 32 + r * a.d + c0 + 4 * (y & 3);
 #pragma unroll 4
@@ -367,7 +380,7 @@ __global__ void __launch_bounds__(256) cache_join_kernel(CacheArgs a, int ntile)
   for (int n = 0; n < 4; ++n) o[n] *= inv;
   IoT<BF>::st4(row_of_w<E>(a.y, b, hq, qt) + c0 + 4 * y, o);
   if (a.lse && c0 == 0 && y == 0)
-    a.lse[((long)b * a.H + hq) * a.T + qt] = total == 0.0f ? -INFINITY : fmaf(m, a.scale, logf(total));
+    a.lse[((long)b * a.H + hq) * a.T + qt] = some ? fmaf(m, a.scale, logf(total)) : -INFINITY;
 }
 
 int tiles_of(const CacheArgs& a) { return (int)(((long)a.H / a.HK * a.T + 15) / 16); }

@@ -263,3 +263,51 @@ def test_graph_of_decode_steps_and_other_stream():
         torch.cuda.synchronize()
         assert torch.equal(out, ref), i
     assert torch.equal(cache, mine)
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+@pytest.mark.parametrize("P", [2, 70])      # (70 pages are split)
+@pytest.mark.parametrize("how", ["up", "down", "raw"])
+def test_scores_out_of_range(P, how, io):
+    """Finite queries and keys whose scores pass the range of fp32, as q . k or times the
+    scale: NaN, and not the zeros of a token that sees no key; those keep theirs."""
+    n, T = 64 * P - 3, 2
+    cfg = e2ttt.CacheConfig(3, 1, 3, T, 64, P, IO(io), scale=2.0 ** 127 if how != "raw" else 1.0)
+    fill = e2ttt.CacheConfig(3, 1, 3, n, 64, P, IO(io))
+    dt = torch.bfloat16 if io == "bf16" else torch.float32
+    cache, table = e2ttt.alloc_cache(cfg, 3 * P), table_of(3, P, 3 * P).to(torch.int32).cuda()
+    k = torch.full((3, 1, n, 64), dict(up=1.0, down=-1.0, raw=-1e25)[how], dtype=dt, device="cuda")
+    e2ttt.cache_write(fill, k, torch.randn(k.shape, device="cuda").to(dt), cache, table)
+    table[1] = -1
+    q = torch.full((3, 3, T, 64), 1e25 if how == "raw" else 1.0, dtype=dt, device="cuda")
+    lse = torch.zeros(3, 3, T, device="cuda")
+    out, _ = e2ttt.cache_attention(cfg, q, cache, table, i32([n - 2, n - 2, n - 1]), i32([2, 2, 1]), lse=lse)
+    assert torch.isnan(out[0]).all() and torch.isnan(lse[0]).all()
+    assert torch.isnan(out[2, :, 0]).all() and torch.isnan(lse[2, :, 0]).all()
+    for o, l in ((out[1], lse[1]), (out[2, :, 1], lse[2, :, 1])):
+        assert (o == 0).all() and (l == -math.inf).all()
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+@pytest.mark.parametrize("P", [4, 70])
+def test_keys_whose_scores_vanish_below_the_range(P, io):
+    """Pages, and whole stretches of them, with q . k below fp32's range weigh nothing
+    beside the other keys."""
+    n, d = 64 * P, 64
+    m = n // 2 + 5
+    cfg = e2ttt.CacheConfig(1, 1, 2, 1, d, P, IO(io))
+    fill = e2ttt.CacheConfig(1, 1, 2, n, d, P, IO(io))
+    v = rounded(torch.randn(1, 1, n, d, generator=torch.Generator().manual_seed(7), dtype=torch.float64), io)
+    k = torch.zeros_like(v)
+    k[:, :, :m, 0] = -2.0 ** 80
+    cache, table = e2ttt.alloc_cache(cfg, P), table_of(1, P, P).to(torch.int32).cuda()
+    e2ttt.cache_write(fill, dev(k, io), dev(v, io), cache, table)
+    q = torch.zeros(1, 2, 1, d, dtype=torch.float64)
+    q[..., 0] = 2.0 ** 80
+    lse = torch.zeros(1, 2, 1, device="cuda")
+    out, _ = e2ttt.cache_attention(cfg, dev(q, io), cache, table, i32([n - 1]), lse=lse)
+    held = cacheref.values(*cacheref.quantise(v))[0, 0, m:]
+    # (weights of 2^0, sums of n terms, the out's rounding)
+    lim = 2.0 ** -24 * (n + 16) * held.abs().mean(0) + (2.0 ** -8 if io == "bf16" else 2.0 ** -23) * held.mean(0).abs()
+    assert ((out[0, :, 0].double().cpu() - held.mean(0)).abs() <= 1.01 * lim).all()
+    assert (lse.double().cpu() - math.log(n - m)).abs().max() <= 2.0 ** -20
