@@ -17,7 +17,7 @@ constexpr double kMostRowGroups = 0xffffff, kMostGroups = 0x7fffff;
 CacheArgs args_of(const e2ttt_cache_desc* d) {
   CacheArgs a{};
   a.B = d->B; a.HK = d->HK; a.H = d->H; a.T = d->T; a.d = d->d; a.P = d->pages;
-  a.left = std::min(d->left, (1 << 30) - 1);
+  a.left = d->left;
   a.scale = d->scale;
   return a;
 }

@@ -38,7 +38,7 @@ struct CacheArgs {
   float* part;              // attention: partial results
   long n_pages;
   int B, HK, H, T, d, P;
-  int left;                 // at most 2^30 - 1; negative: no bound
+  int left;                 // negative: no bound
   int nsplit;
   Div by_split, by_tile, by_HK, by_rep, by_P;   // attention: of the workgroup's number, of columns, pages
   float scale;

@@ -311,3 +311,27 @@ def test_keys_whose_scores_vanish_below_the_range(P, io):
     lim = 2.0 ** -24 * (n + 16) * held.abs().mean(0) + (2.0 ** -8 if io == "bf16" else 2.0 ** -23) * held.mean(0).abs()
     assert ((out[0, :, 0].double().cpu() - held.mean(0)).abs() <= 1.01 * lim).all()
     assert (lse.double().cpu() - math.log(n - m)).abs().max() <= 2.0 ** -20
+
+
+def test_a_window_beyond_half_of_the_positions():
+    """left of 2^30 and more: a key that far back is seen, the one before it is not."""
+    P, left, start, d = 2 ** 24 + 2, 2 ** 30 + 10, 2 ** 30 + 100, 32
+    table = torch.full((1, P), -1, dtype=torch.int32, device="cuda")
+    table[0, 1], table[0, start // 64] = 0, 1                # positions 64 .. 127 and the last ones
+    g = torch.Generator().manual_seed(3)
+    k, v, q = (rounded(torch.randn(1, 1, 64, d, generator=g, dtype=torch.float64), "f32") for _ in "kvq")
+    at = lambda T: e2ttt.CacheConfig(1, 1, 1, T, d, P, e2ttt.DT_F32, left=left)
+    cache = e2ttt.alloc_cache(at(1), 2)
+    e2ttt.cache_write(at(64), dev(k, "f32"), dev(v, "f32"), cache, table, i32([64]))
+    n = start % 64 + 1
+    e2ttt.cache_write(at(n), dev(k.flip(2)[:, :, :n], "f32"), dev(v.flip(2)[:, :, :n], "f32"), cache, table,
+                      i32([start + 1 - n]))
+    lse = torch.zeros(1, 1, 1, device="cuda")
+    out, _ = e2ttt.cache_attention(at(1), dev(q[:, :, :1], "f32"), cache, table, i32([start]), lse=lse)
+    kv = [cacheref.values(*cacheref.quantise(x))[0] for x in (k, v)]
+    kv = tuple(torch.cat([x[:, start - left - 64:], x.flip(1)[:, :n]], 1) for x in kv)
+    m = kv[0].shape[1]
+    ref, ls, bounds = cacheref.attend(q[:, :, :1], [kv], [m - 1], [1], 2, -1, 1.0)
+    bo, bl = bounds(False)
+    within("out", out, ref, bo, 2.0 ** -18)
+    within("lse", lse, ls, bl, 2.0 ** -18)
