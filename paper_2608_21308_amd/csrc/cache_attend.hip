@@ -181,7 +181,7 @@ __global__ void __launch_bounds__(64 * NW, 2) cache_attend_kernel(CacheArgs a, i
     const bool cut = j0 < any0 || j0 + kPage > h.start + 1 || (a.left >= 0 && j0 < h.end - 1 - a.left);
     if (cut) {
       // (tokens of the lane counted from 4 g on)
-      const int k0 = (int)max(see0 - j0, -1L) - 4 * g, k1 = (int)min(see1 - j0, 64L) - 4 * g;
+      const int k0 = (int)max(see0 - j0, -1L) - 4 * g, k1 = (int)max(min(see1 - j0, 64L), -1L) - 4 * g;
       const int n0 = (int)max(any0 - j0, -1L) - 4 * g, n1 = (int)min(any1 - j0, 64L) - 4 * g;
 #pragma unroll
       for (int x = 0; x < 4; ++x) {
