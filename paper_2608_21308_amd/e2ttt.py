@@ -1151,11 +1151,35 @@ def _like(t):
     return x if x.stride(-1) == 1 else torch.empty(t.shape, dtype=t.dtype, device=t.device)
 
 
+def _capturing(t):
+    """Whether the current stream of t's device is being captured into a graph."""
+    if not isinstance(t, torch.Tensor) or t.get_device() < 0:
+        return False
+    if t.get_device() == _current_device():
+        return torch.cuda.is_current_stream_capturing()
+    with torch.cuda.device(t.device):
+        return torch.cuda.is_current_stream_capturing()
+
+
+def _no_capture(t):
+    if _capturing(t):
+        raise RuntimeError("AttentionFunction does not take part in a graph capture: "
+                           "capture attention_forward and attention_backward instead")
+
+
 class AttentionFunction(torch.autograd.Function):
     """Autograd wrapper of attention: (out, lse) of (cfg, q, k, v, lengths).  A step to be
-    captured into a graph calls attention_forward and attention_backward: torch ties a
-    capture of its own backward to the stream of any eager step of the same leaves that
-    is still alive, and ends the process."""
+    captured into a graph calls attention_forward and attention_backward; here a capture
+    that wants gradients raises RuntimeError (torch ties a capture of its own backward to
+    the stream of any eager step of the same leaves that is still alive, and ends the
+    process; whether there is one cannot be seen from here)."""
+
+    @classmethod
+    def apply(cls, cfg, q, k, v, lengths=None):
+        if torch.is_grad_enabled() and any(isinstance(t, torch.Tensor) and t.requires_grad
+                                           for t in (q, k, v)):
+            _no_capture(q)
+        return super().apply(cfg, q, k, v, lengths)
 
     @staticmethod
     def forward(ctx, cfg, q, k, v, lengths=None):
@@ -1168,6 +1192,7 @@ class AttentionFunction(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, d_out, d_lse):
+        _no_capture(d_lse if d_out is None else d_out)
         return _once(_attention_grads, ctx, d_out, d_lse)
 
 

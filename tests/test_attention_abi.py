@@ -124,3 +124,37 @@ def test_reference_gradients_by_differences():
             e = e.view_as(x[n])
             num = (loss(dict(x, **{n: x[n] + e})) - loss(dict(x, **{n: x[n] - e}))) / 2e-5
             assert abs(num.item() - ref[n].flatten()[i].item()) < 1e-8
+
+
+def test_autograd_under_capture_is_refused(lib, monkeypatch):
+    """The capture's query stands in here for a capture, and attention's calls for the
+    library's: a wanted gradient is refused before anything is recorded, in either direction."""
+    cfg = e2ttt.AttentionConfig(1, 1, 1, 4, 8)
+    x = torch.zeros(1, 1, 4, 8, dtype=torch.bfloat16)
+    on, calls = [False], []
+    monkeypatch.setattr(e2ttt, "_capturing", lambda t: on[0])
+    monkeypatch.setattr(e2ttt, "attention_forward", lambda cfg, q, k, v, lengths: (
+        calls.append("forward"), (q + k + v, q.sum(-1).float()))[1])
+    monkeypatch.setattr(e2ttt, "_attention_grads", lambda ctx, *g: (calls.append("backward"), None, x, x, x)[1:] +
+                        (None,))
+    for i in range(3):
+        t = [x.clone().requires_grad_(n == i) for n in range(3)]
+        on[0] = True
+        with pytest.raises(RuntimeError, match="attention_forward and attention_backward"):
+            e2ttt.AttentionFunction.apply(cfg, *t)
+        assert calls == []
+        with torch.no_grad():                   # no gradient is wanted: an ordinary call
+            e2ttt.AttentionFunction.apply(cfg, *t)
+        e2ttt.AttentionFunction.apply(cfg, *[y.detach() for y in t])
+        on[0] = False
+        out, _ = e2ttt.AttentionFunction.apply(cfg, *t)
+        on[0] = True
+        assert calls == ["forward"] * 3
+        with pytest.raises(RuntimeError, match="attention_forward and attention_backward"):
+            out.sum().backward()
+        assert calls == ["forward"] * 3
+        on[0] = False
+        out, _ = e2ttt.AttentionFunction.apply(cfg, *t)
+        out.sum().backward()
+        assert calls == ["forward"] * 4 + ["backward"]
+        calls.clear()

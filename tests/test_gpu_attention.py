@@ -401,3 +401,26 @@ def test_an_lse_that_leaves_the_range():
     lse[0, 0, 7] = 3e38
     g = e2ttt.attention_backward(cfg, t["q"], t["k"], t["v"], out, lse, tg)
     assert torch.isnan(g["dq"][0, 0, 7]).all() and torch.isfinite(g["dq"][0, 0, :7]).all()
+
+
+def test_autograd_in_a_capture():
+    """A capture that wants gradients is refused and can go on; without them the call is
+    captured as any other."""
+    cfg, t, tg, _, _ = make(1, 1, 2, 70, 70, 64)
+    leaves = [t[n].detach().clone().requires_grad_(True) for n in "qkv"]
+    ref, _ = e2ttt.attention_forward(cfg, t["q"], t["k"], t["v"])
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        with pytest.raises(RuntimeError, match="attention_forward and attention_backward"):
+            e2ttt.AttentionFunction.apply(cfg, *leaves)
+        with torch.no_grad():
+            out, _ = e2ttt.AttentionFunction.apply(cfg, *leaves)
+    for _ in range(3):
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, ref)
+        got, _ = e2ttt.AttentionFunction.apply(cfg, *leaves)
+        assert torch.equal(got.detach(), ref)
+    assert all(torch.isfinite(g).all() for g in torch.autograd.grad(got, leaves, tg))
