@@ -210,8 +210,6 @@ def _own(s):
                                          scale=c["d"] ** -0.5, left=c["left"])
         if c["kind"] == "store":
             s["read"] = e2ttt.CacheConfig(c["B"], c["HK"], c["H"], c["T"] + c["back"], c["d"], c["P"], io)
-            s["read_starts"] = s["starts"] - c["back"]
-            s["read_lengths"] = s["lengths"] + c["back"] if c["lengths"] else None
         if c["kind"] == "attend":
             s["workspace"] = e2ttt.alloc_cache_workspace(s["cfg"])
     cfg, lengths = s["cfg"], s.get("lengths")
@@ -224,8 +222,10 @@ def _own(s):
         return dict(out=out.detach(), lse=lse.detach(), **dict(zip(("d_q", "d_k", "d_v"), grads)))
     if c["kind"] == "store":
         e2ttt.cache_write(cfg, s["k"], s["v"], s["cache"], s["table"], s["starts"], lengths)
-        return dict(zip(("k", "v"), e2ttt.cache_read(s["read"], s["cache"], s["table"],
-                                                     s["read_starts"], s["read_lengths"])))
+        starts, back = s["starts"], c["back"]
+        if back:                # (the stretch begins before the tokens that were written)
+            starts, lengths = starts - back, lengths + back if c["lengths"] else None
+        return dict(zip(("k", "v"), e2ttt.cache_read(s["read"], s["cache"], s["table"], starts, lengths)))
     return dict(out=e2ttt.cache_attention(cfg, s["q"], s["cache"], s["table"], s["starts"], lengths,
                                           workspace=s["workspace"])[0])
 
