@@ -150,7 +150,6 @@ __global__ void __launch_bounds__(64 * NW, 2) cache_attend_kernel(CacheArgs a, i
   for (int i = 0; i < NB; ++i) o[i][0] = o[i][1] = zero4();
   // (ref stands in for the maximum: it follows once a score passes it by 8 powers of two)
   float top = -INFINITY, ref = 0.0f, sum = 0.0f;
-  bool seen = false;              // whether the column sees a key of the wave's pages
   const float cs = a.scale * kLog2e, slack = 8.0f / cs;
 
   // the wave's pages w, w + NW, ..: their bytes one turn ahead, their places two
@@ -177,7 +176,6 @@ __global__ void __launch_bounds__(64 * NW, 2) cache_attend_kernel(CacheArgs a, i
       }
     }
     const long j0 = (long)pg * kPage;
-    seen = seen || max(see0, j0) < min(see1, j0 + kPage);
     const bool cut = j0 < any0 || j0 + kPage > h.start + 1 || (a.left >= 0 && j0 < h.end - 1 - a.left);
     if (cut) {
       // (tokens of the lane counted from 4 g on)
@@ -268,6 +266,15 @@ __global__ void __launch_bounds__(64 * NW, 2) cache_attend_kernel(CacheArgs a, i
 #pragma unroll
     for (int i = 0; i < NB; ++i) o[i][0] = o[i][1] = zero4();
   }
+  // (of the wave's pages a column sees none, or only scores of -inf: its places tell)
+  const bool none = on && sum == 0.0f && top == -INFINITY;
+  bool seen = false;
+  if (__any(none))
+    for (int pg = s0 + w; pg < s1; pg += NW) {
+      const long j0 = (long)pg * kPage;
+      seen = seen || (none && max(see0, j0) < min(see1, j0 + kPage) &&
+                      page_at(a, b, hk, pg - (int)a.by_P.of(pg) * a.P));
+    }
   // the waves' parts together: lane (g, r) has channels 32 i + 8 g + 2 y + n of column r
   if (g == 0) {
     lm[w][r] = on && (sum != 0.0f || top != -INFINITY) ? ref : seen ? kNoScore : -INFINITY;
