@@ -1153,10 +1153,9 @@ def _like(t):
 
 def _capturing(t):
     """Whether the current stream of t's device is being captured into a graph."""
-    if not isinstance(t, torch.Tensor) or t.get_device() < 0:
-        return False
-    if t.get_device() == _current_device():
-        return torch.cuda.is_current_stream_capturing()
+    dev = t.get_device() if isinstance(t, torch.Tensor) else -1
+    if dev < 0 or dev == _current_device():
+        return dev >= 0 and torch.cuda.is_current_stream_capturing()
     with torch.cuda.device(t.device):
         return torch.cuda.is_current_stream_capturing()
 
