@@ -227,9 +227,12 @@ hipError_t go(AttnArgs a, hipStream_t s) {
 // dk and dv of 32 query and 8 key heads (128) 493 and 403; but 16 of 2048 32.3 / 77 and 31 / 76
 // (64), 39 / 124 and 41 / 136 (128).  float32, 64: 8 of 4096 275 / 959 and 169 / 579, 32
 // of 1024 74 / 252 and 57 / 220.
+// The same for 129 to 160 groups where 256 places give them one stretch each: dk and dv of 128,
+// backward of 4 heads of 4608 210 and 167, of 16 query and 4 key heads 697 and 455; float32, 64:
+// 4 of 4608 306 / 1062 and 164 / 560, 16 of 1152 82 / 280 and 52 / 162.
 int attn_splits(long groups, long tiles, long places, bool halve) {
-  if (groups > 160) return halve && groups <= 256 ? 2 : 1;
-  return (int)std::max(1L, std::min(places / groups, tiles / 6));
+  const long least = halve && groups > 128 && groups <= 256 ? 2 : 1;
+  return (int)(groups > 160 ? least : std::max(least, std::min(places / groups, tiles / 6)));
 }
 
 hipError_t launch_attn_forward(const AttnArgs& a, bool bf, hipStream_t s) {

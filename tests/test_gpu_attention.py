@@ -424,3 +424,15 @@ def test_autograd_in_a_capture():
         got, _ = e2ttt.AttentionFunction.apply(cfg, *leaves)
         assert torch.equal(got.detach(), ref)
     assert all(torch.isfinite(g).all() for g in torch.autograd.grad(got, leaves, tg))
+
+
+@pytest.mark.parametrize("io,B,HK,H,T,S,d,ragged", [
+    ("bf16", 1, 65, 1040, 160, 160, 72, True),     # dk and dv, 130 groups
+    ("f32", 1, 26, 26, 700, 700, 16, False)])      # 156, both directions
+def test_rows_of_unequal_length_on_half_of_the_card(io, B, HK, H, T, S, d, ragged):
+    """129 to 160 groups are split in two as those on either side of them are."""
+    cfg = e2ttt.AttentionConfig(B, HK, H, T, d, e2ttt.DT_BF16 if io == "bf16" else e2ttt.DT_F32, S=S)
+    rows, part = -(-4 * B * H * T // 256) * 256, 8 * B * HK * S * d
+    assert e2ttt.attention_scratch_bytes(cfg) == 2 * rows + 2 * part
+    lengths = torch.randint(T // 3, T + 1, (B,), generator=torch.Generator().manual_seed(T)) if ragged else None
+    check(B, HK, H, T, S, d, -1, 0, io, lengths)
