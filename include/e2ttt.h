@@ -502,14 +502,20 @@ e2ttt_status e2ttt_qk_backward(const e2ttt_qk_desc* desc, const e2ttt_qk_strides
  *   lengths [B] int32 (device; NULL: all T)      of sequence b the first lengths[b]
  *               (clamped to 0..T) queries and the first lengths[b] + S - T keys are
  *               live; what lies behind is not read, its outputs and gradients are
- *               written as zero and its lse as -inf
+ *               written as zero and its lse as -inf (queries and keys end together:
+ *               single queries on sequences of different lengths, T = 1, are calls
+ *               of their own here, or one e2ttt_cache_attend)
  * scale is at least 2^-126.  Outputs do not overlap inputs.  Supported: d <= 128, a multiple
  * of 8, either io type, T and S up to 2^29, and B H ceil(T / 128), B HK ceil(S / 128)
  * below 2^24 (else E2TTT_ERR_UNSUPPORTED).
  *
  * Precision: scores, softmax and sums in fp32.  With bf16 tensors P and dS are
  * rounded to bf16 once as operands of the products that follow (half a step of
- * 2^-8 each, of either sign), and outputs once.  A query's results depend on live
+ * 2^-8 each, of either sign), and outputs once.  The backward's D = sum do o - d_lse
+ * takes a bf16 out as it was rounded, a third such rounding in dq and dk, except where 128
+ * neighbouring queries (0 .. 127, and so on) see 192 keys at most together: there
+ * that rounding is taken out again.  Its P, formed from lse, are off by some 2^-23
+ * |lse| beside the rounding of their scores.  A query's results depend on live
  * values only; a non-finite live key or value may make those of queries within 128
  * tokens of seeing it non-finite too, where they see some key at all, and a
  * non-finite query, its gradient or lse those of live keys.  Where a score that a query
@@ -620,8 +626,10 @@ e2ttt_status e2ttt_cache_read(const e2ttt_cache_desc* desc, const e2ttt_cache_st
  * into the cache before: the query at position p sees the positions p - left .. p
  * that the sequence holds.  out [B][H][T][d], lse [B][H][T] f32 (NULL: not wanted);
  * zeros and -inf for what is not live and where nothing is seen.  Meant for few
- * tokens: each 16 queries of a key head read its pages once.  fp32 throughout,
- * outputs rounded once.  A NaN that the sequence holds may reach every live query of
+ * tokens: each 16 queries of a key head read its pages once.  Queries and cached
+ * values enter as they are; scores, softmax and sums are fp32.  P enters its product
+ * as bf16 terms, two with bf16 tensors (off by 2^-16 of each at most) and three
+ * with fp32; outputs are rounded once.  A NaN that the sequence holds may reach every live query of
  * the call whose 16 read its page, if it sees a key; scores beyond the range of fp32 are
  * as in e2ttt_attn_forward.  workspace:
  * e2ttt_cache_workspace_bytes bytes, not to be shared by calls that may overlap. */

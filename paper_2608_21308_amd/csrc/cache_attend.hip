@@ -6,7 +6,10 @@
 //   S^T = K Q^T,  P^T = 2^(c (S^T - m)),  O^T += V^T P^T,  c = scale log2 e.
 // Codes become bf16 without loss (two to an instruction, scale included).  Queries and
 // probabilities enter as bf16 terms: queries exactly (one term of bf16, three of
-// fp32), P as NP terms, so that out is an fp32 result rounded once.
+// fp32), P as NP: three for fp32 tensors, two for bf16, off by at most 2^-16 of each P
+// ahead of the out's rounding of 2^-8.  fp32 queries cost a tenth to a fifth: 64 x 8 key
+// heads of 128, 8192 tokens: 118 us and 108, 4 x 4, 64k tokens: 39.1 and 33.3, 8 x 16 of
+// 64, 2048 tokens: 12.4 and 11.5.
 // Bound by HBM: 17/16 d bytes a token and key head, read once.  Where sequences and
 // heads are few, the pages are dealt to several workgroups and their parts joined by
 // a second kernel.

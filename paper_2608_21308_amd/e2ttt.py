@@ -822,7 +822,9 @@ def delta_step(cfg: DeltaConfig, q, k, v, eta, log_gamma, w, *, slots=None, out=
 class DeltaFunction(torch.autograd.Function):
     """Autograd wrapper of the gated delta rule: (out, w_out) of (cfg, q, k, v,
     eta, log_gamma, w_in, lengths); the forward saves the workspace where a
-    gradient may be asked for."""
+    gradient may be asked for.  A step to be captured into a graph calls delta_forward
+    and delta_backward: torch's capture of its own backward ends the process where an
+    eager step of the same leaves is still alive."""
 
     @classmethod
     def apply(cls, cfg, q, k, v, eta, log_gamma=None, w_in=None, lengths=None):
@@ -1005,7 +1007,8 @@ def qk_backward(cfg: QKConfig, d_q_out, d_k_out, q=None, k=None, inv_freq=None, 
 
 class QKFunction(torch.autograd.Function):
     """Autograd wrapper of the query/key preparation: (q', k') of (cfg, q, k,
-    inv_freq, positions)."""
+    inv_freq, positions).  A step to be captured into a graph calls qk_forward and
+    qk_backward (see DeltaFunction)."""
 
     @staticmethod
     def forward(ctx, cfg, q, k, inv_freq=None, positions=None):
