@@ -520,8 +520,8 @@ e2ttt_status e2ttt_qk_backward(const e2ttt_qk_desc* desc, const e2ttt_qk_strides
  * tokens of seeing it non-finite too, where they see some key at all, and a
  * non-finite query, its gradient or lse those of live keys.  Where a score that a query
  * sees, as q . k or times scale log2 e, passes the range of fp32, its out and lse may be
- * NaN (and the gradients that they enter); zeros and -inf stand for seeing no key alone.
- * Results do not change from run to run.
+ * NaN (and the gradients that they enter); zeros and -inf are left to what is not live or
+ * sees no key.  Results do not change from run to run.
  */
 typedef struct {
   int32_t B;            /* sequences                            */
